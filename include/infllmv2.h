@@ -15,7 +15,8 @@
  * (infllmv2_params.lse_coarse_ratio), infllmv2_sparse_attn_bwd (the gradients of stage 3), the
  * *_verify variants of the decode step for the n drafted tokens of speculative decoding (section
  * 4.1), and, as a labelled comparison that is NOT the report's method, the *_shared variants with
- * one block set per query block.
+ * one block set per query block.  Next to the path: a cache in 4 bits (infllmv2_quantize_kv and the *_quant calls) and attention
+ * over a sliding window and the first tokens (infllmv2_window_attn_*).
  *
  * Conventions for every entry point
  *   - Returns 0 (INFLLMV2_OK) or a negative INFLLMV2_ERR_* code; never throws, never
@@ -73,6 +74,10 @@ extern "C" {
 #define INFLLMV2_OP_SELECT_VERIFY 5
 #define INFLLMV2_OP_ATTN_VERIFY 6
 #define INFLLMV2_OP_VERIFY_STEP 10
+/* Stage selector for infllmv2_window_workspace_bytes. */
+#define INFLLMV2_OP_WINDOW_PREFILL 11
+#define INFLLMV2_OP_WINDOW_BWD 12
+#define INFLLMV2_OP_WINDOW_DECODE 13
 
 /* Query layout selector for infllmv2_select_blocks. */
 #define INFLLMV2_MODE_PREFILL 0 /* one query per cached token: query t sits at position t        */
@@ -112,6 +117,21 @@ typedef struct infllmv2_tensor {
     int64_t stride_h;
     int64_t stride_t;
 } infllmv2_tensor;
+
+/* A device cache in 4 bits, [batch, Hkv, >=max_seqlen] rows of head_dim values; strides in BYTES.  A row is head_dim / 2 = 64
+ * contiguous bytes of codes (row starts 16-byte aligned: pointer and strides multiples of 16) and head_dim / 32 = 4 contiguous exponent
+ * bytes (pointer and strides multiples of 4).  Channel 2c is the low half of byte c.  A code is a sign (bit 3) and the index (bits 0 to
+ * 2) of 0, 0.5, 1, 1.5, 2, 3, 4, 6; its value is that number times 2^(e - 127), e the exponent byte of the channel's group of 32.
+ * The calls below write e = E - 2, but at least 2 and at most 252, E the biased exponent of the group's largest magnitude rounded to two
+ * significant bits, and the nearest codes, ties to the even index: no value is further from its code's than half the distance of two
+ * neighbouring codes (magnitudes of 1.75 x 2^127 and more: clipped to 1.5 x 2^127).  A group with an infinity or a NaN gets e = 255, codes 0, and stands for NaN.  Other e are not written,
+ * and 0 and 1 not read as anything defined.  Every value is a bf16 number. */
+typedef struct infllmv2_quant_tensor {
+    void *codes;
+    void *scales;
+    int64_t stride_b, stride_h, stride_t;                   /* of codes  */
+    int64_t scale_stride_b, scale_stride_h, scale_stride_t; /* of scales */
+} infllmv2_quant_tensor;
 
 /* Human-readable name of a status code (static storage). */
 const char *infllmv2_status_string(int32_t status);
@@ -379,6 +399,88 @@ int32_t infllmv2_verify_step(const infllmv2_params *prm, const infllmv2_tensor *
                              const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_draft,
                              const uint64_t *tree_mask, int32_t *block_idx, const infllmv2_tensor *out,
                              float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The cache in 4 bits (format: infllmv2_quant_tensor), 68 bytes per row instead of 256.
+ *
+ * infllmv2_quantize_kv      rows of the bf16 caches k, v into kq, vq: after a prompt.
+ * infllmv2_dequantize_kv    the way back: the rows' values, exactly, into bf16 caches.
+ *   k, v          bf16 caches [batch, Hkv, >=max_seqlen, d]
+ *   n_new_tokens  <= 0: rows 0 .. seqlens[b]-1 of every sequence;  > 0: the last n_new_tokens of them.
+ *                 Other rows are left as they are.
+ * infllmv2_append_kv_quant  infllmv2_append_kv / _append_kv_verify on such caches: k_new, v_new bf16 [batch, Hkv, n_draft, d], 1 <= n_draft <= 64,
+ *                           are quantised into rows seqlens[b]-n_draft .. seqlens[b]-1.  With ck != NULL the same launch writes
+ *                           the semantic kernels those rows complete, as means of the values the cache stands for: the bits
+ *                           infllmv2_compress_keys with n_new_tokens = n_draft gives for the cache read back.  A sequence with
+ *                           seqlens[b] < n_draft or > max_seqlen is skipped as a whole.
+ * infllmv2_sparse_attn_decode_quant, infllmv2_sparse_attn_verify_quant
+ *                           infllmv2_sparse_attn_decode / _verify with k, v = the values of kq, vq: the same arguments, block lists, tree
+ *                           masks, results and workspaces (INFLLMV2_OP_ATTN_DECODE, INFLLMV2_OP_ATTN_VERIFY).
+ * The selection reads compressed keys, which stay bf16: infllmv2_select_blocks and _verify serve such a cache as they are.
+ */
+int32_t infllmv2_quantize_kv(const infllmv2_params *prm, const infllmv2_tensor *k, const infllmv2_tensor *v,
+                             const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_new_tokens,
+                             const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq, void *stream);
+int32_t infllmv2_dequantize_kv(const infllmv2_params *prm, const infllmv2_quant_tensor *kq,
+                               const infllmv2_quant_tensor *vq, const int32_t *seqlens, int32_t batch,
+                               int32_t max_seqlen, int32_t n_new_tokens, const infllmv2_tensor *k,
+                               const infllmv2_tensor *v, void *stream);
+int32_t infllmv2_append_kv_quant(const infllmv2_params *prm, const infllmv2_tensor *k_new,
+                                 const infllmv2_tensor *v_new, const infllmv2_quant_tensor *kq,
+                                 const infllmv2_quant_tensor *vq, const infllmv2_tensor *ck, const int32_t *seqlens,
+                                 int32_t batch, int32_t max_seqlen, int32_t n_draft, void *stream);
+int32_t infllmv2_sparse_attn_decode_quant(const infllmv2_params *prm, const infllmv2_tensor *q,
+                                          const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq,
+                                          const int32_t *seqlens, int32_t batch, int32_t max_seqlen,
+                                          const int32_t *block_idx, const infllmv2_tensor *out, float *lse,
+                                          void *workspace, size_t workspace_bytes, void *stream);
+int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infllmv2_tensor *q,
+                                          const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq,
+                                          const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_draft,
+                                          const uint64_t *tree_mask, const int32_t *block_idx,
+                                          const infllmv2_tensor *out, float *lse, void *workspace,
+                                          size_t workspace_bytes, void *stream);
+
+/*
+ * Attention over a sliding window and the first tokens: for the query at position i
+ *     T_i = { t <= i : t < n_sink or i - t < window },   n_sink >= 0, window >= 1 (the query's own token counts)
+ * and out, lse over T_i as in infllmv2_sparse_attn_prefill (bf16 products accumulated in fp32, probabilities rounded to bf16
+ * before the value product, their fp32 sum taken before).  A window of max_seqlen or more is causal attention over everything.
+ * Of prm the head counts, head_dim and softmax_scale count; the rest has to be valid.
+ *
+ * infllmv2_window_attn_prefill  one query per cached token: q, out [batch, max_seqlen, Hq, d], lse fp32 [batch, max_seqlen, Hq]; rows
+ *                               t >= seqlens[b] ignored / not written.
+ * infllmv2_window_attn_bwd      its gradients for an upstream gradient dout, as infllmv2_sparse_attn_bwd's, with the
+ *                               sums for dk, dv in a fixed order: results repeat bit for bit.
+ * infllmv2_window_attn_decode   the query at position seqlens[b]-1: q, out [batch, 1, Hq, d], lse fp32 [batch, Hq]; a sequence with
+ *                               seqlens[b] < 1 gets out 0, lse -inf.
+ * infllmv2_window_attn_decode_quant  the same on a cache in 4 bits.
+ * Workspaces: infllmv2_window_workspace_bytes(INFLLMV2_OP_WINDOW_*, ...) bytes, 256-byte aligned (0: none needed, or the arguments are
+ * invalid); INFLLMV2_OP_WINDOW_DECODE for both decode calls.
+ */
+size_t infllmv2_window_workspace_bytes(int32_t op, const infllmv2_params *prm, int32_t n_sink, int32_t window,
+                                       int32_t batch, int32_t max_seqlen);
+int32_t infllmv2_window_attn_prefill(const infllmv2_params *prm, int32_t n_sink, int32_t window,
+                                     const infllmv2_tensor *q, const infllmv2_tensor *k, const infllmv2_tensor *v,
+                                     const int32_t *seqlens, int32_t batch, int32_t max_seqlen,
+                                     const infllmv2_tensor *out, float *lse, void *workspace, size_t workspace_bytes,
+                                     void *stream);
+int32_t infllmv2_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, int32_t window,
+                                 const infllmv2_tensor *q, const infllmv2_tensor *k, const infllmv2_tensor *v,
+                                 const infllmv2_tensor *out, const infllmv2_tensor *dout, const float *lse,
+                                 const int32_t *seqlens, int32_t batch, int32_t max_seqlen, const infllmv2_tensor *dq,
+                                 const infllmv2_tensor *dk, const infllmv2_tensor *dv, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+int32_t infllmv2_window_attn_decode(const infllmv2_params *prm, int32_t n_sink, int32_t window,
+                                    const infllmv2_tensor *q, const infllmv2_tensor *k, const infllmv2_tensor *v,
+                                    const int32_t *seqlens, int32_t batch, int32_t max_seqlen,
+                                    const infllmv2_tensor *out, float *lse, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_sink, int32_t window,
+                                          const infllmv2_tensor *q, const infllmv2_quant_tensor *kq,
+                                          const infllmv2_quant_tensor *vq, const int32_t *seqlens, int32_t batch,
+                                          int32_t max_seqlen, const infllmv2_tensor *out, float *lse, void *workspace,
+                                          size_t workspace_bytes, void *stream);
 
 /*
  * Query-block-shared selection -- a COMPARISON VARIANT, not the report's method (section 2.1.3 argues

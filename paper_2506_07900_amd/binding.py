@@ -12,11 +12,13 @@ Tensor layouts (bf16, CUDA/HIP device, head_dim contiguous):
   queries, outputs  [B, T, Hq, d]   (decode: T = 1; draft verification: T = n_draft)
   seqlens           int32 [B]
   block_idx         int32 [B, Hkv, Tq, topk]
+  caches in 4 bits  QuantCache: codes uint8 [B, Hkv, T, d/2], scales uint8 [B, Hkv, T, d/32]
 """
 import ctypes
 import importlib.util
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -32,13 +34,17 @@ OP_ATTN_BWD = 7
 OP_DECODE_STEP = 8
 OP_SELECT_SHARED = 9
 OP_VERIFY_STEP = 10
+OP_WINDOW_PREFILL, OP_WINDOW_BWD, OP_WINDOW_DECODE = 11, 12, 13
 MODE_PREFILL, MODE_DECODE = 0, 1
 
 EXPORTS = ["infllmv2_status_string", "infllmv2_workspace_bytes", "infllmv2_compress_keys",
            "infllmv2_select_blocks", "infllmv2_sparse_attn_prefill", "infllmv2_sparse_attn_decode", "infllmv2_sparse_attn_decode_noalloc",
            "infllmv2_sparse_attn_bwd", "infllmv2_append_kv", "infllmv2_decode_step", "infllmv2_select_blocks_shared", "infllmv2_sparse_attn_prefill_shared", "infllmv2_verify_workspace_bytes", "infllmv2_append_kv_verify",
            "infllmv2_select_blocks_verify", "infllmv2_sparse_attn_verify", "infllmv2_verify_step",
-           "infllmv2_block_scores"]
+           "infllmv2_block_scores",
+           "infllmv2_quantize_kv", "infllmv2_dequantize_kv", "infllmv2_append_kv_quant", "infllmv2_sparse_attn_decode_quant",
+           "infllmv2_sparse_attn_verify_quant", "infllmv2_window_workspace_bytes", "infllmv2_window_attn_prefill",
+           "infllmv2_window_attn_bwd", "infllmv2_window_attn_decode", "infllmv2_window_attn_decode_quant"]
 BENCH_EXPORTS = ["infllmv2_probe_peaks", "infllmv2_probe_detail", "infllmv2_timing_enable", "infllmv2_timing_read"]
 
 
@@ -54,6 +60,17 @@ class CParams(ctypes.Structure):
 class CTensor(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
                 ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64)]
+
+
+class CQuantTensor(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("stride_b", "stride_h", "stride_t", "scale_stride_b", "scale_stride_h", "scale_stride_t")]
+
+
+class QuantCache(NamedTuple):
+    """A cache in 4 bits: codes uint8 [B, Hkv, T, d/2], exponent bytes uint8 [B, Hkv, T, d/32] (see infllmv2_quant_tensor)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
 
 
 @dataclass
@@ -147,6 +164,20 @@ def load_library(path=None):
     lib.infllmv2_verify_step.argtypes = [P, T, T, T, T, T, T, vp, i32, i32, i32, vp, vp, T, vp, vp, sz, vp]
     lib.infllmv2_sparse_attn_verify.restype = i32
     lib.infllmv2_sparse_attn_verify.argtypes = [P, T, T, T, vp, i32, i32, i32, vp, vp, T, vp, vp, sz, vp]
+    Q = ctypes.POINTER(CQuantTensor)
+    lib.infllmv2_window_workspace_bytes.restype = sz
+    lib.infllmv2_window_workspace_bytes.argtypes = [i32, P, i32, i32, i32, i32]
+    for name, args in (("quantize_kv", [P, T, T, vp, i32, i32, i32, Q, Q, vp]),
+                       ("dequantize_kv", [P, Q, Q, vp, i32, i32, i32, T, T, vp]),
+                       ("append_kv_quant", [P, T, T, Q, Q, T, vp, i32, i32, i32, vp]),
+                       ("sparse_attn_decode_quant", [P, T, Q, Q, vp, i32, i32, vp, T, vp, vp, sz, vp]),
+                       ("sparse_attn_verify_quant", [P, T, Q, Q, vp, i32, i32, i32, vp, vp, T, vp, vp, sz, vp]),
+                       ("window_attn_prefill", [P, i32, i32, T, T, T, vp, i32, i32, T, vp, vp, sz, vp]),
+                       ("window_attn_bwd", [P, i32, i32, T, T, T, T, T, vp, vp, i32, i32, T, T, T, vp, sz, vp]),
+                       ("window_attn_decode", [P, i32, i32, T, T, T, vp, i32, i32, T, vp, vp, sz, vp]),
+                       ("window_attn_decode_quant", [P, i32, i32, T, Q, Q, vp, i32, i32, T, vp, vp, sz, vp])):
+        fn = getattr(lib, "infllmv2_" + name)
+        fn.restype, fn.argtypes = i32, args
     if hasattr(lib, "infllmv2_timing_enable"):            # the bench build
         lib.infllmv2_probe_peaks.restype = i32
         lib.infllmv2_probe_peaks.argtypes = [vp, sz, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), vp]
@@ -381,6 +412,64 @@ def decode_step(prm, q, k_new, v_new, k, v, ck, seqlens, max_seqlen, block_idx=N
     -> block_idx [B, Hkv, 1, topk], out [B, 1, Hq, d], lse [B, Hq]."""
     return _native().decode_step(prm.packed(), q, k_new, v_new, k, v, ck, seqlens, max_seqlen, block_idx, out, lse,
                                  workspace)
+
+
+# ---- a cache in 4 bits -------------------------------------------------------------------------------
+
+def quantize_kv(prm, k, v, seqlens, max_seqlen, kq=None, vq=None, n_new_tokens=0):
+    """Rows of the caches k, v [B, Hkv, T, d] into 4 bits (all of a sequence's, or its last n_new_tokens) -> QuantCache kq, vq
+    (allocated if not given, both or neither)."""
+    if (kq is None) != (vq is None):
+        raise InfLLMv2Error("kq and vq must be given together")
+    return _native().quantize_kv(prm.packed(), k, v, seqlens, max_seqlen, None if kq is None else (kq, vq), n_new_tokens, QuantCache)
+
+
+def dequantize_kv(prm, kq, vq, seqlens, max_seqlen, k=None, v=None, n_new_tokens=0):
+    """The values of such rows -> k, v [B, Hkv, max_seqlen, d] bf16 (allocated if not given)."""
+    return _native().dequantize_kv(prm.packed(), kq, vq, seqlens, max_seqlen, k, v, n_new_tokens)
+
+
+def append_kv_quant(prm, k_new, v_new, kq, vq, seqlens, max_seqlen, ck=None):
+    """k_new, v_new [B, Hkv, n, d], 1 <= n <= 64, are quantised into rows seqlens[b]-n .. seqlens[b]-1; with ck the compressed
+    keys those rows complete are written too, as means of what the cache stands for."""
+    _native().append_kv_quant(prm.packed(), k_new, v_new, kq, vq, seqlens, max_seqlen, ck)
+
+
+def sparse_attn_decode_quant(prm, q, kq, vq, seqlens, max_seqlen, block_idx, out=None, lse=None, workspace=None):
+    """sparse_attn_decode on a cache in 4 bits: q [B, 1, Hq, d] -> out bf16 [B, 1, Hq, d], lse fp32 [B, Hq]."""
+    return _native().sparse_attn_decode_quant(prm.packed(), q, kq, vq, seqlens, max_seqlen, block_idx, out, lse, workspace)
+
+
+def sparse_attn_verify_quant(prm, q, kq, vq, seqlens, max_seqlen, block_idx, tree_mask=None, out=None, lse=None, workspace=None):
+    """sparse_attn_verify on a cache in 4 bits: q [B, n_draft, Hq, d] -> out bf16 [B, n_draft, Hq, d], lse fp32 [B, n_draft, Hq]."""
+    return _native().sparse_attn_verify_quant(prm.packed(), q, kq, vq, seqlens, max_seqlen, block_idx, tree_mask, out, lse, workspace)
+
+
+# ---- attention over a sliding window and the first tokens ----------------------------------------------
+# The query at position i sees key t <= i when t < n_sink or i - t < window.
+
+def window_workspace_bytes(op, prm, n_sink, window, batch, max_seqlen):
+    return int(load_library().infllmv2_window_workspace_bytes(op, ctypes.byref(prm.c()), n_sink, window, batch, max_seqlen))
+
+
+def window_attn_prefill(prm, n_sink, window, q, k, v, seqlens, max_seqlen, out=None, lse=None, workspace=None):
+    """q [B, T, Hq, d] -> out bf16 [B, T, Hq, d], lse fp32 [B, max_seqlen, Hq]."""
+    return _native().window_attn_prefill(prm.packed(), n_sink, window, q, k, v, seqlens, max_seqlen, out, lse, workspace)
+
+
+def window_attn_bwd(prm, n_sink, window, q, k, v, out, dout, lse, seqlens, max_seqlen, dq=None, dk=None, dv=None, workspace=None):
+    """Backward of window_attn_prefill -> dq [B, T, Hq, d], dk, dv [B, Hkv, T, d] (bf16); results repeat bit for bit."""
+    return _native().window_attn_bwd(prm.packed(), n_sink, window, q, k, v, out, dout, lse, seqlens, max_seqlen, dq, dk, dv, workspace)
+
+
+def window_attn_decode(prm, n_sink, window, q, k, v, seqlens, max_seqlen, out=None, lse=None, workspace=None):
+    """The query at position seqlens[b]-1: q [B, 1, Hq, d] -> out bf16 [B, 1, Hq, d], lse fp32 [B, Hq]."""
+    return _native().window_attn_decode(prm.packed(), n_sink, window, q, k, v, seqlens, max_seqlen, out, lse, workspace)
+
+
+def window_attn_decode_quant(prm, n_sink, window, q, kq, vq, seqlens, max_seqlen, out=None, lse=None, workspace=None):
+    """The same on a cache in 4 bits."""
+    return _native().window_attn_decode_quant(prm.packed(), n_sink, window, q, kq, vq, seqlens, max_seqlen, out, lse, workspace)
 
 
 def select_blocks_shared(prm, q, ck, seqlens, max_seqlen, block_idx=None, workspace=None):

@@ -2,6 +2,7 @@
 // the kernel launchers.  See include/infllmv2.h for the contract of every entry point.
 #include "common.h"
 #include "internal.h"
+#include "quant.h"
 
 using namespace infllmv2;
 
@@ -83,6 +84,32 @@ Tensor make_tensor(const infllmv2_tensor *t) {
     r.sh = t->stride_h;
     r.st = t->stride_t;
     return r;
+}
+
+// a cache in 4 bits; strides in bytes
+int32_t check_quant(const infllmv2_quant_tensor *t) {
+    if (!t || !t->codes || !t->scales) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if ((reinterpret_cast<uintptr_t>(t->codes) & 15u) || (reinterpret_cast<uintptr_t>(t->scales) & 3u)) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const int64_t codes[3] = {t->stride_b, t->stride_h, t->stride_t}, scales[3] = {t->scale_stride_b, t->scale_stride_h, t->scale_stride_t};
+    for (int i = 0; i < 3; ++i)
+        if (codes[i] < 0 || scales[i] < 0 || codes[i] % 16 || scales[i] % 4) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    return INFLLMV2_OK;
+}
+
+QuantTensor make_quant(const infllmv2_quant_tensor *t) {
+    return QuantTensor{reinterpret_cast<uint8_t *>(t->codes), reinterpret_cast<uint8_t *>(t->scales), t->stride_b, t->stride_h, t->stride_t,
+                       t->scale_stride_b, t->scale_stride_h, t->scale_stride_t};
+}
+
+int32_t check_window(int32_t n_sink, int32_t window) { return n_sink < 0 || window < 1 ? INFLLMV2_ERR_INVALID_ARGUMENT : INFLLMV2_OK; }
+
+WindowArgs make_window(int32_t n_sink, int32_t window, int32_t max_seqlen) {   // (none of a sequence lies behind max_seqlen)
+    const int32_t most = max_seqlen > 1 ? max_seqlen : 1;
+    return WindowArgs{n_sink < most ? n_sink : most, window < most ? window : most};
+}
+
+int32_t check_workspace(const void *workspace, size_t bytes, size_t need) {
+    return need > 0 && (!workspace || bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) ? INFLLMV2_ERR_WORKSPACE : INFLLMV2_OK;
 }
 
 int32_t hip_status(int e) { return e == 0 ? INFLLMV2_OK : INFLLMV2_ERR_HIP; }
@@ -493,6 +520,197 @@ int32_t infllmv2_sparse_attn_decode(const infllmv2_params *prm, const infllmv2_t
         return INFLLMV2_ERR_WORKSPACE;
     return hip_status(launch_attn_decode(dm, tq, tk, tv, seqlens, block_idx, nullptr, tout, lse, workspace,
                                          reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2i_quantize_kv(const infllmv2_params *prm, const infllmv2_tensor *k, const infllmv2_tensor *v,
+                              const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_new_tokens,
+                              const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq, void *stream, int32_t fill) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_tensor(k));
+    RETURN_IF_ERR(check_tensor(v));
+    RETURN_IF_ERR(check_quant(kq));
+    RETURN_IF_ERR(check_quant(vq));
+    if (!seqlens) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    return hip_status(launch_quantize_kv(make_dims(prm, batch, max_seqlen, 1, fill), make_tensor(k), make_tensor(v), seqlens, n_new_tokens,
+                                         make_quant(kq), make_quant(vq), reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_quantize_kv(const infllmv2_params *prm, const infllmv2_tensor *k, const infllmv2_tensor *v,
+                             const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_new_tokens,
+                             const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq, void *stream) {
+    return infllmv2i_quantize_kv(prm, k, v, seqlens, batch, max_seqlen, n_new_tokens, kq, vq, stream, 0);
+}
+
+int32_t infllmv2i_dequantize_kv(const infllmv2_params *prm, const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq,
+                                const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_new_tokens,
+                                const infllmv2_tensor *k, const infllmv2_tensor *v, void *stream, int32_t fill) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_quant(kq));
+    RETURN_IF_ERR(check_quant(vq));
+    RETURN_IF_ERR(check_tensor(k));
+    RETURN_IF_ERR(check_tensor(v));
+    if (!seqlens) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    return hip_status(launch_dequantize_kv(make_dims(prm, batch, max_seqlen, 1, fill), make_quant(kq), make_quant(vq), seqlens, n_new_tokens,
+                                           make_tensor(k), make_tensor(v), reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_dequantize_kv(const infllmv2_params *prm, const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq,
+                               const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_new_tokens,
+                               const infllmv2_tensor *k, const infllmv2_tensor *v, void *stream) {
+    return infllmv2i_dequantize_kv(prm, kq, vq, seqlens, batch, max_seqlen, n_new_tokens, k, v, stream, 0);
+}
+
+int32_t infllmv2_append_kv_quant(const infllmv2_params *prm, const infllmv2_tensor *k_new, const infllmv2_tensor *v_new,
+                                 const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq, const infllmv2_tensor *ck,
+                                 const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_draft, void *stream) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_draft(batch, n_draft));
+    RETURN_IF_ERR(check_tensor(k_new));
+    RETURN_IF_ERR(check_tensor(v_new));
+    RETURN_IF_ERR(check_quant(kq));
+    RETURN_IF_ERR(check_quant(vq));
+    if (ck) RETURN_IF_ERR(check_tensor(ck));
+    if (!seqlens) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    Tensor ckt;
+    if (ck) ckt = make_tensor(ck);
+    return hip_status(launch_append_kv_quant(make_dims(prm, batch, max_seqlen, n_draft), make_tensor(k_new), make_tensor(v_new), make_quant(kq),
+                                             make_quant(vq), ck ? &ckt : nullptr, seqlens, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infllmv2_tensor *q, const infllmv2_quant_tensor *kq,
+                                          const infllmv2_quant_tensor *vq, const int32_t *seqlens, int32_t batch, int32_t max_seqlen,
+                                          int32_t n_draft, const uint64_t *tree_mask, const int32_t *block_idx,
+                                          const infllmv2_tensor *out, float *lse, void *workspace, size_t workspace_bytes,
+                                          void *stream) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_draft(batch, n_draft));
+    RETURN_IF_ERR(check_tensor(q));
+    RETURN_IF_ERR(check_quant(kq));
+    RETURN_IF_ERR(check_quant(vq));
+    RETURN_IF_ERR(check_tensor(out));
+    if (!seqlens || !block_idx || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (tree_mask && (reinterpret_cast<uintptr_t>(tree_mask) & 7u) != 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const Dims dm = make_dims(prm, batch, max_seqlen, n_draft);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, attn_decode_ws_bytes(dm)));
+    return hip_status(launch_attn_decode_quant(dm, make_tensor(q), make_quant(kq), make_quant(vq), seqlens, block_idx, tree_mask,
+                                               make_tensor(out), lse, workspace, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_sparse_attn_decode_quant(const infllmv2_params *prm, const infllmv2_tensor *q, const infllmv2_quant_tensor *kq,
+                                          const infllmv2_quant_tensor *vq, const int32_t *seqlens, int32_t batch, int32_t max_seqlen,
+                                          const int32_t *block_idx, const infllmv2_tensor *out, float *lse, void *workspace,
+                                          size_t workspace_bytes, void *stream) {
+    return infllmv2_sparse_attn_verify_quant(prm, q, kq, vq, seqlens, batch, max_seqlen, 1, nullptr, block_idx, out, lse, workspace,
+                                             workspace_bytes, stream);
+}
+
+size_t infllmv2_window_workspace_bytes(int32_t op, const infllmv2_params *prm, int32_t n_sink, int32_t window, int32_t batch,
+                                       int32_t max_seqlen) {
+    if (check_params(prm) != INFLLMV2_OK || check_window(n_sink, window) != INFLLMV2_OK || check_sizes(batch, max_seqlen) != INFLLMV2_OK) return 0;
+    const Dims dm = make_dims(prm, batch, max_seqlen);
+    const WindowArgs w = make_window(n_sink, window, max_seqlen);
+    switch (op) {
+        case INFLLMV2_OP_WINDOW_PREFILL: return window_prefill_ws_bytes(dm, w);
+        case INFLLMV2_OP_WINDOW_BWD: return window_bwd_ws_bytes(dm, w);
+        case INFLLMV2_OP_WINDOW_DECODE: return window_decode_ws_bytes(dm, w);
+    }
+    return 0;
+}
+
+int32_t infllmv2i_window_attn_prefill(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
+                                      const infllmv2_tensor *k, const infllmv2_tensor *v, const int32_t *seqlens, int32_t batch,
+                                      int32_t max_seqlen, const infllmv2_tensor *out, float *lse, void *workspace,
+                                      size_t workspace_bytes, void *stream, int32_t fill) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_window(n_sink, window));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_tensor(q));
+    RETURN_IF_ERR(check_tensor(k));
+    RETURN_IF_ERR(check_tensor(v));
+    RETURN_IF_ERR(check_tensor(out));
+    if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const Dims dm = make_dims(prm, batch, max_seqlen, 1, fill);
+    const WindowArgs w = make_window(n_sink, window, max_seqlen);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_prefill_ws_bytes(dm, w)));
+    return hip_status(launch_window_prefill(dm, w, make_tensor(q), make_tensor(k), make_tensor(v), seqlens, make_tensor(out), lse, workspace,
+                                            reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_window_attn_prefill(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
+                                     const infllmv2_tensor *k, const infllmv2_tensor *v, const int32_t *seqlens, int32_t batch,
+                                     int32_t max_seqlen, const infllmv2_tensor *out, float *lse, void *workspace,
+                                     size_t workspace_bytes, void *stream) {
+    return infllmv2i_window_attn_prefill(prm, n_sink, window, q, k, v, seqlens, batch, max_seqlen, out, lse, workspace, workspace_bytes, stream, 0);
+}
+
+int32_t infllmv2i_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
+                                  const infllmv2_tensor *k, const infllmv2_tensor *v, const infllmv2_tensor *out,
+                                  const infllmv2_tensor *dout, const float *lse, const int32_t *seqlens, int32_t batch,
+                                  int32_t max_seqlen, const infllmv2_tensor *dq, const infllmv2_tensor *dk,
+                                  const infllmv2_tensor *dv, void *workspace, size_t workspace_bytes, void *stream, int32_t fill) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_window(n_sink, window));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    const infllmv2_tensor *ts[8] = {q, k, v, out, dout, dq, dk, dv};
+    for (int i = 0; i < 8; ++i) RETURN_IF_ERR(check_tensor(ts[i]));
+    if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const Dims dm = make_dims(prm, batch, max_seqlen, 1, fill);
+    const WindowArgs w = make_window(n_sink, window, max_seqlen);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_bwd_ws_bytes(dm, w)));
+    return hip_status(launch_window_bwd(dm, w, make_tensor(q), make_tensor(k), make_tensor(v), make_tensor(out), make_tensor(dout), lse,
+                                        seqlens, make_tensor(dq), make_tensor(dk), make_tensor(dv), workspace,
+                                        reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
+                                 const infllmv2_tensor *k, const infllmv2_tensor *v, const infllmv2_tensor *out,
+                                 const infllmv2_tensor *dout, const float *lse, const int32_t *seqlens, int32_t batch,
+                                 int32_t max_seqlen, const infllmv2_tensor *dq, const infllmv2_tensor *dk,
+                                 const infllmv2_tensor *dv, void *workspace, size_t workspace_bytes, void *stream) {
+    return infllmv2i_window_attn_bwd(prm, n_sink, window, q, k, v, out, dout, lse, seqlens, batch, max_seqlen, dq, dk, dv, workspace,
+                                     workspace_bytes, stream, 0);
+}
+
+int32_t infllmv2_window_attn_decode(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
+                                    const infllmv2_tensor *k, const infllmv2_tensor *v, const int32_t *seqlens, int32_t batch,
+                                    int32_t max_seqlen, const infllmv2_tensor *out, float *lse, void *workspace,
+                                    size_t workspace_bytes, void *stream) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_window(n_sink, window));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_tensor(q));
+    RETURN_IF_ERR(check_tensor(k));
+    RETURN_IF_ERR(check_tensor(v));
+    RETURN_IF_ERR(check_tensor(out));
+    if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const Dims dm = make_dims(prm, batch, max_seqlen);
+    const WindowArgs w = make_window(n_sink, window, max_seqlen);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_decode_ws_bytes(dm, w)));
+    return hip_status(launch_window_decode(dm, w, make_tensor(q), make_tensor(k), make_tensor(v), seqlens, make_tensor(out), lse, workspace,
+                                           reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
+                                          const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq, const int32_t *seqlens,
+                                          int32_t batch, int32_t max_seqlen, const infllmv2_tensor *out, float *lse, void *workspace,
+                                          size_t workspace_bytes, void *stream) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_window(n_sink, window));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_tensor(q));
+    RETURN_IF_ERR(check_quant(kq));
+    RETURN_IF_ERR(check_quant(vq));
+    RETURN_IF_ERR(check_tensor(out));
+    if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const Dims dm = make_dims(prm, batch, max_seqlen);
+    const WindowArgs w = make_window(n_sink, window, max_seqlen);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_decode_ws_bytes(dm, w)));
+    return hip_status(launch_window_decode_quant(dm, w, make_tensor(q), make_quant(kq), make_quant(vq), seqlens, make_tensor(out), lse,
+                                                 workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

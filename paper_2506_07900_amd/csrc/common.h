@@ -80,6 +80,25 @@ __host__ __device__ inline int32_t num_coarse(int32_t n, int32_t rho) {
     return n < 2 * rho - 1 ? 0 : (n - (2 * rho - 1)) / rho + 1;
 }
 
+__device__ inline int clamp_len(int32_t L, int32_t cap) { return L < 0 ? 0 : (L > cap ? cap : L); }
+
+// Every decode-side kernel works on "query rows": row bv = b * n_q + qi is query token qi of sequence b.
+// Plain decode has n_q = 1.  Draft verification (section 4.1, "InfLLM v2 for Target Model") has the
+// n_q drafted tokens in the last n_q cache rows; token qi sits at position seqlens[b] - n_q + qi and
+// selects blocks like any query at that position.  Returns the number of cache rows up to and
+// including the query (0: the row is skipped; a sequence shorter than n_q is skipped as a whole).
+__device__ inline int query_row(const Dims &dm, const int32_t *__restrict__ seqlens, int bv, int &b, int &qi) {
+    if (dm.n_q == 1) {
+        b = bv;
+        qi = 0;
+        return clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
+    }
+    b = (int)__umulhi((uint32_t)bv, dm.n_q_inv);
+    qi = bv - b * dm.n_q;
+    const int L_all = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
+    return L_all < dm.n_q ? 0 : L_all - (dm.n_q - 1 - qi);
+}
+
 // fp64 -> bf16, round to nearest even with a single rounding: first round-to-odd to fp32
 // (24 bits keep a sticky bit), then nearest-even to 8 bits.
 __device__ inline uint16_t f64_to_bf16_rne(double x) {
@@ -574,6 +593,8 @@ int launch_attn_decode(const Dims &dm, Tensor q, Tensor k, Tensor v, const int32
                        const int32_t *block_idx, const uint64_t *tree_mask, Tensor out, float *lse, void *ws,
                        hipStream_t stream);
 size_t attn_decode_ws_bytes(const Dims &dm);
+int launch_decode_merge(const Dims &dm, const float *o_part, const float2 *ml_part, Tensor out, float *lse,
+                        hipStream_t stream);              // dm.topk partials per query head, at most 64
 int launch_attn_bwd(const Dims &dm, Tensor q, Tensor k, Tensor v, Tensor out, Tensor dout, const float *lse,
                     const int32_t *seqlens, const int32_t *block_idx, Tensor dq, Tensor dk, Tensor dv, void *ws,
                     hipStream_t stream);

@@ -25,25 +25,6 @@
 
 namespace infllmv2 {
 
-__device__ inline int clamp_len(int32_t L, int32_t cap) { return L < 0 ? 0 : (L > cap ? cap : L); }
-
-// Every kernel below works on "query rows": row bv = b * n_q + qi is query token qi of sequence b.
-// Plain decode has n_q = 1.  Draft verification (section 4.1, "InfLLM v2 for Target Model") has the
-// n_q drafted tokens in the last n_q cache rows; token qi sits at position seqlens[b] - n_q + qi and
-// selects blocks like any query at that position.  Returns the number of cache rows up to and
-// including the query (0: the row is skipped; a sequence shorter than n_q is skipped as a whole).
-__device__ inline int query_row(const Dims &dm, const int32_t *__restrict__ seqlens, int bv, int &b, int &qi) {
-    if (dm.n_q == 1) {
-        b = bv;
-        qi = 0;
-        return clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
-    }
-    b = (int)__umulhi((uint32_t)bv, dm.n_q_inv);
-    qi = bv - b * dm.n_q;
-    const int L_all = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
-    return L_all < dm.n_q ? 0 : L_all - (dm.n_q - 1 - qi);
-}
-
 // Query operands of parts 1 and 2.  MFMA operand layout: lane (n, g) holds head n, channels
 // 32*ks + 8*g .. +7.  One query per workgroup: straight from memory.  Several (verification): every
 // wave needs the same rows and every workgroup of the launch the same few cache lines, so the
@@ -1738,7 +1719,7 @@ static void launch_decode_partial(const Dims &dm, Tensor q, Tensor k, Tensor v, 
     timing_end(stream);
 }
 
-static int launch_decode_merge(const Dims &dm, const float *o_part, const float2 *ml_part, Tensor out, float *lse,
+int launch_decode_merge(const Dims &dm, const float *o_part, const float2 *ml_part, Tensor out, float *lse,
                                hipStream_t stream) {
     timing_begin("decode_merge_kernel", stream);
     const dim3 grid(dm.Hq, dm.n_q, dm.batch), block(64);

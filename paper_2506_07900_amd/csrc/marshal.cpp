@@ -43,6 +43,16 @@ struct Library {
     INFLLMV2_FNI(select_blocks);
     INFLLMV2_FNI(sparse_attn_prefill);
     INFLLMV2_FNI(sparse_attn_bwd);
+    INFLLMV2_FN(append_kv_quant);
+    INFLLMV2_FN(sparse_attn_decode_quant);
+    INFLLMV2_FN(sparse_attn_verify_quant);
+    INFLLMV2_FN(window_workspace_bytes);
+    INFLLMV2_FN(window_attn_decode);
+    INFLLMV2_FN(window_attn_decode_quant);
+    INFLLMV2_FNI(quantize_kv);
+    INFLLMV2_FNI(dequantize_kv);
+    INFLLMV2_FNI(window_attn_prefill);
+    INFLLMV2_FNI(window_attn_bwd);
 #undef INFLLMV2_FN
 #undef INFLLMV2_FNI
 } lib;
@@ -386,6 +396,293 @@ PyObject *sparse_attn_bwd(Args a) {
     return tuple3(dq, dk, dv);
 }
 
+// ---- the 4-bit cache and the windowed attention -------------------------------------------------------------------------
+// These calls check shapes and devices as well: a tensor has the sizes that the library takes it to have and lies on
+// the current device, whose stream the call goes to.
+void expect(bool ok, const char *name, const char *what) {
+    if (!ok) throw MarshalError(std::string(name) + what);
+}
+void here(const at::Tensor &t, const char *name) {
+    expect(t.is_cuda() && t.device().index() == c10::hip::getCurrentHIPStream().device_index(), name, " must be on the current device");
+}
+const at::Tensor &query(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_params *prm) {       // B < 0: any
+    const at::Tensor &t = bf16_4d(o, name);
+    here(t, name);
+    expect((B < 0 || t.size(0) == B) && t.size(1) >= T && q_shaped(t, prm), name, " must be [batch, tokens, n_q_heads, head_dim]");
+    return t;
+}
+const at::Tensor &kv(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_params *prm) {
+    const at::Tensor &t = bf16_4d(o, name);
+    here(t, name);
+    expect((B < 0 || t.size(0) == B) && t.size(2) >= T && k_shaped(t, prm), name, " must be [batch, n_kv_heads, tokens, head_dim]");
+    return t;
+}
+// (codes uint8 [B, Hkv, T, d / 2], scales uint8 [B, Hkv, T, d / 32])
+struct Quant {
+    at::Tensor codes, scales;
+    infllmv2_quant_tensor desc() const {
+        return {codes.data_ptr(), scales.data_ptr(), codes.stride(0), codes.stride(1), codes.stride(2),
+                scales.stride(0), scales.stride(1), scales.stride(2)};
+    }
+};
+Quant quant(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_params *prm) {
+    expect(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 2, name, " must be a pair (codes, scales)");
+    Quant q{tensor(PyTuple_GET_ITEM(o, 0), name), tensor(PyTuple_GET_ITEM(o, 1), name)};
+    const at::Tensor *ts[2] = {&q.codes, &q.scales};
+    for (int i = 0; i < 2; ++i) {
+        const at::Tensor &t = *ts[i];
+        expect(t.scalar_type() == at::kByte && t.dim() == 4 && t.stride(3) == 1, name, ": codes and scales must be 4-d uint8 tensors with a contiguous last axis");
+        here(t, name);
+        expect((B < 0 || t.size(0) == B) && t.size(1) == prm->n_kv_heads && t.size(2) >= T && t.size(3) == prm->head_dim / (i ? 32 : 2), name,
+               " must be codes [batch, n_kv_heads, tokens, head_dim / 2], scales [batch, n_kv_heads, tokens, head_dim / 32]");
+    }
+    expect(q.codes.size(0) == q.scales.size(0), name, ": codes and scales differ in batch");
+    return q;
+}
+const int32_t *lengths(PyObject *o, int64_t B) {
+    const int32_t *p = i32(o, "seqlens");
+    here(THPVariable_Unpack(o), "seqlens");
+    expect(THPVariable_Unpack(o).numel() == B, "seqlens", " must be [batch]");
+    return p;
+}
+float *lse_of(const at::Tensor &t, int64_t n) {
+    here(t, "lse");
+    expect(t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == n, "lse", " must be a contiguous fp32 device tensor of a value per row and head");
+    return static_cast<float *>(t.data_ptr());
+}
+const int32_t *blocks(PyObject *o, int64_t n) {
+    const int32_t *p = i32(o, "block_idx");
+    here(THPVariable_Unpack(o), "block_idx");
+    expect(THPVariable_Unpack(o).numel() == n, "block_idx", " must be [batch, n_kv_heads, queries, topk]");
+    return p;
+}
+Workspace scratch(PyObject *o, size_t need, const at::Tensor &device_of) {
+    if (o != Py_None) {
+        here(tensor(o, "workspace"), "workspace");
+        expect(tensor(o, "workspace").is_contiguous(), "workspace", " must be contiguous");
+    }
+    return Workspace(o, need, device_of);
+}
+// out and lse of an attention call: the caller's, or made here
+struct Attended {
+    Result out, lse;
+    infllmv2_tensor od;
+    float *lp;
+    int32_t fill;
+    Attended(PyObject *o, PyObject *l, const at::Tensor &q, int64_t T, at::IntArrayRef lse_shape, bool may_fill, const infllmv2_params *prm)
+        : out(o), lse(l), fill(may_fill && out.make() && lse.make() && q.size(1) == T) {
+        const bool whole = fill || (!may_fill && q.size(1) == T);        // every row is written
+        int64_t n = 1;
+        for (const int64_t x : lse_shape) n *= x;
+        if (out.make()) out.own = whole ? at::empty_like(q) : at::zeros_like(q);
+        if (lse.make()) lse.own = whole ? at::empty(lse_shape, like(q, at::kFloat)) : at::zeros(lse_shape, like(q, at::kFloat));
+        od = rows(out.make() ? out.own : query(out.given, "out", q.size(0), T, prm));
+        lp = lse_of(lse.make() ? lse.own : tensor(lse.given, "lse"), n);
+    }
+};
+int32_t capacity(PyObject *o) {
+    const int32_t T = integer(o);
+    expect(T >= 0, "max_seqlen", " must not be negative");
+    return T;
+}
+
+PyObject *quant_pair(Quant &a, Quant &b, PyObject *make) {  // (codes, scales) twice, through `make`: binding.QuantCache
+    PyObject *r = PyTuple_New(2);
+    Quant *q[2] = {&a, &b};
+    for (int i = 0; i < 2; ++i) {
+        PyObject *codes = THPVariable_Wrap(q[i]->codes), *scales = THPVariable_Wrap(q[i]->scales);
+        PyObject *pair = PyObject_CallFunctionObjArgs(make, codes, scales, nullptr);
+        Py_DECREF(codes);
+        Py_DECREF(scales);
+        if (!pair) {
+            Py_DECREF(r);
+            throw python_error();
+        }
+        PyTuple_SET_ITEM(r, i, pair);
+    }
+    return r;
+}
+
+// (prm, k, v, seqlens, max_seqlen, (kq, vq) | None, n_new_tokens, QuantCache) -> (kq, vq)
+PyObject *quantize_kv(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t T = capacity(a[4]), n_new = integer(a[6]);
+    const at::Tensor &k = kv(a[1], "k", -1, T, prm), &v = kv(a[2], "v", k.size(0), T, prm);
+    const int64_t B = k.size(0);
+    Quant kq, vq;
+    const bool make = a[5] == Py_None;
+    const int32_t fill = make && n_new <= 0 && k.size(2) == T;      // the call clears the rows behind a sequence itself
+    if (make) {
+        Quant *q[2] = {&kq, &vq};
+        for (int i = 0; i < 2; ++i) {
+            const at::IntArrayRef::value_type codes[4] = {B, k.size(1), k.size(2), k.size(3) / 2}, scales[4] = {B, k.size(1), k.size(2), k.size(3) / 32};
+            q[i]->codes = fill ? at::empty(codes, like(k, at::kByte)) : at::zeros(codes, like(k, at::kByte));
+            q[i]->scales = fill ? at::empty(scales, like(k, at::kByte)) : at::zeros(scales, like(k, at::kByte));
+        }
+    } else {
+        expect(PyTuple_Check(a[5]) && PyTuple_GET_SIZE(a[5]) == 2, "kq, vq", " must both be given");
+        kq = quant(PyTuple_GET_ITEM(a[5], 0), "kq", B, T, prm);
+        vq = quant(PyTuple_GET_ITEM(a[5], 1), "vq", B, T, prm);
+    }
+    const infllmv2_tensor kd = cache(k), vd = cache(v);
+    const infllmv2_quant_tensor kqd = kq.desc(), vqd = vq.desc();
+    const int32_t *sl = lengths(a[3], B);
+    run("infllmv2_quantize_kv",
+        [&] { return lib.quantize_kv(prm, &kd, &vd, sl, static_cast<int32_t>(B), T, n_new, &kqd, &vqd, current_stream(), fill); });
+    return quant_pair(kq, vq, a[7]);
+}
+
+// (prm, kq, vq, seqlens, max_seqlen, k | None, v | None, n_new_tokens)
+PyObject *dequantize_kv(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t T = capacity(a[4]), n_new = integer(a[7]);
+    const Quant kq = quant(a[1], "kq", -1, T, prm), vq = quant(a[2], "vq", kq.codes.size(0), T, prm);
+    const int64_t B = kq.codes.size(0);
+    Result k(a[5]), v(a[6]);
+    const int32_t fill = k.make() && v.make() && n_new <= 0;
+    const at::IntArrayRef::value_type shape[4] = {B, kq.codes.size(1), T, prm->head_dim};
+    for (Result *r : {&k, &v})
+        if (r->make()) r->own = fill ? at::empty(shape, like(kq.codes, at::kBFloat16)) : at::zeros(shape, like(kq.codes, at::kBFloat16));
+    const infllmv2_tensor kd = cache(k.make() ? k.own : kv(k.given, "k", B, T, prm)), vd = cache(v.make() ? v.own : kv(v.given, "v", B, T, prm));
+    const infllmv2_quant_tensor kqd = kq.desc(), vqd = vq.desc();
+    const int32_t *sl = lengths(a[3], B);
+    run("infllmv2_dequantize_kv",
+        [&] { return lib.dequantize_kv(prm, &kqd, &vqd, sl, static_cast<int32_t>(B), T, n_new, &kd, &vd, current_stream(), fill); });
+    return tuple2(k, v);
+}
+
+// (prm, k_new, v_new, kq, vq, seqlens, max_seqlen, ck | None)
+PyObject *append_kv_quant(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t T = capacity(a[6]);
+    const at::Tensor &kn = kv(a[1], "k_new", -1, 0, prm);
+    const int64_t B = kn.size(0), n = kn.size(2);
+    const at::Tensor &vn = kv(a[2], "v_new", B, n, prm);
+    expect(vn.size(2) == n, "v_new", " must have the rows of k_new");
+    const Quant kq = quant(a[3], "kq", B, T, prm), vq = quant(a[4], "vq", B, T, prm);
+    infllmv2_tensor ck{};
+    if (a[7] != Py_None) {
+        const bool some = prm->kernel_size > 0 && prm->kernel_stride > 0 && T >= prm->kernel_size;
+        ck = cache(kv(a[7], "ck", B, some ? (T - prm->kernel_size) / prm->kernel_stride + 1 : 0, prm));
+    }
+    const infllmv2_tensor knd = cache(kn), vnd = cache(vn);
+    const infllmv2_quant_tensor kqd = kq.desc(), vqd = vq.desc();
+    const int32_t *sl = lengths(a[5], B);
+    run("infllmv2_append_kv_quant", [&] {
+        return lib.append_kv_quant(prm, &knd, &vnd, &kqd, &vqd, a[7] != Py_None ? &ck : nullptr, sl, static_cast<int32_t>(B), T,
+                                   static_cast<int32_t>(n), current_stream());
+    });
+    Py_RETURN_NONE;
+}
+
+// (prm, q, kq, vq, seqlens, max_seqlen, block_idx, out | None, lse | None, workspace | None)
+PyObject *sparse_attn_decode_quant(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t T = capacity(a[5]);
+    const at::Tensor &q = query(a[1], "q", -1, 1, prm);
+    expect(q.size(1) == 1, "q", " must have one row per sequence");
+    const int32_t B = static_cast<int32_t>(q.size(0));
+    const infllmv2_quant_tensor kq = quant(a[2], "kq", B, T, prm).desc(), vq = quant(a[3], "vq", B, T, prm).desc();
+    const int32_t *sl = lengths(a[4], B), *ip = blocks(a[6], static_cast<int64_t>(B) * prm->n_kv_heads * prm->topk);
+    Attended r(a[7], a[8], q, 1, {B, prm->n_q_heads}, false, prm);
+    const Workspace ws = scratch(a[9], a[9] == Py_None ? lib.workspace_bytes(INFLLMV2_OP_ATTN_DECODE, prm, B, T) : 0, q);
+    const infllmv2_tensor qd = rows(q);
+    run("infllmv2_sparse_attn_decode_quant", [&] {
+        return lib.sparse_attn_decode_quant(prm, &qd, &kq, &vq, sl, B, T, ip, &r.od, r.lp, ws.ptr, ws.bytes, current_stream());
+    });
+    return tuple2(r.out, r.lse);
+}
+
+// (prm, q, kq, vq, seqlens, max_seqlen, block_idx, tree_mask | None, out | None, lse | None, workspace | None)
+PyObject *sparse_attn_verify_quant(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t T = capacity(a[5]);
+    const at::Tensor &q = query(a[1], "q", -1, 1, prm);
+    const int32_t B = static_cast<int32_t>(q.size(0)), n = static_cast<int32_t>(q.size(1));
+    const infllmv2_quant_tensor kq = quant(a[2], "kq", B, T, prm).desc(), vq = quant(a[3], "vq", B, T, prm).desc();
+    const int32_t *sl = lengths(a[4], B), *ip = blocks(a[6], static_cast<int64_t>(B) * prm->n_kv_heads * n * prm->topk);
+    const uint64_t *mask = tree_mask(a[7], B, n);
+    if (mask) here(tensor(a[7], "tree_mask"), "tree_mask");
+    Attended r(a[8], a[9], q, n, {B, n, prm->n_q_heads}, false, prm);
+    const Workspace ws = scratch(a[10], a[10] == Py_None ? lib.verify_workspace_bytes(INFLLMV2_OP_ATTN_VERIFY, prm, B, T, n) : 0, q);
+    const infllmv2_tensor qd = rows(q);
+    run("infllmv2_sparse_attn_verify_quant", [&] {
+        return lib.sparse_attn_verify_quant(prm, &qd, &kq, &vq, sl, B, T, n, mask, ip, &r.od, r.lp, ws.ptr, ws.bytes, current_stream());
+    });
+    return tuple2(r.out, r.lse);
+}
+
+// (prm, n_sink, window, q, k, v, seqlens, max_seqlen, out | None, lse | None, workspace | None)
+PyObject *window_attn_prefill(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t sink = integer(a[1]), window = integer(a[2]), T = capacity(a[7]);
+    const at::Tensor &q = query(a[3], "q", -1, T, prm);
+    const int32_t B = static_cast<int32_t>(q.size(0));
+    const infllmv2_tensor kd = cache(kv(a[4], "k", B, T, prm)), vd = cache(kv(a[5], "v", B, T, prm));
+    const int32_t *sl = lengths(a[6], B);
+    Attended r(a[8], a[9], q, T, {B, T, prm->n_q_heads}, true, prm);
+    const Workspace ws = scratch(a[10], a[10] == Py_None ? lib.window_workspace_bytes(INFLLMV2_OP_WINDOW_PREFILL, prm, sink, window, B, T) : 0, q);
+    const infllmv2_tensor qd = rows(q);
+    run("infllmv2_window_attn_prefill", [&] {
+        return lib.window_attn_prefill(prm, sink, window, &qd, &kd, &vd, sl, B, T, &r.od, r.lp, ws.ptr, ws.bytes, current_stream(), r.fill);
+    });
+    return tuple2(r.out, r.lse);
+}
+
+// (prm, n_sink, window, q, k, v, out, dout, lse, seqlens, max_seqlen, dq | None, dk | None, dv | None, workspace | None)
+PyObject *window_attn_bwd(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t sink = integer(a[1]), window = integer(a[2]), T = capacity(a[10]);
+    const at::Tensor &q = query(a[3], "q", -1, T, prm);
+    const int32_t B = static_cast<int32_t>(q.size(0));
+    const at::Tensor &k = kv(a[4], "k", B, T, prm), &v = kv(a[5], "v", B, T, prm);
+    const infllmv2_tensor od = rows(query(a[6], "out", B, T, prm)), gd = rows(query(a[7], "dout", B, T, prm));
+    const float *lp = lse_of(tensor(a[8], "lse"), static_cast<int64_t>(B) * T * prm->n_q_heads);
+    const int32_t *sl = lengths(a[9], B);
+    Result dq(a[11]), dk(a[12]), dv(a[13]);
+    const bool fill = dq.make() && dk.make() && dv.make() && q.size(1) == T && k.size(2) == T && v.size(2) == T;   // (as in the forward)
+    if (dq.make()) dq.own = fill ? at::empty_like(q) : at::zeros_like(q);
+    if (dk.make()) dk.own = fill ? at::empty_like(k) : at::zeros_like(k);
+    if (dv.make()) dv.own = fill ? at::empty_like(v) : at::zeros_like(v);
+    const Workspace ws = scratch(a[14], a[14] == Py_None ? lib.window_workspace_bytes(INFLLMV2_OP_WINDOW_BWD, prm, sink, window, B, T) : 0, q);
+    const infllmv2_tensor qd = rows(q), kd = cache(k), vd = cache(v), dqd = rows(dq.make() ? dq.own : query(dq.given, "dq", B, T, prm)),
+                          dkd = cache(dk.make() ? dk.own : kv(dk.given, "dk", B, T, prm)),
+                          dvd = cache(dv.make() ? dv.own : kv(dv.given, "dv", B, T, prm));
+    run("infllmv2_window_attn_bwd", [&] {
+        return lib.window_attn_bwd(prm, sink, window, &qd, &kd, &vd, &od, &gd, lp, sl, B, T, &dqd, &dkd, &dvd, ws.ptr, ws.bytes,
+                                   current_stream(), fill);
+    });
+    return tuple3(dq, dk, dv);
+}
+
+// (prm, n_sink, window, q, k, v, seqlens, max_seqlen, out | None, lse | None, workspace | None); k, v of either kind
+template <bool kQuant>
+PyObject *window_decode(Args a) {
+    const infllmv2_params *prm = params(a[0]);
+    const int32_t sink = integer(a[1]), window = integer(a[2]), T = capacity(a[7]);
+    const at::Tensor &q = query(a[3], "q", -1, 1, prm);
+    expect(q.size(1) == 1, "q", " must have one row per sequence");
+    const int32_t B = static_cast<int32_t>(q.size(0));
+    const int32_t *sl = lengths(a[6], B);
+    Attended r(a[8], a[9], q, 1, {B, prm->n_q_heads}, false, prm);
+    const Workspace ws = scratch(a[10], a[10] == Py_None ? lib.window_workspace_bytes(INFLLMV2_OP_WINDOW_DECODE, prm, sink, window, B, T) : 0, q);
+    const infllmv2_tensor qd = rows(q);
+    if constexpr (kQuant) {
+        const infllmv2_quant_tensor kq = quant(a[4], "kq", B, T, prm).desc(), vq = quant(a[5], "vq", B, T, prm).desc();
+        run("infllmv2_window_attn_decode_quant", [&] {
+            return lib.window_attn_decode_quant(prm, sink, window, &qd, &kq, &vq, sl, B, T, &r.od, r.lp, ws.ptr, ws.bytes, current_stream());
+        });
+    } else {
+        const infllmv2_tensor kd = cache(kv(a[4], "k", B, T, prm)), vd = cache(kv(a[5], "v", B, T, prm));
+        run("infllmv2_window_attn_decode", [&] {
+            return lib.window_attn_decode(prm, sink, window, &qd, &kd, &vd, sl, B, T, &r.od, r.lp, ws.ptr, ws.bytes, current_stream());
+        });
+    }
+    return tuple2(r.out, r.lse);
+}
+PyObject *window_attn_decode(Args a) { return window_decode<false>(a); }
+PyObject *window_attn_decode_quant(Args a) { return window_decode<true>(a); }
+
 // (path, error class): the library every later call goes through
 PyObject *bind(Args a) {
     const char *path = PyUnicode_AsUTF8(a[0]);
@@ -409,6 +706,16 @@ PyObject *bind(Args a) {
     symbol(handle, "infllmv2i_select_blocks", l.select_blocks);
     symbol(handle, "infllmv2i_sparse_attn_prefill", l.sparse_attn_prefill);
     symbol(handle, "infllmv2i_sparse_attn_bwd", l.sparse_attn_bwd);
+    symbol(handle, "infllmv2_append_kv_quant", l.append_kv_quant);
+    symbol(handle, "infllmv2_sparse_attn_decode_quant", l.sparse_attn_decode_quant);
+    symbol(handle, "infllmv2_sparse_attn_verify_quant", l.sparse_attn_verify_quant);
+    symbol(handle, "infllmv2_window_workspace_bytes", l.window_workspace_bytes);
+    symbol(handle, "infllmv2_window_attn_decode", l.window_attn_decode);
+    symbol(handle, "infllmv2_window_attn_decode_quant", l.window_attn_decode_quant);
+    symbol(handle, "infllmv2i_quantize_kv", l.quantize_kv);
+    symbol(handle, "infllmv2i_dequantize_kv", l.dequantize_kv);
+    symbol(handle, "infllmv2i_window_attn_prefill", l.window_attn_prefill);
+    symbol(handle, "infllmv2i_window_attn_bwd", l.window_attn_bwd);
     lib = l;
     Py_RETURN_NONE;
 }
@@ -443,6 +750,15 @@ PyMethodDef methods[] = {
     METHOD(decode_step, 13),
     METHOD(verify_step, 14),
     METHOD(sparse_attn_bwd, 14),
+    METHOD(quantize_kv, 8),
+    METHOD(dequantize_kv, 8),
+    METHOD(append_kv_quant, 8),
+    METHOD(sparse_attn_decode_quant, 10),
+    METHOD(sparse_attn_verify_quant, 11),
+    METHOD(window_attn_prefill, 11),
+    METHOD(window_attn_bwd, 15),
+    METHOD(window_attn_decode, 11),
+    METHOD(window_attn_decode_quant, 11),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

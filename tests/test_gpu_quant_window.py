@@ -1,0 +1,456 @@
+"""The 4-bit cache and the windowed attention against plain 64-bit computations of their definitions.
+
+Tolerances, derived from the roundings of the calls (half a step of bf16 is 2^-8 of a value):
+  outputs     a probability is rounded to bf16 once, the output once: 2^-8 (sum p |v| + |o|), a sixteenth more for the fp32 sums
+              and the scores' own rounding (a dot product of 128 exact products is off by at most 2^-17 of the sum of their sizes, which moves a
+              probability by that much: 2^-13 at sizes of 16)
+  log-sum-exp 2^-17 of the largest logit's sum of sizes, and 2^-20 for the sum's, the exponentials' and the logarithm's roundings, and the result's
+              own rounding
+  dv          as an output: 2^-8 (sum p |dout| + |dv|)
+  dq, dk      ds is rounded to bf16 once and the result once: 2^-8 (sum |ds| |k| + |dq|); ds itself comes from a difference of two fp32 sums, off by
+              2^-17 of their terms' sizes
+  4 bits      exact: codes, exponents and values are equal
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_07900_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+D = 128
+HALF = 2.0 ** -8
+GARBAGE = float("nan")
+
+
+def normal(gen, *shape, scale=1.0):
+    return (torch.randn(shape, generator=gen, device="cuda") * scale).bfloat16()
+
+
+def lengths_tensor(lengths):
+    return torch.tensor(lengths, dtype=torch.int32, device="cuda")
+
+
+# ---- the format -------------------------------------------------------------------------------------------------
+
+VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def encode(x):
+    """[.., 128] floats -> codes [.., 64], exponents [.., 4], values [.., 128], by search in 64 bits"""
+    x = np.asarray(x, np.float64)
+    g = x.reshape(-1, 32)
+    finite = np.isfinite(g).all(-1)
+    most = np.where(finite, np.abs(np.where(np.isfinite(g), g, 0.0)).max(-1), 1.0)
+    frac, e = np.frexp(np.where(most > 0, most, 1.0))              # 0.5 <= frac < 1
+    e = np.where(most > 0, np.where(frac >= 0.875, e, e - 1), -1000)
+    byte = np.where(finite, np.clip(e + 127 - 2, 2, 252), 255)
+    unit = np.where(finite, 2.0 ** (np.minimum(byte, 254) - 127.0), 1.0)
+    y = np.abs(np.where(finite[:, None], g, 0.0)) / unit[:, None]
+    gap = np.abs(y[..., None] - VALUES)
+    odd = np.arange(8) % 2
+    index = np.lexsort((np.broadcast_to(odd, gap.shape), gap), axis=-1)[..., 0]
+    sign = np.where(finite[:, None], np.signbit(g), False)
+    code = (index + 8 * sign).astype(np.uint8)
+    value = np.where(finite[:, None], VALUES[index] * unit[:, None] * np.where(sign, -1.0, 1.0), np.nan)
+    code = code.reshape(*x.shape[:-1], 64, 2)
+    return code[..., 0] | (code[..., 1] << 4), byte.astype(np.uint8).reshape(*x.shape[:-1], 4), value.reshape(x.shape)
+
+
+def values_of(c):
+    """QuantCache -> fp64 values on its device"""
+    nibble = torch.stack((c.codes & 15, c.codes >> 4), -1).flatten(-2).long()
+    table = torch.tensor(np.concatenate((VALUES, -VALUES)), device=c.codes.device)
+    scale = torch.where(c.scales == 255, math.nan, torch.exp2(c.scales.double() - 127))
+    return table[nibble] * scale.repeat_interleave(32, -1)
+
+
+def test_every_number_is_rounded_to_the_nearest_code():
+    # all 65536 bit patterns, in groups of neighbours (equal exponents: all ties), shuffled within 2^12 of each other (exponents that
+    # differ by a few), and one large number per group of the others
+    bits = torch.arange(65536, dtype=torch.int32)
+    order = torch.cat([torch.randperm(4096, generator=torch.Generator().manual_seed(i)) + 4096 * i for i in range(16)])
+    large = bits.clone().reshape(-1, 32)
+    finite = (large & 0x7f80) < 0x7d80                             # (four binades above: still a number)
+    large[:, 5] = torch.where(finite.all(-1), (large[:, 5] & 0x7f80) + 0x200 + (large[:, 7] & 0x7f), large[:, 5])
+    for x in (bits, bits[order], large.reshape(-1)):
+        k = torch.from_numpy(x.numpy().astype(np.uint16).view(np.int16)).view(torch.bfloat16).reshape(1, 1, 512, D)
+        prm = binding.Params(1, 1)
+        kq, vq = binding.quantize_kv(prm, k.cuda(), (-k).cuda(), lengths_tensor([512]), 512)
+        want = encode(k.double().numpy())
+        minus = encode((-k).double().numpy())
+        for got, ref in ((kq, want), (vq, minus)):
+            assert np.array_equal(got.scales.cpu().numpy(), ref[1])
+            assert np.array_equal(got.codes.cpu().numpy(), ref[0])
+        back, backv = binding.dequantize_kv(prm, kq, vq, lengths_tensor([512]), 512)
+        assert np.array_equal(back.double().cpu().numpy(), want[2], equal_nan=True)
+        assert np.array_equal(backv.double().cpu().numpy(), minus[2], equal_nan=True)
+        # nothing is clipped, so a value is off by half the grid's widest step (4 to 6) at most; but for magnitudes above 1.75 x 2^127, which the next
+        # larger exponent would read back as infinite: up to 8 units become 6
+        ok = np.isfinite(want[2])
+        err = np.abs(k.double().numpy() - want[2])[ok].reshape(-1)
+        byte = np.repeat(want[1].astype(float), 32, -1).reshape(k.shape)[ok].reshape(-1)
+        assert (err <= 2.0 ** (byte - 127) * np.where(byte == 252, 2, 1)).all()
+
+
+@pytest.mark.parametrize("lengths,n_new", [([1], 0), ([0, 5, 64, 65, 200], 0), ([777, 0, 33], 0), ([777, 3, 0], 7), ([128], 200), ([300, 299], 64)])
+def test_quantize_rows(lengths, n_new):
+    gen = torch.Generator(device="cuda").manual_seed(sum(lengths) + n_new)
+    B, H, T = len(lengths), 3, max(max(lengths), 1)
+    prm = binding.Params(6, 3)
+    # heads and tokens in another order in memory than in the tensor
+    k = normal(gen, B, T + 5, H, D).transpose(1, 2)
+    v = normal(gen, H, B, T + 5, D).transpose(0, 1)
+    for b, n in enumerate(lengths):
+        k[b, :, n:], v[b, :, n:] = GARBAGE, GARBAGE
+    base = [torch.randint(0, 255, (B, H, T + 2, w), dtype=torch.uint8, generator=gen, device="cuda") for w in (80, 8, 64, 4)]
+    kq = binding.QuantCache(base[0][..., 16:80], base[1][..., 4:8])
+    vq = binding.QuantCache(base[2], base[3])
+    before = [x.clone() for x in base]
+    sl = lengths_tensor(lengths)
+    binding.quantize_kv(prm, k, v, sl, T, kq, vq, n_new_tokens=n_new)
+    kb = normal(gen, B, H, T + 1, D)
+    vb = normal(gen, B, T + 1, H, D).transpose(1, 2)
+    kept = kb.clone(), vb.clone()
+    binding.dequantize_kv(prm, kq, vq, sl, T, kb, vb, n_new_tokens=n_new)
+    made = binding.quantize_kv(prm, k, v, sl, T)                   # results made by the call: rows behind a sequence are 0
+    read = binding.dequantize_kv(prm, *made, sl, T)
+    want = encode(k.double().cpu().numpy()), encode(v.double().cpu().numpy())
+    for (codes, scales, values), got, back, old, make, rd in zip(want, (kq, vq), (kb, vb), kept, made, read):
+        for b, n in enumerate(lengths):
+            lo = max(0, n - n_new) if n_new > 0 else 0
+            assert np.array_equal(got.codes[b, :, lo:n].cpu().numpy(), codes[b, :, lo:n])
+            assert np.array_equal(got.scales[b, :, lo:n].cpu().numpy(), scales[b, :, lo:n])
+            assert np.array_equal(back[b, :, lo:n].double().cpu().numpy(), values[b, :, lo:n])
+            assert torch.equal(back[b, :, :lo], old[b, :, :lo]) and torch.equal(back[b, :, n:], old[b, :, n:])
+            assert np.array_equal(make.codes[b, :, :n].cpu().numpy(), codes[b, :, :n]) and not make.codes[b, :, n:].any()
+            assert not make.scales[b, :, n:].any() and not rd[b, :, n:].any()
+            assert np.array_equal(rd[b, :, :n].double().cpu().numpy(), values[b, :, :n])
+    for x, y, (lo_c, hi_c) in zip(base, before, ((16, 80), (4, 8), (0, 64), (0, 4))):
+        for b, n in enumerate(lengths):
+            lo = max(0, n - n_new) if n_new > 0 else 0
+            x[b, :, lo:n, lo_c:hi_c] = y[b, :, lo:n, lo_c:hi_c]
+        assert torch.equal(x, y)                                   # nothing else was written
+
+
+@pytest.mark.parametrize("n", [1, 2, 5, 16, 17, 33, 64])
+@pytest.mark.parametrize("with_ck", [True, False])
+def test_append(n, with_ck):
+    # lengths around the completion of a kernel, a sequence that is too short for n rows, one longer than the cache
+    lengths = [n, n + 15, n + 31, n + 32, 256, 255, 200, max(0, n - 1), 300]
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    B, H, T = len(lengths), 2, 256
+    prm = binding.Params(8, 2)
+    k, v = normal(gen, B, H, T, D), normal(gen, B, H, T, D, scale=3.0)
+    sl = lengths_tensor(lengths)
+    old = [max(0, min(x, T) - n) for x in lengths]
+    kq, vq = binding.quantize_kv(prm, k, v, lengths_tensor(old), T)
+    ck = torch.full((B, H, 15, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    before = [x.clone() for x in (*kq, *vq)], ck.clone()
+    new = normal(gen, B, n, H, D).transpose(1, 2), normal(gen, B, H, n + 1, D)[:, :, :n]
+    binding.append_kv_quant(prm, *new, kq, vq, sl, T, ck=ck if with_ck else None)
+    for b, length in enumerate(lengths):
+        if length < n or length > T:
+            for x, y in zip((*kq, *vq), before[0]):
+                assert torch.equal(x[b], y[b])
+            assert torch.equal(ck[b], before[1][b])
+            continue
+        whole_k, whole_v = k[b, :, :length].clone(), v[b, :, :length].clone()
+        whole_k[:, length - n:], whole_v[:, length - n:] = new[0][b], new[1][b]
+        for got, x in ((kq, whole_k), (vq, whole_v)):
+            codes, scales, _ = encode(x.double().cpu().numpy())
+            assert np.array_equal(got.codes[b, :, :length].cpu().numpy(), codes)
+            assert np.array_equal(got.scales[b, :, :length].cpu().numpy(), scales)
+            assert not got.codes[b, :, length:].any() and not got.scales[b, :, length:].any()
+    if with_ck:                                                    # the kernels of the cache as it is read back
+        inside = lengths_tensor([x if n <= x <= T else 0 for x in lengths])
+        kb, _ = binding.dequantize_kv(prm, kq, vq, inside, T)
+        want = before[1].clone()
+        binding.compress_keys(prm, kb, inside, T, ck=want, n_new_tokens=n)
+        assert torch.equal(ck.view(torch.int16), want.view(torch.int16))
+
+
+# ---- attention --------------------------------------------------------------------------------------------------
+
+def attend(q, k, v, seen, scale):
+    """q [R, D], k, v [K, D], seen [R, K] in fp64 -> out, lse, and the sizes their tolerances are measured in"""
+    s = (q @ k.t().contiguous()) * scale
+    size = (q.abs() @ k.abs().t().contiguous()) * scale
+    s = torch.where(seen, s, -math.inf)
+    top = s.amax(-1, keepdim=True)
+    p = torch.exp(s - torch.where(top == -math.inf, 0.0, top))
+    total = p.sum(-1, keepdim=True)
+    w = p / torch.where(total > 0, total, 1.0)
+    v = torch.where(seen.any(0)[:, None], v, 0.0)
+    lse = (torch.where(top == -math.inf, 0.0, top) + torch.log(total))[:, 0]
+    return w @ v, lse, w @ v.abs(), torch.where(seen, size, 0.0).amax(-1)
+
+
+def check(got, got_lse, want):
+    o, lse, mag, size = want
+    got, got_lse = got.double(), got_lse.double()
+    tol = 1.0625 * HALF * (mag + o.abs()) + 1e-30
+    assert ((got - o).abs() <= tol).all(), float(((got - o).abs() / tol).max())
+    empty = lse == -math.inf
+    assert torch.equal(got_lse == -math.inf, empty)
+    tol = 2.0 ** -17 * size + 2.0 ** -20 + 2.0 ** -23 * lse.abs()
+    diff = torch.where(empty, 0.0, (got_lse - lse).abs())
+    assert (diff <= torch.where(empty, 1.0, tol)).all(), float(diff.max())
+
+
+def window_seen(pos, length, n_sink, window, device="cuda"):
+    t, i = torch.arange(length, device=device)[None], pos[:, None]
+    return (t <= i) & ((t < n_sink) | (i - t < window))
+
+
+def random_cache(gen, B, H, T, lengths, spoil=True):
+    k, v = normal(gen, B, H, T, D), normal(gen, B, T, H, D).transpose(1, 2)
+    if spoil:
+        for b, n in enumerate(lengths):
+            k[b, :, n:], v[b, :, n:] = GARBAGE, GARBAGE
+    return k, v
+
+
+def quant_of(prm, k, v, lengths):
+    """the cache in 4 bits; rows behind a sequence stand for NaN"""
+    kq, vq = binding.quantize_kv(prm, k, v, lengths_tensor(lengths), k.shape[2])
+    for c in (kq, vq):
+        for b, n in enumerate(lengths):
+            c.codes[b, :, n:], c.scales[b, :, n:] = 0x77, 255
+    return kq, vq
+
+
+DECODE_CASES = [  # G, Hkv, lengths, n_sink, window
+    (16, 2, [1, 2, 31, 32, 33, 64, 65, 0], 4, 40),
+    (1, 3, [100, 1, 97], 0, 1),
+    (2, 1, [500, 77], 33, 64),
+    (4, 1, [2000], 4, 256),
+    (8, 2, [1999, 1, 640], 100, 10000),
+    (16, 1, [5000, 4097, 4096], 64, 4096),
+    (16, 4, [333] * 5, 400, 7),
+    (16, 2, [30011], 128, 8192),
+]
+
+
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", DECODE_CASES)
+@pytest.mark.parametrize("quant", [False, True])
+def test_window_decode(G, H, lengths, n_sink, window, quant):
+    gen = torch.Generator(device="cuda").manual_seed(G * 1000 + window)
+    B, T = len(lengths), max(lengths) + 3
+    prm = binding.Params(G * H, H)
+    k, v = random_cache(gen, B, H, T, lengths, spoil=False)
+    masked = [(min(n_sink, n), max(min(n_sink, n), n - window)) for n in lengths]     # rows no query sees
+    q = normal(gen, B, G * H, 1, D).transpose(1, 2)
+    sl = lengths_tensor(lengths)
+    if quant:
+        kq, vq = quant_of(prm, k, v, lengths)
+        for b, (lo, hi) in enumerate(masked):
+            for c in (kq, vq):
+                c.scales[b, :, lo:hi] = 255
+        out, lse = binding.window_attn_decode_quant(prm, n_sink, window, q, kq, vq, sl, T)
+        k64, v64 = values_of(kq), values_of(vq)
+    else:
+        for b, (lo, hi) in enumerate(masked):
+            k[b, :, lo:hi], v[b, :, lo:hi] = GARBAGE, math.inf
+            k[b, :, lengths[b]:], v[b, :, lengths[b]:] = math.inf, GARBAGE
+        out, lse = binding.window_attn_decode(prm, n_sink, window, q, k, v, sl, T)
+        k64, v64 = k.double(), v.double()
+    assert out.shape == (B, 1, G * H, D) and lse.shape == (B, G * H)
+    for b, n in enumerate(lengths):
+        for h in range(H):
+            rows = slice(h * G, (h + 1) * G)
+            if n == 0:
+                assert not out[b, 0, rows].any() and (lse[b, rows] == -math.inf).all()
+                continue
+            seen = window_seen(torch.tensor([n - 1], device="cuda"), n, n_sink, window).expand(G, n)
+            at = seen[0].nonzero()[:, 0]
+            check(out[b, 0, rows], lse[b, rows], attend(q[b, 0, rows].double(), k64[b, h, at], v64[b, h, at], seen[:, at], prm.softmax_scale))
+
+
+def block_lists(gen, lengths, H, n, topk, holes):
+    idx = torch.full((len(lengths), H, n, topk), -1, dtype=torch.int32)
+    rng = np.random.default_rng(int(torch.randint(0, 1 << 30, (1,), generator=gen, device="cuda")))
+    for b, length in enumerate(lengths):
+        for h in range(H):
+            for i in range(n):
+                own = max(0, length - n + i) // 64
+                some = rng.permutation(own + 1)[:topk]
+                if len(some) and own not in some:
+                    some[0] = own
+                if holes:
+                    some = some[rng.random(len(some)) < 0.7]
+                some = np.sort(some)
+                idx[b, h, i, :len(some)] = torch.from_numpy(some.astype(np.int32))
+                if holes and topk > len(some):
+                    idx[b, h, i, topk - 1] = 1 << 25               # a block far behind the query: skipped
+    return idx.cuda()
+
+
+@pytest.mark.parametrize("G,H,lengths,topk,holes", [
+    (16, 2, [1, 63, 64, 65, 1000, 0], 8, False), (1, 2, [777, 3], 3, True), (2, 3, [4000], 64, False), (4, 1, [130, 2048, 517], 5, True),
+    (8, 2, [9000, 64], 16, False), (16, 1, [20000] * 3, 64, True), (16, 2, [5000] * 40, 12, False)])
+def test_sparse_decode_quant(G, H, lengths, topk, holes):
+    gen = torch.Generator(device="cuda").manual_seed(G + topk)
+    B, T = len(lengths), max(lengths)
+    prm = binding.Params(G * H, H, topk=topk)
+    k, v = random_cache(gen, B, H, T, lengths, spoil=False)
+    kq, vq = quant_of(prm, k, v, lengths)
+    q = normal(gen, B, 1, G * H, D)
+    idx = block_lists(gen, lengths, H, 1, topk, holes)
+    out, lse = binding.sparse_attn_decode_quant(prm, q, kq, vq, lengths_tensor(lengths), T, idx)
+    k64, v64 = values_of(kq), values_of(vq)
+    for b, n in enumerate(lengths):
+        for h in range(H):
+            rows = slice(h * G, (h + 1) * G)
+            chosen = [j for j in idx[b, h, 0].tolist() if 0 <= j < (n + 63) // 64]
+            at = torch.tensor([t for j in chosen for t in range(64 * j, min(n, 64 * j + 64))], dtype=torch.long, device="cuda")
+            if len(at) == 0:
+                assert not out[b, 0, rows].any() and (lse[b, rows] == -math.inf).all()
+                continue
+            seen = torch.ones((G, len(at)), dtype=torch.bool, device="cuda")
+            check(out[b, 0, rows], lse[b, rows], attend(q[b, 0, rows].double(), k64[b, h, at], v64[b, h, at], seen, prm.softmax_scale))
+
+
+@pytest.mark.parametrize("G,H,lengths,n,topk,kind", [
+    (16, 2, [300, 70, 16, 15], 16, 8, "tree"), (4, 1, [1000, 999], 2, 16, "chain"), (8, 2, [640, 641], 64, 3, "random"),
+    (1, 2, [500], 5, 8, "empty"), (16, 1, [4096, 64, 63], 64, 12, "tree"), (2, 1, [333], 33, 4, "random")])
+def test_sparse_verify_quant(G, H, lengths, n, topk, kind):
+    gen = torch.Generator(device="cuda").manual_seed(n + topk)
+    rng = np.random.default_rng(n)
+    B, T = len(lengths), max(lengths) + 1
+    prm = binding.Params(G * H, H, topk=topk)
+    k, v = random_cache(gen, B, H, T, lengths, spoil=False)
+    kq, vq = quant_of(prm, k, v, lengths)
+    q = normal(gen, B, n, G * H, D)
+    idx = block_lists(gen, lengths, H, n, topk, True)
+    words = np.zeros((B, n), np.uint64)
+    for b in range(B):
+        for t in range(n):
+            if kind == "tree":
+                words[b, t] = (words[b, rng.integers(0, t)] if t else np.uint64(0)) | np.uint64(1) << np.uint64(t)
+            elif kind == "random":                                 # any bits, those from n on ignored
+                words[b, t] = rng.integers(0, 1 << 64, dtype=np.uint64)
+    mask = None if kind == "chain" else torch.from_numpy(words.view(np.int64)).cuda()
+    if kind == "empty":                                            # lists of the drafted tokens' own block only, masks of nothing
+        idx[:] = -1
+        idx[..., 0] = (torch.tensor(lengths) // 64).int().cuda()[:, None, None]
+        lengths = [length // 64 * 64 + n for length in lengths]
+        T = max(T, max(lengths))
+        k, v = random_cache(gen, B, H, T, lengths, spoil=False)
+        kq, vq = quant_of(prm, k, v, lengths)
+    out, lse = binding.sparse_attn_verify_quant(prm, q, kq, vq, lengths_tensor(lengths), T, idx, tree_mask=mask)
+    k64, v64 = values_of(kq), values_of(vq)
+    for b, length in enumerate(lengths):
+        for h in range(H):
+            rows = slice(h * G, (h + 1) * G)
+            for i in range(n):
+                if length < n:
+                    assert not out[b, i, rows].any() and (lse[b, i, rows] == -math.inf).all()
+                    continue
+                first, ts = length - n, []
+                for j in idx[b, h, i].tolist():
+                    for t in range(64 * j, min(64 * j + 64, length)) if j >= 0 else ():
+                        if (t <= first + i) if mask is None else (t < first or int(words[b, i]) >> (t - first) & 1):
+                            ts.append(t)
+                if not ts:
+                    assert not out[b, i, rows].any() and (lse[b, i, rows] == -math.inf).all()
+                    continue
+                at = torch.tensor(ts, device="cuda")
+                seen = torch.ones((G, len(at)), dtype=torch.bool, device="cuda")
+                check(out[b, i, rows], lse[b, i, rows], attend(q[b, i, rows].double(), k64[b, h, at], v64[b, h, at], seen, prm.softmax_scale))
+
+
+PREFILL_CASES = [  # G, Hkv, lengths, n_sink, window
+    (1, 1, [1], 0, 1), (16, 2, [1, 7, 8, 9, 0], 1, 3), (1, 2, [300, 129, 128], 0, 1), (2, 1, [500], 4, 50),
+    (4, 1, [777], 4, 256), (8, 2, [640, 333], 64, 100), (16, 2, [700, 1], 100, 64), (16, 1, [513], 600, 5),
+    (4, 3, [400, 65], 0, 100000), (8, 1, [1500], 33, 1000), (2, 2, [1100], 130, 129), (16, 1, [1030], 0, 512),
+]
+
+
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", PREFILL_CASES)
+def test_window_prefill(G, H, lengths, n_sink, window):
+    gen = torch.Generator(device="cuda").manual_seed(G * 100 + window)
+    B, T = len(lengths), max(lengths) + 2
+    prm = binding.Params(G * H, H)
+    k, v = random_cache(gen, B, H, T, lengths)
+    q = normal(gen, B, G * H, T, D).transpose(1, 2)
+    for b, n in enumerate(lengths):
+        q[b, n:] = GARBAGE
+    sl = lengths_tensor(lengths)
+    out, lse = binding.window_attn_prefill(prm, n_sink, window, q, k, v, sl, T)
+    own = torch.full((B, T + 1, G * H + 1, D), 9.0, dtype=torch.bfloat16, device="cuda")
+    own_lse = torch.full((B, T, G * H), 9.0, dtype=torch.float32, device="cuda")
+    binding.window_attn_prefill(prm, n_sink, window, q, k, v, sl, T, out=own[:, :, 1:], lse=own_lse)
+    for b, n in enumerate(lengths):
+        assert not out[b, n:].any() and not lse[b, n:].any()       # made by the call: cleared
+        assert (own[b, n:] == 9).all() and (own[b, :, 0] == 9).all() and (own_lse[b, n:] == 9).all()   # the caller's: left alone
+        assert torch.equal(own[b, :n, 1:], out[b, :n]) and torch.equal(own_lse[b, :n], lse[b, :n])
+        for hq in range(G * H):
+            if n:
+                seen = window_seen(torch.arange(n, device="cuda"), n, n_sink, window)
+                check(out[b, :n, hq], lse[b, :n, hq],
+                      attend(q[b, :n, hq].double(), k[b, hq // G, :n].double(), v[b, hq // G, :n].double(), seen, prm.softmax_scale))
+
+
+def bwd_reference(q, k, v, out, dout, lse, seen, scale):
+    """one head in fp64 -> (dq, dk, dv) and their tolerances"""
+    s = (q @ k.t().contiguous()) * scale
+    p = torch.where(seen, torch.exp(s - lse[:, None]), 0.0)
+    dp = dout @ v.t().contiguous()
+    d = (dout * out).sum(-1, keepdim=True)
+    ds = p * (dp - d)
+    rough = p * (dout.abs() @ v.abs().t().contiguous() + (dout * out).abs().sum(-1, keepdim=True))
+    move = 2.0 ** -17 * (q.abs() @ k.abs().t().contiguous()) * scale + 2.0 ** -22 * lse.abs()[:, None]   # of a probability
+    t = lambda x: x.t().contiguous()
+    err = HALF * ds.abs() + 2.0 ** -16 * rough + move * ds.abs()
+    errp = (HALF + move) * p
+    return ((ds @ k) * scale, t(ds) @ q * scale, t(p) @ dout,
+            (err @ k.abs()) * scale, t(err) @ q.abs() * scale, t(errp) @ dout.abs())
+
+
+BWD_CASES = PREFILL_CASES + [(16, 2, [1200, 900], 4, 100), (4, 1, [2100], 200, 1500)]
+
+
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", BWD_CASES)
+def test_window_bwd(G, H, lengths, n_sink, window):
+    gen = torch.Generator(device="cuda").manual_seed(G * 10 + window)
+    B, T = len(lengths), max(lengths) + 2
+    prm = binding.Params(G * H, H)
+    k, v = random_cache(gen, B, H, T, lengths)
+    q, dout = normal(gen, B, G * H, T, D).transpose(1, 2), normal(gen, B, T, G * H, D)
+    for b, n in enumerate(lengths):
+        q[b, n:], dout[b, n:] = GARBAGE, GARBAGE
+    sl = lengths_tensor(lengths)
+    out, lse = binding.window_attn_prefill(prm, n_sink, window, q, k, v, sl, T)
+    for b, n in enumerate(lengths):
+        out[b, n:], lse[b, n:] = GARBAGE, GARBAGE
+    grads = binding.window_attn_bwd(prm, n_sink, window, q, k, v, out, dout, lse, sl, T)
+    again = [torch.full_like(x, 9.0) for x in grads]
+    need = binding.window_workspace_bytes(binding.OP_WINDOW_BWD, prm, n_sink, window, B, T)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    binding.window_attn_bwd(prm, n_sink, window, q, k, v, out, dout, lse, sl, T, dq=again[0], dk=again[1], dv=again[2], workspace=ws)
+    for b, n in enumerate(lengths):
+        assert not grads[0][b, n:].any() and not grads[1][b, :, n:].any() and not grads[2][b, :, n:].any()
+        assert (again[0][b, n:] == 9).all() and (again[1][b, :, n:] == 9).all() and (again[2][b, :, n:] == 9).all()
+        assert torch.equal(again[0][b, :n], grads[0][b, :n])       # results repeat
+        assert all(torch.equal(x[b, :, :n], y[b, :, :n]) for x, y in zip(again[1:], grads[1:]))
+        if n == 0:
+            continue
+        seen = window_seen(torch.arange(n, device="cuda"), n, n_sink, window)
+        for h in range(H):
+            sums = None
+            for hq in range(h * G, (h + 1) * G):
+                x = [y.double() for y in (q[b, :n, hq], k[b, h, :n], v[b, h, :n], out[b, :n, hq], dout[b, :n, hq], lse[b, :n, hq])]
+                r = bwd_reference(*x, seen, prm.softmax_scale)
+                tol = 1.0625 * r[3] + HALF * r[0].abs() + 1e-30
+                diff = (grads[0][b, :n, hq].double() - r[0]).abs()
+                assert (diff <= tol).all(), ("dq", float((diff / tol).max()))
+                part = r[1:3] + r[4:6]
+                sums = part if sums is None else [a + c for a, c in zip(sums, part)]
+            for name, got, want, err in (("dk", grads[1], sums[0], sums[2]), ("dv", grads[2], sums[1], sums[3])):
+                tol = 1.0625 * err + HALF * want.abs() + 1e-30
+                diff = (got[b, h, :n].double() - want).abs()
+                assert (diff <= tol).all(), (name, float((diff / tol).max()))
