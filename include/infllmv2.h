@@ -455,6 +455,8 @@ int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infl
  * infllmv2_window_attn_decode   the query at position seqlens[b]-1: q, out [batch, 1, Hq, d], lse fp32 [batch, Hq]; a sequence with
  *                               seqlens[b] < 1 gets out 0, lse -inf.
  * infllmv2_window_attn_decode_quant  the same on a cache in 4 bits.
+ * Prefill and backward: stride_t of k and v at most 2^23 elements; backward: of q and dout as well, and group size x their
+ * stride_h at most 2^29, else INFLLMV2_ERR_UNSUPPORTED.
  * Workspaces: infllmv2_window_workspace_bytes(INFLLMV2_OP_WINDOW_*, ...) bytes, 256-byte aligned (0: none needed, or the arguments are
  * invalid); INFLLMV2_OP_WINDOW_DECODE for both decode calls.
  */

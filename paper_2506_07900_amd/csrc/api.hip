@@ -108,6 +108,18 @@ WindowArgs make_window(int32_t n_sink, int32_t window, int32_t max_seqlen) {   /
     return WindowArgs{n_sink < most ? n_sink : most, window < most ? window : most};
 }
 
+// the prefill and backward kernels address a tile's rows with 32-bit offsets: tokens of k, v, and in the backward of q and dout and
+// their heads of a group
+int32_t check_spans(const infllmv2_params *p, const infllmv2_tensor *k, const infllmv2_tensor *v, const infllmv2_tensor *q, const infllmv2_tensor *dout) {
+    const infllmv2_tensor *ts[4] = {k, v, q, dout};
+    for (int i = 0; i < 4; ++i) {
+        if (!ts[i]) continue;
+        if (ts[i]->stride_t > kMaxTokenStride) return INFLLMV2_ERR_UNSUPPORTED;
+        if (i >= 2 && (p->n_q_heads / p->n_kv_heads) * ts[i]->stride_h > kMaxHeadSpan) return INFLLMV2_ERR_UNSUPPORTED;
+    }
+    return INFLLMV2_OK;
+}
+
 int32_t check_workspace(const void *workspace, size_t bytes, size_t need) {
     return need > 0 && (!workspace || bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) ? INFLLMV2_ERR_WORKSPACE : INFLLMV2_OK;
 }
@@ -633,6 +645,7 @@ int32_t infllmv2i_window_attn_prefill(const infllmv2_params *prm, int32_t n_sink
     RETURN_IF_ERR(check_tensor(v));
     RETURN_IF_ERR(check_tensor(out));
     if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_spans(prm, k, v, nullptr, nullptr));
     const Dims dm = make_dims(prm, batch, max_seqlen, 1, fill);
     const WindowArgs w = make_window(n_sink, window, max_seqlen);
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_prefill_ws_bytes(dm, w)));
@@ -658,6 +671,7 @@ int32_t infllmv2i_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, in
     const infllmv2_tensor *ts[8] = {q, k, v, out, dout, dq, dk, dv};
     for (int i = 0; i < 8; ++i) RETURN_IF_ERR(check_tensor(ts[i]));
     if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_spans(prm, k, v, q, dout));
     const Dims dm = make_dims(prm, batch, max_seqlen, 1, fill);
     const WindowArgs w = make_window(n_sink, window, max_seqlen);
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_bwd_ws_bytes(dm, w)));

@@ -64,6 +64,8 @@ int launch_window_decode(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tenso
                          void *ws, hipStream_t stream);
 int launch_window_decode_quant(const Dims &dm, WindowArgs w, Tensor q, QuantTensor kq, QuantTensor vq, const int32_t *seqlens,
                                Tensor out, float *lse, void *ws, hipStream_t stream);
+// The prefill and backward kernels address rows with 32-bit offsets from a tile's first: what the strides of a call may be.
+constexpr int64_t kMaxTokenStride = 1ll << 23, kMaxHeadSpan = 1ll << 29;   // elements; of a token, and of the heads of a group
 size_t window_prefill_ws_bytes(const Dims &dm, WindowArgs w);
 int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v, const int32_t *seqlens, Tensor out, float *lse,
                           void *ws, hipStream_t stream);

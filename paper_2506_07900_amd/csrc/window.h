@@ -22,26 +22,39 @@ __device__ __forceinline__ float half_reduce(float v, F f) {
     return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
-// Operand reads of 32x32x16 products from a tile of 256-byte rows (swizzled, see row_swizzle).  Lane = 32 hf + c.
+// 32 rows of 128 channels in LDS, as operands of 32x32x16 products: four quarters of 32 channels, in each 32 rows of 64 bytes, whose four 16-byte
+// pieces are XORed with the row's second bit pair.  A row operand takes one piece of 32 rows, a transposing load 32 bytes of each of 4
+// consecutive rows; both touch every bank once, and what changes from one operand to the next is a constant (with whole rows of 256
+// bytes it is an exclusive or, a register and an instruction each).
+constexpr int kHalfTile = 32 * 256;
 struct TileReader {
-    uint32_t row_at, col_at;
-    __device__ __forceinline__ explicit TileReader(int lane) {
-        const uint32_t ln = lane, hf = ln >> 5;
-        row_at = (ln & 31) * 256u + ((hf ^ (uint32_t)row_swizzle((int)(ln & 15))) << 4);
-        const uint32_t t_r = 4u * hf + ((ln & 15) >> 2), t_c = 2u * ((ln >> 4) & 1) + ((ln & 3) >> 1);
-        col_at = t_r * 256u + ((t_c ^ (uint32_t)row_swizzle((int)t_r)) << 4) + 8u * (ln & 1);
+    uint32_t row_at[2], col_at[2];
+    __device__ __forceinline__ explicit TileReader(int lane) {           // lane = 32 hf + c
+        const uint32_t ln = lane, hf = ln >> 5, r = ln & 31, t_r = 4u * hf + ((ln & 15) >> 2), t_c = 2u * ((ln >> 4) & 1) + ((ln & 3) >> 1);
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            row_at[i] = r * 64u + (((2u * i + hf) ^ ((r >> 2) & 3u)) << 4);
+            col_at[i] = (8u * i + t_r) * 64u + ((t_c ^ (2u * i + (t_r >> 2))) << 4) + 8u * (ln & 1);
+        }
     }
-    // row c of the 32 from `tile` on, channels 16 ks + 8 hf .. +7
+    // row c, channels 16 ks + 8 hf .. +7
     __device__ __forceinline__ bf16x8 rows(const char *tile, int ks) const {
-        return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4_t *>(tile + (row_at ^ (uint32_t)(ks << 5))));
+        return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4_t *>(tile + (row_at[ks & 1] + (ks >> 1) * 2048)));
     }
     // channel 32 ct + c of rows 16 s + 4 hf .. +3 and 16 s + 8 + 4 hf .. +3: the rows a lane holds of a product's result
     __device__ __forceinline__ bf16x8 columns(const char *tile, int s, int ct) const {
-        const s16x4 x0 = lds_read_tr16(tile + ((col_at ^ (uint32_t)(ct << 6)) + 16 * s * 256u));
-        const s16x4 x1 = lds_read_tr16(tile + ((col_at ^ (uint32_t)((ct << 6) | (2 << 4))) + (16 * s + 8) * 256u));
+        const s16x4 x0 = lds_read_tr16(tile + (col_at[0] + ct * 2048 + s * 1024));
+        const s16x4 x1 = lds_read_tr16(tile + (col_at[1] + ct * 2048 + s * 1024));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
+// Filling it: a copy is 1 KiB, 16 rows of a quarter; lane l brings row l / 4, and of the quarter's four pieces this one.
+__device__ __forceinline__ int copy_piece(int lane) { return (lane & 3) ^ ((lane >> 4) & 3); }
+constexpr uint32_t kNoRow = 0xffffffffu;                 // an offset that lies outside: reads 0
+__device__ __forceinline__ void copy_rows(char *to, const char *base, uint32_t offset, uint32_t more) {
+    const auto src = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0xfffffffeu, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void *)to, 16, (int)offset, (int)more, 0, 0);
+}
 
 // Entries 8 s .. 8 s + 7 of a product's result as the second operand of the next product: rows 16 s + 4 hf .. and 16 s + 8 + 4 hf ..
 __device__ __forceinline__ bf16x8 pack8(const f32x16 &x, int s) {
@@ -63,6 +76,38 @@ struct KeyTiles {
     }
     __device__ __forceinline__ int key0(int i) const { return kWinKeys * (i < sinks ? i : first + i - sinks); }
 };
+
+// Whether the query at position i sees a key.  No branches: a wavefront tests sixteen keys at a time.
+struct VisibleKeys {
+    int i;
+    uint32_t window, sinks;
+    __device__ __forceinline__ VisibleKeys(WindowArgs w, int i) : i(i), window(w.window), sinks(min(w.n_sink, i + 1)) {}
+    __device__ __forceinline__ bool operator()(int t) const { return ((uint32_t)(i - t) < window) | ((uint32_t)t < sinks); }
+};
+
+// Tiles of 64 keys or values, and their copies by a workgroup of four wavefronts, wavefront w the quarter w of the channels.
+struct __align__(16) Tile64 {
+    char x[2 * kHalfTile];
+};
+struct TileCopier {
+    const char *head;                                    // the head's first row, at this wavefront's channels
+    uint32_t step, at;                                   // bytes from row to row; of this lane's row and piece
+    int L;
+    __device__ __forceinline__ TileCopier(const Tensor &t, int b, int h, int L, int wave, int lane) : L(L) {
+        head = reinterpret_cast<const char *>(t.ptr + b * t.sb + h * t.sh) + 64 * wave;
+        step = 2 * (uint32_t)t.st;
+        at = (lane >> 2) * step + 16 * copy_piece(lane);
+    }
+    // rows r0 .. r0 + 63; those past the sequence as zeros
+    __device__ __forceinline__ void copy(Tile64 &dst, int r0, int wave, int lane) const {
+        const char *base = head + (int64_t)r0 * step;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            copy_rows(dst.x + ((j >> 1) * kHalfTile + wave * 2048 + (j & 1) * 1024), base, r0 + 16 * j + (lane >> 2) < L ? at : kNoRow, 16 * j * step);
+    }
+};
+// The largest of three numbers, one instruction (fmaxf first makes the results of a product canonical, an instruction each).  NaN if any is.
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
 // Workgroups in runs of neighbours per XCD (the hardware deals them to the eight XCDs in turn): neighbours read the same keys, which then
 // lie in one L2.

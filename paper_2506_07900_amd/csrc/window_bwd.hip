@@ -9,15 +9,17 @@
 namespace infllmv2 {
 
 constexpr int kDqRows = 128;
-struct __align__(16) DqTile {
-    char k[kWinKeys * 256], v[kWinKeys * 256];
+struct KVTile {
+    Tile64 k, v;
 };
 
-// rows: (lse in powers of two, D) of row (token, head of the group), [batch, Hkv, max_seqlen * G]
+// What the forward leaves of a row (token, head of the group): its log-sum-exp in powers of two and D, 32 and 32 floats for 32 rows.
+__host__ __device__ static inline int64_t row_blocks(const Dims &dm) { return ((int64_t)dm.max_seqlen * dm.G + 31) / 32; }   // per (sequence, head)
+
 __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, Tensor q, Tensor k,
                                                            Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
-                                                           const int32_t *__restrict__ seqlens, Tensor dq, float2 *__restrict__ rows) {
-    __shared__ DqTile tile0, tile1;
+                                                           const int32_t *__restrict__ seqlens, Tensor dq, float *__restrict__ rows) {
+    __shared__ KVTile tile0, tile1;
     const int id = xcd_run(blockIdx.x, gridDim.x);
     const int ti = id % n_tiles, bh = id / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -32,20 +34,11 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
         return;
     }
     const KeyTiles kt(win, t0, t1);
-    const char *k_head = reinterpret_cast<const char *>(k.ptr + b * k.sb + h * k.sh), *v_head = reinterpret_cast<const char *>(v.ptr + b * v.sb + h * v.sh);
-    auto stage = [&](DqTile &dst, int x) __attribute__((always_inline)) {
+    const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
+    auto stage = [&](KVTile &dst, int x) __attribute__((always_inline)) {
         if (x >= kt.count) return;
-        const int k0 = kt.key0(x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {                    // (as in the forward)
-            const int r = 16 * wave + 4 * j + (lane >> 4);
-            const int64_t t = min(k0 + r, L - 1);
-            const int piece = 16 * ((lane & 15) ^ row_swizzle(r));
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(k_head + t * (2 * k.st) + piece),
-                                             (__attribute__((address_space(3))) void *)(dst.k + (16 * wave + 4 * j) * 256), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(v_head + t * (2 * v.st) + piece),
-                                             (__attribute__((address_space(3))) void *)(dst.v + (16 * wave + 4 * j) * 256), 16, 0, 0);
-        }
+        keys.copy(dst.k, kt.key0(x), wave, lane);
+        values.copy(dst.v, kt.key0(x), wave, lane);
     };
     stage(tile0, 0);
     bf16x8 qf[8], gf[8];
@@ -65,7 +58,8 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
         }
         D = half_reduce(D, [](float a, float d) { return a + d; });
         ref = lse[((int64_t)b * dm.max_seqlen + t) * dm.Hq + hq] * kLog2e;
-        if (hf == 0 && i < L) rows[((int64_t)bh * dm.max_seqlen + i) * dm.G + (row & (dm.G - 1))] = float2{ref, D};
+        const int64_t r = (int64_t)ti * kDqRows + row;
+        if (i < L) rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? D : ref;
     }
     const TileReader rd(lane);
     const float c = dm.scale_log2;
@@ -73,7 +67,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) acc[ct] = zero16();
     const int w_lo = t0 + ((32 * wave) >> lg), w_hi = t0 + ((32 * wave + 31) >> lg);
-    auto step = [&](const DqTile &cur, DqTile &next, int x) __attribute__((always_inline)) {
+    auto step = [&](const KVTile &cur, KVTile &next, int x) __attribute__((always_inline)) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         stage(next, x + 1);
@@ -83,21 +77,23 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
         const bool all = k0 + kWinKeys - 1 <= w_lo && (k0 + kWinKeys <= win.n_sink || w_hi - k0 < win.window);
 #pragma unroll
         for (int kh = 0; kh < 2; ++kh) {
-            const char *kr = cur.k + kh * 32 * 256, *vr = cur.v + kh * 32 * 256;
-            f32x16 s = zero16(), dp = zero16();
+            const char *kr = cur.k.x + kh * kHalfTile, *vr = cur.v.x + kh * kHalfTile;
+            f32x16 s = zero16(), dp;                     // (dp - D straight from the product)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dp[e] = -D;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {
                 s = mfma32(rd.rows(kr, ks), qf[ks], s);
                 dp = mfma32(rd.rows(vr, ks), gf[ks], dp);
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = fast_exp2(__builtin_fmaf(s[e], c, -ref)) * (dp[e] - D);
+            for (int e = 0; e < 16; ++e) s[e] = fast_exp2(__builtin_fmaf(s[e], c, -ref)) * dp[e];
             if (!all) {                                  // (what is not visible may be anything: replaced, not multiplied)
+                int at = k0 + 32 * kh + 4 * hf;
+                asm volatile("" : "+v"(at));
+                const VisibleKeys visible(win, i);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int t = k0 + 32 * kh + 8 * (e >> 2) + 4 * hf + (e & 3);
-                    if (!(t <= i && (t < win.n_sink || i - t < win.window))) s[e] = 0.f;
-                }
+                for (int e = 0; e < 16; ++e) s[e] = visible(at + 8 * (e >> 2) + (e & 3)) ? s[e] : 0.f;
             }
 #pragma unroll
             for (int s2 = 0; s2 < 2; ++s2) {
@@ -149,12 +145,12 @@ struct KvSteps {                                         // the rows that see ke
     }
 };
 struct __align__(16) KvRows {
-    char q[kKvRows * 256], g[kKvRows * 256];
-    float2 ld[kKvRows];
+    char q[kHalfTile], g[kHalfTile];
+    float ref[32], D[32];
 };
 
 __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs win, float scale, int lg, BwdPlan plan, Tensor q, Tensor k,
-                                                             Tensor v, Tensor dout, const float2 *__restrict__ rows,
+                                                             Tensor v, Tensor dout, const float *__restrict__ rows,
                                                              const int32_t *__restrict__ seqlens, Tensor dk, Tensor dv,
                                                              float *__restrict__ part) {
     __shared__ KvRows slot0, slot1;
@@ -177,39 +173,39 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
         const __bf16 *kr = k.ptr + b * k.sb + h * k.sh + (int64_t)min(t, L - 1) * k.st + 8 * hf;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) kf[ks] = load8(kr + 16 * ks);
-        const char *v_head = reinterpret_cast<const char *>(v.ptr + b * v.sb + h * v.sh);
+        const int k0 = tile * kKvKeys;
+        const char *vb = reinterpret_cast<const char *>(v.ptr + b * v.sb + h * v.sh + (int64_t)k0 * v.st) + 64 * wave;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int r = 32 * wave + 4 * j + (lane >> 4);
-            const int64_t row = min(tile * kKvKeys + r, L - 1);
-            const int piece = 16 * ((lane & 15) ^ row_swizzle(r));
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(v_head + row * (2 * v.st) + piece),
-                                             (__attribute__((address_space(3))) void *)(vt + (32 * wave + 4 * j) * 256), 16, 0, 0);
+            const bool row = k0 + 16 * j + (lane >> 2) < L;
+            copy_rows(vt + (j >> 1) * kHalfTile + wave * 2048 + (j & 1) * 1024, vb,
+                      row ? (uint32_t)(lane >> 2) * 2u * (uint32_t)v.st + 16 * copy_piece(lane) : kNoRow, 32 * j * (uint32_t)v.st);
         }
     }
     const int per = kKvRows >> lg;
-    const char *q_head = reinterpret_cast<const char *>(q.ptr + b * q.sb + (int64_t)h * dm.G * q.sh);
-    const char *g_head = reinterpret_cast<const char *>(dout.ptr + b * dout.sb + (int64_t)h * dm.G * dout.sh);
-    const char *ld_head = reinterpret_cast<const char *>(rows + (int64_t)bh * dm.max_seqlen * dm.G);
+    const char *q_head = reinterpret_cast<const char *>(q.ptr + b * q.sb + (int64_t)h * dm.G * q.sh) + 64 * wave;
+    const char *g_head = reinterpret_cast<const char *>(dout.ptr + b * dout.sb + (int64_t)h * dm.G * dout.sh) + 64 * wave;
+    const float *row_head = rows + (int64_t)bh * row_blocks(dm) * 64;
+    uint32_t q_at[2], g_at[2];                           // this lane's row of either half of a step, and its piece
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t r = 16 * j + (lane >> 2), tok = r >> lg, g = r & (dm.G - 1), piece = 16 * copy_piece(lane);
+        q_at[j] = 2u * (tok * (uint32_t)q.st + g * (uint32_t)q.sh) + piece;
+        g_at[j] = 2u * (tok * (uint32_t)dout.st + g * (uint32_t)dout.sh) + piece;
+    }
     auto stage = [&](KvRows &dst, int x) __attribute__((always_inline)) {
         if (x >= x1) return;
         const int i0 = steps.from + x * per;
+        const char *qb = q_head + (int64_t)i0 * (2 * q.st), *gb = g_head + (int64_t)i0 * (2 * dout.st);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int r = 8 * wave + 4 * j + (lane >> 4);
-            const int64_t i = min(i0 + (r >> lg), L - 1), g = r & (dm.G - 1);
-            const int piece = 16 * ((lane & 15) ^ row_swizzle(r));
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(q_head + 2 * (i * q.st + g * q.sh) + piece),
-                                             (__attribute__((address_space(3))) void *)(dst.q + (8 * wave + 4 * j) * 256), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(g_head + 2 * (i * dout.st + g * dout.sh) + piece),
-                                             (__attribute__((address_space(3))) void *)(dst.g + (8 * wave + 4 * j) * 256), 16, 0, 0);
+            const bool row = i0 + ((16 * j + (lane >> 2)) >> lg) < L;
+            copy_rows(dst.q + wave * 2048 + j * 1024, qb, row ? q_at[j] : kNoRow, 0);
+            copy_rows(dst.g + wave * 2048 + j * 1024, gb, row ? g_at[j] : kNoRow, 0);
         }
-        if (wave == 0) {                                 // 32 (lse, D): 256 bytes
-            const int r = lane >> 1;
-            const int64_t i = min(i0 + (r >> lg), L - 1);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(ld_head + 8 * (i * dm.G + (r & (dm.G - 1))) + 4 * (lane & 1)),
-                                             (__attribute__((address_space(3))) void *)dst.ld, 4, 0, 0);
-        }
+        if (wave == 0)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(row_head + ((int64_t)i0 >> (5 - lg)) * 64 + lane),
+                                             (__attribute__((address_space(3))) void *)dst.ref, 4, 0, 0);
     };
     stage(slot0, x0);
     const TileReader rd(lane);
@@ -226,41 +222,65 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
         const bool some = k_lo <= i1 && (k_lo < win.n_sink || i0 - k_hi < win.window);
         if (!some) return;
         const bool all = k_hi <= i0 && (k_hi < win.n_sink || i1 - k_lo < win.window) && i1 < L;
-        const char *qr = cur.q, *gr = cur.g, *vr = vt + wave * 32 * 256;
-        f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-            s = mfma32(rd.rows(qr, ks), kf[ks], s);
-            dp = mfma32(rd.rows(gr, ks), rd.rows(vr, ks), dp);
-        }
-        // entry e: row 8 (e / 4) + 4 hf + e % 4
+        const char *qr = cur.q, *gr = cur.g, *vr = vt + wave * kHalfTile;
+        // entry e: row 8 (e / 4) + 4 hf + e % 4; dp - D straight from the product
+        f32x16 s = zero16(), dp;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
-            const float4 *ld = reinterpret_cast<const float4 *>(&cur.ld[8 * e4 + 4 * hf]);
-            const float4 a = ld[0], d = ld[1];
-            const float ref[4] = {a.x, a.z, d.x, d.z}, D[4] = {a.y, a.w, d.y, d.w};
+            const f32x4 d = *reinterpret_cast<const f32x4 *>(&cur.D[8 * e4 + 4 * hf]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dp[4 * e4 + e] = -d[e];
+        }
+        bf16x8 xq[2], xg[2], xv[2];                      // the next operands are under way while the matrix cores work, and no more: there are no registers
+        xq[0] = rd.rows(qr, 0);
+        xg[0] = rd.rows(gr, 0);
+        xv[0] = rd.rows(vr, 0);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+            if (ks < 7) {
+                xq[(ks + 1) & 1] = rd.rows(qr, ks + 1);
+                xg[(ks + 1) & 1] = rd.rows(gr, ks + 1);
+                xv[(ks + 1) & 1] = rd.rows(vr, ks + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            s = mfma32(xq[ks & 1], kf[ks], s);
+            dp = mfma32(xg[ks & 1], xv[ks & 1], dp);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            const f32x4 ref = *reinterpret_cast<const f32x4 *>(&cur.ref[8 * e4 + 4 * hf]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = fast_exp2(__builtin_fmaf(s[4 * e4 + e], c, -ref[e]));
-                s[4 * e4 + e] = p;
-                dp[4 * e4 + e] = p * (dp[4 * e4 + e] - D[e]);
+                s[4 * e4 + e] = fast_exp2(__builtin_fmaf(s[4 * e4 + e], c, -ref[e]));
+                dp[4 * e4 + e] *= s[4 * e4 + e];
             }
         }
-        if (!all) {
+        if (!all) {                                      // the key is visible to tokens t .. t + reach - 1
+            const int reach = max(0, min(t < win.n_sink ? 0x7fffffff : win.window, L - t));
+            int at = 4 * hf;
+            asm volatile("" : "+v"(at));                 // (formed here: sixteen registers otherwise, held through the loop)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int i = i0 + ((8 * (e >> 2) + 4 * hf + (e & 3)) >> lg);
-                if (!(t <= i && i < L && (t < win.n_sink || i - t < win.window))) s[e] = dp[e] = 0.f;
+                const bool seen = (uint32_t)(i0 + ((8 * (e >> 2) + (e & 3) + at) >> lg) - t) < (uint32_t)reach;
+                s[e] = seen ? s[e] : 0.f;
+                dp[e] = seen ? dp[e] : 0.f;
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        const bf16x8 p[2] = {pack8(s, 0), pack8(s, 1)}, ds[2] = {pack8(dp, 0), pack8(dp, 1)};
+        bf16x8 cg[2], cq[2];
+        cg[0] = rd.columns(gr, 0, 0);
+        cq[0] = rd.columns(qr, 0, 0);
 #pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-            const bf16x8 p = pack8(s, s2), ds = pack8(dp, s2);
-#pragma unroll
-            for (int ct = 0; ct < 4; ++ct) {
-                dva[ct] = mfma32(rd.columns(gr, s2, ct), p, dva[ct]);
-                dka[ct] = mfma32(rd.columns(qr, s2, ct), ds, dka[ct]);
+        for (int i = 0; i < 8; ++i) {                    // (half s of the rows, channel tile ct) = (i / 4, i % 4)
+            if (i < 7) {
+                cg[(i + 1) & 1] = rd.columns(gr, (i + 1) >> 2, (i + 1) & 3);
+                cq[(i + 1) & 1] = rd.columns(qr, (i + 1) >> 2, (i + 1) & 3);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            dva[i & 3] = mfma32(cg[i & 1], p[i >> 2], dva[i & 3]);
+            dka[i & 3] = mfma32(cq[i & 1], ds[i >> 2], dka[i & 3]);
         }
     };
     for (int x = x0; x < x1; x += 2) {
@@ -334,8 +354,6 @@ __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs wi
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
-static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
 // Scratch tiles a call may use in all: a number that grows with the batch and with max_seqlen, so that a buffer for a call is large
 // enough for every smaller one.
 static int64_t most_slots(int64_t tiles) { return min(8 * tiles, 2048 + tiles); }
@@ -360,7 +378,7 @@ static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
 }
 
 size_t window_bwd_ws_bytes(const Dims &dm, WindowArgs) {
-    const size_t rows = align256((size_t)dm.batch * dm.Hq * dm.max_seqlen * sizeof(float2));
+    const size_t rows = (size_t)dm.batch * dm.Hkv * row_blocks(dm) * 64 * sizeof(float);
     const int64_t tiles = (int64_t)dm.batch * dm.Hkv * ((dm.max_seqlen + kKvKeys - 1) / kKvKeys);
     return rows + (size_t)most_slots(tiles) * (2 * kKvKeys * kHeadDim * sizeof(float));
 }
@@ -370,8 +388,7 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
     if (dm.batch <= 0 || dm.max_seqlen <= 0) return 0;
     const int lg = __builtin_ctz(dm.G), per = kDqRows >> lg, n_tiles = (dm.max_seqlen + per - 1) / per;
     const float scale = dm.scale_log2 * kLn2;
-    float2 *rows = reinterpret_cast<float2 *>(ws);
-    float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(ws) + align256((size_t)dm.batch * dm.Hq * dm.max_seqlen * sizeof(float2)));
+    float *rows = reinterpret_cast<float *>(ws), *part = rows + (size_t)dm.batch * dm.Hkv * row_blocks(dm) * 64;
     const BwdPlan plan = bwd_plan(dm, w);
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
     timing_begin("window_dq_kernel", stream);

@@ -10,9 +10,6 @@
 namespace infllmv2 {
 
 constexpr int kFwdRows = 128;
-struct __align__(16) KVTile {
-    char k[kWinKeys * 256], v[kWinKeys * 256];
-};
 
 // The running maximum follows a row's scores only where they exceed it by more than this (in powers of two): probabilities stay
 // below 2^kSlack, and the outputs are rescaled once or twice per row instead of every tile.
@@ -20,7 +17,7 @@ constexpr float kSlack = 8.f;
 
 __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, Tensor q, Tensor k, Tensor v,
                                                                 const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
-    __shared__ KVTile tile0, tile1;
+    __shared__ Tile64 K0, K1, V0, V1;
     const int id = xcd_run(blockIdx.x, gridDim.x);
     const int ti = id % n_tiles, bh = id / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -38,22 +35,13 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
         return;
     }
     const KeyTiles kt(win, t0, t1);
-    const char *k_head = reinterpret_cast<const char *>(k.ptr + b * k.sb + h * k.sh), *v_head = reinterpret_cast<const char *>(v.ptr + b * v.sb + h * v.sh);
-    auto stage = [&](KVTile &dst, int x) __attribute__((always_inline)) {
-        if (x >= kt.count) return;
-        const int k0 = kt.key0(x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {                    // 1 KiB: rows 16 wave + 4 j + lane / 16 (past the sequence: its last again)
-            const int r = 16 * wave + 4 * j + (lane >> 4);
-            const int64_t t = min(k0 + r, L - 1);
-            const int piece = 16 * ((lane & 15) ^ row_swizzle(r));
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(k_head + t * (2 * k.st) + piece),
-                                             (__attribute__((address_space(3))) void *)(dst.k + (16 * wave + 4 * j) * 256), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(v_head + t * (2 * v.st) + piece),
-                                             (__attribute__((address_space(3))) void *)(dst.v + (16 * wave + 4 * j) * 256), 16, 0, 0);
-        }
+    const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
+    auto stage = [&](const TileCopier &from, Tile64 &to, int x) __attribute__((always_inline)) {
+        if (x < kt.count) from.copy(to, kt.key0(x), wave, lane);
     };
-    stage(tile0, 0);
+    stage(keys, K0, 0);
+    stage(values, V0, 0);
+    stage(keys, K1, 1);
     bf16x8 qf[8];
     {
         const __bf16 *qr = q.ptr + b * q.sb + (int64_t)min(i, L - 1) * q.st + (int64_t)hq * q.sh + 8 * hf;
@@ -68,37 +56,47 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
     float m = -INFINITY, l = 0.f;
     // tokens of this wavefront's rows
     const int w_lo = t0 + ((32 * wave) >> lg), w_hi = t0 + ((32 * wave + 31) >> lg);
-    auto step = [&](const KVTile &cur, KVTile &next, int x) __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(0);                   // this wavefront's copies have landed
-        __syncthreads();                                 // everyone's have, and everyone is past the tile before
-        stage(next, x + 1);
-        const int k0 = kt.key0(x);
-        // any of this wavefront's rows sees any of the keys?
-        const bool some = k0 <= w_hi && (k0 < win.n_sink || w_lo - (k0 + kWinKeys - 1) < win.window);
-        if (!some) return;
-        f32x16 s[2];
+    const auto larger = [](float a, float d) { return fmaxf(a, d); };
+    auto scores = [&](const Tile64 &kt_, f32x16 (&s)[2]) __attribute__((always_inline)) {
         s[0] = zero16();
         s[1] = zero16();
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-            s[0] = mfma32(rd.rows(cur.k, ks), qf[ks], s[0]);
-            s[1] = mfma32(rd.rows(cur.k + 32 * 256, ks), qf[ks], s[1]);
+            s[0] = mfma32(rd.rows(kt_.x, ks), qf[ks], s[0]);
+            s[1] = mfma32(rd.rows(kt_.x + kHalfTile, ks), qf[ks], s[1]);
         }
-        // all of them all of the keys?
-        const bool all = k0 + kWinKeys - 1 <= w_lo && (k0 + kWinKeys <= win.n_sink || w_hi - k0 < win.window);
-        if (!all) {
+    };
+    auto largest = [&](const f32x16 (&s)[2]) __attribute__((always_inline)) {
+        float a = max3(s[0][0], s[0][1], s[0][2]), d = max3(s[1][0], s[1][1], s[1][2]);
 #pragma unroll
-            for (int kh = 0; kh < 2; ++kh)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int t = k0 + 32 * kh + 8 * (e >> 2) + 4 * hf + (e & 3);
-                    if (!(t <= i && (t < win.n_sink || i - t < win.window))) s[kh][e] = -INFINITY;
-                }
+        for (int e = 3; e < 15; e += 2) {
+            a = max3(a, s[0][e], s[0][e + 1]);
+            d = max3(d, s[1][e], s[1][e + 1]);
         }
-        float mx = fmaxf(s[0][0], s[1][0]);
+        return max3(max3(a, s[0][15], s[1][15]), d, d);
+    };
+    // the keys a row does not see out of tile x, if there are any, and the largest of the others
+    auto hide = [&](f32x16 (&s)[2], int x, float &mx) __attribute__((always_inline)) {
+        const int k0 = kt.key0(x);
+        if (k0 + kWinKeys - 1 <= w_lo && (k0 + kWinKeys <= win.n_sink || w_hi - k0 < win.window)) return;
+        int at = k0 + 4 * hf;
+        asm volatile("" : "+v"(at));
+        const VisibleKeys visible(win, i);
 #pragma unroll
-        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, fmaxf(s[0][e], s[1][e]));
-        mx = half_reduce(mx, [](float a, float d) { return fmaxf(a, d); }) * c;
+        for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[kh][e] = visible(at + 32 * kh + 8 * (e >> 2) + (e & 3)) ? s[kh][e] : -INFINITY;
+        mx = largest(s);
+    };
+    // Tile x: its probabilities and their product with the values, and between them the next tile's scores, so that the matrix cores have
+    // work while the exponentials run.  (Behind the last tile: scores of what lies in LDS, not used.)
+    auto step = [&](Tile64 &k_cur, const Tile64 &k_next, const Tile64 &v_cur, Tile64 &v_next, f32x16 (&s)[2], f32x16 (&s_next)[2], float &mx,
+                    int x) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(0);                   // this wavefront's copies have landed
+        __syncthreads();                                 // everyone's have, and everyone is past the tile before
+        stage(keys, k_cur, x + 2);
+        stage(values, v_next, x + 1);
+        mx = half_reduce(mx, larger) * c;
         if (__any(mx > m + kSlack)) {
             const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - (m_new == -INFINITY ? 0.f : m_new));
             m = m_new;
@@ -107,25 +105,38 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
             for (int ct = 0; ct < 4; ++ct) o[ct] *= alpha;
         }
         const float base = m == -INFINITY ? 0.f : m;
+        __builtin_amdgcn_sched_barrier(0);
+        scores(k_next, s_next);
+        bf16x8 p[4];
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int kh = 0; kh < 2; ++kh)
+        for (int kh = 0; kh < 2; ++kh) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 s[kh][e] = fast_exp2(__builtin_fmaf(s[kh][e], c, -base));
-                l += s[kh][e];
+                sum[e & 1] += s[kh][e];
             }
+            p[2 * kh] = pack8(s[kh], 0);
+            p[2 * kh + 1] = pack8(s[kh], 1);
+        }
+        l += sum[0] + sum[1];
 #pragma unroll
-        for (int kh = 0; kh < 2; ++kh)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2) {
-                const bf16x8 p = pack8(s[kh], s2);
-#pragma unroll
-                for (int ct = 0; ct < 4; ++ct) o[ct] = mfma32(rd.columns(cur.v, 2 * kh + s2, ct), p, o[ct]);
-            }
+            for (int ct = 0; ct < 4; ++ct) o[ct] = mfma32(rd.columns(v_cur.x + (j >> 1) * kHalfTile, j & 1, ct), p[j], o[ct]);
+        mx = largest(s_next);
+        __builtin_amdgcn_sched_barrier(0);
+        if (x + 1 < kt.count) hide(s_next, x + 1, mx);
     };
+    f32x16 sa[2], sb[2];
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    scores(K0, sa);
+    float mx = largest(sa);
+    hide(sa, 0, mx);
     for (int x = 0; x < kt.count; x += 2) {
-        step(tile0, tile1, x);
-        if (x + 1 < kt.count) step(tile1, tile0, x + 1);
+        step(K0, K1, V0, V1, sa, sb, mx, x);
+        if (x + 1 < kt.count) step(K1, K0, V1, V0, sb, sa, mx, x + 1);
     }
     l = half_reduce(l, [](float a, float d) { return a + d; });
     if (i >= dm.max_seqlen || (i >= L && !dm.fill)) return;

@@ -82,6 +82,13 @@ def test_refusals(lib, name):
     if name.startswith("window"):
         assert call(a1=-1) == INVALID and call(a2=0) == INVALID and call(a2=-5) == INVALID
         assert call(a1=0) == 0 and call(a1=2 ** 31 - 1) == 0 and call(a2=2 ** 31 - 1) == 0
+    if name in ("window_attn_prefill", "window_attn_bwd"):         # tiles' rows have 32-bit offsets
+        far, wide = dense(st=(1 << 23) + 8), dense(sh=1 << 26)
+        assert call(a4=far) == UNSUPPORTED and call(a5=far) == UNSUPPORTED and call(a4=dense(st=1 << 23)) == 0
+        assert call(a4=wide) == 0                                  # heads of k and v: 64-bit
+        if name == "window_attn_bwd":
+            assert call(a3=far) == UNSUPPORTED and call(a7=far) == UNSUPPORTED and call(a3=wide) == UNSUPPORTED and call(a7=wide) == UNSUPPORTED
+            assert call(a6=far) == 0                               # out: 64-bit
     if name == "append_kv_quant":
         assert call(a5=None) == 0
         assert call(a9=0) == INVALID and call(a9=65) == UNSUPPORTED
