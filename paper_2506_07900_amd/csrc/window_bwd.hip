@@ -121,27 +121,34 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
 }
 
 // ---- dk, dv ------------------------------------------------------------------------------------------------------------------
-// A workgroup takes 128 keys, 32 to a wavefront (as columns: their K stays in registers, their V in LDS: both would not fit 256 registers), and a chunk of the steps of 32
-// query rows that see any of them; rows and their scalars go straight into LDS one step ahead.  S = Q . K^T and dP = dout . V^T leave a key
-// in a lane, so P and dS are the second operands of dV^T = dout^T . P and dK^T = Q^T . dS as they come out.  A tile's
-// steps are cut into chunks where there are fewer tiles than the chip holds, and those of the first tokens, which all later rows see;
-// the chunks' sums go to scratch and are added up in order.
+// A workgroup takes 128 keys, 32 to a wavefront (as columns: their K stays in registers, their V in LDS: both would not fit 256 registers),
+// and the rows of a span of tokens that see any of them, in steps of 32; rows and their scalars go straight into LDS one step ahead.
+// S = Q . K^T and dP = dout . V^T leave a key in a lane, so P and dS are the second operands of dV^T = dout^T . P and dK^T = Q^T . dS as they
+// come out.
+// The spans are the same for all keys, and the workgroups of a span are neighbours: they walk the same rows at the same time, which then
+// come out of their XCD's L2 (cut from each key tile's own first row on instead, 94 % of 17 GB came from beyond it: 32K tokens, window 4096).
+// Sums of a tile whose rows lie in several spans go to scratch and are added up in order.
 constexpr int kKvKeys = 128, kKvRows = 32;
 struct BwdPlan {
     int tiles, sink_tiles;                               // key tiles of a sequence; those with any of the first n_sink tokens
-    int chunk;                                           // steps per chunk
-    int sink_chunks, chunks;                             // chunks a tile may have
-    int slots;                                           // scratch tiles per (sequence, key-value head)
-    __host__ __device__ int first_slot(int tile) const { return tile < sink_tiles ? tile * sink_chunks : sink_tiles * sink_chunks + (tile - sink_tiles) * chunks; }
-    __host__ __device__ int of(int tile) const { return tile < sink_tiles ? sink_chunks : chunks; }
+    int span, spans;                                     // tokens of a span (a multiple of kKvKeys), spans
+    int per_span;                                        // key tiles a span may have
+    int parts;                                           // spans a tile may have, sinks' tiles apart
+    __host__ __device__ int slot(int tile) const { return tile < sink_tiles ? tile * spans : sink_tiles * spans + (tile - sink_tiles) * parts; }
+    // the first key tile behind the sinks' that a query of span s sees
+    __host__ __device__ int first_tile(WindowArgs w, int s) const {
+        const int64_t key = (int64_t)s * span + 1 - w.window;
+        const int t = key > 0 ? (int)(key / kKvKeys) : 0;
+        return t > sink_tiles ? t : sink_tiles;
+    }
 };
-struct KvSteps {                                         // the rows that see key tile `tile`: tokens from .. to - 1
-    int from, to, count;
-    __device__ __forceinline__ KvSteps(WindowArgs w, int tile, bool sink, int L, int lg) {
+struct KvSpans {                                         // the tokens that see key tile `tile`, the first and the last of their spans
+    int from, to, first, last;
+    __device__ __forceinline__ KvSpans(const BwdPlan &plan, WindowArgs w, int tile, int L) {
         from = tile * kKvKeys;
-        to = sink ? L : (int)min((int64_t)L, (int64_t)from + kKvKeys - 1 + w.window);
-        const int per = kKvRows >> lg;
-        count = to > from ? (to - from + per - 1) / per : 0;
+        to = tile < plan.sink_tiles ? L : (int)min((int64_t)L, (int64_t)from + kKvKeys - 1 + w.window);
+        first = from / plan.span;
+        last = max(to - 1, from) / plan.span;
     }
 };
 struct __align__(16) KvRows {
@@ -155,21 +162,22 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
                                                              float *__restrict__ part) {
     __shared__ KvRows slot0, slot1;
     __shared__ __align__(16) char vt[kKvKeys * 256];
-    const int per_head = plan.sink_tiles * plan.sink_chunks + (plan.tiles - plan.sink_tiles) * plan.chunks;
+    const int per_head = plan.spans * plan.per_span;
     const int id = xcd_run(blockIdx.x, gridDim.x), bh = id / per_head, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
-    int at = id - bh * per_head;
-    const bool sink = at < plan.sink_tiles * plan.sink_chunks;
-    if (!sink) at -= plan.sink_tiles * plan.sink_chunks;
-    const int n_ch = sink ? plan.sink_chunks : plan.chunks, tile = at / n_ch + (sink ? 0 : plan.sink_tiles), chunk = at % n_ch;
+    const int span = (id - bh * per_head) / plan.per_span, at = id - bh * per_head - span * plan.per_span;
+    const int tile = at < plan.sink_tiles ? at : plan.first_tile(win, span) + at - plan.sink_tiles;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
-    const KvSteps steps(win, tile, sink, L, lg);
-    const int x0 = chunk * plan.chunk, x1 = min(steps.count, x0 + plan.chunk);
-    if (n_ch > 1 ? x0 >= x1 : !dm.fill && x0 >= x1) return;
+    if (tile >= plan.tiles) return;
+    const KvSpans rows_of(plan, win, tile, L);
+    if (span < rows_of.first || span > rows_of.last) return;
+    const int from = max(rows_of.from, span * plan.span), to = (int)min((int64_t)rows_of.to, (int64_t)(span + 1) * plan.span);
+    if (from >= to && !dm.fill) return;
+    const int per = kKvRows >> lg, x1 = from < to ? (to - from + per - 1) / per : 0;
     const int t = tile * kKvKeys + 32 * wave + c32;      // this lane's key
     bf16x8 kf[8];
-    if (x0 < x1) {
+    if (x1 > 0) {
         const __bf16 *kr = k.ptr + b * k.sb + h * k.sh + (int64_t)min(t, L - 1) * k.st + 8 * hf;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) kf[ks] = load8(kr + 16 * ks);
@@ -182,7 +190,6 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
                       row ? (uint32_t)(lane >> 2) * 2u * (uint32_t)v.st + 16 * copy_piece(lane) : kNoRow, 32 * j * (uint32_t)v.st);
         }
     }
-    const int per = kKvRows >> lg;
     const char *q_head = reinterpret_cast<const char *>(q.ptr + b * q.sb + (int64_t)h * dm.G * q.sh) + 64 * wave;
     const char *g_head = reinterpret_cast<const char *>(dout.ptr + b * dout.sb + (int64_t)h * dm.G * dout.sh) + 64 * wave;
     const float *row_head = rows + (int64_t)bh * row_blocks(dm) * 64;
@@ -195,7 +202,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
     }
     auto stage = [&](KvRows &dst, int x) __attribute__((always_inline)) {
         if (x >= x1) return;
-        const int i0 = steps.from + x * per;
+        const int i0 = from + x * per;
         const char *qb = q_head + (int64_t)i0 * (2 * q.st), *gb = g_head + (int64_t)i0 * (2 * dout.st);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -207,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(row_head + ((int64_t)i0 >> (5 - lg)) * 64 + lane),
                                              (__attribute__((address_space(3))) void *)dst.ref, 4, 0, 0);
     };
-    stage(slot0, x0);
+    stage(slot0, 0);
     const TileReader rd(lane);
     const float c = dm.scale_log2;
     f32x16 dka[4], dva[4];
@@ -218,7 +225,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         stage(next, x + 1);
-        const int i0 = steps.from + x * per, i1 = i0 + per - 1;
+        const int i0 = from + x * per, i1 = i0 + per - 1;
         const bool some = k_lo <= i1 && (k_lo < win.n_sink || i0 - k_hi < win.window);
         if (!some) return;
         const bool all = k_hi <= i0 && (k_hi < win.n_sink || i1 - k_lo < win.window) && i1 < L;
@@ -283,12 +290,13 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
             dka[i & 3] = mfma32(cq[i & 1], ds[i >> 2], dka[i & 3]);
         }
     };
-    for (int x = x0; x < x1; x += 2) {
+    for (int x = 0; x < x1; x += 2) {
         step(slot0, slot1, x);
         if (x + 1 < x1) step(slot1, slot0, x + 1);
     }
-    if (n_ch > 1) {                                      // [key][channel], dk then dv
-        float *p = part + ((int64_t)bh * plan.slots + plan.first_slot(tile) + chunk) * (2 * kKvKeys * kHeadDim) + (32 * wave + c32) * kHeadDim + 4 * hf;
+    if (rows_of.first != rows_of.last) {                 // [key][channel], dk then dv
+        const int64_t slot = (int64_t)bh * plan.slot(plan.tiles) + plan.slot(tile) + span - rows_of.first;
+        float *p = part + slot * (2 * kKvKeys * kHeadDim) + (32 * wave + c32) * kHeadDim + 4 * hf;
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
@@ -317,18 +325,17 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
         }
 }
 
-// The chunks' sums of a key tile, added in order.  grid (keys / 16, Hkv, batch) over the tiles that may have several: 16 keys a workgroup, a thread
-// 8 channels of dk and dv.
-__global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs win, int lg, BwdPlan plan, const int32_t *__restrict__ seqlens,
+// The spans' sums of a key tile, added in order.  grid (keys / 16, Hkv, batch): 16 keys a workgroup, a thread 8 channels of dk and dv.
+__global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs win, BwdPlan plan, const int32_t *__restrict__ seqlens,
                                                           const float *__restrict__ part, Tensor dk, Tensor dv) {
     const int h = blockIdx.y, b = blockIdx.z, bh = b * dm.Hkv + h;
     const int t = 16 * (int)blockIdx.x + (threadIdx.x >> 4), c8 = 8 * (threadIdx.x & 15), tile = t / kKvKeys;
-    if (plan.of(tile) == 1 || t >= dm.max_seqlen) return;
+    if (t >= dm.max_seqlen) return;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
-    if (t >= L && !dm.fill) return;
-    const KvSteps steps(win, tile, tile < plan.sink_tiles, L, lg);
-    const int n = t < L ? (steps.count + plan.chunk - 1) / plan.chunk : 0;
-    const float *p = part + ((int64_t)bh * plan.slots + plan.first_slot(tile)) * (2 * kKvKeys * kHeadDim) + (t % kKvKeys) * kHeadDim + c8;
+    const KvSpans rows_of(plan, win, tile, L);
+    if (rows_of.first == rows_of.last || (t >= L && !dm.fill)) return;
+    const int n = t < L ? rows_of.last - rows_of.first + 1 : 0;
+    const float *p = part + ((int64_t)bh * plan.slot(plan.tiles) + plan.slot(tile)) * (2 * kKvKeys * kHeadDim) + (t % kKvKeys) * kHeadDim + c8;
     float x[8], y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
@@ -356,24 +363,34 @@ __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs wi
 // ---- host side -------------------------------------------------------------------------------------------------------------
 // Scratch tiles a call may use in all: a number that grows with the batch and with max_seqlen, so that a buffer for a call is large
 // enough for every smaller one.
-static int64_t most_slots(int64_t tiles) { return min(8 * tiles, 2048 + tiles); }
+static int64_t most_slots(int64_t tiles) { return min(8 * tiles, 2048 + 2 * tiles); }
 
+// The span: of some lengths, each a quarter longer than the one before, the one whose workgroups the chip, which holds 512, is through with first:
+// all steps, about 25 more per workgroup for its start and its sums, and half a longest workgroup's steps in which not all have work.
 static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
-    BwdPlan p;
+    BwdPlan best{};
     const int per = kKvRows / dm.G;
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
-    p.tiles = (dm.max_seqlen + kKvKeys - 1) / kKvKeys;
-    p.sink_tiles = (w.n_sink + kKvKeys - 1) / kKvKeys;
-    const int64_t sink_steps = (dm.max_seqlen + per - 1) / per;
-    const int64_t steps = min(sink_steps, ((int64_t)w.window + kKvKeys - 1 + per - 1) / per);
-    const int64_t total = heads * (p.sink_tiles * sink_steps + (p.tiles - p.sink_tiles) * steps);
-    for (int64_t chunk = max((int64_t)8, total / 1024);; chunk += (chunk + 3) / 4) {
-        p.chunk = (int)min(chunk, (int64_t)1 << 30);
-        p.sink_chunks = (int)((sink_steps + chunk - 1) / chunk);
-        p.chunks = (int)((steps + chunk - 1) / chunk);
-        const int64_t slots = (int64_t)p.sink_tiles * p.sink_chunks + (int64_t)(p.tiles - p.sink_tiles) * (p.chunks > 1 ? p.chunks : 0);
-        p.slots = (int)slots;
-        if (heads * slots <= most_slots(heads * p.tiles)) return p;
+    const int64_t all_steps = (dm.max_seqlen + per - 1) / per, window_steps = min(all_steps, ((int64_t)w.window + kKvKeys - 1 + per - 1) / per);
+    int64_t least = INT64_MAX;
+    for (int64_t blocks = 1;; blocks += (blocks + 3) / 4) {
+        BwdPlan p;
+        p.tiles = (dm.max_seqlen + kKvKeys - 1) / kKvKeys;
+        p.sink_tiles = (w.n_sink + kKvKeys - 1) / kKvKeys;
+        const int64_t steps = heads * (p.sink_tiles * all_steps + (p.tiles - p.sink_tiles) * window_steps);
+        blocks = min(blocks, (int64_t)p.tiles);
+        p.span = (int)(blocks * kKvKeys);
+        p.spans = (int)((p.tiles + blocks - 1) / blocks);
+        const int64_t reach = (w.window + 126) / kKvKeys + 1;              // tiles behind a span's own that its first query may see
+        p.per_span = (int)min((int64_t)p.tiles, p.sink_tiles + blocks + reach);
+        p.parts = (int)min((int64_t)p.spans, ((int64_t)w.window + 126) / p.span + 2);
+        const int64_t items = heads * p.spans * p.per_span, longest = (min(p.span, dm.max_seqlen) + per - 1) / per;
+        const int64_t cost = (steps + 25 * items) / 512 + longest / 2;
+        if (heads * p.slot(p.tiles) <= most_slots(heads * p.tiles) && cost < least) {
+            least = cost;
+            best = p;
+        }
+        if (blocks == p.tiles) return best;              // (one span: a slot per tile at most)
     }
 }
 
@@ -396,14 +413,12 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
                        dout, lse, seqlens, dq, rows);
     timing_end(stream);
     timing_begin("window_dkdv_kernel", stream);
-    const int64_t items = (int64_t)plan.sink_tiles * plan.sink_chunks + (int64_t)(plan.tiles - plan.sink_tiles) * plan.chunks;
-    hipLaunchKernelGGL(window_dkdv_kernel, dim3((unsigned)(items * heads)), dim3(256), 0, stream, dm, w, scale, lg, plan, q, k, v, dout,
-                       rows, seqlens, dk, dv, part);
+    hipLaunchKernelGGL(window_dkdv_kernel, dim3((unsigned)(plan.spans * plan.per_span * heads)), dim3(256), 0, stream, dm, w, scale, lg, plan,
+                       q, k, v, dout, rows, seqlens, dk, dv, part);
     timing_end(stream);
-    if (plan.chunks == 1 && (plan.sink_tiles == 0 || plan.sink_chunks == 1)) return (int)hipGetLastError();
-    const int keys = plan.chunks > 1 ? dm.max_seqlen : min(dm.max_seqlen, plan.sink_tiles * kKvKeys);
+    if (plan.spans == 1) return (int)hipGetLastError();
     timing_begin("window_join_kernel", stream);
-    hipLaunchKernelGGL(window_join_kernel, dim3((keys + 15) / 16, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, w, lg, plan, seqlens, part,
+    hipLaunchKernelGGL(window_join_kernel, dim3((dm.max_seqlen + 15) / 16, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, w, plan, seqlens, part,
                        dk, dv);
     timing_end(stream);
     return (int)hipGetLastError();

@@ -1,9 +1,9 @@
 // Attention over a sliding window and the first tokens, one query per cached token: one pass over the visible keys with a running
 // maximum and sum.
 //
-// A workgroup takes 128 query rows, (token, head of the group) with the heads fastest, so its rows see the same keys but for
-// the few tokens they span, and every key tile is fetched once for them.  Four wavefronts of 32 rows; key and value tiles of 64 tokens go from
-// memory straight into LDS, one tile ahead.  S^T = K . Q^T leaves a row's scores in a lane and its partner, so maxima and sums are
+// Query rows are (token, head of the group) with the heads fastest, so 128 of them see the same keys but for the few tokens they
+// span, and a key tile is fetched once for them.  A wavefront takes 32 rows; key and value tiles of 64 tokens go from
+// memory straight into LDS.  S^T = K . Q^T leaves a row's scores in a lane and its partner, so maxima and sums are
 // per lane, and the probabilities are the second operand of O^T = V^T . P^T in the registers they come out in.
 #include "window.h"
 
@@ -15,22 +15,133 @@ constexpr int kFwdRows = 128;
 // below 2^kSlack, and the outputs are rescaled once or twice per row instead of every tile.
 constexpr float kSlack = 8.f;
 
+// A wavefront's 32 rows: lane 32 hf + c holds row c.
+struct QueryRows {
+    WindowArgs win;
+    float scale;                                         // to powers of two
+    int lane, hf, i, hq, lo, hi;                         // the lane's token and head; first and last token of the wavefront
+    TileReader rd;
+    bf16x8 q[8];
+    f32x16 o[4];                                         // channels 32 ct + 8 (e / 4) + 4 hf + e % 4
+    float m, l;                                          // l: of this lane's keys
+    __device__ __forceinline__ QueryRows(const Dims &dm, WindowArgs w, int lg, int t0, int first_row, int h, int lane)
+        : win(w), scale(dm.scale_log2), lane(lane), hf(lane >> 5), rd(lane), m(-INFINITY), l(0.f) {
+        const int row = first_row + (lane & 31);
+        i = t0 + (row >> lg);
+        hq = h * dm.G + (row & (dm.G - 1));
+        lo = t0 + (first_row >> lg);
+        hi = t0 + ((first_row + 31) >> lg);
+    }
+    __device__ __forceinline__ void load(const Tensor &t, int b, int L) {
+        const __bf16 *qr = t.ptr + b * t.sb + (int64_t)min(i, L - 1) * t.st + (int64_t)hq * t.sh + 8 * hf;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) q[ks] = load8(qr + 16 * ks);
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) o[ct] = zero16();
+    }
+    __device__ __forceinline__ void scores(const Tile64 &k, f32x16 (&s)[2]) const {
+        s[0] = zero16();
+        s[1] = zero16();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+            s[0] = mfma32(rd.rows(k.x, ks), q[ks], s[0]);
+            s[1] = mfma32(rd.rows(k.x + kHalfTile, ks), q[ks], s[1]);
+        }
+    }
+    __device__ __forceinline__ static float largest(const f32x16 (&s)[2]) {
+        float a = max3(s[0][0], s[0][1], s[0][2]), d = max3(s[1][0], s[1][1], s[1][2]);
+#pragma unroll
+        for (int e = 3; e < 15; e += 2) {
+            a = max3(a, s[0][e], s[0][e + 1]);
+            d = max3(d, s[1][e], s[1][e + 1]);
+        }
+        return max3(max3(a, s[0][15], s[1][15]), d, d);
+    }
+    // the keys k0 .. k0 + 63 that a row does not see taken out, if there are any, and the largest of the others
+    __device__ __forceinline__ void hide(f32x16 (&s)[2], int k0, float &mx) const {
+        if (k0 + kWinKeys - 1 <= lo && (k0 + kWinKeys <= win.n_sink || hi - k0 < win.window)) return;
+        int at = k0 + 4 * hf;
+        asm volatile("" : "+v"(at));                     // (formed here: registers otherwise, held through the loop)
+        const VisibleKeys visible(win, i);
+#pragma unroll
+        for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[kh][e] = visible(at + 32 * kh + 8 * (e >> 2) + (e & 3)) ? s[kh][e] : -INFINITY;
+        mx = largest(s);
+    }
+    // mx: the largest of this lane's scores of a tile -> what its exponentials are referred to
+    __device__ __forceinline__ float reference(float mx) {
+        mx = half_reduce(mx, [](float a, float d) { return fmaxf(a, d); }) * scale;
+        if (__any(mx > m + kSlack)) {
+            const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - (m_new == -INFINITY ? 0.f : m_new));
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) o[ct] *= alpha;
+        }
+        return m == -INFINITY ? 0.f : m;
+    }
+    __device__ __forceinline__ void add(f32x16 (&s)[2], float base, const Tile64 &v) {
+        bf16x8 p[4];
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int kh = 0; kh < 2; ++kh) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[kh][e] = fast_exp2(__builtin_fmaf(s[kh][e], scale, -base));
+                sum[e & 1] += s[kh][e];
+            }
+            p[2 * kh] = pack8(s[kh], 0);                 // (bf16: what the matrix cores multiply; the sum is of what they were)
+            p[2 * kh + 1] = pack8(s[kh], 1);
+        }
+        l += sum[0] + sum[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) o[ct] = mfma32(rd.columns(v.x + (j >> 1) * kHalfTile, j & 1, ct), p[j], o[ct]);
+    }
+};
+
+// A product multiplies a key that a row does not see by a probability of 0, and 0 times an infinity or a NaN reaches the row's sum.  A
+// row that does not come out finite is therefore taken again by the whole wavefront, key by key, over the keys it sees; its maximum m and
+// sum l stand, as hidden scores are replaced and not multiplied.  Lane = two channels.
+__device__ __forceinline__ void take_row_again(const Dims &dm, WindowArgs win, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &out,
+                                               int b, int h, int i, int hq, float m, float l, int lane) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    auto pair = [&](const Tensor &t, int64_t row) { return reinterpret_cast<const bf16x2 *>(t.ptr + row)[lane]; };
+    const bf16x2 x = pair(q, b * q.sb + (int64_t)i * q.st + (int64_t)hq * q.sh);
+    const int lo = max(0, i - win.window + 1), first = min(win.n_sink, lo);
+    float y0 = 0.f, y1 = 0.f;
+    for (int n = 0; n < first + i - lo + 1; ++n) {
+        const int64_t t = n < first ? n : lo + n - first;
+        const bf16x2 kt = pair(k, b * k.sb + h * k.sh + t * k.st), vt = pair(v, b * v.sb + h * v.sh + t * v.st);
+        const auto sum = [](float a, float d) { return a + d; };
+        const float s = xgroup_reduce(row_reduce(__builtin_fmaf((float)x[0], (float)kt[0], (float)x[1] * (float)kt[1]), sum), sum);
+        const float p = (float)(__bf16)fast_exp2(__builtin_fmaf(s, dm.scale_log2, -m));
+        y0 = __builtin_fmaf(p, (float)vt[0], y0);
+        y1 = __builtin_fmaf(p, (float)vt[1], y1);
+    }
+    bf16x2 y;
+    y[0] = (__bf16)(y0 / l);
+    y[1] = (__bf16)(y1 / l);
+    reinterpret_cast<bf16x2 *>(out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh)[lane] = y;
+}
+
 __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, Tensor q, Tensor k, Tensor v,
                                                                 const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
     __shared__ Tile64 K0, K1, V0, V1;
     const int id = xcd_run(blockIdx.x, gridDim.x);
     const int ti = id % n_tiles, bh = id / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c32 = lane & 31, hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int t0 = ti * (kFwdRows >> lg), t1 = min(L, t0 + (kFwdRows >> lg));
-    const int row = 32 * wave + c32, i = t0 + (row >> lg), hq = h * dm.G + (row & (dm.G - 1));
-    __bf16 *o_row = out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh + 4 * hf;
-    float *lse_at = lse + ((int64_t)b * dm.max_seqlen + i) * dm.Hq + hq;
+    QueryRows r(dm, win, lg, t0, 32 * wave, h, lane);
+    __bf16 *o_row = out.ptr + b * out.sb + (int64_t)r.i * out.st + (int64_t)r.hq * out.sh + 4 * r.hf;
+    float *lse_at = lse + ((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq;
     if (t0 >= L) {
-        if (dm.fill && i < dm.max_seqlen) {
+        if (dm.fill && r.i < dm.max_seqlen) {
             for (int c = 0; c < 16; ++c) *reinterpret_cast<uint2 *>(o_row + 8 * c) = uint2{0u, 0u};
-            if (hf == 0) *lse_at = 0.f;
+            if (r.hf == 0) *lse_at = 0.f;
         }
         return;
     }
@@ -42,52 +153,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
     stage(keys, K0, 0);
     stage(values, V0, 0);
     stage(keys, K1, 1);
-    bf16x8 qf[8];
-    {
-        const __bf16 *qr = q.ptr + b * q.sb + (int64_t)min(i, L - 1) * q.st + (int64_t)hq * q.sh + 8 * hf;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qf[ks] = load8(qr + 16 * ks);
-    }
-    const TileReader rd(lane);
-    const float c = dm.scale_log2;
-    f32x16 o[4];
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct) o[ct] = zero16();
-    float m = -INFINITY, l = 0.f;
-    // tokens of this wavefront's rows
-    const int w_lo = t0 + ((32 * wave) >> lg), w_hi = t0 + ((32 * wave + 31) >> lg);
-    const auto larger = [](float a, float d) { return fmaxf(a, d); };
-    auto scores = [&](const Tile64 &kt_, f32x16 (&s)[2]) __attribute__((always_inline)) {
-        s[0] = zero16();
-        s[1] = zero16();
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-            s[0] = mfma32(rd.rows(kt_.x, ks), qf[ks], s[0]);
-            s[1] = mfma32(rd.rows(kt_.x + kHalfTile, ks), qf[ks], s[1]);
-        }
-    };
-    auto largest = [&](const f32x16 (&s)[2]) __attribute__((always_inline)) {
-        float a = max3(s[0][0], s[0][1], s[0][2]), d = max3(s[1][0], s[1][1], s[1][2]);
-#pragma unroll
-        for (int e = 3; e < 15; e += 2) {
-            a = max3(a, s[0][e], s[0][e + 1]);
-            d = max3(d, s[1][e], s[1][e + 1]);
-        }
-        return max3(max3(a, s[0][15], s[1][15]), d, d);
-    };
-    // the keys a row does not see out of tile x, if there are any, and the largest of the others
-    auto hide = [&](f32x16 (&s)[2], int x, float &mx) __attribute__((always_inline)) {
-        const int k0 = kt.key0(x);
-        if (k0 + kWinKeys - 1 <= w_lo && (k0 + kWinKeys <= win.n_sink || w_hi - k0 < win.window)) return;
-        int at = k0 + 4 * hf;
-        asm volatile("" : "+v"(at));
-        const VisibleKeys visible(win, i);
-#pragma unroll
-        for (int kh = 0; kh < 2; ++kh)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[kh][e] = visible(at + 32 * kh + 8 * (e >> 2) + (e & 3)) ? s[kh][e] : -INFINITY;
-        mx = largest(s);
-    };
+    r.load(q, b, L);
     // Tile x: its probabilities and their product with the values, and between them the next tile's scores, so that the matrix cores have
     // work while the exponentials run.  (Behind the last tile: scores of what lies in LDS, not used.)
     auto step = [&](Tile64 &k_cur, const Tile64 &k_next, const Tile64 &v_cur, Tile64 &v_next, f32x16 (&s)[2], f32x16 (&s_next)[2], float &mx,
@@ -96,61 +162,159 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
         __syncthreads();                                 // everyone's have, and everyone is past the tile before
         stage(keys, k_cur, x + 2);
         stage(values, v_next, x + 1);
-        mx = half_reduce(mx, larger) * c;
-        if (__any(mx > m + kSlack)) {
-            const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - (m_new == -INFINITY ? 0.f : m_new));
-            m = m_new;
-            l *= alpha;
-#pragma unroll
-            for (int ct = 0; ct < 4; ++ct) o[ct] *= alpha;
-        }
-        const float base = m == -INFINITY ? 0.f : m;
+        const float base = r.reference(mx);
         __builtin_amdgcn_sched_barrier(0);
-        scores(k_next, s_next);
-        bf16x8 p[4];
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int kh = 0; kh < 2; ++kh) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[kh][e] = fast_exp2(__builtin_fmaf(s[kh][e], c, -base));
-                sum[e & 1] += s[kh][e];
-            }
-            p[2 * kh] = pack8(s[kh], 0);
-            p[2 * kh + 1] = pack8(s[kh], 1);
-        }
-        l += sum[0] + sum[1];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int ct = 0; ct < 4; ++ct) o[ct] = mfma32(rd.columns(v_cur.x + (j >> 1) * kHalfTile, j & 1, ct), p[j], o[ct]);
-        mx = largest(s_next);
+        r.scores(k_next, s_next);
+        r.add(s, base, v_cur);
+        mx = QueryRows::largest(s_next);
         __builtin_amdgcn_sched_barrier(0);
-        if (x + 1 < kt.count) hide(s_next, x + 1, mx);
+        if (x + 1 < kt.count) r.hide(s_next, kt.key0(x + 1), mx);
     };
     f32x16 sa[2], sb[2];
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    scores(K0, sa);
-    float mx = largest(sa);
-    hide(sa, 0, mx);
+    r.scores(K0, sa);
+    float mx = QueryRows::largest(sa);
+    r.hide(sa, kt.key0(0), mx);
     for (int x = 0; x < kt.count; x += 2) {
         step(K0, K1, V0, V1, sa, sb, mx, x);
         if (x + 1 < kt.count) step(K1, K0, V1, V0, sb, sa, mx, x + 1);
     }
-    l = half_reduce(l, [](float a, float d) { return a + d; });
-    if (i >= dm.max_seqlen || (i >= L && !dm.fill)) return;
-    const bool live = i < L;
+    r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
+    const bool live = r.i < L, store = r.i < dm.max_seqlen && (live || dm.fill);
+    float check = 0.f;
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-            bf16x4 r;
+        for (int e = 0; e < 16; ++e) check = __builtin_fmaf(r.o[ct][e], 0.f, check);
+    const uint64_t bad_lanes = __ballot(live && check != 0.f);
+    uint32_t bad = (uint32_t)bad_lanes | (uint32_t)(bad_lanes >> 32);
+    if (store && !((bad >> (lane & 31)) & 1u)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = (__bf16)(live ? o[ct][4 * e4 + e] / l : 0.f);
-            *reinterpret_cast<uint2 *>(o_row + 32 * ct + 8 * e4) = __builtin_bit_cast(uint2, r);
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                bf16x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = (__bf16)(live ? r.o[ct][4 * e4 + e] / r.l : 0.f);
+                *reinterpret_cast<uint2 *>(o_row + 32 * ct + 8 * e4) = __builtin_bit_cast(uint2, y);
+            }
+    }
+    if (store && r.hf == 0) *lse_at = live ? lse_of(r.m, r.l) : 0.f;
+    for (; bad; bad &= bad - 1) {
+        const int n = __builtin_ctz(bad);
+        take_row_again(dm, win, q, k, v, out, b, h, __builtin_amdgcn_readlane(r.i, n), __builtin_amdgcn_readlane(r.hq, n),
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.m), n)),
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.l), n)), lane);
+    }
+}
+
+// The same for few rows: a workgroup takes 32 of them, its wavefronts every fourth key tile each, fetched for itself and without a
+// barrier; their four states are joined in LDS at the end.
+struct __align__(16) WaveTiles {
+    Tile64 k[4], v[4];
+};
+__global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, Tensor q, Tensor k, Tensor v,
+                                                                    const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
+    __shared__ WaveTiles tiles;
+    __shared__ float ml[2][4][32];
+    const int ti = blockIdx.x % n_tiles, bh = blockIdx.x / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
+    const int t0 = ti * (32 >> lg), t1 = min(L, t0 + (32 >> lg));
+    QueryRows r(dm, win, lg, t0, 0, h, lane);
+    // the result's row and 16 channels of this thread
+    const int row = tid >> 3, ch = 16 * (tid & 7), i = t0 + (row >> lg), hq = h * dm.G + (row & (dm.G - 1));
+    __bf16 *o_row = out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh + ch;
+    float *lse_at = lse + ((int64_t)b * dm.max_seqlen + i) * dm.Hq + hq;
+    const bool store = i < dm.max_seqlen && (i < L || dm.fill);
+    if (t0 >= L) {
+        if (store) {
+            reinterpret_cast<uint4 *>(o_row)[0] = reinterpret_cast<uint4 *>(o_row)[1] = uint4{0u, 0u, 0u, 0u};
+            if (ch == 0) *lse_at = 0.f;
         }
-    if (hf == 0) *lse_at = live ? lse_of(m, l) : 0.f;
+        return;
+    }
+    const KeyTiles kt(win, t0, t1);
+    Tile64 &kw = tiles.k[wave], &vw = tiles.v[wave];
+    auto stage = [&](const Tensor &t, Tile64 &to, int x) __attribute__((always_inline)) {
+        if (x >= kt.count) return;
+#pragma unroll
+        for (int part = 0; part < 4; ++part) TileCopier(t, b, h, L, part, lane).copy(to, kt.key0(x), part, lane);
+    };
+    stage(k, kw, wave);
+    stage(v, vw, wave);
+    r.load(q, b, L);
+    auto reads_done = [] {                               // of this wavefront, which alone uses its tiles: lgkmcnt 0
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int x = wave; x < kt.count; x += 4) {
+        __builtin_amdgcn_s_waitcnt(0);
+        f32x16 s[2];
+        r.scores(kw, s);
+        reads_done();
+        stage(k, kw, x + 4);
+        float mx = QueryRows::largest(s);
+        r.hide(s, kt.key0(x), mx);
+        const float base = r.reference(mx);
+        r.add(s, base, vw);
+        reads_done();
+        stage(v, vw, x + 4);
+    }
+    r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
+    if (r.hf == 0) {
+        ml[0][wave][lane] = r.m;
+        ml[1][wave][lane] = r.l;
+    }
+    // [row][channel], 16-byte pieces XORed with the row
+    float *mine = reinterpret_cast<float *>(kw.x);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+            *reinterpret_cast<f32x4 *>(mine + (lane & 31) * kHeadDim + 4 * ((8 * ct + 2 * e4 + r.hf) ^ (lane & 7))) =
+                f32x4{r.o[ct][4 * e4], r.o[ct][4 * e4 + 1], r.o[ct][4 * e4 + 2], r.o[ct][4 * e4 + 3]};
+    __syncthreads();
+    float M = -INFINITY, den = 0.f, y[16], check = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[0][w][row]);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = fast_exp2(ml[0][w][row] - M);    // (a row sees its own key: M is a number)
+        den += f * ml[1][w][row];
+        const float *from = reinterpret_cast<const float *>(tiles.k[w].x) + row * kHeadDim;
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            const f32x4 a = *reinterpret_cast<const f32x4 *>(from + 4 * ((ch / 4 + e4) ^ (row & 7)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[4 * e4 + e] += f * a[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) check = __builtin_fmaf(y[e], 0.f, check);
+    uint64_t bad = __ballot(i < L && check != 0.f);
+    const bool whole = ((bad >> (lane & 56)) & 255u) == 0u;                    // this row's eight lanes
+    if (store) {
+        bf16x8 z[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)(i < L ? y[e] / den : 0.f);
+        if (whole) {
+            reinterpret_cast<uint4 *>(o_row)[0] = __builtin_bit_cast(uint4, z[0]);
+            reinterpret_cast<uint4 *>(o_row)[1] = __builtin_bit_cast(uint4, z[1]);
+        }
+        if (ch == 0) *lse_at = i < L ? lse_of(M, den) : 0.f;
+    }
+    while (bad) {
+        const int n = __builtin_ctzll(bad);
+        bad &= ~(255ull << (n & 56));
+        take_row_again(dm, win, q, k, v, out, b, h, __builtin_amdgcn_readlane(i, n), __builtin_amdgcn_readlane(hq, n),
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(M), n)),
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(den), n)), lane);
+    }
 }
 
 size_t window_prefill_ws_bytes(const Dims &, WindowArgs) { return 0; }
@@ -158,10 +322,18 @@ size_t window_prefill_ws_bytes(const Dims &, WindowArgs) { return 0; }
 int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v, const int32_t *seqlens, Tensor out, float *lse,
                           void *, hipStream_t stream) {
     if (dm.batch <= 0 || dm.max_seqlen <= 0) return 0;
-    const int lg = __builtin_ctz(dm.G), per = kFwdRows >> lg, n_tiles = (dm.max_seqlen + per - 1) / per;
-    timing_begin("window_prefill_kernel", stream);
-    hipLaunchKernelGGL(window_prefill_kernel, dim3((unsigned)((int64_t)n_tiles * dm.Hkv * dm.batch)), dim3(256), 0, stream, dm, w, lg,
-                       n_tiles, q, k, v, seqlens, out, lse);
+    const int lg = __builtin_ctz(dm.G);
+    const int64_t heads = (int64_t)dm.Hkv * dm.batch;
+    auto tiles = [&](int rows) { return (dm.max_seqlen + (rows >> lg) - 1) / (rows >> lg); };
+    if (tiles(kFwdRows) * heads <= 64) {
+        timing_begin("window_prefill_few_kernel", stream);
+        hipLaunchKernelGGL(window_prefill_few_kernel, dim3((unsigned)(tiles(32) * heads)), dim3(256), 0, stream, dm, w, lg, tiles(32), q, k, v,
+                           seqlens, out, lse);
+    } else {
+        timing_begin("window_prefill_kernel", stream);
+        hipLaunchKernelGGL(window_prefill_kernel, dim3((unsigned)(tiles(kFwdRows) * heads)), dim3(256), 0, stream, dm, w, lg, tiles(kFwdRows),
+                           q, k, v, seqlens, out, lse);
+    }
     timing_end(stream);
     return (int)hipGetLastError();
 }

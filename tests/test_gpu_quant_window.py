@@ -454,3 +454,25 @@ def test_window_bwd(G, H, lengths, n_sink, window):
                 tol = 1.0625 * err + HALF * want.abs() + 1e-30
                 diff = (got[b, h, :n].double() - want).abs()
                 assert (diff <= tol).all(), (name, float((diff / tol).max()))
+
+
+@pytest.mark.parametrize("G,H,n,n_sink,window,at", [(16, 2, 200, 4, 20, 70), (1, 1, 400, 0, 129, 255), (4, 2, 3000, 3, 100, 1), (8, 4, 1500, 0, 64, 1499)])
+def test_window_prefill_keeps_what_is_not_finite_where_it_is_seen(G, H, n, n_sink, window, at):
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    prm = binding.Params(G * H, H)
+    k, v = random_cache(gen, 1, H, n, [n])
+    q = normal(gen, 1, n, G * H, D)
+    v[0, 0, at, 5], v[0, H - 1, at, 127] = math.inf, GARBAGE
+    out, lse = binding.window_attn_prefill(prm, n_sink, window, q, k, v, lengths_tensor([n]), n)
+    seen = window_seen(torch.arange(n, device="cuda"), n, n_sink, window)
+    hit = seen[:, at]
+    for hq in range(G * H):
+        h = hq // G
+        clean = torch.nan_to_num(v[0, h].double(), nan=0.0, posinf=0.0)
+        want = attend(q[0, :, hq].double(), k[0, h].double(), clean, seen, prm.softmax_scale)
+        check(out[0, ~hit, hq], lse[0, ~hit, hq], [x[~hit] for x in want])
+        finite = torch.isfinite(out[0, :, hq])
+        bad = [c for c, hh in ((5, 0), (127, H - 1)) if hh == h]
+        assert not finite[hit][:, bad].any() and finite[~hit].all()
+        rest = [c for c in range(D) if c not in bad]               # the other channels of the same value: whole
+        check(out[0, hit, hq][:, rest], lse[0, hit, hq], [x[hit][:, rest] if x.dim() == 2 else x[hit] for x in want])
