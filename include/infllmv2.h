@@ -415,7 +415,8 @@ int32_t infllmv2_verify_step(const infllmv2_params *prm, const infllmv2_tensor *
  *                           seqlens[b] < n_draft or > max_seqlen is skipped as a whole.
  * infllmv2_sparse_attn_decode_quant, infllmv2_sparse_attn_verify_quant
  *                           infllmv2_sparse_attn_decode / _verify with k, v = the values of kq, vq: the same arguments, block lists, tree
- *                           masks, results and workspaces (INFLLMV2_OP_ATTN_DECODE, INFLLMV2_OP_ATTN_VERIFY).
+ *                           masks, results and workspaces (INFLLMV2_OP_ATTN_DECODE, INFLLMV2_OP_ATTN_VERIFY).  stride_t and scale_stride_t
+ *                           at most 2^26 bytes, else INFLLMV2_ERR_UNSUPPORTED.
  * The selection reads compressed keys, which stay bf16: infllmv2_select_blocks and _verify serve such a cache as they are.
  */
 int32_t infllmv2_quantize_kv(const infllmv2_params *prm, const infllmv2_tensor *k, const infllmv2_tensor *v,
@@ -455,7 +456,7 @@ int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infl
  *                               sums for dk, dv in a fixed order: results repeat bit for bit.
  * infllmv2_window_attn_decode   the query at position seqlens[b]-1: q, out [batch, 1, Hq, d], lse fp32 [batch, Hq]; a sequence with
  *                               seqlens[b] < 1 gets out 0, lse -inf.
- * infllmv2_window_attn_decode_quant  the same on a cache in 4 bits.
+ * infllmv2_window_attn_decode_quant  the same on a cache in 4 bits (strides as for infllmv2_sparse_attn_decode_quant).
  * Prefill and backward: stride_t of k and v at most 2^23 elements; backward: of q and dout as well, and group size x their
  * stride_h at most 2^29, else INFLLMV2_ERR_UNSUPPORTED.
  * Workspaces: infllmv2_window_workspace_bytes(INFLLMV2_OP_WINDOW_*, ...) bytes, 256-byte aligned (0: none needed, or the arguments are

@@ -120,6 +120,14 @@ int32_t check_spans(const infllmv2_params *p, const infllmv2_tensor *k, const in
     return INFLLMV2_OK;
 }
 
+// and so do the attention calls in the rows of a cache in 4 bits
+int32_t check_rows(const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq) {
+    const int64_t st[4] = {kq->stride_t, kq->scale_stride_t, vq->stride_t, vq->scale_stride_t};
+    for (int i = 0; i < 4; ++i)
+        if (st[i] > kMaxQuantStride) return INFLLMV2_ERR_UNSUPPORTED;
+    return INFLLMV2_OK;
+}
+
 int32_t check_workspace(const void *workspace, size_t bytes, size_t need) {
     return need > 0 && (!workspace || bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) ? INFLLMV2_ERR_WORKSPACE : INFLLMV2_OK;
 }
@@ -606,6 +614,7 @@ int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infl
     RETURN_IF_ERR(check_tensor(out));
     if (!seqlens || !block_idx || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (tree_mask && (reinterpret_cast<uintptr_t>(tree_mask) & 7u) != 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_rows(kq, vq));
     const Dims dm = make_dims(prm, batch, max_seqlen, n_draft);
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, attn_decode_ws_bytes(dm)));
     return hip_status(launch_attn_decode_quant(dm, make_tensor(q), make_quant(kq), make_quant(vq), seqlens, block_idx, tree_mask,
@@ -720,6 +729,7 @@ int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_
     RETURN_IF_ERR(check_quant(vq));
     RETURN_IF_ERR(check_tensor(out));
     if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_rows(kq, vq));
     const Dims dm = make_dims(prm, batch, max_seqlen);
     const WindowArgs w = make_window(n_sink, window, max_seqlen);
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_decode_ws_bytes(dm, w)));

@@ -66,6 +66,7 @@ int launch_window_decode_quant(const Dims &dm, WindowArgs w, Tensor q, QuantTens
                                Tensor out, float *lse, void *ws, hipStream_t stream);
 // The prefill and backward kernels address rows with 32-bit offsets from a tile's first: what the strides of a call may be.
 constexpr int64_t kMaxTokenStride = 1ll << 23, kMaxHeadSpan = 1ll << 29;   // elements; of a token, and of the heads of a group
+constexpr int64_t kMaxQuantStride = 1ll << 26;               // bytes; of a row of a cache in 4 bits that the attention reads
 size_t window_prefill_ws_bytes(const Dims &dm, WindowArgs w);
 int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v, const int32_t *seqlens, Tensor out, float *lse,
                           void *ws, hipStream_t stream);

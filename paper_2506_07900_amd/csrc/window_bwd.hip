@@ -16,12 +16,13 @@ struct KVTile {
 // What the forward leaves of a row (token, head of the group): its log-sum-exp in powers of two and D, 32 and 32 floats for 32 rows.
 __host__ __device__ static inline int64_t row_blocks(const Dims &dm) { return ((int64_t)dm.max_seqlen * dm.G + 31) / 32; }   // per (sequence, head)
 
-__global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, Tensor q, Tensor k,
+__global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, int run, Tensor q, Tensor k,
                                                            Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
                                                            const int32_t *__restrict__ seqlens, Tensor dq, float *__restrict__ rows) {
     __shared__ KVTile tile0, tile1;
-    const int id = xcd_run(blockIdx.x, gridDim.x);
-    const int ti = id % n_tiles, bh = id / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int item = xcd_item(blockIdx.x, run), bh = item / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    if (b >= dm.batch) return;
+    const int ti = (bh + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
@@ -162,9 +163,9 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
                                                              float *__restrict__ part) {
     __shared__ KvRows slot0, slot1;
     __shared__ __align__(16) char vt[kKvKeys * 256];
-    const int per_head = plan.spans * plan.per_span;
-    const int id = xcd_run(blockIdx.x, gridDim.x), bh = id / per_head, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
-    const int span = (id - bh * per_head) / plan.per_span, at = id - bh * per_head - span * plan.per_span;
+    const int item = xcd_item(blockIdx.x, plan.per_span), group = item / plan.per_span, bh = group / plan.spans;     // a span is a run
+    const int b = bh / dm.Hkv, h = bh - b * dm.Hkv, span = (bh + 1) * plan.spans - 1 - group, at = item - group * plan.per_span;
+    if (b >= dm.batch) return;
     const int tile = at < plan.sink_tiles ? at : plan.first_tile(win, span) + at - plan.sink_tiles;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
@@ -366,7 +367,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs wi
 static int64_t most_slots(int64_t tiles) { return min(8 * tiles, 2048 + 2 * tiles); }
 
 // The span: of some lengths, each a quarter longer than the one before, the one whose workgroups the chip, which holds 512, is through with first:
-// all steps, about 25 more per workgroup for its start and its sums, and half a longest workgroup's steps in which not all have work.
+// all steps, about 50 more per workgroup for its start and its sums, and half a longest workgroup's steps in which not all have work.
 static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
     BwdPlan best{};
     const int per = kKvRows / dm.G;
@@ -385,7 +386,7 @@ static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
         p.per_span = (int)min((int64_t)p.tiles, p.sink_tiles + blocks + reach);
         p.parts = (int)min((int64_t)p.spans, ((int64_t)w.window + 126) / p.span + 2);
         const int64_t items = heads * p.spans * p.per_span, longest = (min(p.span, dm.max_seqlen) + per - 1) / per;
-        const int64_t cost = (steps + 25 * items) / 512 + longest / 2;
+        const int64_t cost = (steps + 50 * items) / 512 + longest / 2;
         if (heads * p.slot(p.tiles) <= most_slots(heads * p.tiles) && cost < least) {
             least = cost;
             best = p;
@@ -409,11 +410,12 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
     const BwdPlan plan = bwd_plan(dm, w);
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
     timing_begin("window_dq_kernel", stream);
-    hipLaunchKernelGGL(window_dq_kernel, dim3((unsigned)(n_tiles * heads)), dim3(256), 0, stream, dm, w, scale, lg, n_tiles, q, k, v, out,
-                       dout, lse, seqlens, dq, rows);
+    const int run = xcd_run_length(n_tiles * heads);
+    hipLaunchKernelGGL(window_dq_kernel, dim3(xcd_grid(n_tiles * heads, run)), dim3(256), 0, stream, dm, w, scale, lg, n_tiles, run, q, k, v,
+                       out, dout, lse, seqlens, dq, rows);
     timing_end(stream);
     timing_begin("window_dkdv_kernel", stream);
-    hipLaunchKernelGGL(window_dkdv_kernel, dim3((unsigned)(plan.spans * plan.per_span * heads)), dim3(256), 0, stream, dm, w, scale, lg, plan,
+    hipLaunchKernelGGL(window_dkdv_kernel, dim3(xcd_grid(plan.spans * plan.per_span * heads, plan.per_span)), dim3(256), 0, stream, dm, w, scale, lg, plan,
                        q, k, v, dout, rows, seqlens, dk, dv, part);
     timing_end(stream);
     if (plan.spans == 1) return (int)hipGetLastError();

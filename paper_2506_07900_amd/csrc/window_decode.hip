@@ -7,7 +7,7 @@
 // so the probabilities are the second product's operand in the registers they come out in.  At the end the four
 // states are joined in LDS; where a row is split over workgroups, decode_merge_kernel joins those.
 #include "quant.h"
-#include "token_union.h"
+#include "window.h"
 
 namespace infllmv2 {
 
@@ -19,11 +19,21 @@ struct RowSource {                                       // a cache of either ki
 };
 
 
+// An address that is the same for all lanes, in scalar registers.
+__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p) {
+    const uint64_t x = (uint64_t)(uintptr_t)p;
+    return (const uint8_t *)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32 |
+                                        (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x));
+}
+
 // One unit of K and V on its way.  Lane (n, g): key rows n and 16 + n.
 template <bool kQuant>
 struct UnitRows;
 template <>
 struct UnitRows<false> {
+    struct Head {
+        __device__ __forceinline__ Head(const RowSource &, int, int, int) {}
+    };
     bf16x8 k[2][4];                                      // channels 32 ks + 8 g ..
     uint4 v[8];                                          // row lane / 16 + 4 i, channels 8 (lane % 16) ..
     __device__ __forceinline__ void load(const RowSource &s, int64_t k_head, int64_t v_head, int key0, int last, int lane) {
@@ -51,36 +61,61 @@ struct UnitRows<false> {
 };
 template <>
 struct UnitRows<true> {
-    uint4 k[2], v[2];                                    // K: channels 32 g .. of its row; V: row lane / 4 + 16 i, channels 32 (lane % 4) ..
-    uint8_t ke[2], ve[2];
-    __device__ __forceinline__ void load(const RowSource &s, int64_t, int64_t, int key0, int last, int lane, int b, int h) {
-        const int n = lane & 15, g = lane >> 4;
-        const int64_t kc = b * s.kq.sb + h * s.kq.sh, kx = b * s.kq.eb + h * s.kq.eh;
-        const int64_t vc = b * s.vq.sb + h * s.vq.sh, vx = b * s.vq.eb + h * s.vq.eh;
+    uint4 k[2], v[2];                                    // row n + 16 t, channels 32 g ..
+    uint32_t ke[2], ve[2];
+    // The head's first row, and bytes from a unit's first row to this lane's codes and exponents, of K and of V.
+    struct Head {
+        const uint8_t *kc, *ke, *vc, *ve;
+        uint32_t at[4];
+        __device__ __forceinline__ Head(const RowSource &s, int b, int h, int lane)
+            : kc(uniform(s.kq.codes + b * s.kq.sb + h * s.kq.sh)), ke(uniform(s.kq.scales + b * s.kq.eb + h * s.kq.eh)),
+              vc(uniform(s.vq.codes + b * s.vq.sb + h * s.vq.sh)), ve(uniform(s.vq.scales + b * s.vq.eb + h * s.vq.eh)) {
+            const uint32_t n = lane & 15, g = lane >> 4;
+            at[0] = n * (uint32_t)s.kq.st + 16 * g;
+            at[1] = n * (uint32_t)s.kq.et + g;
+            at[2] = n * (uint32_t)s.vq.st + 16 * g;
+            at[3] = n * (uint32_t)s.vq.et + g;
+        }
+    };
+    __device__ __forceinline__ void load(const RowSource &s, const Head &head, int key0, int rows, int lane) {    // the cache has `rows` from key0 on
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        key0 = __builtin_amdgcn_readfirstlane(key0);
+        auto from = [&](const uint8_t *p, int64_t st) __attribute__((always_inline)) {
+            return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p + key0 * st), 0, 0xfffffffeu, 0x00027000);
+        };
+        const auto kc = from(head.kc, s.kq.st), ke_ = from(head.ke, s.kq.et), vc = from(head.vc, s.vq.st), ve_ = from(head.ve, s.vq.et);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int64_t r = min(key0 + 16 * t + n, last), rv = min(key0 + 16 * t + (lane >> 2), last);
-            k[t] = *reinterpret_cast<const uint4 *>(s.kq.codes + kc + r * s.kq.st + 16 * g);
-            ke[t] = s.kq.scales[kx + r * s.kq.et + g];
-            v[t] = *reinterpret_cast<const uint4 *>(s.vq.codes + vc + rv * s.vq.st + 16 * (lane & 3));
-            ve[t] = s.vq.scales[vx + rv * s.vq.et + (lane & 3)];
+            const bool row = (lane & 15) + 16 * t < rows;
+            k[t] = __builtin_bit_cast(uint4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(kc, row ? head.at[0] + 16 * t * (uint32_t)s.kq.st : kNoRow, 0, 0));
+            v[t] = __builtin_bit_cast(uint4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(vc, row ? head.at[2] + 16 * t * (uint32_t)s.vq.st : kNoRow, 0, 0));
+            ke[t] = __builtin_amdgcn_raw_buffer_load_b8(ke_, row ? head.at[1] + 16 * t * (uint32_t)s.kq.et : kNoRow, 0, 0);
+            ve[t] = __builtin_amdgcn_raw_buffer_load_b8(ve_, row ? head.at[3] + 16 * t * (uint32_t)s.vq.et : kNoRow, 0, 0);
         }
     }
     __device__ __forceinline__ bf16x8 key(int t, int ks) const {
         const uint32_t w = ks == 0 ? k[t].x : ks == 1 ? k[t].y : ks == 2 ? k[t].z : k[t].w;
         return __builtin_bit_cast(bf16x8, dequant8(w, ke[t]));
     }
+    // Values into LDS: four quarters of 32 channels, in each 32 rows of 64 bytes, whose four pieces are XORed with row / 4 % 4, its bits
+    // exchanged: a store takes a piece of each of 16 rows, two groups of lanes of a transposing load 32 bytes of each of 8; both touch every
+    // bank once.
+    __device__ __forceinline__ static uint32_t swizzle(uint32_t i) { return ((i & 1) << 1) | (i >> 1); }
     __device__ __forceinline__ void values(char *vs, uint32_t allow, int lane) const {
+        const uint32_t n = lane & 15, g = lane >> 4;
+        char *at = vs + g * 2048 + n * 64;
+        const uint32_t x = swizzle(n >> 2) << 4;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int r = 16 * t + (lane >> 2);
-            const bool seen = (allow >> r) & 1u;
-            const uint32_t w[4] = {v[t].x, v[t].y, v[t].z, v[t].w};
+            uint32_t w[4] = {v[t].x, v[t].y, v[t].z, v[t].w}, e = ve[t];
+            if (allow != ~0u) {                          // what is not seen: zeros
+                const uint32_t seen = 0u - ((allow >> (16 * t + n)) & 1u);
+                e = seen ? e : 127u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 y = seen ? dequant8(w[i], ve[t]) : uint4{0u, 0u, 0u, 0u};
-                *reinterpret_cast<uint4 *>(vs + r * 256 + (((4 * (lane & 3) + i) ^ row_swizzle(r)) << 4)) = y;
+                for (int i = 0; i < 4; ++i) w[i] &= seen;
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(at + 1024 * t + ((16 * i) ^ x)) = dequant8(w[i], e);
         }
     }
 };
@@ -88,7 +123,7 @@ struct UnitRows<true> {
 // grid (splits, Hkv, rows).  kList: a row's units are the halves of its list's entries, `per` entries to a split; otherwise its share
 // of the units of its window.  With one split the result is written as it is, else as a partial (o, maximum, sum).
 template <bool kQuant, bool kList>
-__global__ __launch_bounds__(256) void stream_attn_kernel(Dims dm, WindowArgs win, Tensor q, RowSource src, const int32_t *__restrict__ seqlens,
+__global__ __launch_bounds__(256, kQuant ? 3 : 2) void stream_attn_kernel(Dims dm, WindowArgs win, Tensor q, RowSource src, const int32_t *__restrict__ seqlens,
                                                           const int32_t *__restrict__ block_idx, const uint64_t *__restrict__ tree_mask,
                                                           int per, Tensor out, float *__restrict__ lse, float *__restrict__ o_part,
                                                           float2 *__restrict__ ml_part) {
@@ -98,7 +133,9 @@ __global__ __launch_bounds__(256) void stream_attn_kernel(Dims dm, WindowArgs wi
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4, G = dm.G;
     int b, qi;
-    const int L = query_row(dm, seqlens, bv, b, qi);
+    const int L = __builtin_amdgcn_readfirstlane(query_row(dm, seqlens, bv, b, qi));
+    b = __builtin_amdgcn_readfirstlane(b);               // (uniform: the compiler divides in vector registers)
+    qi = __builtin_amdgcn_readfirstlane(qi);
     // ---- the query: lane (n, g) holds head n, channels 32 ks + 8 g .. (4-bit keys: 32 g + 8 ks ..) --------------------
     bf16x8 bq[4];
     {
@@ -153,8 +190,9 @@ __global__ __launch_bounds__(256) void stream_attn_kernel(Dims dm, WindowArgs wi
     };
     const int64_t k_head = kQuant ? 0 : b * src.k.sb + h * src.k.sh, v_head = kQuant ? 0 : b * src.v.sb + h * src.v.sh;
     const int last = dm.max_seqlen - 1;
+    const typename UnitRows<kQuant>::Head rows_of(src, b, h, lane);
     auto fetch = [&](UnitRows<kQuant> &x, int key0) __attribute__((always_inline)) {
-        if constexpr (kQuant) x.load(src, 0, 0, key0, last, lane, b, h);
+        if constexpr (kQuant) x.load(src, rows_of, key0, dm.max_seqlen - key0, lane);
         else x.load(src, k_head, v_head, key0, last, lane);
     };
     // ---- the walk ------------------------------------------------------------------------------------------------------
@@ -170,37 +208,53 @@ __global__ __launch_bounds__(256) void stream_attn_kernel(Dims dm, WindowArgs wi
             s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) s[t] = mfma16(x.key(t, ks), bq[ks], s[t]);
+            if constexpr (kQuant) __builtin_amdgcn_sched_barrier(0);   // (one tile's keys in bf16 at a time: registers)
         }
         x.values(vs, allow, lane);
-        float y[8], mx = -INFINITY;
+        if constexpr (kQuant) __builtin_amdgcn_sched_barrier(0);
+        float y[8];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int e = 0; e < 8; ++e) y[e] = s[e >> 2][e & 3];         // key 16 (e / 4) + 4 g + e % 4
+        if (allow != ~0u) {
+            const uint32_t mine = allow >> (4 * g);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {                // key 16 t + 4 g + j
-                y[4 * t + j] = (allow >> (16 * t + 4 * g + j)) & 1u ? s[t][j] * dm.scale_log2 : -INFINITY;
-                mx = fmaxf(mx, y[4 * t + j]);
-            }
-        const float m_new = fmaxf(m, xgroup_max(mx)), base = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = fast_exp2(m - base);
-        m = m_new;
+            for (int e = 0; e < 8; ++e) y[e] = (mine >> (16 * (e >> 2) + (e & 3))) & 1u ? y[e] : -INFINITY;
+        }
+        const float mx = xgroup_max(max3(max3(max3(y[0], y[1], y[2]), y[3], y[4]), max3(y[5], y[6], y[7]), y[7])) * dm.scale_log2;
+        // the maximum follows only where scores exceed it by a factor of 2^8: outputs are rescaled once or twice, not every unit
+        if (__any(mx > m + 8.f)) {
+            const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - (m_new == -INFINITY ? 0.f : m_new));
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o[c] *= alpha;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
         float ps = 0.f;
         bf16x8 p;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float e = fast_exp2(y[j] - base);
+            const float e = fast_exp2(__builtin_fmaf(y[j], dm.scale_log2, -base));
             ps += e;
             p[j] = (__bf16)e;
         }
-        l = l * alpha + ps;                              // (this lane's keys only: joined over g at the end)
+        l += ps;                                         // (this lane's keys only: joined over g at the end)
         __builtin_amdgcn_wave_barrier();                 // same wavefront: LDS keeps the order
 #pragma unroll
         for (int c = 0; c < 8; ++c) {                    // A: channel 16 c + n, keys 4 g .. and 16 + 4 g ..
             const int r = 4 * g + (n >> 2);
-            const char *at = vs + 8 * (n & 1);
-            const int piece = 2 * c + ((n & 3) >> 1);
-            const s16x4 x0 = lds_read_tr16(at + r * 256 + ((piece ^ row_swizzle(r)) << 4));
-            const s16x4 x1 = lds_read_tr16(at + (r + 16) * 256 + ((piece ^ row_swizzle(r + 16)) << 4));
-            o[c] = mfma16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7)), p, o[c] * alpha);
+            s16x4 x0, x1;
+            if constexpr (kQuant) {
+                const char *at = vs + (r * 64 + (((2 * (c & 1) + ((n & 3) >> 1)) ^ UnitRows<true>::swizzle(g)) << 4) + 8 * (n & 1)) + (c >> 1) * 2048;
+                x0 = lds_read_tr16(at);
+                x1 = lds_read_tr16(at + 1024);
+            } else {
+                const char *at = vs + 8 * (n & 1);
+                const int piece = 2 * c + ((n & 3) >> 1);
+                x0 = lds_read_tr16(at + r * 256 + ((piece ^ row_swizzle(r)) << 4));
+                x1 = lds_read_tr16(at + (r + 16) * 256 + ((piece ^ row_swizzle(r + 16)) << 4));
+            }
+            o[c] = mfma16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7)), p, o[c]);
         }
         __builtin_amdgcn_wave_barrier();
     };
@@ -272,12 +326,19 @@ __global__ __launch_bounds__(256) void stream_attn_kernel(Dims dm, WindowArgs wi
 // ---- host side -------------------------------------------------------------------------------------------------------------
 static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// How many workgroups a row's `units` are split over: enough to fill the chip, at least four units (one per wavefront) each.
+// How many workgroups a row's `units` are split over: as many as the chip holds (three per compute unit; two with a bf16 cache, whose rows take
+// more registers), and a number of units to each that its four wavefronts share evenly.  With more the last of them wait for the
+// first ones' places (64 sequences, window 8192, 4 bits: 1024 / 768 / 512 workgroups 35 / 30 / 33 us), uneven ones do as if they had more (16 drafted
+// tokens x 32 blocks, 6 / 8 units each: 11.8 / 10.1 us).
 constexpr int kMaxSplits = 64;                           // what decode_merge_kernel joins
-static int stream_splits(const Dims &dm, int64_t units) {
-    const int64_t rows = max((int64_t)1, (int64_t)dm.batch * dm.n_q * dm.Hkv);
-    const int64_t want = (1024 + rows - 1) / rows, most = (units + 3) / 4;
-    return (int)max((int64_t)1, min(min(want, most), (int64_t)kMaxSplits));
+static int stream_units(const Dims &dm, int64_t units, bool quant) {
+    const int64_t rows = max((int64_t)1, (int64_t)dm.batch * dm.n_q * dm.Hkv), chip = quant ? 768 : 512;
+    const int64_t want = min((chip + rows - 1) / rows, (int64_t)kMaxSplits);
+    return (int)((units + 4 * want - 1) / (4 * want) * 4);
+}
+static int stream_splits(const Dims &dm, int64_t units, bool quant) {
+    const int each = stream_units(dm, units, quant);
+    return (int)max((int64_t)1, (units + each - 1) / max(each, 1));
 }
 // The most units a window may touch: the sinks', and one more than fill the window.
 static int64_t window_units(const Dims &dm, WindowArgs w) {
@@ -306,27 +367,29 @@ int launch_attn_decode_quant(const Dims &dm, Tensor q, QuantTensor kq, QuantTens
                              const int32_t *block_idx, const uint64_t *tree_mask, Tensor out, float *lse, void *ws,
                              hipStream_t stream) {
     if (dm.batch <= 0) return 0;
-    const int want = stream_splits(dm, 2 * dm.topk), per = (dm.topk + want - 1) / want;
+    const int per = stream_units(dm, 2 * dm.topk, true) / 2;
     return launch_stream<true, true>("sparse_attn_quant_kernel", dm, WindowArgs{0, 0}, (dm.topk + per - 1) / per, per, q,
                                      RowSource{Tensor{}, Tensor{}, kq, vq}, seqlens, block_idx, tree_mask, out, lse, ws, stream);
 }
 
+// (An upper bound that grows with the batch and with max_seqlen: a buffer for a call is large enough for every smaller one.)
 size_t window_decode_ws_bytes(const Dims &dm, WindowArgs w) {
-    const size_t rows = (size_t)dm.batch * dm.Hq * stream_splits(dm, window_units(dm, w));
-    return align256(rows * kHeadDim * sizeof(float)) + align256(rows * sizeof(float2));
+    const int64_t rows = (int64_t)dm.batch * dm.Hkv, most = min((int64_t)kMaxSplits, (window_units(dm, w) + 3) / 4);
+    const size_t parts = (size_t)(min(rows * most, rows + 768) * dm.G);
+    return align256(parts * kHeadDim * sizeof(float)) + align256(parts * sizeof(float2));
 }
 
 int launch_window_decode(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v, const int32_t *seqlens, Tensor out, float *lse,
                          void *ws, hipStream_t stream) {
     if (dm.batch <= 0) return 0;
-    return launch_stream<false, false>("window_decode_kernel", dm, w, stream_splits(dm, window_units(dm, w)), 0, q,
+    return launch_stream<false, false>("window_decode_kernel", dm, w, stream_splits(dm, window_units(dm, w), false), 0, q,
                                        RowSource{k, v, QuantTensor{}, QuantTensor{}}, seqlens, nullptr, nullptr, out, lse, ws, stream);
 }
 
 int launch_window_decode_quant(const Dims &dm, WindowArgs w, Tensor q, QuantTensor kq, QuantTensor vq, const int32_t *seqlens,
                                Tensor out, float *lse, void *ws, hipStream_t stream) {
     if (dm.batch <= 0) return 0;
-    return launch_stream<true, false>("window_decode_quant_kernel", dm, w, stream_splits(dm, window_units(dm, w)), 0, q,
+    return launch_stream<true, false>("window_decode_quant_kernel", dm, w, stream_splits(dm, window_units(dm, w), true), 0, q,
                                       RowSource{Tensor{}, Tensor{}, kq, vq}, seqlens, nullptr, nullptr, out, lse, ws, stream);
 }
 

@@ -127,11 +127,12 @@ __device__ __forceinline__ void take_row_again(const Dims &dm, WindowArgs win, c
     reinterpret_cast<bf16x2 *>(out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh)[lane] = y;
 }
 
-__global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, Tensor q, Tensor k, Tensor v,
+__global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k, Tensor v,
                                                                 const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
     __shared__ Tile64 K0, K1, V0, V1;
-    const int id = xcd_run(blockIdx.x, gridDim.x);
-    const int ti = id % n_tiles, bh = id / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int item = xcd_item(blockIdx.x, run), bh = item / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    if (b >= dm.batch) return;
+    const int ti = (bh + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int t0 = ti * (kFwdRows >> lg), t1 = min(L, t0 + (kFwdRows >> lg));
@@ -331,8 +332,10 @@ int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tens
                            seqlens, out, lse);
     } else {
         timing_begin("window_prefill_kernel", stream);
-        hipLaunchKernelGGL(window_prefill_kernel, dim3((unsigned)(tiles(kFwdRows) * heads)), dim3(256), 0, stream, dm, w, lg, tiles(kFwdRows),
-                           q, k, v, seqlens, out, lse);
+        const int64_t items = tiles(kFwdRows) * heads;
+        const int run = xcd_run_length(items);
+        hipLaunchKernelGGL(window_prefill_kernel, dim3(xcd_grid(items, run)), dim3(256), 0, stream, dm, w, lg, tiles(kFwdRows), run, q, k, v,
+                           seqlens, out, lse);
     }
     timing_end(stream);
     return (int)hipGetLastError();

@@ -82,6 +82,10 @@ def test_refusals(lib, name):
     if name.startswith("window"):
         assert call(a1=-1) == INVALID and call(a2=0) == INVALID and call(a2=-5) == INVALID
         assert call(a1=0) == 0 and call(a1=2 ** 31 - 1) == 0 and call(a2=2 ** 31 - 1) == 0
+    if name in ("sparse_attn_decode_quant", "sparse_attn_verify_quant", "window_attn_decode_quant"):
+        for i in [i for i, x in enumerate(good) if isinstance(x, CQuantTensor)]:
+            assert call(**{"a%d" % i: packed(st=(1 << 26) + 16)}) == UNSUPPORTED and call(**{"a%d" % i: packed(et=(1 << 26) + 4)}) == UNSUPPORTED
+            assert call(**{"a%d" % i: packed(st=1 << 26, et=1 << 26, sb=1 << 40, eh=1 << 40)}) == 0
     if name in ("window_attn_prefill", "window_attn_bwd"):         # tiles' rows have 32-bit offsets
         far, wide = dense(st=(1 << 23) + 8), dense(sh=1 << 26)
         assert call(a4=far) == UNSUPPORTED and call(a5=far) == UNSUPPORTED and call(a4=dense(st=1 << 23)) == 0
@@ -111,6 +115,9 @@ def test_workspaces(lib):
     for b in (1, 3, 8):
         sizes = [size(bwd, P, 4, 256, b, t) for t in (1, 127, 128, 129, 1000, 4096, 4097, 32768, 131072)]
         assert sizes == sorted(sizes) and len({size(bwd, P, s, w, b, 4096) for s in (0, 100, 5000) for w in (1, 300, 9000)}) == 1
+    for w in (1, 300, 100000):
+        sizes = [[size(dec, P, 4, w, b, t) for t in (1, 127, 1000, 4096, 4097, 32768, 131072)] for b in (1, 2, 3, 8, 40, 64, 300, 1000)]
+        assert all(x == sorted(x) for x in sizes) and all(list(x) == sorted(x) for x in zip(*sizes))
     for op, name in ((pre, "window_attn_prefill"), (dec, "window_attn_decode"), (dec, "window_attn_decode_quant"), (bwd, "window_attn_bwd")):
         need = size(op, P, 4, 256, 2, 4096)
         args, at = CALLS[name]
