@@ -476,3 +476,255 @@ def test_window_prefill_keeps_what_is_not_finite_where_it_is_seen(G, H, n, n_sin
         assert not finite[hit][:, bad].any() and finite[~hit].all()
         rest = [c for c in range(D) if c not in bad]               # the other channels of the same value: whole
         check(out[0, hit, hq][:, rest], lse[0, hit, hq], [x[hit][:, rest] if x.dim() == 2 else x[hit] for x in want])
+
+
+# ---- as they are used ---------------------------------------------------------------------------------------------
+
+def test_gradients_are_differences():
+    # a loss <out, w> along random directions: the calls' gradients against central differences of the definition in 64 bits
+    G, H, n, n_sink, window = 4, 2, 90, 3, 17
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    prm = binding.Params(G * H, H)
+    q, w = normal(gen, 1, n, G * H, D), normal(gen, 1, n, G * H, D)
+    k, v = random_cache(gen, 1, H, n, [n], spoil=False)
+    sl = lengths_tensor([n])
+    seen = window_seen(torch.arange(n, device="cuda"), n, n_sink, window)
+
+    def loss(q, k, v):
+        total = 0.0
+        for hq in range(G * H):
+            o, *_ = attend(q[0, :, hq], k[0, hq // G], v[0, hq // G], seen, prm.softmax_scale)
+            total = total + (o * w[0, :, hq].double()).sum()
+        return float(total)
+
+    out, lse = binding.window_attn_prefill(prm, n_sink, window, q, k, v, sl, n)
+    grads = binding.window_attn_bwd(prm, n_sink, window, q, k, v, out, w, lse, sl, n)
+    x = [q.double(), k.double(), v.double()]
+    for i, g in enumerate(grads):
+        for _ in range(4):
+            d = torch.randn(x[i].shape, generator=gen, device="cuda", dtype=torch.float64)
+            h = 1e-4                                               # central: error h^2 of the third derivative, 64-bit rounding 1e-16 / h
+            at = lambda s: loss(*[y + s * d if j == i else y for j, y in enumerate(x)])
+            slope = (at(h) - at(-h)) / (2 * h)
+            # a gradient's elements are rounded independently, 2^-8 of each at most (two roundings of 2^-9 on average): their sum along d is
+            # off by that of the root of the sum of squares, five times over
+            tol = 5 * 2.0 ** -8 * float((g.double() * d).norm()) + 1e-3
+            assert abs(float((g.double() * d).sum()) - slope) <= tol, (i, float((g.double() * d).sum()), slope, tol)
+
+
+def serve(prm, gen, lengths, steps, graph):
+    """a prompt, its cache in 4 bits, then decode steps on it: append, select, attend; checked against the path's own calls on the cache read
+    back.  Returns the outputs."""
+    B, H, Hq, T = len(lengths), prm.n_kv_heads, prm.n_q_heads, max(lengths) + steps
+    k, v = random_cache(gen, B, H, T, lengths, spoil=False)
+    q = normal(gen, B, T, Hq, D)
+    sl = lengths_tensor(lengths)
+    ck = torch.zeros((B, H, binding.num_kernels(T, prm), D), dtype=torch.bfloat16, device="cuda")
+    binding.compress_keys(prm, k, sl, T, ck=ck)
+    idx = binding.select_blocks(prm, binding.MODE_PREFILL, q, ck, sl, T)
+    binding.sparse_attn_prefill(prm, q, k, v, sl, T, idx)
+    kq, vq = binding.quantize_kv(prm, k, v, sl, T)
+    new = [normal(gen, steps, B, H, 1, D) for _ in range(2)]
+    queries = normal(gen, steps, B, 1, Hq, D)
+    ws = torch.empty(max(binding.workspace_bytes(op, prm, B, T) for op in (binding.OP_SELECT_DECODE, binding.OP_ATTN_DECODE)),
+                     dtype=torch.uint8, device="cuda")
+    now = [torch.empty_like(x[0]) for x in (*new, queries)]
+    bufs = dict(out=torch.empty((B, 1, Hq, D), dtype=torch.bfloat16, device="cuda"),
+                lse=torch.empty((B, Hq), dtype=torch.float32, device="cuda"), workspace=ws)
+    block_idx = torch.empty((B, H, 1, prm.topk), dtype=torch.int32, device="cuda")
+
+    def step():
+        sl.add_(1)
+        binding.append_kv_quant(prm, now[0], now[1], kq, vq, sl, T, ck=ck)
+        binding.select_blocks(prm, binding.MODE_DECODE, now[2], ck, sl, T, block_idx=block_idx, workspace=ws)
+        binding.sparse_attn_decode_quant(prm, now[2], kq, vq, sl, T, block_idx, **bufs)
+
+    captured = None
+    if graph:
+        saved = [x.clone() for x in (sl, ck, *kq, *vq)]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for x, y in zip(now, (*new, queries)):
+                x.copy_(y[0])
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+        captured = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(captured, stream=side):
+            step()
+        for x, y in zip((sl, ck, *kq, *vq), saved):
+            x.copy_(y)
+    results = []
+    for i in range(steps):
+        for x, y in zip(now, (*new, queries)):
+            x.copy_(y[i])
+        captured.replay() if captured else step()
+        kb, vb = binding.dequantize_kv(prm, kq, vq, sl, T)         # the program's own work between the steps
+        want, want_lse = binding.sparse_attn_decode(prm, now[2], kb, vb, sl, T, block_idx)
+        # both round probabilities to bf16 (2^-8 of |o| <= sum p |v|) and the result; |v| of N(0,1) in 4 bits is at most 6
+        assert (bufs["out"].float() - want.float()).abs().max() <= 4 * HALF * 6
+        assert (bufs["lse"] - want_lse).abs().max() <= 1e-4
+        own = (sl - 1) // 64
+        assert torch.equal(block_idx.amax(-1)[:, :, 0], own[:, None].expand(-1, H).to(torch.int32))
+        results.append([x.clone() for x in (bufs["out"], bufs["lse"], block_idx, ck, *kq, *vq)])
+    return results
+
+
+@pytest.mark.parametrize("hq,hkv,lengths,topk", [(32, 2, [777, 1300], 8), (4, 1, [4090], 16), (2, 2, [100, 40, 63], 3)])
+def test_a_prompt_and_decode_steps_on_the_4_bit_cache(hq, hkv, lengths, topk):
+    prm = binding.Params(hq, hkv, topk=topk)
+    eager = serve(prm, torch.Generator(device="cuda").manual_seed(3), lengths, 18, False)
+    replayed = serve(prm, torch.Generator(device="cuda").manual_seed(3), lengths, 18, True)
+    for a, b in zip(eager, replayed):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_verification_step_on_the_4_bit_cache():
+    # append and verify n drafted tokens; without a mask it is n decode steps
+    prm = binding.Params(8, 2, topk=8)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    lengths, n, T = [500, 37], 7, 512
+    k, v = random_cache(gen, 2, 2, T, lengths, spoil=False)
+    new = [normal(gen, 2, 2, n, D) for _ in range(2)]
+    q = normal(gen, 2, n, 8, D)
+    ck = binding.compress_keys(prm, k, lengths_tensor(lengths), T)
+    one, two = [[binding.QuantCache(*(y.clone() for y in x)) for x in binding.quantize_kv(prm, k, v, lengths_tensor(lengths), T)] + [ck.clone()] for _ in range(2)]
+    sl = lengths_tensor([x + n for x in lengths])
+    binding.append_kv_quant(prm, *new, one[0], one[1], sl, T, ck=one[2])
+    idx = binding.select_blocks_verify(prm, q, one[2], sl, T)
+    out, lse = binding.sparse_attn_verify_quant(prm, q, one[0], one[1], sl, T, idx)
+    for i in range(n):
+        at = lengths_tensor([x + i + 1 for x in lengths])
+        binding.append_kv_quant(prm, new[0][:, :, i:i + 1], new[1][:, :, i:i + 1], two[0], two[1], at, T, ck=two[2])
+        qi = q[:, i:i + 1]
+        di = binding.select_blocks(prm, binding.MODE_DECODE, qi, two[2], at, T)
+        assert torch.equal(di, idx[:, :, i:i + 1])
+        o, z = binding.sparse_attn_decode_quant(prm, qi, two[0], two[1], at, T, di)
+        assert (o[:, 0].float() - out[:, i].float()).abs().max() <= 4 * HALF * 6 and (z - lse[:, i]).abs().max() <= 1e-5
+    for x, y in zip((*one[0], *one[1], one[2]), (*two[0], *two[1], two[2])):
+        assert torch.equal(x, y)
+
+
+def test_window_training_step_captured():
+    # forward and backward in one graph, replayed with new inputs, eager work and synchronisations in between
+    prm = binding.Params(16, 2)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    B, T, n_sink, window = 2, 900, 4, 200
+    sl = lengths_tensor([900, 650])
+    x = [normal(gen, B, T, 16, D), normal(gen, B, 2, T, D), normal(gen, B, 2, T, D), normal(gen, B, T, 16, D)]
+
+    def both(q, k, v, dout):
+        out, lse = binding.window_attn_prefill(prm, n_sink, window, q, k, v, sl, T)
+        return (out, lse, *binding.window_attn_bwd(prm, n_sink, window, q, k, v, out, dout, lse, sl, T))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both(*x)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = both(*x)
+    for i in range(4):
+        for y in x:
+            y.normal_(generator=gen)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, both(*x))), i
+
+
+def test_two_streams_at_once():
+    # calls on two streams with workspaces of their own, and results and scratch made by the call on each
+    prm = binding.Params(16, 1)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    T, sl = 2048, lengths_tensor([2048])
+    sets = [(normal(gen, 1, T, 16, D), *random_cache(gen, 1, 1, T, [T])) for _ in range(2)]
+
+    def work(q, k, v):
+        kq, vq = binding.quantize_kv(prm, k, v, sl, T)
+        out, lse = binding.window_attn_prefill(prm, 4, 500, q, k, v, sl, T)
+        last = q[:, -1:]
+        return [out, lse, *binding.window_attn_bwd(prm, 4, 500, q, k, v, out, q, lse, sl, T), *kq, *vq,
+                *binding.window_attn_decode(prm, 4, 500, last, k, v, sl, T), *binding.window_attn_decode_quant(prm, 4, 500, last, kq, vq, sl, T)]
+
+    want = [work(*s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for s, st in zip(sets, streams):
+            with torch.cuda.stream(st):
+                got.append(work(*s))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+def test_caches_beyond_32_bits():
+    # a cache whose last head lies 4 GiB and more behind the first: offsets of heads and sequences are 64-bit
+    prm = binding.Params(2, 2)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    T, n = 9_000_000, 100
+    k = torch.zeros((1, 2, T, D), dtype=torch.bfloat16, device="cuda")     # 4.6 GB
+    k[:, :, :n], k[:, :, T - n:] = normal(gen, 1, 2, n, D), normal(gen, 1, 2, n, D)
+    q = normal(gen, 1, 1, 2, D)
+    sl = lengths_tensor([T])
+    seen = torch.ones((1, 2 * n), dtype=torch.bool, device="cuda")
+    kq, vq = binding.quantize_kv(prm, k, k, sl, T)
+    for out, lse, src in ((*binding.window_attn_decode(prm, n, n, q, k, k, sl, T), k),
+                          (*binding.window_attn_decode_quant(prm, n, n, q, kq, vq, sl, T), None)):
+        for h in range(2):
+            x = values_of(binding.QuantCache(*(torch.cat((y[0, h, :n], y[0, h, T - n:])) for y in kq))) if src is None else \
+                torch.cat((k[0, h, :n], k[0, h, T - n:])).double()
+            check(out[0, 0, h:h + 1], lse[0, h:h + 1], attend(q[0, 0, h:h + 1].double(), x, x, seen, prm.softmax_scale))
+
+
+def test_refusals_of_the_binding():
+    prm = binding.Params(4, 1)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    T = 64
+    q, k, v = normal(gen, 1, T, 4, D), normal(gen, 1, 1, T, D), normal(gen, 1, 1, T, D)
+    sl = lengths_tensor([T])
+    kq, vq = binding.quantize_kv(prm, k, v, sl, T)
+    idx = torch.zeros((1, 1, 1, prm.topk), dtype=torch.int32, device="cuda")
+    one = q[:, :1]
+    lse = torch.zeros((1, T, 4), device="cuda")
+    QC = binding.QuantCache
+    bad = [
+        lambda: binding.quantize_kv(prm, k, v, sl, T + 1),                                   # longer than the cache
+        lambda: binding.quantize_kv(prm, k, v.float(), sl, T),
+        lambda: binding.quantize_kv(prm, k, v[:, :, :T - 1], sl, T),
+        lambda: binding.quantize_kv(prm, k, v, sl.long(), T),
+        lambda: binding.quantize_kv(prm, k, v, lengths_tensor([T, T]), T),
+        lambda: binding.quantize_kv(prm, k, v, sl, -1),
+        lambda: binding.quantize_kv(prm, k, v, sl, T, QC(kq.codes[..., :32], kq.scales), vq),
+        lambda: binding.quantize_kv(prm, k, v, sl, T, kq),
+        lambda: binding.dequantize_kv(prm, QC(kq.codes, kq.scales.int()), vq, sl, T),
+        lambda: binding.dequantize_kv(prm, QC(kq.codes.cpu(), kq.scales), vq, sl, T),
+        lambda: binding.dequantize_kv(prm, kq, vq, sl, T, k=k[..., :64]),
+        lambda: binding.append_kv_quant(prm, k[:, :, :2], v[:, :, :1], kq, vq, sl, T),
+        lambda: binding.append_kv_quant(prm, k[:, :, :0], v[:, :, :0], kq, vq, sl, T),
+        lambda: binding.append_kv_quant(prm, k[:, :, :1], v[:, :, :1], kq, vq, sl, T, ck=k[:, :, :2]),
+        lambda: binding.sparse_attn_decode_quant(prm, q, kq, vq, sl, T, idx),                # more than one row
+        lambda: binding.sparse_attn_decode_quant(prm, one, kq, vq, sl, T, idx[..., :3]),
+        lambda: binding.sparse_attn_decode_quant(prm, one, kq, vq, sl, T, idx, out=q[:, :, :2]),
+        lambda: binding.sparse_attn_verify_quant(prm, q[:, :3], kq, vq, sl, T, idx),
+        lambda: binding.window_attn_prefill(prm, -1, 8, q, k, v, sl, T),
+        lambda: binding.window_attn_prefill(prm, 0, 0, q, k, v, sl, T),
+        lambda: binding.window_attn_prefill(prm, 0, 8, q[:, :T - 1], k, v, sl, T),
+        lambda: binding.window_attn_prefill(prm, 0, 8, q, k, v, sl, T, lse=lse[:, :, :2]),
+        lambda: binding.window_attn_prefill(prm, 0, 1 << 31, q, k, v, sl, T),
+        lambda: binding.window_attn_bwd(prm, 0, 8, q, k, v, q, q, lse.half(), sl, T),
+        lambda: binding.window_attn_bwd(prm, 0, 8, q, k, v, q, q, lse, sl, T, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")),
+        lambda: binding.window_attn_decode(prm, 0, 8, q, k, v, sl, T),
+        lambda: binding.window_attn_decode_quant(prm, 0, 8, one, k, v, sl, T),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(binding.InfLLMv2Error):
+            call()
+            pytest.fail("call %d was not refused" % i)
+    # a sequence that claims to be longer than max_seqlen is clamped to it, a negative length is none
+    out, _ = binding.window_attn_prefill(prm, 0, 8, q, k, v, sl, T)
+    assert torch.equal(binding.window_attn_prefill(prm, 0, 8, q, k, v, lengths_tensor([1000]), T)[0], out)
+    assert not binding.window_attn_prefill(prm, 0, 8, q, k, v, lengths_tensor([-5]), T)[0].any()
+    assert torch.equal(binding.window_attn_decode(prm, 0, 8, one, k, v, lengths_tensor([1000]), T)[0],
+                       binding.window_attn_decode(prm, 0, 8, one, k, v, sl, T)[0])
