@@ -166,7 +166,9 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
     const int item = xcd_item(blockIdx.x, plan.per_span), group = item / plan.per_span, bh = group / plan.spans;     // a span is a run
     const int b = bh / dm.Hkv, h = bh - b * dm.Hkv, span = (bh + 1) * plan.spans - 1 - group, at = item - group * plan.per_span;
     if (b >= dm.batch) return;
-    const int tile = at < plan.sink_tiles ? at : plan.first_tile(win, span) + at - plan.sink_tiles;
+    // the sinks' tiles; from the span's first tile back, which all of its queries see, down to the window's edge; the span's other tiles
+    const int begin = max(plan.sink_tiles, span * (plan.span / kKvKeys)), back = begin - plan.first_tile(win, span), y = at - plan.sink_tiles;
+    const int tile = y < 0 ? at : y <= back ? begin - y : begin + y - back;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
