@@ -64,17 +64,18 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16 &x, int s) {
     return r;
 }
 
-// Tiles of kKeys keys that any of the queries t0 .. t1 - 1 sees: `sinks` tiles from the first on, then those from `first` to `last`.
+// Tiles of kKeys keys that any of the queries t0 .. t1 - 1 sees: `sinks` tiles from the first on, then those from `first` to the last.
 constexpr int kWinKeys = 64;
+template <int kKeys>
 struct KeyTiles {
     int sinks, first, count;
     __device__ __forceinline__ KeyTiles(WindowArgs w, int t0, int t1) {
         const int lo = max(0, t0 - w.window + 1);
-        sinks = (min(w.n_sink, lo) + kWinKeys - 1) / kWinKeys;
-        first = max(lo / kWinKeys, sinks);
-        count = sinks + (t1 - 1) / kWinKeys - first + 1;
+        sinks = (min(w.n_sink, lo) + kKeys - 1) / kKeys;
+        first = max(lo / kKeys, sinks);
+        count = sinks + (t1 - 1) / kKeys - first + 1;
     }
-    __device__ __forceinline__ int key0(int i) const { return kWinKeys * (i < sinks ? i : first + i - sinks); }
+    __device__ __forceinline__ int key0(int i) const { return kKeys * (i < sinks ? i : first + i - sinks); }
 };
 
 // Whether the query at position i sees a key.  No branches: a wavefront tests sixteen keys at a time.
@@ -106,6 +107,55 @@ struct TileCopier {
             copy_rows(dst.x + ((j >> 1) * kHalfTile + wave * 2048 + (j & 1) * 1024), base, r0 + 16 * j + (lane >> 2) < L ? at : kNoRow, 16 * j * step);
     }
 };
+// The same for few rows, a wavefront by itself: 32 keys and their values, all four quarters, into tiles of its own.
+struct __align__(16) KVHalf {
+    char k[kHalfTile], v[kHalfTile];
+};
+constexpr int kHalfCopies = 16;                          // copies of a half
+__device__ __forceinline__ void copy_half(KVHalf &dst, const Tensor &k, const Tensor &v, int64_t k_head, int64_t v_head, int k0, int L, int lane) {
+    const char *kb = reinterpret_cast<const char *>(k.ptr + k_head + (int64_t)k0 * k.st), *vb = reinterpret_cast<const char *>(v.ptr + v_head + (int64_t)k0 * v.st);
+    const uint32_t piece = 16 * copy_piece(lane), k_at = (lane >> 2) * (2 * (uint32_t)k.st) + piece, v_at = (lane >> 2) * (2 * (uint32_t)v.st) + piece;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const bool row = k0 + 16 * j + (lane >> 2) < L;
+#pragma unroll
+        for (int quarter = 0; quarter < 4; ++quarter) {
+            copy_rows(dst.k + quarter * 2048 + j * 1024, kb + 64 * quarter, row ? k_at : kNoRow, 32 * j * (uint32_t)k.st);
+            copy_rows(dst.v + quarter * 2048 + j * 1024, vb + 64 * quarter, row ? v_at : kNoRow, 32 * j * (uint32_t)v.st);
+        }
+    }
+}
+// All but the newest kHalfCopies copies have landed, or all.
+__device__ __forceinline__ void copies_landed(bool but_the_newest) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (but_the_newest) __builtin_amdgcn_s_waitcnt(0x4f70);              // vmcnt 16
+    else __builtin_amdgcn_s_waitcnt(0x0f70);                             // vmcnt 0
+    __builtin_amdgcn_sched_barrier(0);
+}
+// This wavefront's LDS reads have ended: what they read may be overwritten.
+__device__ __forceinline__ void reads_done() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);                  // lgkmcnt 0
+    __builtin_amdgcn_sched_barrier(0);
+}
+// A wavefront's walk over units wave, wave + 4, ..: one ahead under way.
+template <typename F>
+__device__ __forceinline__ void walk_halves(KVHalf &slot0, KVHalf &slot1, const Tensor &k, const Tensor &v, int b, int h, const KeyTiles<32> &kt, int L,
+                                            int wave, int lane, F unit) {
+    const int64_t k_head = b * k.sb + h * k.sh, v_head = b * v.sb + h * v.sh;
+    auto step = [&](const KVHalf &cur, KVHalf &next, int x) __attribute__((always_inline)) {
+        reads_done();
+        if (x + 4 < kt.count) copy_half(next, k, v, k_head, v_head, kt.key0(x + 4), L, lane);
+        copies_landed(x + 4 < kt.count);
+        unit(cur, kt.key0(x));
+    };
+    if (wave < kt.count) copy_half(slot0, k, v, k_head, v_head, kt.key0(wave), L, lane);
+    for (int x = wave; x < kt.count; x += 8) {
+        step(slot0, slot1, x);
+        if (x + 4 < kt.count) step(slot1, slot0, x + 4);
+    }
+}
+
 // The largest of three numbers, one instruction (fmaxf first makes the results of a product canonical, an instruction each).  NaN if any is.
 __device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
             for (int c = 0; c < 16; ++c) *reinterpret_cast<uint2 *>(dq_row + 8 * c) = uint2{0u, 0u};
         return;
     }
-    const KeyTiles kt(win, t0, t1);
+    const KeyTiles<kWinKeys> kt(win, t0, t1);
     const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
     auto stage = [&](KVTile &dst, int x) __attribute__((always_inline)) {
         if (x >= kt.count) return;
@@ -121,6 +121,99 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
         }
 }
 
+// The same for few rows, as in the forward: 32 rows to a workgroup, every fourth unit of 32 keys to a wavefront, four sums joined in LDS.
+__global__ __launch_bounds__(256, 1) void window_dq_few_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, Tensor q, Tensor k,
+                                                               Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
+                                                               const int32_t *__restrict__ seqlens, Tensor dq, float *__restrict__ rows) {
+    __shared__ KVHalf slot0[4], slot1[4];
+    const int bh = blockIdx.x / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int ti = (bh + 1) * n_tiles - 1 - (int)blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
+    const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
+    const int t0 = ti * (32 >> lg), t1 = min(L, t0 + (32 >> lg));
+    // the result's row and 16 channels of this thread
+    const int o_row = tid >> 3, ch = 16 * (tid & 7), o_i = t0 + (o_row >> lg), o_hq = h * dm.G + (o_row & (dm.G - 1));
+    __bf16 *dq_row = dq.ptr + b * dq.sb + (int64_t)o_i * dq.st + (int64_t)o_hq * dq.sh + ch;
+    const bool store = o_i < dm.max_seqlen && (o_i < L || dm.fill);
+    if (t0 >= L) {
+        if (store) reinterpret_cast<uint4 *>(dq_row)[0] = reinterpret_cast<uint4 *>(dq_row)[1] = uint4{0u, 0u, 0u, 0u};
+        return;
+    }
+    const KeyTiles<32> kt(win, t0, t1);
+    const int row = lane & 31, i = t0 + (row >> lg), hq = h * dm.G + (row & (dm.G - 1));
+    bf16x8 qf[8], gf[8];
+    float D = 0.f;
+    const int64_t t = min(i, L - 1);
+    const __bf16 *qr = q.ptr + b * q.sb + t * q.st + (int64_t)hq * q.sh + 8 * hf;
+    const __bf16 *gr = dout.ptr + b * dout.sb + t * dout.st + (int64_t)hq * dout.sh + 8 * hf;
+    const __bf16 *orow = out.ptr + b * out.sb + t * out.st + (int64_t)hq * out.sh + 8 * hf;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+        qf[ks] = load8(qr + 16 * ks);
+        gf[ks] = load8(gr + 16 * ks);
+        const bf16x8 x = load8(orow + 16 * ks);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) D = __builtin_fmaf((float)gf[ks][e], (float)x[e], D);
+    }
+    D = half_reduce(D, [](float a, float d) { return a + d; });
+    const float ref = lse[((int64_t)b * dm.max_seqlen + t) * dm.Hq + hq] * kLog2e, c = dm.scale_log2;
+    if (wave == 0 && i < L) {
+        const int64_t r = (int64_t)ti * 32 + row;
+        rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? D : ref;
+    }
+    const TileReader rd(lane);
+    f32x16 acc[4];
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) acc[ct] = zero16();
+    const int hi = t0 + (31 >> lg);
+    walk_halves(slot0[wave], slot1[wave], k, v, b, h, kt, L, wave, lane, [&](const KVHalf &cur, int k0) __attribute__((always_inline)) {
+        f32x16 s = zero16(), dp;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dp[e] = -D;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+            s = mfma32(rd.rows(cur.k, ks), qf[ks], s);
+            dp = mfma32(rd.rows(cur.v, ks), gf[ks], dp);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = fast_exp2(__builtin_fmaf(s[e], c, -ref)) * dp[e];
+        if (!(k0 + 31 <= t0 && (k0 + 32 <= win.n_sink || hi - k0 < win.window))) {
+            const VisibleKeys visible(win, i);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = visible(k0 + 4 * hf + 8 * (e >> 2) + (e & 3)) ? s[e] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const bf16x8 ds = pack8(s, j);
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) acc[ct] = mfma32(rd.columns(cur.k, j, ct), ds, acc[ct]);
+        }
+    });
+    reads_done();
+    // [row][channel], 16-byte pieces XORed with the row
+    float *mine = reinterpret_cast<float *>(&slot0[wave]);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+            *reinterpret_cast<f32x4 *>(mine + row * kHeadDim + 4 * ((8 * ct + 2 * e4 + hf) ^ (lane & 7))) =
+                f32x4{acc[ct][4 * e4], acc[ct][4 * e4 + 1], acc[ct][4 * e4 + 2], acc[ct][4 * e4 + 3]};
+    __syncthreads();
+    if (!store) return;
+    bf16x8 z[2];
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            y += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(&slot0[w]) + o_row * kHeadDim + 4 * ((ch / 4 + e4) ^ (o_row & 7)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e4 >> 1][4 * (e4 & 1) + e] = (__bf16)(o_i < L ? y[e] * scale : 0.f);
+    }
+    reinterpret_cast<uint4 *>(dq_row)[0] = __builtin_bit_cast(uint4, z[0]);
+    reinterpret_cast<uint4 *>(dq_row)[1] = __builtin_bit_cast(uint4, z[1]);
+}
+
 // ---- dk, dv ------------------------------------------------------------------------------------------------------------------
 // A workgroup takes 128 keys, 32 to a wavefront (as columns: their K stays in registers, their V in LDS: both would not fit 256 registers),
 // and the rows of a span of tokens that see any of them, in steps of 32; rows and their scalars go straight into LDS one step ahead.
@@ -132,7 +225,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
 constexpr int kKvKeys = 128, kKvRows = 32;
 struct BwdPlan {
     int tiles, sink_tiles;                               // key tiles of a sequence; those with any of the first n_sink tokens
-    int span, spans;                                     // tokens of a span (a multiple of kKvKeys), spans
+    int span, spans;                                     // tokens of a span (a multiple of 32), spans
     int per_span;                                        // key tiles a span may have
     int parts;                                           // spans a tile may have, sinks' tiles apart
     __host__ __device__ int slot(int tile) const { return tile < sink_tiles ? tile * spans : sink_tiles * spans + (tile - sink_tiles) * parts; }
@@ -157,17 +250,21 @@ struct __align__(16) KvRows {
     float ref[32], D[32];
 };
 
-__global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs win, float scale, int lg, BwdPlan plan, Tensor q, Tensor k,
+// kSlots: rows two steps (one ahead) or four (three ahead) at a time.  A compute unit with one workgroup does not hide a round trip to memory under
+// the other's step; with four slots it holds one only.
+template <int kSlots>
+__global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(Dims dm, WindowArgs win, float scale, int lg, BwdPlan plan, Tensor q, Tensor k,
                                                              Tensor v, Tensor dout, const float *__restrict__ rows,
                                                              const int32_t *__restrict__ seqlens, Tensor dk, Tensor dv,
                                                              float *__restrict__ part) {
     __shared__ KvRows slot0, slot1;
+    __shared__ std::conditional_t<kSlots == 4, KvRows, char> slot2, slot3;
     __shared__ __align__(16) char vt[kKvKeys * 256];
     const int item = xcd_item(blockIdx.x, plan.per_span), group = item / plan.per_span, bh = group / plan.spans;     // a span is a run
     const int b = bh / dm.Hkv, h = bh - b * dm.Hkv, span = (bh + 1) * plan.spans - 1 - group, at = item - group * plan.per_span;
     if (b >= dm.batch) return;
     // the sinks' tiles; from the span's first tile back, which all of its queries see, down to the window's edge; the span's other tiles
-    const int begin = max(plan.sink_tiles, span * (plan.span / kKvKeys)), back = begin - plan.first_tile(win, span), y = at - plan.sink_tiles;
+    const int begin = max(plan.sink_tiles, (int)((int64_t)span * plan.span / kKvKeys)), back = begin - plan.first_tile(win, span), y = at - plan.sink_tiles;
     const int tile = y < 0 ? at : y <= back ? begin - y : begin + y - back;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
@@ -203,21 +300,28 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
         q_at[j] = 2u * (tok * (uint32_t)q.st + g * (uint32_t)q.sh) + piece;
         g_at[j] = 2u * (tok * (uint32_t)dout.st + g * (uint32_t)dout.sh) + piece;
     }
+    // (with four slots as many copies for every step: those past the last bring zeros)
     auto stage = [&](KvRows &dst, int x) __attribute__((always_inline)) {
-        if (x >= x1) return;
-        const int i0 = from + x * per;
+        if (kSlots == 2 && x >= x1) return;
+        const int i0 = from + min(x, x1 - 1) * per;
         const char *qb = q_head + (int64_t)i0 * (2 * q.st), *gb = g_head + (int64_t)i0 * (2 * dout.st);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const bool row = i0 + ((16 * j + (lane >> 2)) >> lg) < L;
+            const bool row = x < x1 && i0 + ((16 * j + (lane >> 2)) >> lg) < L;
             copy_rows(dst.q + wave * 2048 + j * 1024, qb, row ? q_at[j] : kNoRow, 0);
             copy_rows(dst.g + wave * 2048 + j * 1024, gb, row ? g_at[j] : kNoRow, 0);
         }
-        if (wave == 0)
+        if (lane >> 4 == wave)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(row_head + ((int64_t)i0 >> (5 - lg)) * 64 + lane),
                                              (__attribute__((address_space(3))) void *)dst.ref, 4, 0, 0);
     };
-    stage(slot0, 0);
+    if (x1 > 0) {
+        stage(slot0, 0);
+        if constexpr (kSlots == 4) {
+            stage(slot1, 1);
+            stage(slot2, 2);
+        }
+    }
     const TileReader rd(lane);
     const float c = dm.scale_log2;
     f32x16 dka[4], dva[4];
@@ -225,9 +329,16 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
     for (int ct = 0; ct < 4; ++ct) dka[ct] = dva[ct] = zero16();
     const int k_lo = tile * kKvKeys + 32 * wave, k_hi = k_lo + 31;
     auto step = [&](const KvRows &cur, KvRows &next, int x) __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        stage(next, x + 1);
+        if constexpr (kSlots == 2) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+        } else {                                         // all copies but those of the next two steps, five each (vmcnt 10)
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0f7a);
+            asm volatile("s_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        stage(next, x + kSlots - 1);
         const int i0 = from + x * per, i1 = i0 + per - 1;
         const bool some = k_lo <= i1 && (k_lo < win.n_sink || i0 - k_hi < win.window);
         if (!some) return;
@@ -293,9 +404,19 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs
             dka[i & 3] = mfma32(cq[i & 1], ds[i >> 2], dka[i & 3]);
         }
     };
-    for (int x = 0; x < x1; x += 2) {
-        step(slot0, slot1, x);
-        if (x + 1 < x1) step(slot1, slot0, x + 1);
+    if constexpr (kSlots == 2) {
+        for (int x = 0; x < x1; x += 2) {
+            step(slot0, slot1, x);
+            if (x + 1 < x1) step(slot1, slot0, x + 1);
+        }
+    } else {
+        for (int x = 0; x < x1; x += 4) {
+            step(slot0, slot3, x);
+            if (x + 1 < x1) step(slot1, slot0, x + 1);
+            if (x + 2 < x1) step(slot2, slot1, x + 2);
+            if (x + 3 < x1) step(slot3, slot2, x + 3);
+        }
+        __builtin_amdgcn_s_waitcnt(0);                   // (the copies past the last step have landed: the memory may go to another workgroup)
     }
     if (rows_of.first != rows_of.last) {                 // [key][channel], dk then dv
         const int64_t slot = (int64_t)bh * plan.slot(plan.tiles) + plan.slot(tile) + span - rows_of.first;
@@ -368,32 +489,31 @@ __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs wi
 // enough for every smaller one.
 static int64_t most_slots(int64_t tiles) { return min(8 * tiles, 2048 + 2 * tiles); }
 
-// The span: of some lengths, each a quarter longer than the one before, the one whose workgroups the chip, which holds 512, is through with first:
-// all steps, about 50 more per workgroup for its start and its sums, and half a longest workgroup's steps in which not all have work.
+// The span: of some lengths the one whose workgroups the chip, which holds 512, is through with first: all steps, about 50 more per
+// workgroup for its start and its sums (but not less than the longest workgroup), and half a longest workgroup's steps in which not all have work.
 static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
     BwdPlan best{};
     const int per = kKvRows / dm.G;
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
     const int64_t all_steps = (dm.max_seqlen + per - 1) / per, window_steps = min(all_steps, ((int64_t)w.window + kKvKeys - 1 + per - 1) / per);
+    BwdPlan p;
+    p.tiles = (dm.max_seqlen + kKvKeys - 1) / kKvKeys;
+    p.sink_tiles = (w.n_sink + kKvKeys - 1) / kKvKeys;
+    const int64_t steps = heads * (p.sink_tiles * all_steps + (p.tiles - p.sink_tiles) * window_steps), whole = (int64_t)p.tiles * kKvKeys;
     int64_t least = INT64_MAX;
-    for (int64_t blocks = 1;; blocks += (blocks + 3) / 4) {
-        BwdPlan p;
-        p.tiles = (dm.max_seqlen + kKvKeys - 1) / kKvKeys;
-        p.sink_tiles = (w.n_sink + kKvKeys - 1) / kKvKeys;
-        const int64_t steps = heads * (p.sink_tiles * all_steps + (p.tiles - p.sink_tiles) * window_steps);
-        blocks = min(blocks, (int64_t)p.tiles);
-        p.span = (int)(blocks * kKvKeys);
-        p.spans = (int)((p.tiles + blocks - 1) / blocks);
-        const int64_t reach = (w.window + 126) / kKvKeys + 1;              // tiles behind a span's own that its first query may see
-        p.per_span = (int)min((int64_t)p.tiles, p.sink_tiles + blocks + reach);
-        p.parts = (int)min((int64_t)p.spans, ((int64_t)w.window + 126) / p.span + 2);
-        const int64_t items = heads * p.spans * p.per_span, longest = (min(p.span, dm.max_seqlen) + per - 1) / per;
-        const int64_t cost = (steps + 50 * items) / 512 + longest / 2;
+    for (int64_t span = 32;; span = span < kKvKeys ? 2 * span : span + (span / kKvKeys + 3) / 4 * kKvKeys) {
+        span = min(span, whole);
+        p.span = (int)span;
+        p.spans = (int)((dm.max_seqlen + span - 1) / span);
+        p.per_span = (int)min((int64_t)p.tiles, p.sink_tiles + (span + w.window - 2) / kKvKeys + 2);
+        p.parts = (int)min((int64_t)p.spans, ((int64_t)w.window + 126) / span + 2);
+        const int64_t items = heads * p.spans * p.per_span, longest = (min(span, (int64_t)dm.max_seqlen) + per - 1) / per;
+        const int64_t cost = max((steps + 50 * items) / 512, longest) + longest / 2;
         if (heads * p.slot(p.tiles) <= most_slots(heads * p.tiles) && cost < least) {
             least = cost;
             best = p;
         }
-        if (blocks == p.tiles) return best;              // (one span: a slot per tile at most)
+        if (span == whole) return best;                  // (one span: a slot per tile at most)
     }
 }
 
@@ -411,14 +531,19 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
     float *rows = reinterpret_cast<float *>(ws), *part = rows + (size_t)dm.batch * dm.Hkv * row_blocks(dm) * 64;
     const BwdPlan plan = bwd_plan(dm, w);
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
+    const int few_tiles = (dm.max_seqlen + (32 >> lg) - 1) / (32 >> lg), run = xcd_run_length(n_tiles * heads);
     timing_begin("window_dq_kernel", stream);
-    const int run = xcd_run_length(n_tiles * heads);
-    hipLaunchKernelGGL(window_dq_kernel, dim3(xcd_grid(n_tiles * heads, run)), dim3(256), 0, stream, dm, w, scale, lg, n_tiles, run, q, k, v,
+    if (n_tiles * heads <= 64)
+        hipLaunchKernelGGL(window_dq_few_kernel, dim3((unsigned)(few_tiles * heads)), dim3(256), 0, stream, dm, w, scale, lg, few_tiles, q, k, v, out,
+                           dout, lse, seqlens, dq, rows);
+    else
+        hipLaunchKernelGGL(window_dq_kernel, dim3(xcd_grid(n_tiles * heads, run)), dim3(256), 0, stream, dm, w, scale, lg, n_tiles, run, q, k, v,
                        out, dout, lse, seqlens, dq, rows);
     timing_end(stream);
     timing_begin("window_dkdv_kernel", stream);
-    hipLaunchKernelGGL(window_dkdv_kernel, dim3(xcd_grid(plan.spans * plan.per_span * heads, plan.per_span)), dim3(256), 0, stream, dm, w, scale, lg, plan,
-                       q, k, v, dout, rows, seqlens, dk, dv, part);
+    const int64_t items = plan.spans * plan.per_span * heads;
+    hipLaunchKernelGGL(items <= 256 ? window_dkdv_kernel<4> : window_dkdv_kernel<2>, dim3(xcd_grid(items, plan.per_span)), dim3(256), 0, stream,
+                       dm, w, scale, lg, plan, q, k, v, dout, rows, seqlens, dk, dv, part);
     timing_end(stream);
     if (plan.spans == 1) return (int)hipGetLastError();
     timing_begin("window_join_kernel", stream);

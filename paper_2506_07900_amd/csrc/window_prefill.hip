@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
         }
         return;
     }
-    const KeyTiles kt(win, t0, t1);
+    const KeyTiles<kWinKeys> kt(win, t0, t1);
     const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
     auto stage = [&](const TileCopier &from, Tile64 &to, int x) __attribute__((always_inline)) {
         if (x < kt.count) from.copy(to, kt.key0(x), wave, lane);
@@ -154,6 +154,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
     stage(keys, K0, 0);
     stage(values, V0, 0);
     stage(keys, K1, 1);
+    stage(values, V1, 1);
     r.load(q, b, L);
     // Tile x: its probabilities and their product with the values, and between them the next tile's scores, so that the matrix cores have
     // work while the exponentials run.  (Behind the last tile: scores of what lies in LDS, not used.)
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
         __builtin_amdgcn_s_waitcnt(0);                   // this wavefront's copies have landed
         __syncthreads();                                 // everyone's have, and everyone is past the tile before
         stage(keys, k_cur, x + 2);
-        stage(values, v_next, x + 1);
+        if (x > 0) stage(values, v_next, x + 1);         // (the first two at once: a short walk is a chain of round trips)
         const float base = r.reference(mx);
         __builtin_amdgcn_sched_barrier(0);
         r.scores(k_next, s_next);
@@ -210,16 +211,14 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
     }
 }
 
-// The same for few rows: a workgroup takes 32 of them, its wavefronts every fourth key tile each, fetched for itself and without a
+// The same for few rows: a workgroup takes 32 of them, its wavefronts every fourth unit of 32 keys each, fetched for itself and without a
 // barrier; their four states are joined in LDS at the end.
-struct __align__(16) WaveTiles {
-    Tile64 k[4], v[4];
-};
 __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, Tensor q, Tensor k, Tensor v,
                                                                     const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
-    __shared__ WaveTiles tiles;
+    __shared__ KVHalf slot0[4], slot1[4];
     __shared__ float ml[2][4][32];
-    const int ti = blockIdx.x % n_tiles, bh = blockIdx.x / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int bh = blockIdx.x / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int ti = (bh + 1) * n_tiles - 1 - (int)blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int t0 = ti * (32 >> lg), t1 = min(L, t0 + (32 >> lg));
@@ -236,41 +235,41 @@ __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, Win
         }
         return;
     }
-    const KeyTiles kt(win, t0, t1);
-    Tile64 &kw = tiles.k[wave], &vw = tiles.v[wave];
-    auto stage = [&](const Tensor &t, Tile64 &to, int x) __attribute__((always_inline)) {
-        if (x >= kt.count) return;
-#pragma unroll
-        for (int part = 0; part < 4; ++part) TileCopier(t, b, h, L, part, lane).copy(to, kt.key0(x), part, lane);
-    };
-    stage(k, kw, wave);
-    stage(v, vw, wave);
+    const KeyTiles<32> kt(win, t0, t1);
     r.load(q, b, L);
-    auto reads_done = [] {                               // of this wavefront, which alone uses its tiles: lgkmcnt 0
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    for (int x = wave; x < kt.count; x += 4) {
-        __builtin_amdgcn_s_waitcnt(0);
-        f32x16 s[2];
-        r.scores(kw, s);
-        reads_done();
-        stage(k, kw, x + 4);
-        float mx = QueryRows::largest(s);
-        r.hide(s, kt.key0(x), mx);
-        const float base = r.reference(mx);
-        r.add(s, base, vw);
-        reads_done();
-        stage(v, vw, x + 4);
-    }
+    walk_halves(slot0[wave], slot1[wave], k, v, b, h, kt, L, wave, lane, [&](const KVHalf &cur, int k0) __attribute__((always_inline)) {
+        f32x16 s = zero16();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) s = mfma32(r.rd.rows(cur.k, ks), r.q[ks], s);
+        if (!(k0 + 31 <= r.lo && (k0 + 32 <= win.n_sink || r.hi - k0 < win.window))) {
+            const VisibleKeys visible(win, r.i);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = visible(k0 + 4 * r.hf + 8 * (e >> 2) + (e & 3)) ? s[e] : -INFINITY;
+        }
+        float mx = max3(s[0], s[1], s[2]);
+#pragma unroll
+        for (int e = 3; e < 15; e += 2) mx = max3(mx, s[e], s[e + 1]);
+        const float base = r.reference(max3(mx, s[15], s[15]));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = fast_exp2(__builtin_fmaf(s[e], r.scale, -base));
+            r.l += s[e];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const bf16x8 p = pack8(s, j);
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) r.o[ct] = mfma32(r.rd.columns(cur.v, j, ct), p, r.o[ct]);
+        }
+    });
+    reads_done();
     r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
     if (r.hf == 0) {
         ml[0][wave][lane] = r.m;
         ml[1][wave][lane] = r.l;
     }
     // [row][channel], 16-byte pieces XORed with the row
-    float *mine = reinterpret_cast<float *>(kw.x);
+    float *mine = reinterpret_cast<float *>(&slot0[wave]);
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
@@ -287,7 +286,7 @@ __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, Win
     for (int w = 0; w < 4; ++w) {
         const float f = fast_exp2(ml[0][w][row] - M);    // (a row sees its own key: M is a number)
         den += f * ml[1][w][row];
-        const float *from = reinterpret_cast<const float *>(tiles.k[w].x) + row * kHeadDim;
+        const float *from = reinterpret_cast<const float *>(&slot0[w]) + row * kHeadDim;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
             const f32x4 a = *reinterpret_cast<const f32x4 *>(from + 4 * ((ch / 4 + e4) ^ (row & 7)));
