@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256, 1) void window_dq_few_kernel(Dims dm, WindowAr
 constexpr int kKvKeys = 128, kKvRows = 32;
 struct BwdPlan {
     int tiles, sink_tiles;                               // key tiles of a sequence; those with any of the first n_sink tokens
-    int span, spans;                                     // tokens of a span (a multiple of 32), spans
+    int span, spans;                                     // tokens of a span (a multiple of a step's), spans
     int per_span;                                        // key tiles a span may have
     int parts;                                           // spans a tile may have, sinks' tiles apart
     __host__ __device__ int slot(int tile) const { return tile < sink_tiles ? tile * spans : sink_tiles * spans + (tile - sink_tiles) * parts; }
@@ -352,20 +352,26 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
 #pragma unroll
             for (int e = 0; e < 4; ++e) dp[4 * e4 + e] = -d[e];
         }
-        bf16x8 xq[2], xg[2], xv[2];                      // the next operands are under way while the matrix cores work, and no more: there are no registers
-        xq[0] = rd.rows(qr, 0);
-        xg[0] = rd.rows(gr, 0);
-        xv[0] = rd.rows(vr, 0);
+        // the next operands are under way while the matrix cores work, and no more: there are no registers (two to seven ahead: slower also where
+        // a wavefront is alone on its SIMD)
+        constexpr int kAhead = 1, kRing = kAhead + 1;
+        bf16x8 xq[kRing], xg[kRing], xv[kRing];
+#pragma unroll
+        for (int ks = 0; ks < kAhead; ++ks) {
+            xq[ks] = rd.rows(qr, ks);
+            xg[ks] = rd.rows(gr, ks);
+            xv[ks] = rd.rows(vr, ks);
+        }
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-            if (ks < 7) {
-                xq[(ks + 1) & 1] = rd.rows(qr, ks + 1);
-                xg[(ks + 1) & 1] = rd.rows(gr, ks + 1);
-                xv[(ks + 1) & 1] = rd.rows(vr, ks + 1);
+            if (ks + kAhead < 8) {
+                xq[(ks + kAhead) % kRing] = rd.rows(qr, ks + kAhead);
+                xg[(ks + kAhead) % kRing] = rd.rows(gr, ks + kAhead);
+                xv[(ks + kAhead) % kRing] = rd.rows(vr, ks + kAhead);
             }
             __builtin_amdgcn_sched_barrier(0);
-            s = mfma32(xq[ks & 1], kf[ks], s);
-            dp = mfma32(xg[ks & 1], xv[ks & 1], dp);
+            s = mfma32(xq[ks % kRing], kf[ks], s);
+            dp = mfma32(xg[ks % kRing], xv[ks % kRing], dp);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -390,18 +396,22 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
         }
         __builtin_amdgcn_sched_barrier(0);
         const bf16x8 p[2] = {pack8(s, 0), pack8(s, 1)}, ds[2] = {pack8(dp, 0), pack8(dp, 1)};
-        bf16x8 cg[2], cq[2];
-        cg[0] = rd.columns(gr, 0, 0);
-        cq[0] = rd.columns(qr, 0, 0);
+        bf16x8 cg[kRing], cq[kRing];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            cg[i] = rd.columns(gr, i >> 2, i & 3);
+            cq[i] = rd.columns(qr, i >> 2, i & 3);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {                    // (half s of the rows, channel tile ct) = (i / 4, i % 4)
-            if (i < 7) {
-                cg[(i + 1) & 1] = rd.columns(gr, (i + 1) >> 2, (i + 1) & 3);
-                cq[(i + 1) & 1] = rd.columns(qr, (i + 1) >> 2, (i + 1) & 3);
+            const int j = i + kAhead;
+            if (j < 8) {
+                cg[j % kRing] = rd.columns(gr, j >> 2, j & 3);
+                cq[j % kRing] = rd.columns(qr, j >> 2, j & 3);
             }
             __builtin_amdgcn_sched_barrier(0);
-            dva[i & 3] = mfma32(cg[i & 1], p[i >> 2], dva[i & 3]);
-            dka[i & 3] = mfma32(cq[i & 1], ds[i >> 2], dka[i & 3]);
+            dva[i & 3] = mfma32(cg[i % kRing], p[i >> 2], dva[i & 3]);
+            dka[i & 3] = mfma32(cq[i % kRing], ds[i >> 2], dka[i & 3]);
         }
     };
     if constexpr (kSlots == 2) {
@@ -449,45 +459,52 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
         }
 }
 
-// The spans' sums of a key tile, added in order.  grid (keys / 16, Hkv, batch): 16 keys a workgroup, a thread 8 channels of dk and dv.
+// The spans' sums of a key tile, added in order.  grid (keys / 8, Hkv, batch): 8 keys a workgroup, a thread 4 channels of dk and dv, four sums
+// of each asked for at once.
 __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs win, BwdPlan plan, const int32_t *__restrict__ seqlens,
                                                           const float *__restrict__ part, Tensor dk, Tensor dv) {
     const int h = blockIdx.y, b = blockIdx.z, bh = b * dm.Hkv + h;
-    const int t = 16 * (int)blockIdx.x + (threadIdx.x >> 4), c8 = 8 * (threadIdx.x & 15), tile = t / kKvKeys;
+    const int t = 8 * (int)blockIdx.x + (threadIdx.x >> 5), c4 = 4 * (threadIdx.x & 31), tile = t / kKvKeys;
     if (t >= dm.max_seqlen) return;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const KvSpans rows_of(plan, win, tile, L);
     if (rows_of.first == rows_of.last || (t >= L && !dm.fill)) return;
     const int n = t < L ? rows_of.last - rows_of.first + 1 : 0;
-    const float *p = part + ((int64_t)bh * plan.slot(plan.tiles) + plan.slot(tile)) * (2 * kKvKeys * kHeadDim) + (t % kKvKeys) * kHeadDim + c8;
-    float x[8], y[8];
+    constexpr int64_t kPart = 2 * kKvKeys * kHeadDim;
+    const float *p = part + ((int64_t)bh * plan.slot(plan.tiles) + plan.slot(tile)) * kPart + (t % kKvKeys) * kHeadDim + c4;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    int i = 0;
+    for (; i + 4 <= n; i += 4, p += 4 * kPart) {
+        f32x4 a[4], d[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
-    for (int i = 0; i < n; ++i, p += 2 * kKvKeys * kHeadDim) {
-        const f32x4 a = *reinterpret_cast<const f32x4 *>(p), d = *reinterpret_cast<const f32x4 *>(p + 4);
-        const f32x4 e0 = *reinterpret_cast<const f32x4 *>(p + kKvKeys * kHeadDim), e1 = *reinterpret_cast<const f32x4 *>(p + kKvKeys * kHeadDim + 4);
+        for (int j = 0; j < 4; ++j) {
+            a[j] = *reinterpret_cast<const f32x4 *>(p + j * kPart);
+            d[j] = *reinterpret_cast<const f32x4 *>(p + j * kPart + kKvKeys * kHeadDim);
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[e] += a[e];
-            x[4 + e] += d[e];
-            y[e] += e0[e];
-            y[4 + e] += e1[e];
+        for (int j = 0; j < 4; ++j) {
+            x += a[j];
+            y += d[j];
         }
     }
-    bf16x8 r, s;
+    for (; i < n; ++i, p += kPart) {
+        x += *reinterpret_cast<const f32x4 *>(p);
+        y += *reinterpret_cast<const f32x4 *>(p + kKvKeys * kHeadDim);
+    }
+    bf16x4 r, s;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 4; ++e) {
         r[e] = (__bf16)x[e];
         s[e] = (__bf16)y[e];
     }
-    *reinterpret_cast<uint4 *>(dk.ptr + b * dk.sb + h * dk.sh + (int64_t)t * dk.st + c8) = __builtin_bit_cast(uint4, r);
-    *reinterpret_cast<uint4 *>(dv.ptr + b * dv.sb + h * dv.sh + (int64_t)t * dv.st + c8) = __builtin_bit_cast(uint4, s);
+    *reinterpret_cast<uint2 *>(dk.ptr + b * dk.sb + h * dk.sh + (int64_t)t * dk.st + c4) = __builtin_bit_cast(uint2, r);
+    *reinterpret_cast<uint2 *>(dv.ptr + b * dv.sb + h * dv.sh + (int64_t)t * dv.st + c4) = __builtin_bit_cast(uint2, s);
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
 // Scratch tiles a call may use in all: a number that grows with the batch and with max_seqlen, so that a buffer for a call is large
 // enough for every smaller one.
-static int64_t most_slots(int64_t tiles) { return min(8 * tiles, 2048 + 2 * tiles); }
+static int64_t most_slots(int64_t tiles) { return min(32 * tiles, 2048 + 2 * tiles); }
 
 // The span: of some lengths the one whose workgroups the chip, which holds 512, is through with first: all steps, about 50 more per
 // workgroup for its start and its sums (but not less than the longest workgroup), and half a longest workgroup's steps in which not all have work.
@@ -501,7 +518,7 @@ static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
     p.sink_tiles = (w.n_sink + kKvKeys - 1) / kKvKeys;
     const int64_t steps = heads * (p.sink_tiles * all_steps + (p.tiles - p.sink_tiles) * window_steps), whole = (int64_t)p.tiles * kKvKeys;
     int64_t least = INT64_MAX;
-    for (int64_t span = 32;; span = span < kKvKeys ? 2 * span : span + (span / kKvKeys + 3) / 4 * kKvKeys) {
+    for (int64_t span = max(16, per);; span = span < kKvKeys ? 2 * span : span + (span / kKvKeys + 3) / 4 * kKvKeys) {
         span = min(span, whole);
         p.span = (int)span;
         p.spans = (int)((dm.max_seqlen + span - 1) / span);
@@ -547,7 +564,7 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
     timing_end(stream);
     if (plan.spans == 1) return (int)hipGetLastError();
     timing_begin("window_join_kernel", stream);
-    hipLaunchKernelGGL(window_join_kernel, dim3((dm.max_seqlen + 15) / 16, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, w, plan, seqlens, part,
+    hipLaunchKernelGGL(window_join_kernel, dim3((dm.max_seqlen + 7) / 8, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, w, plan, seqlens, part,
                        dk, dv);
     timing_end(stream);
     return (int)hipGetLastError();
