@@ -64,6 +64,31 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16 &x, int s) {
     return r;
 }
 
+// A wavefront's result, channel 32 ct + 8 (e / 4) + 4 hf + e % 4 of row c in lane 32 hf + c, times the lane's factor, to rows of memory: through 8 KiB
+// of LDS of its own, so that 16 lanes write a row's 256 bytes together (as the lanes hold it, an instruction would write 16 bytes of each of 32
+// rows).  to(row): where row `row` goes, null: nowhere.
+template <typename F>
+__device__ __forceinline__ void store_rows(char *lds, const f32x16 (&o)[4], float factor, int lane, F to) {
+    const uint32_t c = lane & 31, hf = lane >> 5;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            bf16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[ct][4 * e4 + e] * factor);
+            *reinterpret_cast<uint2 *>(lds + c * 256 + (((4 * ct + e4) ^ (c & 15)) << 4) + 8 * hf) = __builtin_bit_cast(uint2, y);
+        }
+    __builtin_amdgcn_wave_barrier();                     // same wavefront: LDS keeps the order
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t row = 4 * j + (lane >> 4), piece = lane & 15;
+        const uint4 y = *reinterpret_cast<const uint4 *>(lds + row * 256 + ((piece ^ (row & 15)) << 4));
+        __bf16 *p = to((int)row);
+        if (p) *reinterpret_cast<uint4 *>(p + 8 * piece) = y;
+    }
+}
+
 // Tiles of kKeys keys that any of the queries t0 .. t1 - 1 sees: `sinks` tiles from the first on, then those from `first` to the last.
 constexpr int kWinKeys = 64;
 template <int kKeys>

@@ -108,17 +108,19 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
         step(tile0, tile1, x);
         if (x + 1 < kt.count) step(tile1, tile0, x + 1);
     }
-    if (i >= dm.max_seqlen || (i >= L && !dm.fill)) return;
-    const float f = i < L ? scale : 0.f;
+    __syncthreads();                                     // the tiles are free
+    const bool live = i < L;
+    const uint32_t alive = (uint32_t)__ballot(live);
+    if (alive != ~0u) {                                  // (rows behind the sequence: zeros, where they are written at all)
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
+        for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-            bf16x4 r;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = (__bf16)(i < L ? acc[ct][4 * e4 + e] * f : 0.f);
-            *reinterpret_cast<uint2 *>(dq_row + 32 * ct + 8 * e4) = __builtin_bit_cast(uint2, r);
-        }
+            for (int e = 0; e < 16; ++e) acc[ct][e] = live ? acc[ct][e] : 0.f;
+    }
+    store_rows((wave < 2 ? tile0.k.x : tile0.v.x) + (wave & 1) * kHalfTile, acc, scale, lane, [&](int r) __attribute__((always_inline)) -> __bf16 * {
+        const int t = t0 + ((32 * wave + r) >> lg), head = h * dm.G + ((32 * wave + r) & (dm.G - 1));
+        return t < dm.max_seqlen && ((alive >> r) & 1u || dm.fill) ? dq.ptr + b * dq.sb + (int64_t)t * dq.st + (int64_t)head * dq.sh : nullptr;
+    });
 }
 
 // The same for few rows, as in the forward: 32 rows to a workgroup, every fourth unit of 32 keys to a wavefront, four sums joined in LDS.

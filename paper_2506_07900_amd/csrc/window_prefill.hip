@@ -102,6 +102,37 @@ struct QueryRows {
     }
 };
 
+// A unit of 32 keys, k0 ..: scores, and what they add.
+__device__ __forceinline__ void take_half(QueryRows &r, const KVHalf &cur, int k0) {
+    f32x16 s = zero16();
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) s = mfma32(r.rd.rows(cur.k, ks), r.q[ks], s);
+    if (!(k0 + 31 <= r.lo && (k0 + 32 <= r.win.n_sink || r.hi - k0 < r.win.window))) {
+        int at = k0 + 4 * r.hf;
+        asm volatile("" : "+v"(at));
+        const VisibleKeys visible(r.win, r.i);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = visible(at + 8 * (e >> 2) + (e & 3)) ? s[e] : -INFINITY;
+    }
+    float mx = max3(s[0], s[1], s[2]);
+#pragma unroll
+    for (int e = 3; e < 15; e += 2) mx = max3(mx, s[e], s[e + 1]);
+    const float base = r.reference(max3(mx, s[15], s[15]));
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        s[e] = fast_exp2(__builtin_fmaf(s[e], r.scale, -base));
+        sum[e & 1] += s[e];
+    }
+    r.l += sum[0] + sum[1];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const bf16x8 p = pack8(s, j);
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) r.o[ct] = mfma32(r.rd.columns(cur.v, j, ct), p, r.o[ct]);
+    }
+}
+
 // A product multiplies a key that a row does not see by a probability of 0, and 0 times an infinity or a NaN reaches the row's sum.  A
 // row that does not come out finite is therefore taken again by the whole wavefront, key by key, over the keys it sees; its maximum m and
 // sum l stand, as hidden scores are replaced and not multiplied.  Lane = two channels.
@@ -127,6 +158,46 @@ __device__ __forceinline__ void take_row_again(const Dims &dm, WindowArgs win, c
     reinterpret_cast<bf16x2 *>(out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh)[lane] = y;
 }
 
+// The end of a wavefront's 32 rows, with 8 KiB of LDS.
+__device__ __forceinline__ void finish_rows(const Dims &dm, WindowArgs win, int lg, int t0, QueryRows &r, const Tensor &q, const Tensor &k, const Tensor &v,
+                                            int b, int h, int L, int wave, int lane, char *lds, const Tensor &out, float *__restrict__ lse) {
+    r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
+    const bool live = r.i < L;
+    float check = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) check = __builtin_fmaf(r.o[ct][e], 0.f, check);
+    const uint64_t bad_lanes = __ballot(live && check != 0.f), live_lanes = __ballot(live);
+    uint32_t bad = (uint32_t)bad_lanes | (uint32_t)(bad_lanes >> 32);
+    const uint32_t alive = (uint32_t)live_lanes;
+    if (alive != ~0u) {                                  // (rows behind the sequence: zeros, where they are written at all)
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r.o[ct][e] = live ? r.o[ct][e] : 0.f;
+    }
+    store_rows(lds, r.o, live ? 1.f / r.l : 0.f, lane, [&](int row) __attribute__((always_inline)) -> __bf16 * {
+        const int i = t0 + ((32 * wave + row) >> lg), hq = h * dm.G + ((32 * wave + row) & (dm.G - 1));
+        const bool store = i < dm.max_seqlen && ((alive >> row) & 1u || dm.fill) && !((bad >> row) & 1u);
+        return store ? out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh : nullptr;
+    });
+    if (r.hf == 0 && r.i < dm.max_seqlen && (live || dm.fill)) lse[((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq] = live ? lse_of(r.m, r.l) : 0.f;
+    for (; bad; bad &= bad - 1) {
+        const int n = __builtin_ctz(bad);
+        take_row_again(dm, win, q, k, v, out, b, h, __builtin_amdgcn_readlane(r.i, n), __builtin_amdgcn_readlane(r.hq, n),
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.m), n)),
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.l), n)), lane);
+    }
+}
+// A wavefront's rows that lie behind the sequence.
+__device__ __forceinline__ void clear_rows(const Dims &dm, const QueryRows &r, int b, const Tensor &out, float *__restrict__ lse) {
+    if (!dm.fill || r.i >= dm.max_seqlen) return;
+    __bf16 *o_row = out.ptr + b * out.sb + (int64_t)r.i * out.st + (int64_t)r.hq * out.sh + 64 * r.hf;
+    for (int c = 0; c < 8; ++c) reinterpret_cast<uint4 *>(o_row)[c] = uint4{0u, 0u, 0u, 0u};
+    if (r.hf == 0) lse[((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq] = 0.f;
+}
+
 __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k, Tensor v,
                                                                 const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
     __shared__ Tile64 K0, K1, V0, V1;
@@ -137,15 +208,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int t0 = ti * (kFwdRows >> lg), t1 = min(L, t0 + (kFwdRows >> lg));
     QueryRows r(dm, win, lg, t0, 32 * wave, h, lane);
-    __bf16 *o_row = out.ptr + b * out.sb + (int64_t)r.i * out.st + (int64_t)r.hq * out.sh + 4 * r.hf;
-    float *lse_at = lse + ((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq;
-    if (t0 >= L) {
-        if (dm.fill && r.i < dm.max_seqlen) {
-            for (int c = 0; c < 16; ++c) *reinterpret_cast<uint2 *>(o_row + 8 * c) = uint2{0u, 0u};
-            if (r.hf == 0) *lse_at = 0.f;
-        }
-        return;
-    }
+    if (t0 >= L) return clear_rows(dm, r, b, out, lse);
     const KeyTiles<kWinKeys> kt(win, t0, t1);
     const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
     auto stage = [&](const TileCopier &from, Tile64 &to, int x) __attribute__((always_inline)) {
@@ -182,33 +245,59 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
         step(K0, K1, V0, V1, sa, sb, mx, x);
         if (x + 1 < kt.count) step(K1, K0, V1, V0, sb, sa, mx, x + 1);
     }
-    r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
-    const bool live = r.i < L, store = r.i < dm.max_seqlen && (live || dm.fill);
-    float check = 0.f;
+    __syncthreads();                                     // the tiles are free
+    finish_rows(dm, win, lg, t0, r, q, k, v, b, h, L, wave, lane, (wave < 2 ? K0.x : K1.x) + (wave & 1) * kHalfTile, out, lse);
+}
+
+// The same for many rows: three workgroups to a compute unit instead of two, so that one's exponentials run under another's products and round trips,
+// with units of 32 keys, two ahead, in three slots, and a unit's scores at a time.  Its smaller units also leave less to hide.
+__global__ __launch_bounds__(256, 3) void window_prefill_many_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k,
+                                                                     Tensor v, const int32_t *__restrict__ seqlens, Tensor out,
+                                                                     float *__restrict__ lse) {
+    __shared__ KVHalf slot0, slot1, slot2;
+    const int item = xcd_item(blockIdx.x, run), bh = item / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    if (b >= dm.batch) return;
+    const int ti = (bh + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
+    const int t0 = ti * (kFwdRows >> lg), t1 = min(L, t0 + (kFwdRows >> lg));
+    QueryRows r(dm, win, lg, t0, 32 * wave, h, lane);
+    if (t0 >= L) return clear_rows(dm, r, b, out, lse);
+    const KeyTiles<32> kt(win, t0, t1);
+    const char *k_head = reinterpret_cast<const char *>(k.ptr + b * k.sb + h * k.sh) + 64 * wave;
+    const char *v_head = reinterpret_cast<const char *>(v.ptr + b * v.sb + h * v.sh) + 64 * wave;
+    const uint32_t k_at = (lane >> 2) * (2 * (uint32_t)k.st) + 16 * copy_piece(lane), v_at = (lane >> 2) * (2 * (uint32_t)v.st) + 16 * copy_piece(lane);
+    // four copies for every unit: those past the last bring zeros
+    auto stage = [&](KVHalf &dst, int x) __attribute__((always_inline)) {
+        const int k0 = kt.key0(min(x, kt.count - 1)), end = x < kt.count ? L : 0;
+        const char *kb = k_head + (int64_t)k0 * (2 * k.st), *vb = v_head + (int64_t)k0 * (2 * v.st);
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) check = __builtin_fmaf(r.o[ct][e], 0.f, check);
-    const uint64_t bad_lanes = __ballot(live && check != 0.f);
-    uint32_t bad = (uint32_t)bad_lanes | (uint32_t)(bad_lanes >> 32);
-    if (store && !((bad >> (lane & 31)) & 1u)) {
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                bf16x4 y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = (__bf16)(live ? r.o[ct][4 * e4 + e] / r.l : 0.f);
-                *reinterpret_cast<uint2 *>(o_row + 32 * ct + 8 * e4) = __builtin_bit_cast(uint2, y);
-            }
+        for (int j = 0; j < 2; ++j) {
+            const bool row = k0 + 16 * j + (lane >> 2) < end;
+            copy_rows(dst.k + wave * 2048 + j * 1024, kb, row ? k_at : kNoRow, 32 * j * (uint32_t)k.st);
+            copy_rows(dst.v + wave * 2048 + j * 1024, vb, row ? v_at : kNoRow, 32 * j * (uint32_t)v.st);
+        }
+    };
+    r.load(q, b, L);
+    stage(slot0, 0);
+    stage(slot1, 1);
+    auto step = [&](const KVHalf &cur, KVHalf &next, int x) __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0f74);              // all copies but the next unit's four
+        asm volatile("s_barrier" ::: "memory");          // everyone's, and everyone is past the unit before
+        __builtin_amdgcn_sched_barrier(0);
+        stage(next, x + 2);
+        const int k0 = kt.key0(x);
+        if (k0 <= r.hi && (k0 < win.n_sink || r.lo - (k0 + 31) < win.window)) take_half(r, cur, k0);   // (some of the rows see some of the keys)
+    };
+    for (int x = 0; x < kt.count; x += 3) {
+        step(slot0, slot2, x);
+        if (x + 1 < kt.count) step(slot1, slot0, x + 1);
+        if (x + 2 < kt.count) step(slot2, slot1, x + 2);
     }
-    if (store && r.hf == 0) *lse_at = live ? lse_of(r.m, r.l) : 0.f;
-    for (; bad; bad &= bad - 1) {
-        const int n = __builtin_ctz(bad);
-        take_row_again(dm, win, q, k, v, out, b, h, __builtin_amdgcn_readlane(r.i, n), __builtin_amdgcn_readlane(r.hq, n),
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.m), n)),
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.l), n)), lane);
-    }
+    __builtin_amdgcn_s_waitcnt(0);                       // (the copies past the last unit have landed)
+    __syncthreads();
+    finish_rows(dm, win, lg, t0, r, q, k, v, b, h, L, wave, lane, (wave < 2 ? slot0.k : slot1.k) + (wave & 1) * kHalfTile, out, lse);
 }
 
 // The same for few rows: a workgroup takes 32 of them, its wavefronts every fourth unit of 32 keys each, fetched for itself and without a
@@ -237,31 +326,8 @@ __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, Win
     }
     const KeyTiles<32> kt(win, t0, t1);
     r.load(q, b, L);
-    walk_halves(slot0[wave], slot1[wave], k, v, b, h, kt, L, wave, lane, [&](const KVHalf &cur, int k0) __attribute__((always_inline)) {
-        f32x16 s = zero16();
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) s = mfma32(r.rd.rows(cur.k, ks), r.q[ks], s);
-        if (!(k0 + 31 <= r.lo && (k0 + 32 <= win.n_sink || r.hi - k0 < win.window))) {
-            const VisibleKeys visible(win, r.i);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = visible(k0 + 4 * r.hf + 8 * (e >> 2) + (e & 3)) ? s[e] : -INFINITY;
-        }
-        float mx = max3(s[0], s[1], s[2]);
-#pragma unroll
-        for (int e = 3; e < 15; e += 2) mx = max3(mx, s[e], s[e + 1]);
-        const float base = r.reference(max3(mx, s[15], s[15]));
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            s[e] = fast_exp2(__builtin_fmaf(s[e], r.scale, -base));
-            r.l += s[e];
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const bf16x8 p = pack8(s, j);
-#pragma unroll
-            for (int ct = 0; ct < 4; ++ct) r.o[ct] = mfma32(r.rd.columns(cur.v, j, ct), p, r.o[ct]);
-        }
-    });
+    walk_halves(slot0[wave], slot1[wave], k, v, b, h, kt, L, wave, lane,
+                [&](const KVHalf &cur, int k0) __attribute__((always_inline)) { take_half(r, cur, k0); });
     reads_done();
     r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
     if (r.hf == 0) {
@@ -299,9 +365,10 @@ __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, Win
     uint64_t bad = __ballot(i < L && check != 0.f);
     const bool whole = ((bad >> (lane & 56)) & 255u) == 0u;                    // this row's eight lanes
     if (store) {
+        const float inv = 1.f / den;
         bf16x8 z[2];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)(i < L ? y[e] / den : 0.f);
+        for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)(i < L ? y[e] * inv : 0.f);
         if (whole) {
             reinterpret_cast<uint4 *>(o_row)[0] = __builtin_bit_cast(uint4, z[0]);
             reinterpret_cast<uint4 *>(o_row)[1] = __builtin_bit_cast(uint4, z[1]);
@@ -325,16 +392,19 @@ int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tens
     const int lg = __builtin_ctz(dm.G);
     const int64_t heads = (int64_t)dm.Hkv * dm.batch;
     auto tiles = [&](int rows) { return (dm.max_seqlen + (rows >> lg) - 1) / (rows >> lg); };
-    if (tiles(kFwdRows) * heads <= 64) {
+    const int64_t items = tiles(kFwdRows) * heads;
+    const int run = xcd_run_length(items);
+    // Up to 64 workgroups of 128 rows: four times as many of 32 (2048 tokens, 4 heads : 1, whole window 42 -> 20 us; 256: 23 -> 41).  Up to 512, two per
+    // compute unit: the pipelined form (4096 tokens, 8 : 2, whole window, 78 us, with three per compute unit 91; 16K, 4 : 4 142 / 151), beyond three
+    // (32K, 32 : 2, window 4096 / 512 / 36: 2110 / 456 / 236 -> 2056 / 391 / 206).
+    if (items <= 64) {
         timing_begin("window_prefill_few_kernel", stream);
         hipLaunchKernelGGL(window_prefill_few_kernel, dim3((unsigned)(tiles(32) * heads)), dim3(256), 0, stream, dm, w, lg, tiles(32), q, k, v,
                            seqlens, out, lse);
     } else {
-        timing_begin("window_prefill_kernel", stream);
-        const int64_t items = tiles(kFwdRows) * heads;
-        const int run = xcd_run_length(items);
-        hipLaunchKernelGGL(window_prefill_kernel, dim3(xcd_grid(items, run)), dim3(256), 0, stream, dm, w, lg, tiles(kFwdRows), run, q, k, v,
-                           seqlens, out, lse);
+        timing_begin(items <= 512 ? "window_prefill_kernel" : "window_prefill_many_kernel", stream);
+        hipLaunchKernelGGL(items <= 512 ? window_prefill_kernel : window_prefill_many_kernel, dim3(xcd_grid(items, run)), dim3(256), 0, stream, dm, w,
+                           lg, tiles(kFwdRows), run, q, k, v, seqlens, out, lse);
     }
     timing_end(stream);
     return (int)hipGetLastError();
