@@ -13,7 +13,7 @@ struct KVTile {
     Tile64 k, v;
 };
 
-// What the forward leaves of a row (token, head of the group): its log-sum-exp in powers of two and D, 32 and 32 floats for 32 rows.
+// What the forward leaves of a row (token, head of the group): its log-sum-exp in powers of two and -D, 32 and 32 floats for 32 rows.
 __host__ __device__ static inline int64_t row_blocks(const Dims &dm) { return ((int64_t)dm.max_seqlen * dm.G + 31) / 32; }   // per (sequence, head)
 
 __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, int run, Tensor q, Tensor k,
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
         D = half_reduce(D, [](float a, float d) { return a + d; });
         ref = lse[((int64_t)b * dm.max_seqlen + t) * dm.Hq + hq] * kLog2e;
         const int64_t r = (int64_t)ti * kDqRows + row;
-        if (i < L) rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? D : ref;
+        if (i < L) rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? -D : ref;
     }
     const TileReader rd(lane);
     const float c = dm.scale_log2;
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256, 1) void window_dq_few_kernel(Dims dm, WindowAr
     const float ref = lse[((int64_t)b * dm.max_seqlen + t) * dm.Hq + hq] * kLog2e, c = dm.scale_log2;
     if (wave == 0 && i < L) {
         const int64_t r = (int64_t)ti * 32 + row;
-        rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? D : ref;
+        rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? -D : ref;
     }
     const TileReader rd(lane);
     f32x16 acc[4];
@@ -249,7 +249,7 @@ struct KvSpans {                                         // the tokens that see 
 };
 struct __align__(16) KvRows {
     char q[kHalfTile], g[kHalfTile];
-    float ref[32], D[32];
+    float ref[32], minus_D[32];
 };
 
 // kSlots: rows two steps (one ahead) or four (three ahead) at a time.  A compute unit with one workgroup does not hide a round trip to memory under
@@ -350,9 +350,9 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
         f32x16 s = zero16(), dp;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
-            const f32x4 d = *reinterpret_cast<const f32x4 *>(&cur.D[8 * e4 + 4 * hf]);
+            const f32x4 d = *reinterpret_cast<const f32x4 *>(&cur.minus_D[8 * e4 + 4 * hf]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) dp[4 * e4 + e] = -d[e];
+            for (int e = 0; e < 4; ++e) dp[4 * e4 + e] = d[e];
         }
         // the next operands are under way while the matrix cores work, and no more: there are no registers (two to seven ahead: slower also where
         // a wavefront is alone on its SIMD)
