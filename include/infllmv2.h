@@ -418,6 +418,7 @@ int32_t infllmv2_verify_step(const infllmv2_params *prm, const infllmv2_tensor *
  *                           masks, results and workspaces (INFLLMV2_OP_ATTN_DECODE, INFLLMV2_OP_ATTN_VERIFY).  stride_t and scale_stride_t
  *                           at most 2^26 bytes, else INFLLMV2_ERR_UNSUPPORTED.
  * The selection reads compressed keys, which stay bf16: infllmv2_select_blocks and _verify serve such a cache as they are.
+ * max_seqlen of these calls and of the next is at most 2^30, else INFLLMV2_ERR_UNSUPPORTED.
  */
 int32_t infllmv2_quantize_kv(const infllmv2_params *prm, const infllmv2_tensor *k, const infllmv2_tensor *v,
                              const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_new_tokens,

@@ -101,6 +101,9 @@ QuantTensor make_quant(const infllmv2_quant_tensor *t) {
                        t->scale_stride_b, t->scale_stride_h, t->scale_stride_t};
 }
 
+// (the kernels number a cache's rows, rounded up to tiles, in 32 bits)
+int32_t check_capacity(int32_t max_seqlen) { return max_seqlen > (1 << 30) ? INFLLMV2_ERR_UNSUPPORTED : INFLLMV2_OK; }
+
 int32_t check_window(int32_t n_sink, int32_t window) { return n_sink < 0 || window < 1 ? INFLLMV2_ERR_INVALID_ARGUMENT : INFLLMV2_OK; }
 
 WindowArgs make_window(int32_t n_sink, int32_t window, int32_t max_seqlen) {   // (none of a sequence lies behind max_seqlen)
@@ -547,6 +550,7 @@ int32_t infllmv2i_quantize_kv(const infllmv2_params *prm, const infllmv2_tensor 
                               const infllmv2_quant_tensor *kq, const infllmv2_quant_tensor *vq, void *stream, int32_t fill) {
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_tensor(k));
     RETURN_IF_ERR(check_tensor(v));
     RETURN_IF_ERR(check_quant(kq));
@@ -567,6 +571,7 @@ int32_t infllmv2i_dequantize_kv(const infllmv2_params *prm, const infllmv2_quant
                                 const infllmv2_tensor *k, const infllmv2_tensor *v, void *stream, int32_t fill) {
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_quant(kq));
     RETURN_IF_ERR(check_quant(vq));
     RETURN_IF_ERR(check_tensor(k));
@@ -587,6 +592,7 @@ int32_t infllmv2_append_kv_quant(const infllmv2_params *prm, const infllmv2_tens
                                  const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t n_draft, void *stream) {
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_draft(batch, n_draft));
     RETURN_IF_ERR(check_tensor(k_new));
     RETURN_IF_ERR(check_tensor(v_new));
@@ -607,6 +613,7 @@ int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infl
                                           void *stream) {
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_draft(batch, n_draft));
     RETURN_IF_ERR(check_tensor(q));
     RETURN_IF_ERR(check_quant(kq));
@@ -631,7 +638,9 @@ int32_t infllmv2_sparse_attn_decode_quant(const infllmv2_params *prm, const infl
 
 size_t infllmv2_window_workspace_bytes(int32_t op, const infllmv2_params *prm, int32_t n_sink, int32_t window, int32_t batch,
                                        int32_t max_seqlen) {
-    if (check_params(prm) != INFLLMV2_OK || check_window(n_sink, window) != INFLLMV2_OK || check_sizes(batch, max_seqlen) != INFLLMV2_OK) return 0;
+    if (check_params(prm) != INFLLMV2_OK || check_window(n_sink, window) != INFLLMV2_OK || check_sizes(batch, max_seqlen) != INFLLMV2_OK ||
+        check_capacity(max_seqlen) != INFLLMV2_OK)
+        return 0;
     const Dims dm = make_dims(prm, batch, max_seqlen);
     const WindowArgs w = make_window(n_sink, window, max_seqlen);
     switch (op) {
@@ -649,6 +658,7 @@ int32_t infllmv2i_window_attn_prefill(const infllmv2_params *prm, int32_t n_sink
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_window(n_sink, window));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_tensor(q));
     RETURN_IF_ERR(check_tensor(k));
     RETURN_IF_ERR(check_tensor(v));
@@ -677,6 +687,7 @@ int32_t infllmv2i_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, in
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_window(n_sink, window));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     const infllmv2_tensor *ts[8] = {q, k, v, out, dout, dq, dk, dv};
     for (int i = 0; i < 8; ++i) RETURN_IF_ERR(check_tensor(ts[i]));
     if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
@@ -705,6 +716,7 @@ int32_t infllmv2_window_attn_decode(const infllmv2_params *prm, int32_t n_sink, 
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_window(n_sink, window));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_tensor(q));
     RETURN_IF_ERR(check_tensor(k));
     RETURN_IF_ERR(check_tensor(v));
@@ -724,6 +736,7 @@ int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_
     RETURN_IF_ERR(check_params(prm));
     RETURN_IF_ERR(check_window(n_sink, window));
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_tensor(q));
     RETURN_IF_ERR(check_quant(kq));
     RETURN_IF_ERR(check_quant(vq));

@@ -142,19 +142,20 @@ __device__ __forceinline__ void take_row_again(const Dims &dm, WindowArgs win, c
     auto pair = [&](const Tensor &t, int64_t row) { return reinterpret_cast<const bf16x2 *>(t.ptr + row)[lane]; };
     const bf16x2 x = pair(q, b * q.sb + (int64_t)i * q.st + (int64_t)hq * q.sh);
     const int lo = max(0, i - win.window + 1), first = min(win.n_sink, lo);
+    const float inv = 1.f / l;
     float y0 = 0.f, y1 = 0.f;
     for (int n = 0; n < first + i - lo + 1; ++n) {
         const int64_t t = n < first ? n : lo + n - first;
         const bf16x2 kt = pair(k, b * k.sb + h * k.sh + t * k.st), vt = pair(v, b * v.sb + h * v.sh + t * v.st);
         const auto sum = [](float a, float d) { return a + d; };
         const float s = xgroup_reduce(row_reduce(__builtin_fmaf((float)x[0], (float)kt[0], (float)x[1] * (float)kt[1]), sum), sum);
-        const float p = (float)(__bf16)fast_exp2(__builtin_fmaf(s, dm.scale_log2, -m));
+        const float p = (float)(__bf16)fast_exp2(__builtin_fmaf(s, dm.scale_log2, -m)) * inv;   // (at most 1: no sum of large values overflows)
         y0 = __builtin_fmaf(p, (float)vt[0], y0);
         y1 = __builtin_fmaf(p, (float)vt[1], y1);
     }
     bf16x2 y;
-    y[0] = (__bf16)(y0 / l);
-    y[1] = (__bf16)(y1 / l);
+    y[0] = (__bf16)y0;
+    y[1] = (__bf16)y1;
     reinterpret_cast<bf16x2 *>(out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh)[lane] = y;
 }
 

@@ -367,6 +367,7 @@ PREFILL_CASES = [  # G, Hkv, lengths, n_sink, window
     (1, 1, [1], 0, 1), (16, 2, [1, 7, 8, 9, 0], 1, 3), (1, 2, [300, 129, 128], 0, 1), (2, 1, [500], 4, 50),
     (4, 1, [777], 4, 256), (8, 2, [640, 333], 64, 100), (16, 2, [700, 1], 100, 64), (16, 1, [513], 600, 5),
     (4, 3, [400, 65], 0, 100000), (8, 1, [1500], 33, 1000), (2, 2, [1100], 130, 129), (16, 1, [1030], 0, 512),
+    (16, 4, [1100, 3], 4, 100), (2, 8, [4200], 33, 70), (16, 8, [650], 0, 100000),
 ]
 
 
@@ -393,6 +394,19 @@ def test_window_prefill(G, H, lengths, n_sink, window):
                 seen = window_seen(torch.arange(n, device="cuda"), n, n_sink, window)
                 check(out[b, :n, hq], lse[b, :n, hq],
                       attend(q[b, :n, hq].double(), k[b, hq // G, :n].double(), v[b, hq // G, :n].double(), seen, prm.softmax_scale))
+
+
+def test_window_prefill_of_large_values():
+    # values near bf16's largest: their sums overflow 32 bits before they are divided, their means do not
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    n, prm = 300, binding.Params(4, 2)
+    k, v = random_cache(gen, 1, 2, n, [n], spoil=False)
+    v = (v.float().clamp(-1, 1) * 3e38).bfloat16()
+    q = normal(gen, 1, n, 4, D)
+    out, lse = binding.window_attn_prefill(prm, 4, 50, q, k, v, lengths_tensor([n]), n)
+    seen = window_seen(torch.arange(n, device="cuda"), n, 4, 50)
+    for hq in range(4):
+        check(out[0, :, hq], lse[0, :, hq], attend(q[0, :, hq].double(), k[0, hq // 2].double(), v[0, hq // 2].double(), seen, prm.softmax_scale))
 
 
 def bwd_reference(q, k, v, out, dout, lse, seen, scale):
@@ -456,7 +470,7 @@ def test_window_bwd(G, H, lengths, n_sink, window):
                 assert (diff <= tol).all(), (name, float((diff / tol).max()))
 
 
-@pytest.mark.parametrize("G,H,n,n_sink,window,at", [(16, 2, 200, 4, 20, 70), (1, 1, 400, 0, 129, 255), (4, 2, 3000, 3, 100, 1), (8, 4, 1500, 0, 64, 1499)])
+@pytest.mark.parametrize("G,H,n,n_sink,window,at", [(16, 2, 200, 4, 20, 70), (1, 1, 400, 0, 129, 255), (4, 2, 3000, 3, 100, 1), (8, 4, 1500, 0, 64, 1499), (16, 4, 1100, 70, 33, 1000)])
 def test_window_prefill_keeps_what_is_not_finite_where_it_is_seen(G, H, n, n_sink, window, at):
     gen = torch.Generator(device="cuda").manual_seed(n)
     prm = binding.Params(G * H, H)

@@ -68,6 +68,7 @@ def test_refusals(lib, name):
     assert call(**{"a%d" % (at_lengths + 1): -1}) == INVALID
     assert call(**{"a%d" % (at_lengths + 1): 65536}) == UNSUPPORTED
     assert call(**{"a%d" % (at_lengths + 2): -1}) == INVALID
+    assert call(**{"a%d" % (at_lengths + 2): (1 << 30) + 1}) == UNSUPPORTED
     for i, x in enumerate(good):
         if isinstance(x, CTensor):
             if not (name == "append_kv_quant" and i == 5):         # ck may be left out
