@@ -1,10 +1,10 @@
 // Attention of single queries over a cache in 4 bits (the selected blocks, or a window) and over the window of a bf16 cache.
 //
 // The keys of a query row are walked in units of 32 tokens: halves of the selected blocks, or the units that hold the first
-// n_sink tokens and the window.  A workgroup takes a run of a row's units, its four wavefronts every fourth of them, each by
+// n_sink tokens and the window.  A workgroup takes a run of a row's units, its wavefronts (four, or eight) take them in turn, each by
 // itself: keys as rows of the first product (S^T = K . Q^T, 16 heads as columns), a running maximum and sum per head, the values through
 // 8 KiB of LDS of the wavefront's own (stored as rows, read transposed) into the second (O^T = V^T . P^T).  The order of keys within a product is free,
-// so the probabilities are the second product's operand in the registers they come out in.  At the end the four
+// so the probabilities are the second product's operand in the registers they come out in.  At the end their
 // states are joined in LDS; where a row is split over workgroups, decode_merge_kernel joins those.
 #include "quant.h"
 #include "window.h"
@@ -122,13 +122,13 @@ struct UnitRows<true> {
 
 // grid (splits, Hkv, rows).  kList: a row's units are the halves of its list's entries, `per` entries to a split; otherwise its share
 // of the units of its window.  With one split the result is written as it is, else as a partial (o, maximum, sum).
-template <bool kQuant, bool kList>
-__global__ __launch_bounds__(256, kQuant ? 3 : 2) void stream_attn_kernel(Dims dm, WindowArgs win, Tensor q, RowSource src, const int32_t *__restrict__ seqlens,
+template <bool kQuant, bool kList, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void stream_attn_kernel(Dims dm, WindowArgs win, Tensor q, RowSource src, const int32_t *__restrict__ seqlens,
                                                           const int32_t *__restrict__ block_idx, const uint64_t *__restrict__ tree_mask,
                                                           int per, Tensor out, float *__restrict__ lse, float *__restrict__ o_part,
                                                           float2 *__restrict__ ml_part) {
-    __shared__ __align__(16) char Vs[4][kUnit * 256];
-    __shared__ float2 ml_s[4][16];
+    __shared__ __align__(16) char Vs[kWaves][kUnit * 256];
+    __shared__ float2 ml_s[kWaves][16];
     const int split = blockIdx.x, n_split = gridDim.x, h = blockIdx.y, bv = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4, G = dm.G;
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256, kQuant ? 3 : 2) void stream_attn_kernel(Dims d
     };
     // the next unit of the wavefront that has a visible key
     auto advance = [&](int x, int &key0, uint32_t &allow) __attribute__((always_inline)) {
-        while (x < u_end && (allow = place(x, key0)) == 0u) x += 4;
+        while (x < u_end && (allow = place(x, key0)) == 0u) x += kWaves;
         return x;
     };
     UnitRows<kQuant> a, c;
@@ -269,21 +269,24 @@ __global__ __launch_bounds__(256, kQuant ? 3 : 2) void stream_attn_kernel(Dims d
     u = advance(u, ka, aa);
     if (u < u_end) fetch(a, ka);
     while (u < u_end) {
-        int next = advance(u + 4, kc, ac);
+        int next = advance(u + kWaves, kc, ac);
         if (next < u_end) fetch(c, kc);
         attend(a, aa);
         u = next;
         if (u >= u_end) break;
-        next = advance(u + 4, ka, aa);
+        next = advance(u + kWaves, ka, aa);
         if (next < u_end) fetch(a, ka);
         attend(c, ac);
         u = next;
     }
     l = xgroup_sum(l);
-    // ---- the four wavefronts' states into one --------------------------------------------------------------------------
+    // ---- the wavefronts' states into one --------------------------------------------------------------------------
     if (g == 0) ml_s[wave][n] = float2{m, l};
     __syncthreads();
-    const float M = fmaxf(fmaxf(ml_s[0][n].x, ml_s[1][n].x), fmaxf(ml_s[2][n].x, ml_s[3][n].x)), base = M == -INFINITY ? 0.f : M;
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
+    const float base = M == -INFINITY ? 0.f : M;
     const float w = fast_exp2(m - base);
     float *mine = reinterpret_cast<float *>(vs);         // [head][channel]: its 8 KiB
 #pragma unroll
@@ -291,16 +294,16 @@ __global__ __launch_bounds__(256, kQuant ? 3 : 2) void stream_attn_kernel(Dims d
         *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (ch ^ (n & 7)) + 4 * g) = o[ch] * w;
     __syncthreads();
     const int head = tid >> 4, c8 = 8 * (tid & 15);      // eight channels of a head
-    if (head < G) {
+    if (head < G) {                                      // (of eight wavefronts the first four)
         float den = 0.f, Mh = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) Mh = fmaxf(Mh, ml_s[i][head].x);
+        for (int i = 0; i < kWaves; ++i) Mh = fmaxf(Mh, ml_s[i][head].x);
         const float bh = Mh == -INFINITY ? 0.f : Mh;
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kWaves; ++i) {
             den += ml_s[i][head].y * fast_exp2(ml_s[i][head].x - bh);
             const float *from = reinterpret_cast<const float *>(Vs[i]) + head * kHeadDim + 16 * ((c8 >> 4) ^ (head & 7)) + (c8 & 15);
 #pragma unroll
@@ -326,19 +329,30 @@ __global__ __launch_bounds__(256, kQuant ? 3 : 2) void stream_attn_kernel(Dims d
 // ---- host side -------------------------------------------------------------------------------------------------------------
 static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// How many workgroups a row's `units` are split over: as many as the chip holds (three per compute unit; two with a bf16 cache, whose rows take
-// more registers), and a number of units to each that its four wavefronts share evenly.  With more the last of them wait for the
-// first ones' places (64 sequences, window 8192, 4 bits: 1024 / 768 / 512 workgroups 35 / 30 / 33 us), uneven ones do as if they had more (16 drafted
-// tokens x 32 blocks, 6 / 8 units each: 11.8 / 10.1 us).
+// Whether each row is one workgroup of eight wavefronts, and the call one launch.  Where rows fill the chip once (64 to 512 of them)
+// and a wavefront has at most five units, that beats a split over workgroups of four with a second launch to join them (4 bits, 1024
+// tokens: 128 rows 11.6 / 13.3 us, 512 rows 24.5 / 27; bf16: 64 rows of 450 tokens 8.6 / 10, 256 rows of 1000 tokens 24 / 27).  With more
+// rows three workgroups of four per compute unit hide more than the one of eight that fits (1024 rows 44 / 36).  With fewer the units
+// that a wavefront takes one after the other are what is waited for (2 rows of 1024 tokens 10.4 / 8.7), but for up to two of them at
+// 4 bits (7.0 / 8.1).
+static bool stream_alone(const Dims &dm, int64_t units, bool quant) {
+    const int64_t rows = (int64_t)dm.batch * dm.n_q * dm.Hkv;
+    return units <= 40 && rows <= 512 && (rows >= 64 || (quant && units <= 16));
+}
+// The rest is split over workgroups of four wavefronts, as many as the chip holds (three per compute unit; two with a bf16 cache, whose
+// rows take more registers), and a number of units to each that its wavefronts share evenly.  With more workgroups the last of them wait
+// for the first ones' places (64 sequences, window 8192, 4 bits: 1024 / 768 / 512 workgroups 35 / 30 / 33 us), uneven ones do as if they
+// had more (16 drafted tokens x 32 blocks, 6 / 8 units each: 11.8 / 10.1 us).
 constexpr int kMaxSplits = 64;                           // what decode_merge_kernel joins
 static int stream_units(const Dims &dm, int64_t units, bool quant) {
+    if (stream_alone(dm, units, quant)) return (int)max((int64_t)1, units);
     const int64_t rows = max((int64_t)1, (int64_t)dm.batch * dm.n_q * dm.Hkv), chip = quant ? 768 : 512;
     const int64_t want = min((chip + rows - 1) / rows, (int64_t)kMaxSplits);
     return (int)((units + 4 * want - 1) / (4 * want) * 4);
 }
 static int stream_splits(const Dims &dm, int64_t units, bool quant) {
     const int each = stream_units(dm, units, quant);
-    return (int)max((int64_t)1, (units + each - 1) / max(each, 1));
+    return (int)max((int64_t)1, (units + each - 1) / each);
 }
 // The most units a window may touch: the sinks', and one more than fill the window.
 static int64_t window_units(const Dims &dm, WindowArgs w) {
@@ -347,15 +361,16 @@ static int64_t window_units(const Dims &dm, WindowArgs w) {
 }
 
 template <bool kQuant, bool kList>
-static int launch_stream(const char *name, const Dims &dm, WindowArgs win, int splits, int per, Tensor q, const RowSource &src,
+static int launch_stream(const char *name, const Dims &dm, WindowArgs win, int64_t units, int splits, int per, Tensor q, const RowSource &src,
                          const int32_t *seqlens, const int32_t *block_idx, const uint64_t *tree_mask, Tensor out, float *lse, void *ws,
                          hipStream_t stream) {
     float *o_part = reinterpret_cast<float *>(ws);
     float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) +
                                                  align256((size_t)dm.batch * dm.n_q * dm.Hq * splits * kHeadDim * sizeof(float)));
     timing_begin(name, stream);
-    hipLaunchKernelGGL((stream_attn_kernel<kQuant, kList>), dim3(splits, dm.Hkv, dm.batch * dm.n_q), dim3(256), 0, stream, dm, win, q, src,
-                       seqlens, block_idx, tree_mask, per, out, lse, o_part, ml_part);
+    const bool alone = stream_alone(dm, units, kQuant);
+    hipLaunchKernelGGL((alone ? stream_attn_kernel<kQuant, kList, 8> : stream_attn_kernel<kQuant, kList, 4>), dim3(splits, dm.Hkv, dm.batch * dm.n_q),
+                       dim3(alone ? 512 : 256), 0, stream, dm, win, q, src, seqlens, block_idx, tree_mask, per, out, lse, o_part, ml_part);
     timing_end(stream);
     if (splits == 1) return (int)hipGetLastError();
     Dims parts = dm;
@@ -367,8 +382,8 @@ int launch_attn_decode_quant(const Dims &dm, Tensor q, QuantTensor kq, QuantTens
                              const int32_t *block_idx, const uint64_t *tree_mask, Tensor out, float *lse, void *ws,
                              hipStream_t stream) {
     if (dm.batch <= 0) return 0;
-    const int per = stream_units(dm, 2 * dm.topk, true) / 2;
-    return launch_stream<true, true>("sparse_attn_quant_kernel", dm, WindowArgs{0, 0}, (dm.topk + per - 1) / per, per, q,
+    const int per = min(stream_units(dm, 2 * dm.topk, true) / 2, dm.topk);
+    return launch_stream<true, true>("sparse_attn_quant_kernel", dm, WindowArgs{0, 0}, 2 * dm.topk, (dm.topk + per - 1) / per, per, q,
                                      RowSource{Tensor{}, Tensor{}, kq, vq}, seqlens, block_idx, tree_mask, out, lse, ws, stream);
 }
 
@@ -382,14 +397,14 @@ size_t window_decode_ws_bytes(const Dims &dm, WindowArgs w) {
 int launch_window_decode(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v, const int32_t *seqlens, Tensor out, float *lse,
                          void *ws, hipStream_t stream) {
     if (dm.batch <= 0) return 0;
-    return launch_stream<false, false>("window_decode_kernel", dm, w, stream_splits(dm, window_units(dm, w), false), 0, q,
+    return launch_stream<false, false>("window_decode_kernel", dm, w, window_units(dm, w), stream_splits(dm, window_units(dm, w), false), 0, q,
                                        RowSource{k, v, QuantTensor{}, QuantTensor{}}, seqlens, nullptr, nullptr, out, lse, ws, stream);
 }
 
 int launch_window_decode_quant(const Dims &dm, WindowArgs w, Tensor q, QuantTensor kq, QuantTensor vq, const int32_t *seqlens,
                                Tensor out, float *lse, void *ws, hipStream_t stream) {
     if (dm.batch <= 0) return 0;
-    return launch_stream<true, false>("window_decode_quant_kernel", dm, w, stream_splits(dm, window_units(dm, w), true), 0, q,
+    return launch_stream<true, false>("window_decode_quant_kernel", dm, w, window_units(dm, w), stream_splits(dm, window_units(dm, w), true), 0, q,
                                       RowSource{Tensor{}, Tensor{}, kq, vq}, seqlens, nullptr, nullptr, out, lse, ws, stream);
 }
 

@@ -363,6 +363,27 @@ def test_sparse_verify_quant(G, H, lengths, n, topk, kind):
                 check(out[b, i, rows], lse[b, i, rows], attend(q[b, i, rows].double(), k64[b, h, at], v64[b, h, at], seen, prm.softmax_scale))
 
 
+# 63 to 66, 512 and 514 rows, units of 16, 17, 40 and 41: the sizes at which a row changes from one workgroup to several
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", [
+    (16, 2, [1200 + 3 * i for i in range(32)] + [0, 1], 4, 1000), (16, 1, [1300] * 63, 0, 1200), (4, 2, [1300, 31, 900] * 11, 0, 1217),
+    (8, 2, [700, 0] * 16, 0, 1250), (2, 4, [90 + i for i in range(128)], 1, 64), (1, 2, [200 + i % 7 for i in range(257)], 33, 97),
+    (16, 1, [2000], 0, 480), (16, 1, [2000], 0, 481)])
+@pytest.mark.parametrize("quant", [False, True])
+def test_window_decode_rows_and_units(G, H, lengths, n_sink, window, quant):
+    test_window_decode(G, H, lengths, n_sink, window, quant)
+
+
+@pytest.mark.parametrize("G,H,lengths,n,topk,kind", [
+    (16, 2, [900, 70], 16, 20, "tree"), (4, 2, [1700, 65], 16, 21, "random"), (16, 1, [800, 799], 31, 12, "tree"), (2, 8, [500, 40, 16], 22, 5, "chain")])
+def test_sparse_verify_quant_rows_and_units(G, H, lengths, n, topk, kind):
+    test_sparse_verify_quant(G, H, lengths, n, topk, kind)
+
+
+@pytest.mark.parametrize("G,H,lengths,topk,holes", [(16, 2, [3000, 1, 0, 700] * 8, 20, True), (16, 2, [100 + 9 * i for i in range(260)], 4, False), (8, 1, [900], 8, True), (8, 1, [900], 9, True)])
+def test_sparse_decode_quant_rows_and_units(G, H, lengths, topk, holes):
+    test_sparse_decode_quant(G, H, lengths, topk, holes)
+
+
 PREFILL_CASES = [  # G, Hkv, lengths, n_sink, window
     (1, 1, [1], 0, 1), (16, 2, [1, 7, 8, 9, 0], 1, 3), (1, 2, [300, 129, 128], 0, 1), (2, 1, [500], 4, 50),
     (4, 1, [777], 4, 256), (8, 2, [640, 333], 64, 100), (16, 2, [700, 1], 100, 64), (16, 1, [513], 600, 5),
