@@ -402,8 +402,15 @@ PyObject *sparse_attn_bwd(Args a) {
 void expect(bool ok, const char *name, const char *what) {
     if (!ok) throw MarshalError(std::string(name) + what);
 }
+// the current device, asked for once in a call (asking costs as much as all other checks of a tensor)
+thread_local int device_now;
+const infllmv2_params *enter(PyObject *prm) {
+    device_now = -1;
+    return params(prm);
+}
 void here(const at::Tensor &t, const char *name) {
-    expect(t.is_cuda() && t.device().index() == c10::hip::getCurrentHIPStream().device_index(), name, " must be on the current device");
+    if (t.is_cuda() && device_now < 0) device_now = c10::hip::getCurrentHIPStream().device_index();
+    expect(t.is_cuda() && t.device().index() == device_now, name, " must be on the current device");
 }
 const at::Tensor &query(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_params *prm) {       // B < 0: any
     const at::Tensor &t = bf16_4d(o, name);
@@ -418,17 +425,13 @@ const at::Tensor &kv(PyObject *o, const char *name, int64_t B, int64_t T, const 
     return t;
 }
 // (codes uint8 [B, Hkv, T, d / 2], scales uint8 [B, Hkv, T, d / 32])
-struct Quant {
-    at::Tensor codes, scales;
-    infllmv2_quant_tensor desc() const {
-        return {codes.data_ptr(), scales.data_ptr(), codes.stride(0), codes.stride(1), codes.stride(2),
-                scales.stride(0), scales.stride(1), scales.stride(2)};
-    }
-};
-Quant quant(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_params *prm) {
+infllmv2_quant_tensor quant(const at::Tensor &codes, const at::Tensor &scales) {
+    return {codes.data_ptr(), scales.data_ptr(), codes.stride(0), codes.stride(1), codes.stride(2), scales.stride(0), scales.stride(1), scales.stride(2)};
+}
+infllmv2_quant_tensor quant(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_params *prm, int64_t *batch = nullptr) {
     expect(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 2, name, " must be a pair (codes, scales)");
-    Quant q{tensor(PyTuple_GET_ITEM(o, 0), name), tensor(PyTuple_GET_ITEM(o, 1), name)};
-    const at::Tensor *ts[2] = {&q.codes, &q.scales};
+    const at::Tensor &codes = tensor(PyTuple_GET_ITEM(o, 0), name), &scales = tensor(PyTuple_GET_ITEM(o, 1), name);
+    const at::Tensor *ts[2] = {&codes, &scales};
     for (int i = 0; i < 2; ++i) {
         const at::Tensor &t = *ts[i];
         expect(t.scalar_type() == at::kByte && t.dim() == 4 && t.stride(3) == 1, name, ": codes and scales must be 4-d uint8 tensors with a contiguous last axis");
@@ -436,8 +439,9 @@ Quant quant(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_
         expect((B < 0 || t.size(0) == B) && t.size(1) == prm->n_kv_heads && t.size(2) >= T && t.size(3) == prm->head_dim / (i ? 32 : 2), name,
                " must be codes [batch, n_kv_heads, tokens, head_dim / 2], scales [batch, n_kv_heads, tokens, head_dim / 32]");
     }
-    expect(q.codes.size(0) == q.scales.size(0), name, ": codes and scales differ in batch");
-    return q;
+    expect(codes.size(0) == scales.size(0), name, ": codes and scales differ in batch");
+    if (batch) *batch = codes.size(0);
+    return quant(codes, scales);
 }
 const int32_t *lengths(PyObject *o, int64_t B) {
     const int32_t *p = i32(o, "seqlens");
@@ -486,12 +490,40 @@ int32_t capacity(PyObject *o) {
     return T;
 }
 
-PyObject *quant_pair(Quant &a, Quant &b, PyObject *make) {  // (codes, scales) twice, through `make`: binding.QuantCache
+// (prm, k, v, seqlens, max_seqlen, (kq, vq) | None, n_new_tokens, QuantCache) -> (kq, vq)
+PyObject *quantize_kv(Args a) {
+    const infllmv2_params *prm = enter(a[0]);
+    const int32_t T = capacity(a[4]), n_new = integer(a[6]);
+    const at::Tensor &k = kv(a[1], "k", -1, T, prm), &v = kv(a[2], "v", k.size(0), T, prm);
+    const int64_t B = k.size(0);
+    const bool make = a[5] == Py_None;
+    const int32_t fill = make && n_new <= 0 && k.size(2) == T;      // the call clears the rows behind a sequence itself
+    at::Tensor own[4];                                    // codes and scales of K, of V
+    infllmv2_quant_tensor kq, vq;
+    if (make) {
+        for (int i = 0; i < 4; ++i) {
+            const at::IntArrayRef::value_type shape[4] = {B, k.size(1), k.size(2), k.size(3) / (i & 1 ? 32 : 2)};
+            own[i] = fill ? at::empty(shape, like(k, at::kByte)) : at::zeros(shape, like(k, at::kByte));
+        }
+        kq = quant(own[0], own[1]);
+        vq = quant(own[2], own[3]);
+    } else {
+        expect(PyTuple_Check(a[5]) && PyTuple_GET_SIZE(a[5]) == 2, "kq, vq", " must both be given");
+        kq = quant(PyTuple_GET_ITEM(a[5], 0), "kq", B, T, prm);
+        vq = quant(PyTuple_GET_ITEM(a[5], 1), "vq", B, T, prm);
+    }
+    const infllmv2_tensor kd = cache(k), vd = cache(v);
+    const int32_t *sl = lengths(a[3], B);
+    run("infllmv2_quantize_kv",
+        [&] { return lib.quantize_kv(prm, &kd, &vd, sl, static_cast<int32_t>(B), T, n_new, &kq, &vq, current_stream(), fill); });
+    if (!make) {
+        Py_INCREF(a[5]);
+        return a[5];
+    }
     PyObject *r = PyTuple_New(2);
-    Quant *q[2] = {&a, &b};
-    for (int i = 0; i < 2; ++i) {
-        PyObject *codes = THPVariable_Wrap(q[i]->codes), *scales = THPVariable_Wrap(q[i]->scales);
-        PyObject *pair = PyObject_CallFunctionObjArgs(make, codes, scales, nullptr);
+    for (int i = 0; i < 2; ++i) {                         // (codes, scales) twice, as binding.QuantCache
+        PyObject *codes = THPVariable_Wrap(own[2 * i]), *scales = THPVariable_Wrap(own[2 * i + 1]);
+        PyObject *pair = PyObject_CallFunctionObjArgs(a[7], codes, scales, nullptr);
         Py_DECREF(codes);
         Py_DECREF(scales);
         if (!pair) {
@@ -503,73 +535,43 @@ PyObject *quant_pair(Quant &a, Quant &b, PyObject *make) {  // (codes, scales) t
     return r;
 }
 
-// (prm, k, v, seqlens, max_seqlen, (kq, vq) | None, n_new_tokens, QuantCache) -> (kq, vq)
-PyObject *quantize_kv(Args a) {
-    const infllmv2_params *prm = params(a[0]);
-    const int32_t T = capacity(a[4]), n_new = integer(a[6]);
-    const at::Tensor &k = kv(a[1], "k", -1, T, prm), &v = kv(a[2], "v", k.size(0), T, prm);
-    const int64_t B = k.size(0);
-    Quant kq, vq;
-    const bool make = a[5] == Py_None;
-    const int32_t fill = make && n_new <= 0 && k.size(2) == T;      // the call clears the rows behind a sequence itself
-    if (make) {
-        Quant *q[2] = {&kq, &vq};
-        for (int i = 0; i < 2; ++i) {
-            const at::IntArrayRef::value_type codes[4] = {B, k.size(1), k.size(2), k.size(3) / 2}, scales[4] = {B, k.size(1), k.size(2), k.size(3) / 32};
-            q[i]->codes = fill ? at::empty(codes, like(k, at::kByte)) : at::zeros(codes, like(k, at::kByte));
-            q[i]->scales = fill ? at::empty(scales, like(k, at::kByte)) : at::zeros(scales, like(k, at::kByte));
-        }
-    } else {
-        expect(PyTuple_Check(a[5]) && PyTuple_GET_SIZE(a[5]) == 2, "kq, vq", " must both be given");
-        kq = quant(PyTuple_GET_ITEM(a[5], 0), "kq", B, T, prm);
-        vq = quant(PyTuple_GET_ITEM(a[5], 1), "vq", B, T, prm);
-    }
-    const infllmv2_tensor kd = cache(k), vd = cache(v);
-    const infllmv2_quant_tensor kqd = kq.desc(), vqd = vq.desc();
-    const int32_t *sl = lengths(a[3], B);
-    run("infllmv2_quantize_kv",
-        [&] { return lib.quantize_kv(prm, &kd, &vd, sl, static_cast<int32_t>(B), T, n_new, &kqd, &vqd, current_stream(), fill); });
-    return quant_pair(kq, vq, a[7]);
-}
-
 // (prm, kq, vq, seqlens, max_seqlen, k | None, v | None, n_new_tokens)
 PyObject *dequantize_kv(Args a) {
-    const infllmv2_params *prm = params(a[0]);
+    const infllmv2_params *prm = enter(a[0]);
     const int32_t T = capacity(a[4]), n_new = integer(a[7]);
-    const Quant kq = quant(a[1], "kq", -1, T, prm), vq = quant(a[2], "vq", kq.codes.size(0), T, prm);
-    const int64_t B = kq.codes.size(0);
+    int64_t B;
+    const infllmv2_quant_tensor kq = quant(a[1], "kq", -1, T, prm, &B), vq = quant(a[2], "vq", B, T, prm);
     Result k(a[5]), v(a[6]);
     const int32_t fill = k.make() && v.make() && n_new <= 0;
-    const at::IntArrayRef::value_type shape[4] = {B, kq.codes.size(1), T, prm->head_dim};
+    const at::IntArrayRef::value_type shape[4] = {B, prm->n_kv_heads, T, prm->head_dim};
+    const at::Tensor &codes = THPVariable_Unpack(PyTuple_GET_ITEM(a[1], 0));
     for (Result *r : {&k, &v})
-        if (r->make()) r->own = fill ? at::empty(shape, like(kq.codes, at::kBFloat16)) : at::zeros(shape, like(kq.codes, at::kBFloat16));
+        if (r->make()) r->own = fill ? at::empty(shape, like(codes, at::kBFloat16)) : at::zeros(shape, like(codes, at::kBFloat16));
     const infllmv2_tensor kd = cache(k.make() ? k.own : kv(k.given, "k", B, T, prm)), vd = cache(v.make() ? v.own : kv(v.given, "v", B, T, prm));
-    const infllmv2_quant_tensor kqd = kq.desc(), vqd = vq.desc();
     const int32_t *sl = lengths(a[3], B);
     run("infllmv2_dequantize_kv",
-        [&] { return lib.dequantize_kv(prm, &kqd, &vqd, sl, static_cast<int32_t>(B), T, n_new, &kd, &vd, current_stream(), fill); });
+        [&] { return lib.dequantize_kv(prm, &kq, &vq, sl, static_cast<int32_t>(B), T, n_new, &kd, &vd, current_stream(), fill); });
     return tuple2(k, v);
 }
 
 // (prm, k_new, v_new, kq, vq, seqlens, max_seqlen, ck | None)
 PyObject *append_kv_quant(Args a) {
-    const infllmv2_params *prm = params(a[0]);
+    const infllmv2_params *prm = enter(a[0]);
     const int32_t T = capacity(a[6]);
     const at::Tensor &kn = kv(a[1], "k_new", -1, 0, prm);
     const int64_t B = kn.size(0), n = kn.size(2);
     const at::Tensor &vn = kv(a[2], "v_new", B, n, prm);
     expect(vn.size(2) == n, "v_new", " must have the rows of k_new");
-    const Quant kq = quant(a[3], "kq", B, T, prm), vq = quant(a[4], "vq", B, T, prm);
+    const infllmv2_quant_tensor kq = quant(a[3], "kq", B, T, prm), vq = quant(a[4], "vq", B, T, prm);
     infllmv2_tensor ck{};
     if (a[7] != Py_None) {
         const bool some = prm->kernel_size > 0 && prm->kernel_stride > 0 && T >= prm->kernel_size;
         ck = cache(kv(a[7], "ck", B, some ? (T - prm->kernel_size) / prm->kernel_stride + 1 : 0, prm));
     }
     const infllmv2_tensor knd = cache(kn), vnd = cache(vn);
-    const infllmv2_quant_tensor kqd = kq.desc(), vqd = vq.desc();
     const int32_t *sl = lengths(a[5], B);
     run("infllmv2_append_kv_quant", [&] {
-        return lib.append_kv_quant(prm, &knd, &vnd, &kqd, &vqd, a[7] != Py_None ? &ck : nullptr, sl, static_cast<int32_t>(B), T,
+        return lib.append_kv_quant(prm, &knd, &vnd, &kq, &vq, a[7] != Py_None ? &ck : nullptr, sl, static_cast<int32_t>(B), T,
                                    static_cast<int32_t>(n), current_stream());
     });
     Py_RETURN_NONE;
@@ -577,12 +579,12 @@ PyObject *append_kv_quant(Args a) {
 
 // (prm, q, kq, vq, seqlens, max_seqlen, block_idx, out | None, lse | None, workspace | None)
 PyObject *sparse_attn_decode_quant(Args a) {
-    const infllmv2_params *prm = params(a[0]);
+    const infllmv2_params *prm = enter(a[0]);
     const int32_t T = capacity(a[5]);
     const at::Tensor &q = query(a[1], "q", -1, 1, prm);
     expect(q.size(1) == 1, "q", " must have one row per sequence");
     const int32_t B = static_cast<int32_t>(q.size(0));
-    const infllmv2_quant_tensor kq = quant(a[2], "kq", B, T, prm).desc(), vq = quant(a[3], "vq", B, T, prm).desc();
+    const infllmv2_quant_tensor kq = quant(a[2], "kq", B, T, prm), vq = quant(a[3], "vq", B, T, prm);
     const int32_t *sl = lengths(a[4], B), *ip = blocks(a[6], static_cast<int64_t>(B) * prm->n_kv_heads * prm->topk);
     Attended r(a[7], a[8], q, 1, {B, prm->n_q_heads}, false, prm);
     const Workspace ws = scratch(a[9], a[9] == Py_None ? lib.workspace_bytes(INFLLMV2_OP_ATTN_DECODE, prm, B, T) : 0, q);
@@ -595,11 +597,11 @@ PyObject *sparse_attn_decode_quant(Args a) {
 
 // (prm, q, kq, vq, seqlens, max_seqlen, block_idx, tree_mask | None, out | None, lse | None, workspace | None)
 PyObject *sparse_attn_verify_quant(Args a) {
-    const infllmv2_params *prm = params(a[0]);
+    const infllmv2_params *prm = enter(a[0]);
     const int32_t T = capacity(a[5]);
     const at::Tensor &q = query(a[1], "q", -1, 1, prm);
     const int32_t B = static_cast<int32_t>(q.size(0)), n = static_cast<int32_t>(q.size(1));
-    const infllmv2_quant_tensor kq = quant(a[2], "kq", B, T, prm).desc(), vq = quant(a[3], "vq", B, T, prm).desc();
+    const infllmv2_quant_tensor kq = quant(a[2], "kq", B, T, prm), vq = quant(a[3], "vq", B, T, prm);
     const int32_t *sl = lengths(a[4], B), *ip = blocks(a[6], static_cast<int64_t>(B) * prm->n_kv_heads * n * prm->topk);
     const uint64_t *mask = tree_mask(a[7], B, n);
     if (mask) here(tensor(a[7], "tree_mask"), "tree_mask");
@@ -614,7 +616,7 @@ PyObject *sparse_attn_verify_quant(Args a) {
 
 // (prm, n_sink, window, q, k, v, seqlens, max_seqlen, out | None, lse | None, workspace | None)
 PyObject *window_attn_prefill(Args a) {
-    const infllmv2_params *prm = params(a[0]);
+    const infllmv2_params *prm = enter(a[0]);
     const int32_t sink = integer(a[1]), window = integer(a[2]), T = capacity(a[7]);
     const at::Tensor &q = query(a[3], "q", -1, T, prm);
     const int32_t B = static_cast<int32_t>(q.size(0));
@@ -631,7 +633,7 @@ PyObject *window_attn_prefill(Args a) {
 
 // (prm, n_sink, window, q, k, v, out, dout, lse, seqlens, max_seqlen, dq | None, dk | None, dv | None, workspace | None)
 PyObject *window_attn_bwd(Args a) {
-    const infllmv2_params *prm = params(a[0]);
+    const infllmv2_params *prm = enter(a[0]);
     const int32_t sink = integer(a[1]), window = integer(a[2]), T = capacity(a[10]);
     const at::Tensor &q = query(a[3], "q", -1, T, prm);
     const int32_t B = static_cast<int32_t>(q.size(0));
@@ -658,7 +660,7 @@ PyObject *window_attn_bwd(Args a) {
 // (prm, n_sink, window, q, k, v, seqlens, max_seqlen, out | None, lse | None, workspace | None); k, v of either kind
 template <bool kQuant>
 PyObject *window_decode(Args a) {
-    const infllmv2_params *prm = params(a[0]);
+    const infllmv2_params *prm = enter(a[0]);
     const int32_t sink = integer(a[1]), window = integer(a[2]), T = capacity(a[7]);
     const at::Tensor &q = query(a[3], "q", -1, 1, prm);
     expect(q.size(1) == 1, "q", " must have one row per sequence");
@@ -668,7 +670,7 @@ PyObject *window_decode(Args a) {
     const Workspace ws = scratch(a[10], a[10] == Py_None ? lib.window_workspace_bytes(INFLLMV2_OP_WINDOW_DECODE, prm, sink, window, B, T) : 0, q);
     const infllmv2_tensor qd = rows(q);
     if constexpr (kQuant) {
-        const infllmv2_quant_tensor kq = quant(a[4], "kq", B, T, prm).desc(), vq = quant(a[5], "vq", B, T, prm).desc();
+        const infllmv2_quant_tensor kq = quant(a[4], "kq", B, T, prm), vq = quant(a[5], "vq", B, T, prm);
         run("infllmv2_window_attn_decode_quant", [&] {
             return lib.window_attn_decode_quant(prm, sink, window, &qd, &kq, &vq, sl, B, T, &r.od, r.lp, ws.ptr, ws.bytes, current_stream());
         });
