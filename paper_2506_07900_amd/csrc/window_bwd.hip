@@ -506,7 +506,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs wi
 // ---- host side -------------------------------------------------------------------------------------------------------------
 // Scratch tiles a call may use in all: a number that grows with the batch and with max_seqlen, so that a buffer for a call is large
 // enough for every smaller one.
-static int64_t most_slots(int64_t tiles) { return min(32 * tiles, 2048 + 2 * tiles); }
+static int64_t most_slots(int64_t tiles) { return min(32 * tiles, 4096 + 2 * tiles); }
 
 // The span: of some lengths the one whose workgroups the chip, which holds 512, is through with first: all steps, about 50 more per
 // workgroup for its start and its sums (but not less than the longest workgroup), and half a longest workgroup's steps in which not all have work.
@@ -526,7 +526,8 @@ static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
         p.spans = (int)((dm.max_seqlen + span - 1) / span);
         p.per_span = (int)min((int64_t)p.tiles, p.sink_tiles + (span + w.window - 2) / kKvKeys + 2);
         p.parts = (int)min((int64_t)p.spans, ((int64_t)w.window + 126) / span + 2);
-        const int64_t items = heads * p.spans * p.per_span, longest = (min(span, (int64_t)dm.max_seqlen) + per - 1) / per;
+        const int64_t items = heads * p.spans * p.per_span / (p.per_span == p.tiles ? 2 : 1);   // (of whole pasts half exist)
+        const int64_t longest = (min(span, (int64_t)dm.max_seqlen) + per - 1) / per;
         const int64_t cost = max((steps + 50 * items) / 512, longest) + longest / 2;
         if (heads * p.slot(p.tiles) <= most_slots(heads * p.tiles) && cost < least) {
             least = cost;
