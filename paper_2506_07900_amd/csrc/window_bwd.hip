@@ -553,7 +553,7 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
     const int few_tiles = (dm.max_seqlen + (32 >> lg) - 1) / (32 >> lg), run = xcd_run_length(n_tiles * heads);
     timing_begin("window_dq_kernel", stream);
-    if (n_tiles * heads <= 64)
+    if (few_rows(dm, w, n_tiles * heads))
         hipLaunchKernelGGL(window_dq_few_kernel, dim3((unsigned)(few_tiles * heads)), dim3(256), 0, stream, dm, w, scale, lg, few_tiles, q, k, v, out,
                            dout, lse, seqlens, dq, rows);
     else

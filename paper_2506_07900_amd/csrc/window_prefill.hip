@@ -395,10 +395,11 @@ int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tens
     auto tiles = [&](int rows) { return (dm.max_seqlen + (rows >> lg) - 1) / (rows >> lg); };
     const int64_t items = tiles(kFwdRows) * heads;
     const int run = xcd_run_length(items);
-    // Up to 64 workgroups of 128 rows: four times as many of 32 (2048 tokens, 4 heads : 1, whole window 42 -> 20 us; 256: 23 -> 41).  Up to 512, two per
-    // compute unit: the pipelined form (4096 tokens, 8 : 2, whole window, 78 us, with three per compute unit 91; 16K, 4 : 4 142 / 151), beyond three
-    // (32K, 32 : 2, window 4096 / 512 / 36: 2110 / 456 / 236 -> 2056 / 391 / 206).
-    if (items <= 64) {
+    // few_rows: workgroups of 32 (2048 tokens, 4 heads : 1, whole window 42 -> 20 us; 4096 tokens, window 4096 / 1000 / 256: 79 / 28 / 13.8 -> 43 /
+    // 27 / 15.6; twice as many rows, whole window: 84 -> 88).  Up to 512 workgroups of 128 rows, two per compute unit: the pipelined form
+    // (4096 tokens, 8 : 2, whole window, 78 us, with three per compute unit 91; 16K, 4 : 4 142 / 151), beyond three (32K, 32 : 2, window 4096 / 512 /
+    // 36: 2110 / 456 / 236 -> 2056 / 391 / 206).
+    if (few_rows(dm, w, items)) {
         timing_begin("window_prefill_few_kernel", stream);
         hipLaunchKernelGGL(window_prefill_few_kernel, dim3((unsigned)(tiles(32) * heads)), dim3(256), 0, stream, dm, w, lg, tiles(32), q, k, v,
                            seqlens, out, lse);

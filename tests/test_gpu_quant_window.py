@@ -417,6 +417,12 @@ def test_window_prefill(G, H, lengths, n_sink, window):
                       attend(q[b, :n, hq].double(), k[b, hq // G, :n].double(), v[b, hq // G, :n].double(), seen, prm.softmax_scale))
 
 
+# around 64 and 128 workgroups of 128 rows and walks of 512 keys, and more runs of rows than XCDs
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", [(4, 1, [2049], 0, 511), (4, 1, [2049], 0, 512), (4, 1, [2080], 9, 503), (4, 1, [4096], 0, 600), (4, 1, [4097], 0, 600), (16, 2, [1000] * 8, 0, 1000)])
+def test_window_prefill_rows_and_walks(G, H, lengths, n_sink, window):
+    test_window_prefill(G, H, lengths, n_sink, window)
+
+
 def test_window_prefill_of_large_values():
     # values near bf16's largest: their sums overflow 32 bits before they are divided, their means do not
     gen = torch.Generator(device="cuda").manual_seed(6)
@@ -489,6 +495,11 @@ def test_window_bwd(G, H, lengths, n_sink, window):
                 tol = 1.0625 * err + HALF * want.abs() + 1e-30
                 diff = (got[b, h, :n].double() - want).abs()
                 assert (diff <= tol).all(), (name, float((diff / tol).max()))
+
+
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", [(4, 1, [2049], 0, 511), (4, 1, [2080], 9, 503), (4, 1, [4097], 0, 600), (16, 2, [1000] * 8, 0, 1000), (2, 1, [1100, 1, 0, 515] * 3, 0, 1100)])
+def test_window_bwd_rows_and_walks(G, H, lengths, n_sink, window):
+    test_window_bwd(G, H, lengths, n_sink, window)
 
 
 @pytest.mark.parametrize("G,H,n,n_sink,window,at", [(16, 2, 200, 4, 20, 70), (1, 1, 400, 0, 129, 255), (4, 2, 3000, 3, 100, 1), (8, 4, 1500, 0, 64, 1499), (16, 4, 1100, 70, 33, 1000)])
