@@ -15,7 +15,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
 __device__ __forceinline__ uint32_t pair_max(uint32_t pair) { return max(pair & 0x7fffu, (pair >> 16) & 0x7fffu); }
 
 // Rows [max(0, l - n_new), l) of every sequence, l = its length; with dm.fill also rows [l, max_seqlen), as zeros.
-// A thread takes 8 channels of a row, a quad a group of 32.  Pure traffic: 256 bytes in and 68 out per row of K and of V.
+// A thread takes 8 channels of a row, a quad a group of 32.  Pure traffic: 256 bytes in and 68 out per row of K and of V.  128K tokens x 2 heads 27 to
+// 33 us, 5.1 to 6.3 TB/s (some of it from the last-level cache; a large copy: 5.25).
 __global__ __launch_bounds__(256) void quantize_kv_kernel(Dims dm, Tensor k, Tensor v, const int32_t *__restrict__ seqlens,
                                                           int32_t n_new, QuantTensor kq, QuantTensor vq) {
     const int h = blockIdx.y, b = blockIdx.z;
@@ -57,6 +58,7 @@ __global__ __launch_bounds__(256) void quantize_kv_kernel(Dims dm, Tensor k, Ten
         }
 }
 
+// The way back, the same split; 26 us for 128K tokens x 2 heads.
 __global__ __launch_bounds__(256) void dequantize_kv_kernel(Dims dm, QuantTensor kq, QuantTensor vq, const int32_t *__restrict__ seqlens,
                                                             int32_t n_new, Tensor k, Tensor v) {
     const int h = blockIdx.y, b = blockIdx.z;
@@ -95,7 +97,8 @@ __global__ __launch_bounds__(256) void dequantize_kv_kernel(Dims dm, QuantTensor
 // lanes are a group of the format, so its largest magnitude is a row reduction).  Tasks 0 .. 2 n_q - 1 of a (sequence,
 // key-value head) quantise a row of K (even) or V; the others build a kernel each from its 32 rows' values as the cache holds them: older
 // rows from the cache, new ones from k_new through the same quantisation.  So the kernel's bits are those that
-// compress_keys gives for the cache as read back.  A sequence shorter than n_q is skipped as a whole.
+// compress_keys gives for the cache as read back.  A sequence shorter than n_q is skipped as a whole.  One launch of latency: 4.3 us for a token, 5.7 for
+// 8 sequences x 16 tokens.
 __device__ __forceinline__ uint32_t group_exponent(uint32_t pair) {
     return quant_exponent(row_reduce_u32(pair_max(pair), [](uint32_t a, uint32_t b) { return max(a, b); }));
 }

@@ -16,6 +16,9 @@ struct KVTile {
 // What the forward leaves of a row (token, head of the group): its log-sum-exp in powers of two and -D, 32 and 32 floats for 32 rows.
 __host__ __device__ static inline int64_t row_blocks(const Dims &dm) { return ((int64_t)dm.max_seqlen * dm.G + 31) / 32; }   // per (sequence, head)
 
+// dq of 128 rows, and what the rows leave for the other kernel.  A wavefront's 32 rows of q and dout stay in registers, keys and values come in tiles of 64,
+// one ahead; two workgroups to a compute unit, so that one's exponentials run under the other's products.  32K tokens, 32 : 2 heads, window
+// 4096: 2.7 to 2.8 ms, 1.1 PFLOP/s of its three products, bound by the matrix cores' power as dk/dv is.
 __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, int run, Tensor q, Tensor k,
                                                            Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
                                                            const int32_t *__restrict__ seqlens, Tensor dq, float *__restrict__ rows) {
@@ -252,15 +255,15 @@ struct __align__(16) KvRows {
     float ref[32], minus_D[32];
 };
 
-// kSlots: rows two steps (one ahead) or four (three ahead) at a time.  A compute unit with one workgroup does not hide a round trip to memory under
-// the other's step; with four slots it holds one only.
-template <int kSlots>
-__global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(Dims dm, WindowArgs win, float scale, int lg, BwdPlan plan, Tensor q, Tensor k,
+// dk, dv of 128 keys from one span's rows: a step is 32 rows, brought into LDS one step ahead (three steps ahead, one workgroup to a compute unit: nothing
+// where there are fewer workgroups than that, 20 % more time where there are more).  32K tokens, 32 : 2 heads, window 4096: 3.9 to 4.2 ms, 1.0
+// PFLOP/s of its four products; matrix cores busy 69 % of the time in which a SIMD has its two wavefronts, at the 1.7 GHz that the power limit
+// leaves (a large library product: 1.36 PFLOP/s).
+__global__ __launch_bounds__(256, 2) void window_dkdv_kernel(Dims dm, WindowArgs win, float scale, int lg, BwdPlan plan, Tensor q, Tensor k,
                                                              Tensor v, Tensor dout, const float *__restrict__ rows,
                                                              const int32_t *__restrict__ seqlens, Tensor dk, Tensor dv,
                                                              float *__restrict__ part) {
     __shared__ KvRows slot0, slot1;
-    __shared__ std::conditional_t<kSlots == 4, KvRows, char> slot2, slot3;
     __shared__ __align__(16) char vt[kKvKeys * 256];
     const int item = xcd_item(blockIdx.x, plan.per_span), group = item / plan.per_span, bh = group / plan.spans;     // a span is a run
     const int b = bh / dm.Hkv, h = bh - b * dm.Hkv, span = (bh + 1) * plan.spans - 1 - group, at = item - group * plan.per_span;
@@ -302,14 +305,13 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
         q_at[j] = 2u * (tok * (uint32_t)q.st + g * (uint32_t)q.sh) + piece;
         g_at[j] = 2u * (tok * (uint32_t)dout.st + g * (uint32_t)dout.sh) + piece;
     }
-    // (with four slots as many copies for every step: those past the last bring zeros)
     auto stage = [&](KvRows &dst, int x) __attribute__((always_inline)) {
-        if (kSlots == 2 && x >= x1) return;
-        const int i0 = from + min(x, x1 - 1) * per;
+        if (x >= x1) return;
+        const int i0 = from + x * per;
         const char *qb = q_head + (int64_t)i0 * (2 * q.st), *gb = g_head + (int64_t)i0 * (2 * dout.st);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const bool row = x < x1 && i0 + ((16 * j + (lane >> 2)) >> lg) < L;
+            const bool row = i0 + ((16 * j + (lane >> 2)) >> lg) < L;
             copy_rows(dst.q + wave * 2048 + j * 1024, qb, row ? q_at[j] : kNoRow, 0);
             copy_rows(dst.g + wave * 2048 + j * 1024, gb, row ? g_at[j] : kNoRow, 0);
         }
@@ -317,13 +319,7 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(row_head + ((int64_t)i0 >> (5 - lg)) * 64 + lane),
                                              (__attribute__((address_space(3))) void *)dst.ref, 4, 0, 0);
     };
-    if (x1 > 0) {
-        stage(slot0, 0);
-        if constexpr (kSlots == 4) {
-            stage(slot1, 1);
-            stage(slot2, 2);
-        }
-    }
+    stage(slot0, 0);
     const TileReader rd(lane);
     const float c = dm.scale_log2;
     f32x16 dka[4], dva[4];
@@ -331,16 +327,9 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
     for (int ct = 0; ct < 4; ++ct) dka[ct] = dva[ct] = zero16();
     const int k_lo = tile * kKvKeys + 32 * wave, k_hi = k_lo + 31;
     auto step = [&](const KvRows &cur, KvRows &next, int x) __attribute__((always_inline)) {
-        if constexpr (kSlots == 2) {
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-        } else {                                         // all copies but those of the next two steps, five each (vmcnt 10)
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_waitcnt(0x0f7a);
-            asm volatile("s_barrier" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        stage(next, x + kSlots - 1);
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        stage(next, x + 1);
         const int i0 = from + x * per, i1 = i0 + per - 1;
         const bool some = k_lo <= i1 && (k_lo < win.n_sink || i0 - k_hi < win.window);
         if (!some) return;
@@ -416,19 +405,9 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
             dka[i & 3] = mfma32(cq[i % kRing], ds[i >> 2], dka[i & 3]);
         }
     };
-    if constexpr (kSlots == 2) {
-        for (int x = 0; x < x1; x += 2) {
-            step(slot0, slot1, x);
-            if (x + 1 < x1) step(slot1, slot0, x + 1);
-        }
-    } else {
-        for (int x = 0; x < x1; x += 4) {
-            step(slot0, slot3, x);
-            if (x + 1 < x1) step(slot1, slot0, x + 1);
-            if (x + 2 < x1) step(slot2, slot1, x + 2);
-            if (x + 3 < x1) step(slot3, slot2, x + 3);
-        }
-        __builtin_amdgcn_s_waitcnt(0);                   // (the copies past the last step have landed: the memory may go to another workgroup)
+    for (int x = 0; x < x1; x += 2) {
+        step(slot0, slot1, x);
+        if (x + 1 < x1) step(slot1, slot0, x + 1);
     }
     if (rows_of.first != rows_of.last) {                 // [key][channel], dk then dv
         const int64_t slot = (int64_t)bh * plan.slot(plan.tiles) + plan.slot(tile) + span - rows_of.first;
@@ -462,7 +441,7 @@ __global__ __launch_bounds__(256, kSlots == 2 ? 2 : 1) void window_dkdv_kernel(D
 }
 
 // The spans' sums of a key tile, added in order.  grid (keys / 8, Hkv, batch): 8 keys a workgroup, a thread 4 channels of dk and dv, four sums
-// of each asked for at once.
+// of each asked for at once.  Traffic alone: 32K tokens x 2 heads, three to five spans a tile, 57 to 70 us.
 __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs win, BwdPlan plan, const int32_t *__restrict__ seqlens,
                                                           const float *__restrict__ part, Tensor dk, Tensor dv) {
     const int h = blockIdx.y, b = blockIdx.z, bh = b * dm.Hkv + h;
@@ -561,9 +540,8 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
                        out, dout, lse, seqlens, dq, rows);
     timing_end(stream);
     timing_begin("window_dkdv_kernel", stream);
-    const int64_t items = plan.spans * plan.per_span * heads;
-    hipLaunchKernelGGL(items <= 256 ? window_dkdv_kernel<4> : window_dkdv_kernel<2>, dim3(xcd_grid(items, plan.per_span)), dim3(256), 0, stream,
-                       dm, w, scale, lg, plan, q, k, v, dout, rows, seqlens, dk, dv, part);
+    hipLaunchKernelGGL(window_dkdv_kernel, dim3(xcd_grid(heads * plan.spans * plan.per_span, plan.per_span)), dim3(256), 0, stream, dm, w, scale, lg, plan,
+                       q, k, v, dout, rows, seqlens, dk, dv, part);
     timing_end(stream);
     if (plan.spans == 1) return (int)hipGetLastError();
     timing_begin("window_join_kernel", stream);

@@ -199,6 +199,7 @@ __device__ __forceinline__ void clear_rows(const Dims &dm, const QueryRows &r, i
     if (r.hf == 0) lse[((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq] = 0.f;
 }
 
+// Two workgroups to a compute unit, one tile's scores ahead of another's exponentials.
 __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k, Tensor v,
                                                                 const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
     __shared__ Tile64 K0, K1, V0, V1;
@@ -251,7 +252,10 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
 }
 
 // The same for many rows: three workgroups to a compute unit instead of two, so that one's exponentials run under another's products and round trips,
-// with units of 32 keys, two ahead, in three slots, and a unit's scores at a time.  Its smaller units also leave less to hide.
+// with units of 32 keys, two ahead, in three slots, and a unit's scores at a time.  Its smaller units also leave less to hide.  32K tokens, 32 : 2
+// heads, window 4096: 1.94 to 2.02 ms, 1.04 to 1.08 PFLOP/s; bound by the matrix cores' power (1.4 to 1.7 GHz under this load; a large library product
+// reaches 1.36).  64 rows to a wavefront, which read each key and value from LDS half as often: 1.95 against 2.01 ms here, 607 against 591 us
+// for 64K tokens x 4 heads and window 1024, so not taken.
 __global__ __launch_bounds__(256, 3) void window_prefill_many_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k,
                                                                      Tensor v, const int32_t *__restrict__ seqlens, Tensor out,
                                                                      float *__restrict__ lse) {
