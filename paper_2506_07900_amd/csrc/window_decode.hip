@@ -351,7 +351,7 @@ static int stream_units(const Dims &dm, int64_t units, bool quant) {
     if (stream_alone(dm, units, quant)) return (int)max((int64_t)1, units);
     const int64_t rows = max((int64_t)1, (int64_t)dm.batch * dm.n_q * dm.Hkv), chip = quant ? 768 : 512;
     const int64_t want = min((chip + rows - 1) / rows, (int64_t)kMaxSplits);
-    return (int)((units + 4 * want - 1) / (4 * want) * 4);
+    return (int)max((int64_t)4, (units + 4 * want - 1) / (4 * want) * 4);   // (no units: a cache of no rows)
 }
 static int stream_splits(const Dims &dm, int64_t units, bool quant) {
     const int each = stream_units(dm, units, quant);

@@ -724,6 +724,25 @@ def test_caches_beyond_32_bits():
             check(out[0, 0, h:h + 1], lse[0, h:h + 1], attend(q[0, 0, h:h + 1].double(), x, x, seen, prm.softmax_scale))
 
 
+def test_caches_of_no_rows():
+    """max_seqlen 0: nothing is seen; where results have no memory the call is refused, as everywhere."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    prm = binding.Params(8, 2, topk=4)
+    k, v = normal(gen, 3, 2, 64, D), normal(gen, 3, 2, 64, D)
+    q, sl = normal(gen, 3, 1, 8, D), lengths_tensor([5, 0, -1])
+    kq, vq = binding.quantize_kv(prm, k, v, sl, 0)
+    assert not kq.codes.any() and not vq.scales.any()
+    assert not any(x.any() for x in binding.dequantize_kv(prm, kq, vq, sl, 0, k=torch.zeros_like(k), v=torch.zeros_like(v)))
+    idx = torch.zeros((3, 2, 1, 4), dtype=torch.int32, device="cuda")
+    for out, lse in (binding.window_attn_decode(prm, 0, 8, q, k, v, sl, 0), binding.window_attn_decode(prm, 3, 8, q, k, v, sl, 0),
+                     binding.window_attn_decode_quant(prm, 3, 8, q, kq, vq, sl, 0), binding.sparse_attn_decode_quant(prm, q, kq, vq, sl, 0, idx)):
+        assert not out.any() and (lse == -math.inf).all()
+    qs = normal(gen, 3, 64, 8, D)
+    for call in (lambda: binding.dequantize_kv(prm, kq, vq, sl, 0), lambda: binding.window_attn_prefill(prm, 0, 8, qs, k, v, sl, 0)):
+        with pytest.raises(binding.InfLLMv2Error):
+            call()
+
+
 def test_refusals_of_the_binding():
     prm = binding.Params(4, 1)
     gen = torch.Generator(device="cuda").manual_seed(1)
