@@ -233,7 +233,9 @@ struct BwdPlan {
     int span, spans;                                     // tokens of a span (a multiple of a step's), spans
     int per_span;                                        // key tiles a span may have
     int parts;                                           // spans a tile may have, sinks' tiles apart
-    __host__ __device__ int slot(int tile) const { return tile < sink_tiles ? tile * spans : sink_tiles * spans + (tile - sink_tiles) * parts; }
+    __host__ __device__ int64_t slot(int tile) const {
+        return tile < sink_tiles ? (int64_t)tile * spans : (int64_t)sink_tiles * spans + (int64_t)(tile - sink_tiles) * parts;
+    }
     // the first key tile behind the sinks' that a query of span s sees
     __host__ __device__ int first_tile(WindowArgs w, int s) const {
         const int64_t key = (int64_t)s * span + 1 - w.window;
