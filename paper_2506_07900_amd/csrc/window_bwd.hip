@@ -490,7 +490,9 @@ __global__ __launch_bounds__(256) void window_join_kernel(Dims dm, WindowArgs wi
 static int64_t most_slots(int64_t tiles) { return min(32 * tiles, 4096 + 2 * tiles); }
 
 // The span: of some lengths the one whose workgroups the chip, which holds 512, is through with first: all steps, about 50 more per
-// workgroup for its start and its sums (but not less than the longest workgroup), and half a longest workgroup's steps in which not all have work.
+// workgroup for its start and its sums but for the first 256, which have a compute unit each (not less than the longest workgroup), and half a
+// longest workgroup's steps in which not all have work.  (4096 tokens, 4 heads : 1, window 256, spans of 32 / 64 / 128 tokens: dk/dv and join 31 /
+// 26 / 32 us; 2 x 4096, 16 : 2, window 1000, of 128 / 256 / 384 / 512: 183 / 208 / 180 / 218.)
 static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
     BwdPlan best{};
     const int per = kKvRows / dm.G;
@@ -509,7 +511,7 @@ static BwdPlan bwd_plan(const Dims &dm, WindowArgs w) {
         p.parts = (int)min((int64_t)p.spans, ((int64_t)w.window + 126) / span + 2);
         const int64_t items = heads * p.spans * p.per_span / (p.per_span == p.tiles ? 2 : 1);   // (of whole pasts half exist)
         const int64_t longest = (min(span, (int64_t)dm.max_seqlen) + per - 1) / per;
-        const int64_t cost = max((steps + 50 * items) / 512, longest) + longest / 2;
+        const int64_t cost = max((steps + 50 * max((int64_t)0, items - 256)) / 512, longest) + longest / 2;
         if (heads * p.slot(p.tiles) <= most_slots(heads * p.tiles) && cost < least) {
             least = cost;
             best = p;
