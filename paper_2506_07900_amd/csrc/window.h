@@ -197,10 +197,10 @@ inline unsigned xcd_grid(int64_t items, int run) { return (unsigned)((items + 8 
 // sequence's start; dq of 2 x 4096 tokens, runs of 8 / 32 / 128 of its 1024 workgroups: 113 / 123 / 119 us).
 inline int xcd_run_length(int64_t items) { return (int)max((int64_t)1, min((int64_t)64, items / 128)); }
 
+// Whether rows see 512 keys or more, at which walks shared by wavefronts and joined are shorter by more than the joining costs.
+inline bool long_walks(const Dims &dm, WindowArgs w) { return min((int64_t)dm.max_seqlen, (int64_t)w.window + w.n_sink) >= 512; }
 // Whether workgroups of 128 rows are so few that a wavefront's walk over its keys is what is waited for: then a workgroup takes 32 rows and its
-// wavefronts share the keys.  Of short walks the halves that are joined cost more than they save.
-inline bool few_rows(const Dims &dm, WindowArgs w, int64_t items) {
-    return items <= (min((int64_t)dm.max_seqlen, (int64_t)w.window + w.n_sink) >= 512 ? 128 : 64);
-}
+// wavefronts share the keys.
+inline bool few_rows(const Dims &dm, WindowArgs w, int64_t items) { return items <= (long_walks(dm, w) ? 128 : 64); }
 
 }  // namespace infllmv2

@@ -18,31 +18,35 @@ __host__ __device__ static inline int64_t row_blocks(const Dims &dm) { return ((
 
 // dq of 128 rows, and what the rows leave for the other kernel.  A wavefront's 32 rows of q and dout stay in registers, keys and values come in tiles of 64,
 // one ahead; two workgroups to a compute unit, so that one's exponentials run under the other's products.  32K tokens, 32 : 2 heads, window
-// 4096: 2.7 to 2.8 ms, 1.1 PFLOP/s of its three products, bound by the matrix cores' power as dk/dv is.
-__global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, int run, Tensor q, Tensor k,
-                                                           Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
-                                                           const int32_t *__restrict__ seqlens, Tensor dq, float *__restrict__ rows) {
-    __shared__ KVTile tile0, tile1;
+// 4096: 2.7 to 2.8 ms, 1.1 PFLOP/s of its three products, bound by the matrix cores' power as dk/dv is.  kHalves 2, as in the forward: 4096 tokens, 8 : 2,
+// whole window, 106 -> 88 us; 8192, 4 : 1, window 1000, 40 -> 38.
+template <int kHalves>
+__global__ __launch_bounds__(256 * kHalves, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, int run, Tensor q,
+                                                                     Tensor k, Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
+                                                                     const int32_t *__restrict__ seqlens, Tensor dq, float *__restrict__ rows) {
+    __shared__ KVTile tile0[kHalves], tile1[kHalves];
     const int item = xcd_item(blockIdx.x, run), bh = item / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     if (b >= dm.batch) return;
     const int ti = (bh + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, id = __builtin_amdgcn_readfirstlane(tid >> 6), half = kHalves == 1 ? 0 : id >> 2, wave = id & 3;
     const int c32 = lane & 31, hf = lane >> 5;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int t0 = ti * (kDqRows >> lg), t1 = min(L, t0 + (kDqRows >> lg));
     const int row = 32 * wave + c32, i = t0 + (row >> lg), hq = h * dm.G + (row & (dm.G - 1));
     __bf16 *dq_row = dq.ptr + b * dq.sb + (int64_t)i * dq.st + (int64_t)hq * dq.sh + 4 * hf;
     if (t0 >= L) {
-        if (dm.fill && i < dm.max_seqlen)
+        if (dm.fill && half == 0 && i < dm.max_seqlen)
             for (int c = 0; c < 16; ++c) *reinterpret_cast<uint2 *>(dq_row + 8 * c) = uint2{0u, 0u};
         return;
     }
     const KeyTiles<kWinKeys> kt(win, t0, t1);
     const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
-    auto stage = [&](KVTile &dst, int x) __attribute__((always_inline)) {
-        if (x >= kt.count) return;
-        keys.copy(dst.k, kt.key0(x), wave, lane);
-        values.copy(dst.v, kt.key0(x), wave, lane);
+    const int count = (kt.count + kHalves - 1 - half) / kHalves, steps = (kt.count + kHalves - 1) / kHalves;   // this half's tiles; the first one's
+    auto key0 = [&](int x) __attribute__((always_inline)) { return kt.key0(kHalves * x + half); };
+    auto stage = [&](KVTile *dst, int x) __attribute__((always_inline)) {
+        if (x >= count) return;
+        keys.copy(dst[half].k, key0(x), wave, lane);
+        values.copy(dst[half].v, key0(x), wave, lane);
     };
     stage(tile0, 0);
     bf16x8 qf[8], gf[8];
@@ -63,7 +67,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
         D = half_reduce(D, [](float a, float d) { return a + d; });
         ref = lse[((int64_t)b * dm.max_seqlen + t) * dm.Hq + hq] * kLog2e;
         const int64_t r = (int64_t)ti * kDqRows + row;
-        if (i < L) rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? -D : ref;
+        if (i < L && half == 0) rows[((int64_t)bh * row_blocks(dm) + (r >> 5)) * 64 + 32 * hf + (r & 31)] = hf ? -D : ref;
     }
     const TileReader rd(lane);
     const float c = dm.scale_log2;
@@ -71,17 +75,18 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) acc[ct] = zero16();
     const int w_lo = t0 + ((32 * wave) >> lg), w_hi = t0 + ((32 * wave + 31) >> lg);
-    auto step = [&](const KVTile &cur, KVTile &next, int x) __attribute__((always_inline)) {
+    auto step = [&](const KVTile *cur, KVTile *next, int x) __attribute__((always_inline)) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         stage(next, x + 1);
-        const int k0 = kt.key0(x);
+        if (kHalves > 1 && x >= count) return;           // (the other half has one more)
+        const int k0 = key0(x);
         const bool some = k0 <= w_hi && (k0 < win.n_sink || w_lo - (k0 + kWinKeys - 1) < win.window);
         if (!some) return;
         const bool all = k0 + kWinKeys - 1 <= w_lo && (k0 + kWinKeys <= win.n_sink || w_hi - k0 < win.window);
 #pragma unroll
         for (int kh = 0; kh < 2; ++kh) {
-            const char *kr = cur.k.x + kh * kHalfTile, *vr = cur.v.x + kh * kHalfTile;
+            const char *kr = cur[half].k.x + kh * kHalfTile, *vr = cur[half].v.x + kh * kHalfTile;
             f32x16 s = zero16(), dp;                     // (dp - D straight from the product)
 #pragma unroll
             for (int e = 0; e < 16; ++e) dp[e] = -D;
@@ -107,11 +112,31 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
             }
         }
     };
-    for (int x = 0; x < kt.count; x += 2) {
+    for (int x = 0; x < steps; x += 2) {
         step(tile0, tile1, x);
-        if (x + 1 < kt.count) step(tile1, tile0, x + 1);
+        if (x + 1 < steps) step(tile1, tile0, x + 1);
     }
     __syncthreads();                                     // the tiles are free
+    if constexpr (kHalves == 2) {                        // (as in the forward)
+        KVTile &theirs = (wave & 1 ? tile1 : tile0)[1];
+        char *at = (wave < 2 ? theirs.k : theirs.v).x + 16 * lane;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4)
+                if (half == 1)
+                    *reinterpret_cast<f32x4 *>(at + 1024 * (4 * ct + e4)) = f32x4{acc[ct][4 * e4], acc[ct][4 * e4 + 1], acc[ct][4 * e4 + 2], acc[ct][4 * e4 + 3]};
+        __syncthreads();
+        if (half == 1) return;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(at + 1024 * (4 * ct + e4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[ct][4 * e4 + e] += x[e];
+            }
+    }
     const bool live = i < L;
     const uint32_t alive = (uint32_t)__ballot(live);
     if (alive != ~0u) {                                  // (rows behind the sequence: zeros, where they are written at all)
@@ -120,7 +145,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(Dims dm, WindowArgs w
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[ct][e] = live ? acc[ct][e] : 0.f;
     }
-    store_rows((wave < 2 ? tile0.k.x : tile0.v.x) + (wave & 1) * kHalfTile, acc, scale, lane, [&](int r) __attribute__((always_inline)) -> __bf16 * {
+    store_rows((wave < 2 ? tile0[0].k.x : tile0[0].v.x) + (wave & 1) * kHalfTile, acc, scale, lane, [&](int r) __attribute__((always_inline)) -> __bf16 * {
         const int t = t0 + ((32 * wave + r) >> lg), head = h * dm.G + ((32 * wave + r) & (dm.G - 1));
         return t < dm.max_seqlen && ((alive >> r) & 1u || dm.fill) ? dq.ptr + b * dq.sb + (int64_t)t * dq.st + (int64_t)head * dq.sh : nullptr;
     });
@@ -535,13 +560,14 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
     const BwdPlan plan = bwd_plan(dm, w);
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
     const int few_tiles = (dm.max_seqlen + (32 >> lg) - 1) / (32 >> lg), run = xcd_run_length(n_tiles * heads);
+    const bool halves = n_tiles * heads <= 256 && long_walks(dm, w);
     timing_begin("window_dq_kernel", stream);
     if (few_rows(dm, w, n_tiles * heads))
         hipLaunchKernelGGL(window_dq_few_kernel, dim3((unsigned)(few_tiles * heads)), dim3(256), 0, stream, dm, w, scale, lg, few_tiles, q, k, v, out,
                            dout, lse, seqlens, dq, rows);
     else
-        hipLaunchKernelGGL(window_dq_kernel, dim3(xcd_grid(n_tiles * heads, run)), dim3(256), 0, stream, dm, w, scale, lg, n_tiles, run, q, k, v,
-                       out, dout, lse, seqlens, dq, rows);
+        hipLaunchKernelGGL(halves ? window_dq_kernel<2> : window_dq_kernel<1>, dim3(xcd_grid(n_tiles * heads, run)), dim3(halves ? 512 : 256), 0,
+                           stream, dm, w, scale, lg, n_tiles, run, q, k, v, out, dout, lse, seqlens, dq, rows);
     timing_end(stream);
     timing_begin("window_dkdv_kernel", stream);
     hipLaunchKernelGGL(window_dkdv_kernel, dim3(xcd_grid(heads * plan.spans * plan.per_span, plan.per_span)), dim3(256), 0, stream, dm, w, scale, lg, plan,

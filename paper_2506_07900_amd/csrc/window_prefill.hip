@@ -199,22 +199,30 @@ __device__ __forceinline__ void clear_rows(const Dims &dm, const QueryRows &r, i
     if (r.hf == 0) lse[((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq] = 0.f;
 }
 
-// Two workgroups to a compute unit, one tile's scores ahead of another's exponentials.
-__global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k, Tensor v,
-                                                                const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
-    __shared__ Tile64 K0, K1, V0, V1;
+// One tile's scores ahead of another's exponentials; two wavefronts to a SIMD, of two workgroups or of one whose halves take every other tile (kHalves 2, for
+// fewer workgroups than compute units) and are joined at the end.
+template <int kHalves>
+__global__ __launch_bounds__(256 * kHalves, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k,
+                                                                          Tensor v, const int32_t *__restrict__ seqlens, Tensor out,
+                                                                          float *__restrict__ lse) {
+    __shared__ Tile64 K0[kHalves], K1[kHalves], V0[kHalves], V1[kHalves];
     const int item = xcd_item(blockIdx.x, run), bh = item / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     if (b >= dm.batch) return;
     const int ti = (bh + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = kHalves == 1 ? 0 : id >> 2, wave = id & 3;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int t0 = ti * (kFwdRows >> lg), t1 = min(L, t0 + (kFwdRows >> lg));
     QueryRows r(dm, win, lg, t0, 32 * wave, h, lane);
-    if (t0 >= L) return clear_rows(dm, r, b, out, lse);
+    if (t0 >= L) {
+        if (half == 0) clear_rows(dm, r, b, out, lse);
+        return;
+    }
     const KeyTiles<kWinKeys> kt(win, t0, t1);
+    const int count = (kt.count + kHalves - 1 - half) / kHalves, steps = (kt.count + kHalves - 1) / kHalves;   // this half's tiles; the first one's
+    auto key0 = [&](int x) __attribute__((always_inline)) { return kt.key0(kHalves * x + half); };
     const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
-    auto stage = [&](const TileCopier &from, Tile64 &to, int x) __attribute__((always_inline)) {
-        if (x < kt.count) from.copy(to, kt.key0(x), wave, lane);
+    auto stage = [&](const TileCopier &from, Tile64 *to, int x) __attribute__((always_inline)) {
+        if (x < count) from.copy(to[half], key0(x), wave, lane);
     };
     stage(keys, K0, 0);
     stage(values, V0, 0);
@@ -223,32 +231,59 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(Dims dm, WindowA
     r.load(q, b, L);
     // Tile x: its probabilities and their product with the values, and between them the next tile's scores, so that the matrix cores have
     // work while the exponentials run.  (Behind the last tile: scores of what lies in LDS, not used.)
-    auto step = [&](Tile64 &k_cur, const Tile64 &k_next, const Tile64 &v_cur, Tile64 &v_next, f32x16 (&s)[2], f32x16 (&s_next)[2], float &mx,
+    auto step = [&](Tile64 *k_cur, const Tile64 *k_next, const Tile64 *v_cur, Tile64 *v_next, f32x16 (&s)[2], f32x16 (&s_next)[2], float &mx,
                     int x) __attribute__((always_inline)) {
         __builtin_amdgcn_s_waitcnt(0);                   // this wavefront's copies have landed
         __syncthreads();                                 // everyone's have, and everyone is past the tile before
         stage(keys, k_cur, x + 2);
         if (x > 0) stage(values, v_next, x + 1);         // (the first two at once: a short walk is a chain of round trips)
+        if (kHalves > 1 && x >= count) return;           // (the other half has one more)
         const float base = r.reference(mx);
         __builtin_amdgcn_sched_barrier(0);
-        r.scores(k_next, s_next);
-        r.add(s, base, v_cur);
+        r.scores(k_next[half], s_next);
+        r.add(s, base, v_cur[half]);
         mx = QueryRows::largest(s_next);
         __builtin_amdgcn_sched_barrier(0);
-        if (x + 1 < kt.count) r.hide(s_next, kt.key0(x + 1), mx);
+        if (x + 1 < count) r.hide(s_next, key0(x + 1), mx);
     };
     f32x16 sa[2], sb[2];
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    r.scores(K0, sa);
+    r.scores(K0[half], sa);
     float mx = QueryRows::largest(sa);
-    r.hide(sa, kt.key0(0), mx);
-    for (int x = 0; x < kt.count; x += 2) {
+    r.hide(sa, key0(0), mx);
+    for (int x = 0; x < steps; x += 2) {
         step(K0, K1, V0, V1, sa, sb, mx, x);
-        if (x + 1 < kt.count) step(K1, K0, V1, V0, sb, sa, mx, x + 1);
+        if (x + 1 < steps) step(K1, K0, V1, V0, sb, sa, mx, x + 1);
     }
     __syncthreads();                                     // the tiles are free
-    finish_rows(dm, win, lg, t0, r, q, k, v, b, h, L, wave, lane, (wave < 2 ? K0.x : K1.x) + (wave & 1) * kHalfTile, out, lse);
+    if constexpr (kHalves == 2) {                        // a row's state is in the same lanes of both: the second hands its own over
+        __shared__ float2 ml[4][64];
+        char *at = (wave == 0 ? K0 : wave == 1 ? K1 : wave == 2 ? V0 : V1)[1].x + 16 * lane;
+        if (half == 1) {
+            ml[wave][lane] = float2{r.m, r.l};
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4)
+                    *reinterpret_cast<f32x4 *>(at + 1024 * (4 * ct + e4)) = f32x4{r.o[ct][4 * e4], r.o[ct][4 * e4 + 1], r.o[ct][4 * e4 + 2], r.o[ct][4 * e4 + 3]};
+        }
+        __syncthreads();
+        if (half == 1) return;
+        const float2 other = ml[wave][lane];
+        const float M = fmaxf(r.m, other.x), base = M == -INFINITY ? 0.f : M, mine = fast_exp2(r.m - base), theirs = fast_exp2(other.x - base);
+        r.m = M;
+        r.l = r.l * mine + other.y * theirs;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(at + 1024 * (4 * ct + e4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r.o[ct][4 * e4 + e] = r.o[ct][4 * e4 + e] * mine + x[e] * theirs;
+            }
+    }
+    finish_rows(dm, win, lg, t0, r, q, k, v, b, h, L, wave, lane, (wave < 2 ? K0 : K1)[0].x + (wave & 1) * kHalfTile, out, lse);
 }
 
 // The same for many rows: three workgroups to a compute unit instead of two, so that one's exponentials run under another's products and round trips,
@@ -400,7 +435,8 @@ int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tens
     const int64_t items = tiles(kFwdRows) * heads;
     const int run = xcd_run_length(items);
     // few_rows: workgroups of 32 (2048 tokens, 4 heads : 1, whole window 42 -> 20 us; 4096 tokens, window 4096 / 1000 / 256: 79 / 28 / 13.8 -> 43 /
-    // 27 / 15.6; twice as many rows, whole window: 84 -> 88).  Up to 512 workgroups of 128 rows, two per compute unit: the pipelined form
+    // 27 / 15.6; twice as many rows, whole window: 84 -> 88).  Up to 512 workgroups of 128 rows, two per compute unit: the pipelined form, up to 256 by halves
+    // where walks are long (4096 tokens, 8 : 2, whole window 83 -> 70 us; 1024, 32 : 2 26.6 -> 24.9; 4096, 4 : 1, window 256 13.2 -> 13.8)
     // (4096 tokens, 8 : 2, whole window, 78 us, with three per compute unit 91; 16K, 4 : 4 142 / 151), beyond three (32K, 32 : 2, window 4096 / 512 /
     // 36: 2110 / 456 / 236 -> 2056 / 391 / 206).
     if (few_rows(dm, w, items)) {
@@ -408,9 +444,10 @@ int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tens
         hipLaunchKernelGGL(window_prefill_few_kernel, dim3((unsigned)(tiles(32) * heads)), dim3(256), 0, stream, dm, w, lg, tiles(32), q, k, v,
                            seqlens, out, lse);
     } else {
+        const bool halves = items <= 256 && long_walks(dm, w);
         timing_begin(items <= 512 ? "window_prefill_kernel" : "window_prefill_many_kernel", stream);
-        hipLaunchKernelGGL(items <= 512 ? window_prefill_kernel : window_prefill_many_kernel, dim3(xcd_grid(items, run)), dim3(256), 0, stream, dm, w,
-                           lg, tiles(kFwdRows), run, q, k, v, seqlens, out, lse);
+        hipLaunchKernelGGL(halves ? window_prefill_kernel<2> : items <= 512 ? window_prefill_kernel<1> : window_prefill_many_kernel,
+                           dim3(xcd_grid(items, run)), dim3(halves ? 512 : 256), 0, stream, dm, w, lg, tiles(kFwdRows), run, q, k, v, seqlens, out, lse);
     }
     timing_end(stream);
     return (int)hipGetLastError();

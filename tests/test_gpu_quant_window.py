@@ -423,6 +423,20 @@ def test_window_prefill_rows_and_walks(G, H, lengths, n_sink, window):
     test_window_prefill(G, H, lengths, n_sink, window)
 
 
+# workgroups by halves: up to 256 of them, walks of 512 keys or more, one tile and odd numbers of tiles among them
+HALVES = [(4, 1, [5000], 0, 700), (16, 1, [700, 40, 64], 5, 600), (16, 2, [65, 900, 0, 1], 70, 500), (2, 4, [2048, 1985], 0, 513)]
+
+
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", HALVES)
+def test_window_prefill_by_halves(G, H, lengths, n_sink, window):
+    test_window_prefill(G, H, lengths, n_sink, window)
+
+
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", HALVES)
+def test_window_bwd_by_halves(G, H, lengths, n_sink, window):
+    test_window_bwd(G, H, lengths, n_sink, window)
+
+
 def test_window_prefill_of_large_values():
     # values near bf16's largest: their sums overflow 32 bits before they are divided, their means do not
     gen = torch.Generator(device="cuda").manual_seed(6)
@@ -525,6 +539,11 @@ def test_window_prefill_keeps_what_is_not_finite_where_it_is_seen(G, H, n, n_sin
 
 
 # ---- as they are used ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("G,H,n,n_sink,window,at", [(16, 2, 700, 0, 600, 50), (16, 2, 700, 3, 513, 127), (4, 1, 5000, 0, 700, 4000)])
+def test_halves_keep_what_is_not_finite_where_it_is_seen(G, H, n, n_sink, window, at):
+    test_window_prefill_keeps_what_is_not_finite_where_it_is_seen(G, H, n, n_sink, window, at)
+
 
 def test_gradients_are_differences():
     # a loss <out, w> along random directions: the calls' gradients against central differences of the definition in 64 bits
