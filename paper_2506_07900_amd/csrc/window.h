@@ -203,4 +203,10 @@ inline bool long_walks(const Dims &dm, WindowArgs w) { return min((int64_t)dm.ma
 // wavefronts share the keys.
 inline bool few_rows(const Dims &dm, WindowArgs w, int64_t items) { return items <= (long_walks(dm, w) ? 128 : 64); }
 
+// Whether a workgroup of 128 rows is two halves that share its walk: walks are long, and there are fewer workgroups than compute units, or up to twice as many
+// where windows are whole, so that walks are of all lengths and a compute unit's second place would stand empty behind a short one.
+inline bool by_halves(const Dims &dm, WindowArgs w, int64_t items) {
+    return long_walks(dm, w) && items <= ((int64_t)w.window + w.n_sink >= dm.max_seqlen ? 512 : 256);
+}
+
 }  // namespace infllmv2

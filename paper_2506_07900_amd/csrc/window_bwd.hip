@@ -19,7 +19,7 @@ __host__ __device__ static inline int64_t row_blocks(const Dims &dm) { return ((
 // dq of 128 rows, and what the rows leave for the other kernel.  A wavefront's 32 rows of q and dout stay in registers, keys and values come in tiles of 64,
 // one ahead; two workgroups to a compute unit, so that one's exponentials run under the other's products.  32K tokens, 32 : 2 heads, window
 // 4096: 2.7 to 2.8 ms, 1.1 PFLOP/s of its three products, bound by the matrix cores' power as dk/dv is.  kHalves 2, as in the forward: 4096 tokens, 8 : 2,
-// whole window, 106 -> 88 us; 8192, 4 : 1, window 1000, 40 -> 38.
+// whole window, 106 -> 88 us; 8192, 8 : 2, whole window 316 -> 224, but window 4096 183 -> 191.
 template <int kHalves>
 __global__ __launch_bounds__(256 * kHalves, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, int run, Tensor q,
                                                                      Tensor k, Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
@@ -560,7 +560,7 @@ int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v
     const BwdPlan plan = bwd_plan(dm, w);
     const int64_t heads = (int64_t)dm.batch * dm.Hkv;
     const int few_tiles = (dm.max_seqlen + (32 >> lg) - 1) / (32 >> lg), run = xcd_run_length(n_tiles * heads);
-    const bool halves = n_tiles * heads <= 256 && long_walks(dm, w);
+    const bool halves = by_halves(dm, w, n_tiles * heads);
     timing_begin("window_dq_kernel", stream);
     if (few_rows(dm, w, n_tiles * heads))
         hipLaunchKernelGGL(window_dq_few_kernel, dim3((unsigned)(few_tiles * heads)), dim3(256), 0, stream, dm, w, scale, lg, few_tiles, q, k, v, out,

@@ -199,17 +199,16 @@ __device__ __forceinline__ void clear_rows(const Dims &dm, const QueryRows &r, i
     if (r.hf == 0) lse[((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq] = 0.f;
 }
 
-// One tile's scores ahead of another's exponentials; two wavefronts to a SIMD, of two workgroups or of one whose halves take every other tile (kHalves 2, for
-// fewer workgroups than compute units) and are joined at the end.
-template <int kHalves>
-__global__ __launch_bounds__(256 * kHalves, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k,
-                                                                          Tensor v, const int32_t *__restrict__ seqlens, Tensor out,
-                                                                          float *__restrict__ lse) {
-    __shared__ Tile64 K0[kHalves], K1[kHalves], V0[kHalves], V1[kHalves];
+// A workgroup's 128 rows by two halves, which take every other tile and are joined at the end; in each one tile's scores are ahead of another's
+// exponentials.
+__global__ __launch_bounds__(512, 2) void window_prefill_kernel(Dims dm, WindowArgs win, int lg, int n_tiles, int run, Tensor q, Tensor k, Tensor v,
+                                                                const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse) {
+    __shared__ Tile64 K0[2], K1[2], V0[2], V1[2];
+    __shared__ float2 ml[4][64];
     const int item = xcd_item(blockIdx.x, run), bh = item / n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     if (b >= dm.batch) return;
     const int ti = (bh + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
-    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = kHalves == 1 ? 0 : id >> 2, wave = id & 3;
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = id >> 2, wave = id & 3;
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int t0 = ti * (kFwdRows >> lg), t1 = min(L, t0 + (kFwdRows >> lg));
     QueryRows r(dm, win, lg, t0, 32 * wave, h, lane);
@@ -218,8 +217,8 @@ __global__ __launch_bounds__(256 * kHalves, 2) void window_prefill_kernel(Dims d
         return;
     }
     const KeyTiles<kWinKeys> kt(win, t0, t1);
-    const int count = (kt.count + kHalves - 1 - half) / kHalves, steps = (kt.count + kHalves - 1) / kHalves;   // this half's tiles; the first one's
-    auto key0 = [&](int x) __attribute__((always_inline)) { return kt.key0(kHalves * x + half); };
+    const int count = (kt.count + 1 - half) >> 1, steps = (kt.count + 1) >> 1;   // this half's tiles; the first one's
+    auto key0 = [&](int x) __attribute__((always_inline)) { return kt.key0(2 * x + half); };
     const TileCopier keys(k, b, h, L, wave, lane), values(v, b, h, L, wave, lane);
     auto stage = [&](const TileCopier &from, Tile64 *to, int x) __attribute__((always_inline)) {
         if (x < count) from.copy(to[half], key0(x), wave, lane);
@@ -237,7 +236,7 @@ __global__ __launch_bounds__(256 * kHalves, 2) void window_prefill_kernel(Dims d
         __syncthreads();                                 // everyone's have, and everyone is past the tile before
         stage(keys, k_cur, x + 2);
         if (x > 0) stage(values, v_next, x + 1);         // (the first two at once: a short walk is a chain of round trips)
-        if (kHalves > 1 && x >= count) return;           // (the other half has one more)
+        if (x >= count) return;           // (the other half has one more)
         const float base = r.reference(mx);
         __builtin_amdgcn_sched_barrier(0);
         r.scores(k_next[half], s_next);
@@ -257,36 +256,34 @@ __global__ __launch_bounds__(256 * kHalves, 2) void window_prefill_kernel(Dims d
         if (x + 1 < steps) step(K1, K0, V1, V0, sb, sa, mx, x + 1);
     }
     __syncthreads();                                     // the tiles are free
-    if constexpr (kHalves == 2) {                        // a row's state is in the same lanes of both: the second hands its own over
-        __shared__ float2 ml[4][64];
-        char *at = (wave == 0 ? K0 : wave == 1 ? K1 : wave == 2 ? V0 : V1)[1].x + 16 * lane;
-        if (half == 1) {
-            ml[wave][lane] = float2{r.m, r.l};
-#pragma unroll
-            for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4)
-                    *reinterpret_cast<f32x4 *>(at + 1024 * (4 * ct + e4)) = f32x4{r.o[ct][4 * e4], r.o[ct][4 * e4 + 1], r.o[ct][4 * e4 + 2], r.o[ct][4 * e4 + 3]};
-        }
-        __syncthreads();
-        if (half == 1) return;
-        const float2 other = ml[wave][lane];
-        const float M = fmaxf(r.m, other.x), base = M == -INFINITY ? 0.f : M, mine = fast_exp2(r.m - base), theirs = fast_exp2(other.x - base);
-        r.m = M;
-        r.l = r.l * mine + other.y * theirs;
+    // a row's state is in the same lanes of both halves: the second hands its own over
+    char *at = (wave == 0 ? K0 : wave == 1 ? K1 : wave == 2 ? V0 : V1)[1].x + 16 * lane;
+    if (half == 1) {
+        ml[wave][lane] = float2{r.m, r.l};
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(at + 1024 * (4 * ct + e4));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) r.o[ct][4 * e4 + e] = r.o[ct][4 * e4 + e] * mine + x[e] * theirs;
-            }
+            for (int e4 = 0; e4 < 4; ++e4)
+                *reinterpret_cast<f32x4 *>(at + 1024 * (4 * ct + e4)) = f32x4{r.o[ct][4 * e4], r.o[ct][4 * e4 + 1], r.o[ct][4 * e4 + 2], r.o[ct][4 * e4 + 3]};
     }
+    __syncthreads();
+    if (half == 1) return;
+    const float2 other = ml[wave][lane];
+    const float M = fmaxf(r.m, other.x), base = M == -INFINITY ? 0.f : M, mine = fast_exp2(r.m - base), theirs = fast_exp2(other.x - base);
+    r.m = M;
+    r.l = r.l * mine + other.y * theirs;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(at + 1024 * (4 * ct + e4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.o[ct][4 * e4 + e] = r.o[ct][4 * e4 + e] * mine + x[e] * theirs;
+        }
     finish_rows(dm, win, lg, t0, r, q, k, v, b, h, L, wave, lane, (wave < 2 ? K0 : K1)[0].x + (wave & 1) * kHalfTile, out, lse);
 }
 
-// The same for many rows: three workgroups to a compute unit instead of two, so that one's exponentials run under another's products and round trips,
+// The same for many rows: three workgroups of four wavefronts to a compute unit, so that one's exponentials run under another's products and round trips,
 // with units of 32 keys, two ahead, in three slots, and a unit's scores at a time.  Its smaller units also leave less to hide.  32K tokens, 32 : 2
 // heads, window 4096: 1.94 to 2.02 ms, 1.04 to 1.08 PFLOP/s; bound by the matrix cores' power (1.4 to 1.7 GHz under this load; a large library product
 // reaches 1.36).  64 rows to a wavefront, which read each key and value from LDS half as often: 1.95 against 2.01 ms here, 607 against 591 us
@@ -435,19 +432,17 @@ int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tens
     const int64_t items = tiles(kFwdRows) * heads;
     const int run = xcd_run_length(items);
     // few_rows: workgroups of 32 (2048 tokens, 4 heads : 1, whole window 42 -> 20 us; 4096 tokens, window 4096 / 1000 / 256: 79 / 28 / 13.8 -> 43 /
-    // 27 / 15.6; twice as many rows, whole window: 84 -> 88).  Up to 512 workgroups of 128 rows, two per compute unit: the pipelined form, up to 256 by halves
-    // where walks are long (4096 tokens, 8 : 2, whole window 83 -> 70 us; 1024, 32 : 2 26.6 -> 24.9; 4096, 4 : 1, window 256 13.2 -> 13.8)
-    // (4096 tokens, 8 : 2, whole window, 78 us, with three per compute unit 91; 16K, 4 : 4 142 / 151), beyond three (32K, 32 : 2, window 4096 / 512 /
-    // 36: 2110 / 456 / 236 -> 2056 / 391 / 206).
+    // 27 / 15.6; twice as many rows, whole window: 84 -> 88).  by_halves (8192 tokens, 4 : 1, window 8192 / 3000 / 1000: 166 / 69 / 32 -> 123 / 55 / 30;
+    // 8 : 2, window 8192: 245 -> 178, but 4096: 136 -> 147).  Beyond three workgroups per compute unit.
+    const bool halves = by_halves(dm, w, items);
     if (few_rows(dm, w, items)) {
         timing_begin("window_prefill_few_kernel", stream);
         hipLaunchKernelGGL(window_prefill_few_kernel, dim3((unsigned)(tiles(32) * heads)), dim3(256), 0, stream, dm, w, lg, tiles(32), q, k, v,
                            seqlens, out, lse);
     } else {
-        const bool halves = items <= 256 && long_walks(dm, w);
-        timing_begin(items <= 512 ? "window_prefill_kernel" : "window_prefill_many_kernel", stream);
-        hipLaunchKernelGGL(halves ? window_prefill_kernel<2> : items <= 512 ? window_prefill_kernel<1> : window_prefill_many_kernel,
-                           dim3(xcd_grid(items, run)), dim3(halves ? 512 : 256), 0, stream, dm, w, lg, tiles(kFwdRows), run, q, k, v, seqlens, out, lse);
+        timing_begin(halves ? "window_prefill_kernel" : "window_prefill_many_kernel", stream);
+        hipLaunchKernelGGL(halves ? window_prefill_kernel : window_prefill_many_kernel, dim3(xcd_grid(items, run)), dim3(halves ? 512 : 256), 0, stream,
+                           dm, w, lg, tiles(kFwdRows), run, q, k, v, seqlens, out, lse);
     }
     timing_end(stream);
     return (int)hipGetLastError();

@@ -424,7 +424,7 @@ def test_window_prefill_rows_and_walks(G, H, lengths, n_sink, window):
 
 
 # workgroups by halves: up to 256 of them, walks of 512 keys or more, one tile and odd numbers of tiles among them
-HALVES = [(4, 1, [5000], 0, 700), (16, 1, [700, 40, 64], 5, 600), (16, 2, [65, 900, 0, 1], 70, 500), (2, 4, [2048, 1985], 0, 513)]
+HALVES = [(4, 1, [5000], 0, 700), (16, 1, [700, 40, 64], 5, 600), (16, 2, [65, 900, 0, 1], 70, 500), (2, 4, [2048, 1985], 0, 513), (16, 2, [1200, 63], 100, 1100), (16, 2, [1200, 63], 99, 1100)]
 
 
 @pytest.mark.parametrize("G,H,lengths,n_sink,window", HALVES)
