@@ -18,8 +18,9 @@ __host__ __device__ static inline int64_t row_blocks(const Dims &dm) { return ((
 
 // dq of 128 rows, and what the rows leave for the other kernel.  A wavefront's 32 rows of q and dout stay in registers, keys and values come in tiles of 64,
 // one ahead; two workgroups to a compute unit, so that one's exponentials run under the other's products.  32K tokens, 32 : 2 heads, window
-// 4096: 2.7 to 2.8 ms, 1.1 PFLOP/s of its three products, bound by the matrix cores' power as dk/dv is.  kHalves 2, as in the forward: 4096 tokens, 8 : 2,
-// whole window, 106 -> 88 us; 8192, 8 : 2, whole window 316 -> 224, but window 4096 183 -> 191.
+// 4096: 2.65 ms, 1.18 PFLOP/s of its three products, bound by the matrix cores' power as dk/dv is.  kHalves 2, as in the forward: 4096 tokens, 8 : 2,
+// whole window, 106 -> 88 us; 8192, 8 : 2, whole window 316 -> 224, but window 4096 183 -> 191.  Half a tile's exponentials stand between the other half's
+// products, and a product's operands are read one ahead (2 x 4096, 16 : 2, window 1000: 110.4 -> 104; two ahead the same).
 template <int kHalves>
 __global__ __launch_bounds__(256 * kHalves, 2) void window_dq_kernel(Dims dm, WindowArgs win, float scale, int lg, int n_tiles, int run, Tensor q,
                                                                      Tensor k, Tensor v, Tensor out, Tensor dout, const float *__restrict__ lse,
@@ -84,33 +85,59 @@ __global__ __launch_bounds__(256 * kHalves, 2) void window_dq_kernel(Dims dm, Wi
         const bool some = k0 <= w_hi && (k0 < win.n_sink || w_lo - (k0 + kWinKeys - 1) < win.window);
         if (!some) return;
         const bool all = k0 + kWinKeys - 1 <= w_lo && (k0 + kWinKeys <= win.n_sink || w_hi - k0 < win.window);
-#pragma unroll
-        for (int kh = 0; kh < 2; ++kh) {
+        f32x16 s[2], dp[2];                              // (dp - D straight from the product)
+        // (the next operands are under way while the matrix cores work; `more`: vector work to put between)
+        auto products = [&](int kh, auto more) __attribute__((always_inline)) {
             const char *kr = cur[half].k.x + kh * kHalfTile, *vr = cur[half].v.x + kh * kHalfTile;
-            f32x16 s = zero16(), dp;                     // (dp - D straight from the product)
+            bf16x8 xk[2] = {rd.rows(kr, 0)}, xv[2] = {rd.rows(vr, 0)};
+            s[kh] = zero16();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) dp[e] = -D;
+            for (int e = 0; e < 16; ++e) dp[kh][e] = -D;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {
-                s = mfma32(rd.rows(kr, ks), qf[ks], s);
-                dp = mfma32(rd.rows(vr, ks), gf[ks], dp);
+                if (ks < 7) {
+                    xk[(ks + 1) & 1] = rd.rows(kr, ks + 1);
+                    xv[(ks + 1) & 1] = rd.rows(vr, ks + 1);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                s[kh] = mfma32(xk[ks & 1], qf[ks], s[kh]);
+                dp[kh] = mfma32(xv[ks & 1], gf[ks], dp[kh]);
+                more(ks);
             }
+        };
+        auto exponentials = [&](int kh, int i) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = fast_exp2(__builtin_fmaf(s[e], c, -ref)) * dp[e];
-            if (!all) {                                  // (what is not visible may be anything: replaced, not multiplied)
-                int at = k0 + 32 * kh + 4 * hf;
-                asm volatile("" : "+v"(at));
-                const VisibleKeys visible(win, i);
+            for (int e = 2 * i; e < 2 * i + 2; ++e) s[kh][e] = fast_exp2(__builtin_fmaf(s[kh][e], c, -ref)) * dp[kh][e];
+        };
+        auto hide = [&](int kh) __attribute__((always_inline)) {
+            if (all) return;                             // (what is not visible may be anything: replaced, not multiplied)
+            int at = k0 + 32 * kh + 4 * hf;
+            asm volatile("" : "+v"(at));
+            const VisibleKeys visible(win, i);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = visible(at + 8 * (e >> 2) + (e & 3)) ? s[e] : 0.f;
+            for (int e = 0; e < 16; ++e) s[kh][e] = visible(at + 8 * (e >> 2) + (e & 3)) ? s[kh][e] : 0.f;
+        };
+        auto sums = [&](int kh, auto more) __attribute__((always_inline)) {
+            const char *kr = cur[half].k.x + kh * kHalfTile;
+            bf16x8 xk[2] = {rd.columns(kr, 0, 0)};
+            const bf16x8 ds[2] = {pack8(s[kh], 0), pack8(s[kh], 1)};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j < 7) xk[(j + 1) & 1] = rd.columns(kr, (j + 1) >> 2, (j + 1) & 3);
+                __builtin_amdgcn_sched_barrier(0);
+                acc[j & 3] = mfma32(xk[j & 1], ds[j >> 2], acc[j & 3]);
+                more(j);
             }
-#pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2) {
-                const bf16x8 ds = pack8(s, s2);
-#pragma unroll
-                for (int ct = 0; ct < 4; ++ct) acc[ct] = mfma32(rd.columns(kr, s2, ct), ds, acc[ct]);
-            }
-        }
+        };
+        // one half's exponentials under the other's products
+        products(0, [](int) {});
+        products(1, [&](int j) __attribute__((always_inline)) { exponentials(0, j); });
+        __builtin_amdgcn_sched_barrier(0);
+        hide(0);
+        sums(0, [&](int j) __attribute__((always_inline)) { exponentials(1, j); });
+        __builtin_amdgcn_sched_barrier(0);
+        hide(1);
+        sums(1, [](int) {});
     };
     for (int x = 0; x < steps; x += 2) {
         step(tile0, tile1, x);
