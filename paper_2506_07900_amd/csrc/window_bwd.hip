@@ -227,11 +227,21 @@ __global__ __launch_bounds__(256, 1) void window_dq_few_kernel(Dims dm, WindowAr
         f32x16 s = zero16(), dp;
 #pragma unroll
         for (int e = 0; e < 16; ++e) dp[e] = -D;
+        bf16x8 x[8], y[8];                               // (alone on its SIMD: all operands asked for before any is used)
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-            s = mfma32(rd.rows(cur.k, ks), qf[ks], s);
-            dp = mfma32(rd.rows(cur.v, ks), gf[ks], dp);
+            x[ks] = rd.rows(cur.k, ks);
+            y[ks] = rd.rows(cur.v, ks);
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+            s = mfma32(x[ks], qf[ks], s);
+            dp = mfma32(y[ks], gf[ks], dp);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = rd.columns(cur.k, j >> 2, j & 3);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = fast_exp2(__builtin_fmaf(s[e], c, -ref)) * dp[e];
         if (!(k0 + 31 <= t0 && (k0 + 32 <= win.n_sink || hi - k0 < win.window))) {
@@ -243,7 +253,7 @@ __global__ __launch_bounds__(256, 1) void window_dq_few_kernel(Dims dm, WindowAr
         for (int j = 0; j < 2; ++j) {
             const bf16x8 ds = pack8(s, j);
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct) acc[ct] = mfma32(rd.columns(cur.k, j, ct), ds, acc[ct]);
+            for (int ct = 0; ct < 4; ++ct) acc[ct] = mfma32(x[4 * j + ct], ds, acc[ct]);
         }
     });
     reads_done();

@@ -102,11 +102,24 @@ struct QueryRows {
     }
 };
 
-// A unit of 32 keys, k0 ..: scores, and what they add.
+// A unit of 32 keys, k0 ..: scores, and what they add.  kAhead: a wavefront that is alone on its SIMD asks for all operands before it uses them
+// (4096 tokens, 4 : 1, whole window: 43.2 -> 41.5 us; dq 51.6 -> 50.0).
+template <bool kAhead>
 __device__ __forceinline__ void take_half(QueryRows &r, const KVHalf &cur, int k0) {
     f32x16 s = zero16();
+    bf16x8 x[8];
+    if constexpr (kAhead) {
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) s = mfma32(r.rd.rows(cur.k, ks), r.q[ks], s);
+        for (int ks = 0; ks < 8; ++ks) x[ks] = r.rd.rows(cur.k, ks);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) s = mfma32(kAhead ? x[ks] : r.rd.rows(cur.k, ks), r.q[ks], s);
+    if constexpr (kAhead) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = r.rd.columns(cur.v, i >> 2, i & 3);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     if (!(k0 + 31 <= r.lo && (k0 + 32 <= r.win.n_sink || r.hi - k0 < r.win.window))) {
         int at = k0 + 4 * r.hf;
         asm volatile("" : "+v"(at));
@@ -129,7 +142,7 @@ __device__ __forceinline__ void take_half(QueryRows &r, const KVHalf &cur, int k
     for (int j = 0; j < 2; ++j) {
         const bf16x8 p = pack8(s, j);
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct) r.o[ct] = mfma32(r.rd.columns(cur.v, j, ct), p, r.o[ct]);
+        for (int ct = 0; ct < 4; ++ct) r.o[ct] = mfma32(kAhead ? x[4 * j + ct] : r.rd.columns(cur.v, j, ct), p, r.o[ct]);
     }
 }
 
@@ -325,7 +338,7 @@ __global__ __launch_bounds__(256, 3) void window_prefill_many_kernel(Dims dm, Wi
         __builtin_amdgcn_sched_barrier(0);
         stage(next, x + 2);
         const int k0 = kt.key0(x);
-        if (k0 <= r.hi && (k0 < win.n_sink || r.lo - (k0 + 31) < win.window)) take_half(r, cur, k0);   // (some of the rows see some of the keys)
+        if (k0 <= r.hi && (k0 < win.n_sink || r.lo - (k0 + 31) < win.window)) take_half<false>(r, cur, k0);   // (some of the rows see some of the keys)
     };
     for (int x = 0; x < kt.count; x += 3) {
         step(slot0, slot2, x);
@@ -364,7 +377,7 @@ __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, Win
     const KeyTiles<32> kt(win, t0, t1);
     r.load(q, b, L);
     walk_halves(slot0[wave], slot1[wave], k, v, b, h, kt, L, wave, lane,
-                [&](const KVHalf &cur, int k0) __attribute__((always_inline)) { take_half(r, cur, k0); });
+                [&](const KVHalf &cur, int k0) __attribute__((always_inline)) { take_half<true>(r, cur, k0); });
     reads_done();
     r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
     if (r.hf == 0) {
