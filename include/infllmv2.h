@@ -417,6 +417,8 @@ int32_t infllmv2_verify_step(const infllmv2_params *prm, const infllmv2_tensor *
  *                           infllmv2_sparse_attn_decode / _verify with k, v = the values of kq, vq: the same arguments, block lists, tree
  *                           masks, results and workspaces (INFLLMV2_OP_ATTN_DECODE, INFLLMV2_OP_ATTN_VERIFY).  stride_t and scale_stride_t
  *                           at most 2^26 bytes, else INFLLMV2_ERR_UNSUPPORTED.
+ * A query that sees a key whose score is NaN or +inf (in 4 bits: a key with a group that stands for NaN) has out and lse NaN, as in the decode
+ * and verification calls on bf16 caches; out 0 with lse -inf says that it sees no key.
  * The selection reads compressed keys, which stay bf16: infllmv2_select_blocks and _verify serve such a cache as they are.
  * max_seqlen of these calls and of the next is at most 2^30, else INFLLMV2_ERR_UNSUPPORTED.
  */

@@ -1489,10 +1489,10 @@ __global__ __launch_bounds__(64) void decode_merge_kernel(Dims dm, const float *
     }
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     bf16x2 o;                                            // (quotients: a reciprocal for both would round once more, and saves under 0.1 us a step)
-    o[0] = (__bf16)(den > 0.f ? num.x / den : 0.f);
-    o[1] = (__bf16)(den > 0.f ? num.y / den : 0.f);
+    o[0] = (__bf16)(den == 0.f ? 0.f : num.x / den);     // (0: no key is seen; a NaN among the scores stays one)
+    o[1] = (__bf16)(den == 0.f ? 0.f : num.y / den);
     *reinterpret_cast<bf16x2 *>(out.ptr + b * out.sb + qi * out.st + (int64_t)hq * out.sh + 2 * lane) = o;
-    if (lane == 0) lse[row] = den > 0.f ? (M + fast_log2(den)) * kLn2 : -INFINITY;
+    if (lane == 0) lse[row] = den == 0.f ? -INFINITY : (M + fast_log2(den)) * kLn2;
 }
 
 // ---- host side -------------------------------------------------------------------------------------

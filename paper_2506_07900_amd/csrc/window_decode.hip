@@ -316,9 +316,9 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void st
         if (n_split == 1) {
             bf16x8 r;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] = (__bf16)(den > 0.f ? y[e] / den : 0.f);
+            for (int e = 0; e < 8; ++e) r[e] = (__bf16)(den == 0.f ? 0.f : y[e] / den);   // (0: no key is seen; a NaN among the scores stays one)
             *reinterpret_cast<uint4 *>(out.ptr + b * out.sb + qi * out.st + (int64_t)hq * out.sh + c8) = __builtin_bit_cast(uint4, r);
-            if (c8 == 0) lse[(int64_t)bv * dm.Hq + hq] = den > 0.f ? lse_of(bh, den) : -INFINITY;
+            if (c8 == 0) lse[(int64_t)bv * dm.Hq + hq] = den == 0.f ? -INFINITY : lse_of(bh, den);
         } else {
             const int64_t at = ((int64_t)bv * dm.Hq + hq) * n_split + split;
             float4 *op = reinterpret_cast<float4 *>(o_part + at * kHeadDim + c8);

@@ -1,0 +1,113 @@
+"""The 4-bit cache's and the windowed attention's calls on values that are not finite and on the largest that are.
+
+A key that a query sees and whose score is a NaN (or an infinity above) leaves it no answer: its row is NaN, as the softmax's definition
+gives it, and not the 0 and -inf of a row that sees nothing.  Tolerances of finite rows are those of test_gpu_quant_window.
+"""
+import math
+
+import pytest
+import torch
+
+import test_gpu_quant_window as base
+from paper_2506_07900_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+D = base.D
+NAN, INF = math.nan, math.inf
+
+
+def spoil_key(kq, k, b, h, t, value):
+    """a key of one head, in whichever cache"""
+    if kq is None:
+        k[b, h, t, 7] = value
+    else:
+        kq.scales[b, h, t, 2], kq.codes[b, h, t] = 255, 0
+
+
+# a row in one workgroup, of four and of eight wavefronts; rows split over several; groups below 16
+@pytest.mark.parametrize("G,H,lengths,n_sink,window,at", [
+    (16, 2, [40, 33], 0, 64, 5), (4, 2, [2000], 4, 256, 2), (8, 2, [2000], 4, 256, 1999), (16, 2, [9000], 64, 4096, 6000), (1, 2, [300] * 40, 0, 200, 250),
+    (16, 2, [1000] * 40, 3, 900, 777)])
+@pytest.mark.parametrize("quant", [False, True])
+def test_window_decode_of_a_visible_nan_key(G, H, lengths, n_sink, window, at, quant):
+    gen = torch.Generator(device="cuda").manual_seed(at)
+    B, T = len(lengths), max(lengths)
+    prm = binding.Params(G * H, H)
+    k, v = base.random_cache(gen, B, H, T, lengths)
+    kq, vq = base.quant_of(prm, k, v, lengths) if quant else (None, None)
+    q, sl = base.normal(gen, B, 1, G * H, D), base.lengths_tensor(lengths)
+    spoil_key(kq, k, B - 1, 0, at, NAN)
+    out, lse = (binding.window_attn_decode_quant(prm, n_sink, window, q, kq, vq, sl, T) if quant else
+                binding.window_attn_decode(prm, n_sink, window, q, k, v, sl, T))
+    k64, v64 = (base.values_of(kq), base.values_of(vq)) if quant else (k.double(), v.double())
+    for b, n in enumerate(lengths):
+        for h in range(H):
+            rows = slice(h * G, (h + 1) * G)
+            if b == B - 1 and h == 0:
+                assert out[b, 0, rows].isnan().all() and lse[b, rows].isnan().all()
+                continue
+            seen = base.window_seen(torch.tensor([n - 1], device="cuda"), n, n_sink, window).expand(G, n)
+            base.check(out[b, 0, rows], lse[b, rows], base.attend(q[b, 0, rows].double(), k64[b, h, :n], v64[b, h, :n], seen, prm.softmax_scale))
+
+
+def test_window_decode_of_a_visible_infinite_key():
+    # scores of +inf have no softmax, scores of -inf take their key out
+    G, H, n = 16, 2, 700
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    prm = binding.Params(G * H, H)
+    k, v = base.random_cache(gen, 1, H, n, [n])
+    q = base.normal(gen, 1, 1, G * H, D)
+    k[0, 1, 650, 7] = INF
+    out, lse = binding.window_attn_decode(prm, 4, 300, q, k, v, base.lengths_tensor([n]), n)
+    up = q[0, 0, G:, 7] > 0
+    assert up.any() and not up.all()
+    assert out[0, 0, G:][up].isnan().all() and lse[0, G:][up].isnan().all()
+    seen = base.window_seen(torch.tensor([n - 1], device="cuda"), n, 4, 300).expand(G, n).clone()
+    base.check(out[0, 0, :G], lse[0, :G], base.attend(q[0, 0, :G].double(), k[0, 0].double(), v[0, 0].double(), seen, prm.softmax_scale))
+    seen[:, 650], k[0, 1, 650, 7] = False, 0.0
+    want = base.attend(q[0, 0, G:].double(), k[0, 1].double(), v[0, 1].double(), seen, prm.softmax_scale)
+    base.check(out[0, 0, G:][~up], lse[0, G:][~up], [x[~up] for x in want])
+
+
+@pytest.mark.parametrize("G,H,lengths,topk", [(16, 2, [500, 100], 3), (4, 1, [4000], 16), (16, 2, [700] * 40, 8), (8, 2, [9000], 64)])
+@pytest.mark.parametrize("quant", [False, True])
+def test_sparse_decode_of_a_visible_nan_key(G, H, lengths, topk, quant):
+    """On either cache: the two calls promise the same results."""
+    gen = torch.Generator(device="cuda").manual_seed(topk)
+    B, T = len(lengths), max(lengths)
+    prm = binding.Params(G * H, H, topk=topk)
+    k, v = base.random_cache(gen, B, H, T, lengths)
+    kq, vq = base.quant_of(prm, k, v, lengths) if quant else (None, None)
+    q, sl = base.normal(gen, B, 1, G * H, D), base.lengths_tensor(lengths)
+    idx = base.block_lists(gen, lengths, H, 1, topk, False)
+    call = lambda: (binding.sparse_attn_decode_quant(prm, q, kq, vq, sl, T, idx) if quant else binding.sparse_attn_decode(prm, q, k, v, sl, T, idx))
+    clean, clean_lse = [x.clone() for x in call()]
+    at = 64 * int(idx[0, H - 1, 0, 0]) + 9
+    spoil_key(kq, k, 0, H - 1, at, NAN)
+    out, lse = call()
+    rows = slice((H - 1) * G, H * G)
+    assert out[0, 0, rows].isnan().all() and lse[0, rows].isnan().all()
+    clean[0, 0, rows], clean_lse[0, rows] = NAN, NAN
+    assert torch.equal(out.nan_to_num(7.0), clean.nan_to_num(7.0)) and torch.equal(lse.nan_to_num(7.0), clean_lse.nan_to_num(7.0))   # no other row has changed
+
+
+def test_sparse_verify_of_a_nan_key_that_some_drafted_tokens_see():
+    # a drafted token whose key is NaN: the tokens that descend from it are NaN, the others as if it were not there
+    G, H, n, topk, length = 8, 2, 6, 4, 300
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    prm = binding.Params(G * H, H, topk=topk)
+    k, v = base.random_cache(gen, 1, H, length, [length])
+    kq, vq = base.quant_of(prm, k, v, [length])
+    q, sl = base.normal(gen, 1, n, G * H, D), base.lengths_tensor([length])
+    idx = torch.tensor([0, 3, 4, -1], dtype=torch.int32, device="cuda").expand(1, H, n, topk).contiguous()
+    words = [0b000001, 0b000011, 0b000101, 0b001011, 0b010101, 0b000000]
+    mask = torch.tensor([words], dtype=torch.int64, device="cuda")
+    clean, clean_lse = binding.sparse_attn_verify_quant(prm, q, kq, vq, sl, length, idx, tree_mask=mask)
+    kq.scales[:, :, length - n + 1, 0], kq.codes[:, :, length - n + 1] = 255, 0
+    out, lse = binding.sparse_attn_verify_quant(prm, q, kq, vq, sl, length, idx, tree_mask=mask)
+    for i, w in enumerate(words):
+        if w >> 1 & 1:
+            assert out[0, i].isnan().all() and lse[0, i].isnan().all()
+        else:
+            assert torch.equal(out[0, i], clean[0, i]) and torch.equal(lse[0, i], clean_lse[0, i])
