@@ -1480,17 +1480,19 @@ __global__ __launch_bounds__(64) void decode_merge_kernel(Dims dm, const float *
     den = row_reduce(den, sum);
     if constexpr (kTop >= 32) den = xgroup_reduce(den, sum);
     den = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(den)));
+    // (both sides of the quotient times 2^-7: 64 sums that are numbers stay one)
+    const float w_num = w * 0x1p-7f;
     float2 num = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < kTop; ++c) {
-        const float wc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), c));
+        const float wc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w_num), c));
         num.x += wc * __uint_as_float(ov[c][0]);
         num.y += wc * __uint_as_float(ov[c][1]);
     }
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     bf16x2 o;                                            // (quotients: a reciprocal for both would round once more, and saves under 0.1 us a step)
-    o[0] = (__bf16)(den == 0.f ? 0.f : num.x / den);     // (0: no key is seen; a NaN among the scores stays one)
-    o[1] = (__bf16)(den == 0.f ? 0.f : num.y / den);
+    o[0] = (__bf16)(den == 0.f ? 0.f : num.x / (den * 0x1p-7f));     // (0: no key is seen; a NaN among the scores stays one)
+    o[1] = (__bf16)(den == 0.f ? 0.f : num.y / (den * 0x1p-7f));
     *reinterpret_cast<bf16x2 *>(out.ptr + b * out.sb + qi * out.st + (int64_t)hq * out.sh + 2 * lane) = o;
     if (lane == 0) lse[row] = den == 0.f ? -INFINITY : (M + fast_log2(den)) * kLn2;
 }

@@ -6,6 +6,8 @@
 // 8 KiB of LDS of the wavefront's own (stored as rows, read transposed) into the second (O^T = V^T . P^T).  The order of keys within a product is free,
 // so the probabilities are the second product's operand in the registers they come out in.  At the end their
 // states are joined in LDS; where a row is split over workgroups, decode_merge_kernel joins those.
+#include <type_traits>
+
 #include "quant.h"
 #include "window.h"
 
@@ -132,9 +134,11 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void st
     float2 *__restrict__ ml_part) {
     __shared__ __align__(16) char Vs[kWaves][kUnit * 256];
     __shared__ float2 ml_s[kWaves][16];
+    __shared__ bool again_s[kWaves];
     const int split = blockIdx.x, n_split = gridDim.x, h = blockIdx.y, bv = blockIdx.z;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 15, g = lane >> 4, G = dm.G;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int G = dm.G;
     int b, qi;
     const int L = __builtin_amdgcn_readfirstlane(query_row(dm, seqlens, bv, b, qi));
     b = __builtin_amdgcn_readfirstlane(b);               // (uniform: the compiler divides in vector registers)
@@ -200,9 +204,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void st
     };
     // ---- the walk ------------------------------------------------------------------------------------------------------
     f32x4 o[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
+    float m, l, shift = 0.f;                             // probabilities are 2^(score - m - shift)
     char *vs = Vs[wave];
     auto attend = [&](const UnitRows<kQuant> &x, uint32_t allow) __attribute__((always_inline)) {
         f32x4 s[2];
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void st
 #pragma unroll
             for (int c = 0; c < 8; ++c) o[c] *= alpha;
         }
-        const float base = m == -INFINITY ? 0.f : m;
+        const float base = (m == -INFINITY ? 0.f : m) + shift;
         float ps = 0.f;
         bf16x8 p;
 #pragma unroll
@@ -266,38 +268,54 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void st
         while (x < u_end && (allow = place(x, key0)) == 0u) x += kWaves;
         return x;
     };
-    UnitRows<kQuant> a, c;
-    int ka = 0, kc = 0;
-    uint32_t aa = 0u, ac = 0u;
-    u = advance(u, ka, aa);
-    if (u < u_end) fetch(a, ka);
-    while (u < u_end) {
-        int next = advance(u + kWaves, kc, ac);
-        if (next < u_end) fetch(c, kc);
-        attend(a, aa);
-        u = next;
-        if (u >= u_end) break;
-        next = advance(u + kWaves, ka, aa);
-        if (next < u_end) fetch(a, ka);
-        attend(c, ac);
-        u = next;
-    }
-    l = xgroup_sum(l);
-    // ---- the wavefronts' states into one --------------------------------------------------------------------------
-    if (g == 0) ml_s[wave][n] = float2{m, l};
-    __syncthreads();
-    float M = -INFINITY;
+    // A pass: the walk, the wavefronts' states into one, the result.  -> whether a sum of a row that has one came out as no number
+    const int first = u, head = tid >> 4, c8 = 8 * (tid & 15);       // (a thread joins eight channels of a head)
+    auto pass = [&](auto ahead) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
-    const float base = M == -INFINITY ? 0.f : M;
-    const float w = fast_exp2(m - base);
-    float *mine = reinterpret_cast<float *>(vs);         // [head][channel]: its 8 KiB
+        for (int i = 0; i < 8; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m = -INFINITY;
+        l = 0.f;
+        UnitRows<kQuant> a, c;
+        int ka = 0, kc = 0;
+        uint32_t aa = 0u, ac = 0u;
+        u = first;
+        if constexpr (!ahead) {
+            asm volatile("" : "+s"(u), "+v"(lane), "+v"(n), "+v"(g));   // (nothing of this pass is worked out before the other)
+            u = advance(u, ka, aa);
+            for (; u < u_end; u = advance(u + kWaves, ka, aa)) {
+                fetch(a, ka);
+                attend(a, aa);
+            }
+        } else if ((u = advance(u, ka, aa)) < u_end) {
+            fetch(a, ka);
+            for (;;) {
+                int next = advance(u + kWaves, kc, ac);
+                if (next < u_end) fetch(c, kc);
+                attend(a, aa);
+                u = next;
+                if (u >= u_end) break;
+                next = advance(u + kWaves, ka, aa);
+                if (next < u_end) fetch(a, ka);
+                attend(c, ac);
+                u = next;
+                if (u >= u_end) break;
+            }
+        }
+        l = xgroup_sum(l);
+        // ---- the wavefronts' states into one ----------------------------------------------------------------------
+        if (g == 0) ml_s[wave][n] = float2{m, l};
+        __syncthreads();
+        float M = -INFINITY;
 #pragma unroll
-    for (int ch = 0; ch < 8; ++ch)
-        *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (ch ^ (n & 7)) + 4 * g) = o[ch] * w;
-    __syncthreads();
-    const int head = tid >> 4, c8 = 8 * (tid & 15);      // eight channels of a head
-    if (head < G) {                                      // (of eight wavefronts the first four)
+        for (int i = 0; i < kWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
+        const float base = M == -INFINITY ? 0.f : M;
+        const float w = fast_exp2(m - base);
+        float *mine = reinterpret_cast<float *>(vs);     // [head][channel]: its 8 KiB
+#pragma unroll
+        for (int ch = 0; ch < 8; ++ch)
+            *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (ch ^ (n & 7)) + 4 * g) = o[ch] * w;
+        __syncthreads();
+        if (head >= G) return false;                     // (of eight wavefronts the first four have heads)
         float den = 0.f, Mh = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) Mh = fmaxf(Mh, ml_s[i][head].x);
@@ -318,14 +336,32 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void st
 #pragma unroll
             for (int e = 0; e < 8; ++e) r[e] = (__bf16)(den == 0.f ? 0.f : y[e] / den);   // (0: no key is seen; a NaN among the scores stays one)
             *reinterpret_cast<uint4 *>(out.ptr + b * out.sb + qi * out.st + (int64_t)hq * out.sh + c8) = __builtin_bit_cast(uint4, r);
-            if (c8 == 0) lse[(int64_t)bv * dm.Hq + hq] = den == 0.f ? -INFINITY : lse_of(bh, den);
+            if (c8 == 0) lse[(int64_t)bv * dm.Hq + hq] = den == 0.f ? -INFINITY : lse_of(bh + shift, den);
         } else {
             const int64_t at = ((int64_t)bv * dm.Hq + hq) * n_split + split;
             float4 *op = reinterpret_cast<float4 *>(o_part + at * kHeadDim + c8);
             op[0] = float4{y[0], y[1], y[2], y[3]};
             op[1] = float4{y[4], y[5], y[6], y[7]};
-            if (c8 == 0) ml_part[at] = float2{Mh, den};
+            if (c8 == 0) ml_part[at] = float2{Mh + shift, den};
         }
+        float odd = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) odd = __builtin_fmaf(y[e], 0.f, odd);
+        return odd != 0.f && den == den;
+    };
+    // The sums are divided at the end only, so values near the largest, which have a mean, may overflow in them.  Then the workgroup takes its units
+    // again with all probabilities 2^-40 of what they were (2^30 keys at 2^8 weigh 1/4 together), and writes over what it wrote.  The question comes
+    // behind the result's stores, which the workgroup waits for anyway.
+    const bool again = __any(pass(std::true_type()));
+    if (lane == 0) again_s[wave] = again;
+    reads_done();                                        // (LDS is all that the barrier needs: it does not wait for the stores)
+    asm volatile("s_barrier" ::: "memory");
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) any |= again_s[i];
+    if (__builtin_expect(any, 0)) {
+        shift = 40.f;
+        pass(std::false_type());
     }
 }
 

@@ -111,3 +111,79 @@ def test_sparse_verify_of_a_nan_key_that_some_drafted_tokens_see():
             assert out[0, i].isnan().all() and lse[0, i].isnan().all()
         else:
             assert torch.equal(out[0, i], clean[0, i]) and torch.equal(lse[0, i], clean_lse[0, i])
+
+
+# ---- values near the largest: their sums overflow 32 bits before they are divided, their means do not ------------------------
+
+def large(x):
+    return (x.float().clamp(-1, 1) * 3e38).bfloat16()
+
+
+# one workgroup of four wavefronts and of eight, several workgroups, sequences of one token and of none, one wavefront's unit alone
+@pytest.mark.parametrize("G,H,lengths,n_sink,window", [
+    (16, 2, [1, 2, 31, 33, 65, 0], 4, 40), (4, 2, [2000, 100], 4, 256), (16, 2, [9000], 64, 4096), (1, 2, [300, 7] * 20, 0, 200), (16, 2, [1000, 999] * 20, 3, 900),
+    (8, 1, [70000], 0, 100000)])
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("sign", [False, True])
+def test_window_decode_of_large_values(G, H, lengths, n_sink, window, quant, sign):
+    gen = torch.Generator(device="cuda").manual_seed(window)
+    B, T = len(lengths), max(lengths)
+    prm = binding.Params(G * H, H)
+    k, v = base.random_cache(gen, B, H, T, lengths, spoil=False)
+    v = large(v if sign else v.abs())                              # (of one sign: the mean is large too)
+    kq, vq = base.quant_of(prm, k, v, lengths) if quant else (None, None)
+    q, sl = base.normal(gen, B, 1, G * H, D), base.lengths_tensor(lengths)
+    out, lse = (binding.window_attn_decode_quant(prm, n_sink, window, q, kq, vq, sl, T) if quant else
+                binding.window_attn_decode(prm, n_sink, window, q, k, v, sl, T))
+    k64, v64 = (base.values_of(kq), base.values_of(vq)) if quant else (k.double(), v.double())
+    for b, n in enumerate(lengths):
+        for h in range(H):
+            rows = slice(h * G, (h + 1) * G)
+            if n == 0:
+                assert not out[b, 0, rows].any() and (lse[b, rows] == -INF).all()
+                continue
+            seen = base.window_seen(torch.tensor([n - 1], device="cuda"), n, n_sink, window).expand(G, n)
+            base.check(out[b, 0, rows], lse[b, rows], base.attend(q[b, 0, rows].double(), k64[b, h, :n], v64[b, h, :n], seen, prm.softmax_scale))
+
+
+@pytest.mark.parametrize("G,H,lengths,topk", [(16, 2, [500, 100, 1], 3), (4, 1, [4000], 16), (16, 2, [700] * 40, 8), (8, 2, [9000], 64)])
+def test_sparse_decode_of_large_values(G, H, lengths, topk):
+    gen = torch.Generator(device="cuda").manual_seed(topk)
+    B, T = len(lengths), max(lengths)
+    prm = binding.Params(G * H, H, topk=topk)
+    k, v = base.random_cache(gen, B, H, T, lengths, spoil=False)
+    kq, vq = base.quant_of(prm, k, large(v.abs()), lengths)
+    q, sl = base.normal(gen, B, 1, G * H, D), base.lengths_tensor(lengths)
+    idx = base.block_lists(gen, lengths, H, 1, topk, False)
+    out, lse = binding.sparse_attn_decode_quant(prm, q, kq, vq, sl, T, idx)
+    k64, v64 = base.values_of(kq), base.values_of(vq)
+    for b, n in enumerate(lengths):
+        for h in range(H):
+            rows = slice(h * G, (h + 1) * G)
+            at = torch.tensor([t for j in idx[b, h, 0].tolist() if j >= 0 for t in range(64 * j, min(n, 64 * j + 64))], device="cuda")
+            seen = torch.ones((G, len(at)), dtype=torch.bool, device="cuda")
+            base.check(out[b, 0, rows], lse[b, rows], base.attend(q[b, 0, rows].double(), k64[b, h, at], v64[b, h, at], seen, prm.softmax_scale))
+
+
+@pytest.mark.parametrize("quant", [False, True])
+def test_window_decode_of_an_infinite_value(quant):
+    # an infinity (in 4 bits: a group that stands for NaN) among the visible values reaches its channels and no others
+    G, H, n = 16, 2, 5000
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    prm = binding.Params(G * H, H)
+    k, v = base.random_cache(gen, 1, H, n, [n])
+    v[0, 1, 4900, 37] = INF
+    kq, vq = base.quant_of(prm, k, v, [n]) if quant else (None, None)
+    q, sl = base.normal(gen, 1, 1, G * H, D), base.lengths_tensor([n])
+    out, lse = (binding.window_attn_decode_quant(prm, 4, 3000, q, kq, vq, sl, n) if quant else
+                binding.window_attn_decode(prm, 4, 3000, q, k, v, sl, n))
+    hit = torch.zeros(D, dtype=torch.bool, device="cuda")
+    hit[32:64 if quant else 38] = True
+    hit[32:37] = quant
+    assert (out[0, 0, G:, hit].isnan().all() if quant else (out[0, 0, G:, 37] == INF).all())
+    k64, v64 = (base.values_of(kq), base.values_of(vq)) if quant else (k.double(), v.double())
+    seen = base.window_seen(torch.tensor([n - 1], device="cuda"), n, 4, 3000).expand(G, n)
+    for h, keep in ((0, hit | True), (1, ~hit)):
+        rows = slice(h * G, (h + 1) * G)
+        o, z, mag, size = base.attend(q[0, 0, rows].double(), k64[0, h], torch.nan_to_num(v64[0, h], 0.0, 0.0, 0.0), seen, prm.softmax_scale)
+        base.check(out[0, 0, rows][:, keep], lse[0, rows], (o[:, keep], z, mag[:, keep], size))
