@@ -455,6 +455,8 @@ int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infl
  * infllmv2_window_attn_prefill  one query per cached token: q, out [batch, max_seqlen, Hq, d], lse fp32 [batch, max_seqlen, Hq]; rows
  *                               t >= seqlens[b] ignored / not written.  A value of V that is not finite reaches
  *                               the outputs of the queries that see it and of no others (the backward does not promise this).
+ *                               Rows of such tiles, and rows whose sums overflow though their mean does not, are taken a second
+ *                               time: a call in which all rows are takes 3 to 8 times as long.
  * infllmv2_window_attn_bwd      its gradients for an upstream gradient dout, as infllmv2_sparse_attn_bwd's, with the
  *                               sums for dk, dv in a fixed order: results repeat bit for bit.
  * infllmv2_window_attn_decode   the query at position seqlens[b]-1: q, out [batch, 1, Hq, d], lse fp32 [batch, Hq]; a sequence with

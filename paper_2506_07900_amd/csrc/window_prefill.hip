@@ -146,30 +146,86 @@ __device__ __forceinline__ void take_half(QueryRows &r, const KVHalf &cur, int k
     }
 }
 
-// A product multiplies a key that a row does not see by a probability of 0, and 0 times an infinity or a NaN reaches the row's sum.  A
-// row that does not come out finite is therefore taken again by the whole wavefront, key by key, over the keys it sees; its maximum m and
-// sum l stand, as hidden scores are replaced and not multiplied.  Lane = two channels.
-__device__ __forceinline__ void take_row_again(const Dims &dm, WindowArgs win, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &out,
-                                               int b, int h, int i, int hq, float m, float l, int lane) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    auto pair = [&](const Tensor &t, int64_t row) { return reinterpret_cast<const bf16x2 *>(t.ptr + row)[lane]; };
-    const bf16x2 x = pair(q, b * q.sb + (int64_t)i * q.st + (int64_t)hq * q.sh);
-    const int lo = max(0, i - win.window + 1), first = min(win.n_sink, lo);
-    const float inv = 1.f / l;
-    float y0 = 0.f, y1 = 0.f;
-    for (int n = 0; n < first + i - lo + 1; ++n) {
-        const int64_t t = n < first ? n : lo + n - first;
-        const bf16x2 kt = pair(k, b * k.sb + h * k.sh + t * k.st), vt = pair(v, b * v.sb + h * v.sh + t * v.st);
-        const auto sum = [](float a, float d) { return a + d; };
-        const float s = xgroup_reduce(row_reduce(__builtin_fmaf((float)x[0], (float)kt[0], (float)x[1] * (float)kt[1]), sum), sum);
-        const float p = (float)(__bf16)fast_exp2(__builtin_fmaf(s, dm.scale_log2, -m)) * inv;   // (at most 1: no sum of large values overflows)
-        y0 = __builtin_fmaf(p, (float)vt[0], y0);
-        y1 = __builtin_fmaf(p, (float)vt[1], y1);
+// A product multiplies a key that a row does not see by a probability of 0, and 0 times an infinity or a NaN reaches the row's sum; and sums that are divided
+// at the end only overflow where values are near the largest.  Rows that do not come out finite though the sum of their probabilities did are
+// therefore taken again, all of the wavefront's at once: their maxima m and sums l stand (hidden scores are replaced, not multiplied), so probabilities are
+// 2^(score - m - down) with a sum of 1/4 to 1/2.  In a unit of keys that not all rows see whole, values that are not finite are left out
+// of the product and added to the rows that see them.  V goes through 8 KiB of LDS of the wavefront's own; nothing is asked for ahead.  With an
+// infinity that all rows see: 777 tokens, 4 : 1, window 256 10.6 -> 82 us, 4096 tokens, 8 : 2, whole window 94 -> 365, 32K, 32 : 2, window 4096 2.09 -> 6.04 ms
+// (key by key it was 430 us, 29 ms and 423 ms).
+__device__ __forceinline__ int down_of(float l) { return __builtin_amdgcn_frexp_expf(l) + 1; }
+__device__ __forceinline__ void take_again(QueryRows &r, const Tensor &k, const Tensor &v, int b, int h, int L, float m, float down, char *lds) {
+    const KeyTiles<32> kt(r.win, r.lo, min(L, r.hi + 1));
+    int lane = r.lane;
+    asm volatile("" : "+v"(lane));                       // (nothing of this is worked out before it is needed)
+    const int hf = lane >> 5;
+    const TileReader rd(lane);
+    const VisibleKeys visible(r.win, r.i);
+    const int64_t k_head = b * k.sb + h * k.sh, v_head = b * v.sb + h * v.sh;
+    const uint32_t v_at = (lane >> 2) * (2 * (uint32_t)v.st) + 16 * copy_piece(lane);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) r.o[ct] = zero16();
+#pragma unroll 1
+    for (int x = 0; x < kt.count; ++x) {
+        const int k0 = kt.key0(x);
+        const char *vb = reinterpret_cast<const char *>(v.ptr + v_head + (int64_t)k0 * v.st);
+        const __bf16 *kr = k.ptr + k_head + (int64_t)min(k0 + (lane & 31), L - 1) * k.st + 8 * hf;
+        reads_done();                                    // (the unit before)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int quarter = 0; quarter < 4; ++quarter)
+                copy_rows(lds + quarter * 2048 + j * 1024, vb + 64 * quarter, k0 + 16 * j + (lane >> 2) < L ? v_at : kNoRow, 32 * j * (uint32_t)v.st);
+        f32x16 s = zero16();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+            s = mfma32(load8(kr + 16 * ks), r.q[ks], s);
+            if (ks == 3) __builtin_amdgcn_sched_barrier(0);          // (registers)
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            s[e] = visible(k0 + 4 * hf + 8 * (e >> 2) + (e & 3)) ? fast_exp2(__builtin_fmaf(s[e], r.scale, -m) - down) : 0.f;
+        const bool whole = k0 + 31 <= r.lo && (k0 + 32 <= r.win.n_sink || r.hi - k0 < r.win.window);
+        bool odd = false;
+        copies_landed(false);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const bf16x8 p = pack8(s, j);
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) {
+                u32x4_t y = __builtin_bit_cast(u32x4_t, rd.columns(lds, j, ct));
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {        // the halves of a word whose exponents are all ones
+                        const bool low = (y[i] & 0x7f80u) == 0x7f80u, high = (y[i] & 0x7f800000u) == 0x7f800000u;
+                        y[i] = (low ? 0u : y[i] & 0xffffu) | (high ? 0u : y[i] & 0xffff0000u);
+                        odd |= low | high;
+                    }
+                }
+                r.o[ct] = mfma32(__builtin_bit_cast(bf16x8, y), p, r.o[ct]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (!__any(odd)) continue;
+#pragma unroll 1
+        for (int t = 0; t < 32; ++t) {
+            const bool sees = visible(k0 + t);
+            const char *row = lds + 64 * t + 8 * hf;
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const uint2 y = *reinterpret_cast<const uint2 *>(row + ct * 2048 + ((e4 ^ ((t >> 2) & 3)) << 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t w = e < 2 ? y.x : y.y;
+                        const float z = __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+                        r.o[ct][4 * e4 + e] += sees && !(__builtin_fabsf(z) < INFINITY) ? z : 0.f;
+                        __builtin_amdgcn_sched_barrier(0);               // (registers)
+                    }
+                }
+        }
     }
-    bf16x2 y;
-    y[0] = (__bf16)y0;
-    y[1] = (__bf16)y1;
-    reinterpret_cast<bf16x2 *>(out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh)[lane] = y;
 }
 
 // The end of a wavefront's 32 rows, with 8 KiB of LDS.
@@ -182,8 +238,8 @@ __device__ __forceinline__ void finish_rows(const Dims &dm, WindowArgs win, int 
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
         for (int e = 0; e < 16; ++e) check = __builtin_fmaf(r.o[ct][e], 0.f, check);
-    const uint64_t bad_lanes = __ballot(live && check != 0.f), live_lanes = __ballot(live);
-    uint32_t bad = (uint32_t)bad_lanes | (uint32_t)(bad_lanes >> 32);
+    const uint64_t bad_lanes = __ballot(live && check != 0.f && r.l == r.l), live_lanes = __ballot(live);
+    const uint32_t bad = (uint32_t)bad_lanes | (uint32_t)(bad_lanes >> 32);
     const uint32_t alive = (uint32_t)live_lanes;
     if (alive != ~0u) {                                  // (rows behind the sequence: zeros, where they are written at all)
 #pragma unroll
@@ -191,17 +247,21 @@ __device__ __forceinline__ void finish_rows(const Dims &dm, WindowArgs win, int 
 #pragma unroll
             for (int e = 0; e < 16; ++e) r.o[ct][e] = live ? r.o[ct][e] : 0.f;
     }
-    store_rows(lds, r.o, live ? 1.f / r.l : 0.f, lane, [&](int row) __attribute__((always_inline)) -> __bf16 * {
+    auto to = [&](int row) __attribute__((always_inline)) {
         const int i = t0 + ((32 * wave + row) >> lg), hq = h * dm.G + ((32 * wave + row) & (dm.G - 1));
-        const bool store = i < dm.max_seqlen && ((alive >> row) & 1u || dm.fill) && !((bad >> row) & 1u);
-        return store ? out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh : nullptr;
+        return out.ptr + b * out.sb + (int64_t)i * out.st + (int64_t)hq * out.sh;
+    };
+    store_rows(lds, r.o, live ? 1.f / r.l : 0.f, lane, [&](int row) __attribute__((always_inline)) -> __bf16 * {
+        const bool store = t0 + ((32 * wave + row) >> lg) < dm.max_seqlen && ((alive >> row) & 1u || dm.fill) && !((bad >> row) & 1u);
+        return store ? to(row) : nullptr;
     });
     if (r.hf == 0 && r.i < dm.max_seqlen && (live || dm.fill)) lse[((int64_t)b * dm.max_seqlen + r.i) * dm.Hq + r.hq] = live ? lse_of(r.m, r.l) : 0.f;
-    for (; bad; bad &= bad - 1) {
-        const int n = __builtin_ctz(bad);
-        take_row_again(dm, win, q, k, v, out, b, h, __builtin_amdgcn_readlane(r.i, n), __builtin_amdgcn_readlane(r.hq, n),
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.m), n)),
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r.l), n)), lane);
+    if (__builtin_expect(bad != 0u, 0)) {
+        const int down = down_of(r.l);
+        take_again(r, k, v, b, h, L, r.m, (float)down, lds);
+        asm volatile("" : "+v"(lane));                   // (no addresses held meanwhile)
+        store_rows(lds, r.o, 1.f / __builtin_ldexpf(r.l, -down), lane,
+                   [&](int row) __attribute__((always_inline)) -> __bf16 * { return (bad >> row) & 1u ? to(row) : nullptr; });
     }
 }
 // A wavefront's rows that lie behind the sequence.
@@ -412,7 +472,7 @@ __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, Win
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) check = __builtin_fmaf(y[e], 0.f, check);
-    uint64_t bad = __ballot(i < L && check != 0.f);
+    const uint64_t bad = __ballot(i < L && check != 0.f && den == den);
     const bool whole = ((bad >> (lane & 56)) & 255u) == 0u;                    // this row's eight lanes
     if (store) {
         const float inv = 1.f / den;
@@ -425,12 +485,21 @@ __global__ __launch_bounds__(256, 1) void window_prefill_few_kernel(Dims dm, Win
         }
         if (ch == 0) *lse_at = i < L ? lse_of(M, den) : 0.f;
     }
-    while (bad) {
-        const int n = __builtin_ctzll(bad);
-        bad &= ~(255ull << (n & 56));
-        take_row_again(dm, win, q, k, v, out, b, h, __builtin_amdgcn_readlane(i, n), __builtin_amdgcn_readlane(hq, n),
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(M), n)),
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(den), n)), lane);
+    if (__builtin_expect(bad != 0ull, 0)) {              // of the 32 rows the eight of this wavefront's lanes
+        uint32_t rows = 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rows |= (uint32_t)((bad >> (8 * j)) & 255u ? 1u : 0u) << (8 * wave + j);
+        const int n = lane & 31;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][n]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sum += fast_exp2(ml[0][w][n] - top) * ml[1][w][n];
+        const int down = down_of(sum);
+        take_again(r, k, v, b, h, L, top, (float)down, slot1[wave].k);
+        store_rows(slot1[wave].k, r.o, 1.f / __builtin_ldexpf(sum, -down), lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
+            return (rows >> at) & 1u ? out.ptr + b * out.sb + (int64_t)(t0 + (at >> lg)) * out.st + (int64_t)(h * dm.G + (at & (dm.G - 1))) * out.sh : nullptr;
+        });
     }
 }
 
