@@ -466,6 +466,8 @@ int32_t infllmv2_sparse_attn_verify_quant(const infllmv2_params *prm, const infl
  * stride_h at most 2^29, else INFLLMV2_ERR_UNSUPPORTED.
  * Workspaces: infllmv2_window_workspace_bytes(INFLLMV2_OP_WINDOW_*, ...) bytes, 256-byte aligned (0: none needed, or the arguments are
  * invalid); INFLLMV2_OP_WINDOW_DECODE for both decode calls.
+ * The backward's is a bound that suffices for every call with no more sequences and tokens, whatever its window and first tokens: 8 bytes per row and
+ * head, and 128 KiB x min(32 t, 4096 + 2 t) for the t tiles of 128 keys of all sequences and key-value heads.
  */
 size_t infllmv2_window_workspace_bytes(int32_t op, const infllmv2_params *prm, int32_t n_sink, int32_t window,
                                        int32_t batch, int32_t max_seqlen);

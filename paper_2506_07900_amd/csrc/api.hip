@@ -651,6 +651,13 @@ size_t infllmv2_window_workspace_bytes(int32_t op, const infllmv2_params *prm, i
     return 0;
 }
 
+size_t infllmv2i_window_bwd_scratch_bytes(const infllmv2_params *prm, int32_t n_sink, int32_t window, int32_t batch, int32_t max_seqlen) {
+    if (check_params(prm) != INFLLMV2_OK || check_window(n_sink, window) != INFLLMV2_OK || check_sizes(batch, max_seqlen) != INFLLMV2_OK ||
+        check_capacity(max_seqlen) != INFLLMV2_OK)
+        return 0;
+    return window_bwd_scratch_bytes(make_dims(prm, batch, max_seqlen), make_window(n_sink, window, max_seqlen));
+}
+
 int32_t infllmv2i_window_attn_prefill(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
                                       const infllmv2_tensor *k, const infllmv2_tensor *v, const int32_t *seqlens, int32_t batch,
                                       int32_t max_seqlen, const infllmv2_tensor *out, float *lse, void *workspace,
@@ -694,7 +701,7 @@ int32_t infllmv2i_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, in
     RETURN_IF_ERR(check_spans(prm, k, v, q, dout));
     const Dims dm = make_dims(prm, batch, max_seqlen, 1, fill);
     const WindowArgs w = make_window(n_sink, window, max_seqlen);
-    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_bwd_ws_bytes(dm, w)));
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_bwd_scratch_bytes(dm, w)));
     return hip_status(launch_window_bwd(dm, w, make_tensor(q), make_tensor(k), make_tensor(v), make_tensor(out), make_tensor(dout), lse,
                                         seqlens, make_tensor(dq), make_tensor(dk), make_tensor(dv), workspace,
                                         reinterpret_cast<hipStream_t>(stream)));
@@ -705,6 +712,8 @@ int32_t infllmv2_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, int
                                  const infllmv2_tensor *dout, const float *lse, const int32_t *seqlens, int32_t batch,
                                  int32_t max_seqlen, const infllmv2_tensor *dq, const infllmv2_tensor *dk,
                                  const infllmv2_tensor *dv, void *workspace, size_t workspace_bytes, void *stream) {
+    // (its workspace is infllmv2_window_workspace_bytes; where that is 0 the call below has nothing to do or refuses the arguments)
+    if (workspace_bytes < infllmv2_window_workspace_bytes(INFLLMV2_OP_WINDOW_BWD, prm, n_sink, window, batch, max_seqlen)) workspace = nullptr;
     return infllmv2i_window_attn_bwd(prm, n_sink, window, q, k, v, out, dout, lse, seqlens, batch, max_seqlen, dq, dk, dv, workspace,
                                      workspace_bytes, stream, 0);
 }

@@ -38,6 +38,9 @@ int32_t infllmv2i_window_attn_prefill(const infllmv2_params *prm, int32_t n_sink
                                       const infllmv2_tensor *k, const infllmv2_tensor *v, const int32_t *seqlens,
                                       int32_t batch, int32_t max_seqlen, const infllmv2_tensor *out, float *lse,
                                       void *workspace, size_t workspace_bytes, void *stream, int32_t fill);
+/* The backward's scratch for one call, which its plan fills; infllmv2_window_workspace_bytes is a bound for smaller calls too and up to eight times as
+ * much.  infllmv2i_window_attn_bwd takes a workspace of this size. */
+size_t infllmv2i_window_bwd_scratch_bytes(const infllmv2_params *prm, int32_t n_sink, int32_t window, int32_t batch, int32_t max_seqlen);
 int32_t infllmv2i_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, int32_t window, const infllmv2_tensor *q,
                                   const infllmv2_tensor *k, const infllmv2_tensor *v, const infllmv2_tensor *out,
                                   const infllmv2_tensor *dout, const float *lse, const int32_t *seqlens, int32_t batch,

@@ -53,6 +53,7 @@ struct Library {
     INFLLMV2_FNI(dequantize_kv);
     INFLLMV2_FNI(window_attn_prefill);
     INFLLMV2_FNI(window_attn_bwd);
+    INFLLMV2_FNI(window_bwd_scratch_bytes);
 #undef INFLLMV2_FN
 #undef INFLLMV2_FNI
 } lib;
@@ -646,7 +647,10 @@ PyObject *window_attn_bwd(Args a) {
     if (dq.make()) dq.own = fill ? at::empty_like(q) : at::zeros_like(q);
     if (dk.make()) dk.own = fill ? at::empty_like(k) : at::zeros_like(k);
     if (dv.make()) dv.own = fill ? at::empty_like(v) : at::zeros_like(v);
-    const Workspace ws = scratch(a[14], a[14] == Py_None ? lib.window_workspace_bytes(INFLLMV2_OP_WINDOW_BWD, prm, sink, window, B, T) : 0, q);
+    // (made here: what this call uses; the caller's: as large as the header asks)
+    const Workspace ws = scratch(a[14], a[14] == Py_None ? lib.window_bwd_scratch_bytes(prm, sink, window, B, T) : 0, q);
+    expect(a[14] == Py_None || ws.bytes >= lib.window_workspace_bytes(INFLLMV2_OP_WINDOW_BWD, prm, sink, window, B, T), "workspace",
+           " must hold infllmv2_window_workspace_bytes");
     const infllmv2_tensor qd = rows(q), kd = cache(k), vd = cache(v), dqd = rows(dq.make() ? dq.own : query(dq.given, "dq", B, T, prm)),
                           dkd = cache(dk.make() ? dk.own : kv(dk.given, "dk", B, T, prm)),
                           dvd = cache(dv.make() ? dv.own : kv(dv.given, "dv", B, T, prm));
@@ -718,6 +722,7 @@ PyObject *bind(Args a) {
     symbol(handle, "infllmv2i_dequantize_kv", l.dequantize_kv);
     symbol(handle, "infllmv2i_window_attn_prefill", l.window_attn_prefill);
     symbol(handle, "infllmv2i_window_attn_bwd", l.window_attn_bwd);
+    symbol(handle, "infllmv2i_window_bwd_scratch_bytes", l.window_bwd_scratch_bytes);
     lib = l;
     Py_RETURN_NONE;
 }

@@ -70,7 +70,8 @@ constexpr int64_t kMaxQuantStride = 1ll << 26;               // bytes; of a row 
 size_t window_prefill_ws_bytes(const Dims &dm, WindowArgs w);
 int launch_window_prefill(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v, const int32_t *seqlens, Tensor out, float *lse,
                           void *ws, hipStream_t stream);
-size_t window_bwd_ws_bytes(const Dims &dm, WindowArgs w);
+size_t window_bwd_ws_bytes(const Dims &dm, WindowArgs w);        // enough for all calls with fewer sequences or tokens, whatever their window
+size_t window_bwd_scratch_bytes(const Dims &dm, WindowArgs w);   // what a call uses
 int launch_window_bwd(const Dims &dm, WindowArgs w, Tensor q, Tensor k, Tensor v, Tensor out, Tensor dout, const float *lse,
                       const int32_t *seqlens, Tensor dq, Tensor dk, Tensor dv, void *ws, hipStream_t stream);
 
