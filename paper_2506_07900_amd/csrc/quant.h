@@ -11,9 +11,6 @@
 
 namespace infllmv2 {
 
-constexpr int kQuantGroup = 32;                          // channels per exponent
-constexpr int kCodeBytes = kHeadDim / 2, kScaleBytes = kHeadDim / kQuantGroup;
-
 struct QuantTensor {                                     // strides in bytes
     uint8_t *codes, *scales;
     int64_t sb, sh, st;

@@ -136,7 +136,6 @@ struct TileCopier {
 struct __align__(16) KVHalf {
     char k[kHalfTile], v[kHalfTile];
 };
-constexpr int kHalfCopies = 16;                          // copies of a half
 __device__ __forceinline__ void copy_half(KVHalf &dst, const Tensor &k, const Tensor &v, int64_t k_head, int64_t v_head, int k0, int L, int lane) {
     const char *kb = reinterpret_cast<const char *>(k.ptr + k_head + (int64_t)k0 * k.st), *vb = reinterpret_cast<const char *>(v.ptr + v_head + (int64_t)k0 * v.st);
     const uint32_t piece = 16 * copy_piece(lane), k_at = (lane >> 2) * (2 * (uint32_t)k.st) + piece, v_at = (lane >> 2) * (2 * (uint32_t)v.st) + piece;
@@ -150,7 +149,7 @@ __device__ __forceinline__ void copy_half(KVHalf &dst, const Tensor &k, const Te
         }
     }
 }
-// All but the newest kHalfCopies copies have landed, or all.
+// All copies have landed, or all but the newest half's sixteen.
 __device__ __forceinline__ void copies_landed(bool but_the_newest) {
     __builtin_amdgcn_sched_barrier(0);
     if (but_the_newest) __builtin_amdgcn_s_waitcnt(0x4f70);              // vmcnt 16

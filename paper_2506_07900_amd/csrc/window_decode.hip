@@ -100,8 +100,9 @@ struct UnitRows<true> {
         return __builtin_bit_cast(bf16x8, dequant8(w, ke[t]));
     }
     // Values into LDS: four quarters of 32 channels, in each 32 rows of 64 bytes, whose four pieces are XORed with row / 4 % 4, its bits
-    // exchanged: a store takes a piece of each of 16 rows, two groups of lanes of a transposing load 32 bytes of each of 8; both touch every
-    // bank once.
+    // exchanged: a store takes a piece of each of 16 rows, two groups of lanes of a transposing load 32 bytes of each of 8; sixteen lanes of either touch every
+    // bank once, eight of a store's half of them twice.  By the counters 0.45 to 0.5 of this kernel's LDS time are bank conflicts all the same, the join's
+    // stores at the end among them (16 heads at a pitch of 512 bytes, exchanged in pieces of 64: 16 lanes on four places of 16 bytes).
     __device__ __forceinline__ static uint32_t swizzle(uint32_t i) { return ((i & 1) << 1) | (i >> 1); }
     __device__ __forceinline__ void values(char *vs, uint32_t allow, int lane) const {
         const uint32_t n = lane & 15, g = lane >> 4;
