@@ -126,7 +126,7 @@ struct UnitRows<true> {
 // grid (splits, Hkv, rows).  kList: a row's units are the halves of its list's entries, `per` entries to a split; otherwise its share
 // of the units of its window.  With one split the result is written as it is, else as a partial (o, maximum, sum).
 // A unit is 4.25 KiB of a 4-bit cache or 16 KiB of a bf16 one; a wavefront asks for its next one before it works on its present one.  Many rows are bound by
-// traffic (64 sequences of up to 32K, window 8192, 4 bits: 27.5 us, 4.8 TB/s), few by round trips: a launch, a list or a length, a unit, about 5 us
+// traffic (64 sequences of up to 32K, window 8192, 4 bits: 26.4 us, 5.0 TB/s), few by round trips: a launch, a list or a length, a unit, about 5 us
 // (one sequence, 16 blocks or 4096 tokens), and the joining launch 2 to 4 us.
 template <bool kQuant, bool kList, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves == 4 && kQuant ? 3 : 2) void stream_attn_kernel(
