@@ -16,7 +16,9 @@
  * *_verify variants of the decode step for the n drafted tokens of speculative decoding (section
  * 4.1), and, as a labelled comparison that is NOT the report's method, the *_shared variants with
  * one block set per query block.  Next to the path: a cache in 4 bits (infllmv2_quantize_kv and the *_quant calls) and attention
- * over a sliding window and the first tokens (infllmv2_window_attn_*).
+ * over a sliding window and the first tokens (infllmv2_window_attn_*), and a cache in pages: rotary positions (infllmv2_rope,
+ * infllmv2_rope_bwd), the append, attention of a chunk of new tokens, accumulated attention weights and eviction
+ * (infllmv2_paged_*).
  *
  * Conventions for every entry point
  *   - Returns 0 (INFLLMV2_OK) or a negative INFLLMV2_ERR_* code; never throws, never
@@ -78,6 +80,17 @@ extern "C" {
 #define INFLLMV2_OP_WINDOW_PREFILL 11
 #define INFLLMV2_OP_WINDOW_BWD 12
 #define INFLLMV2_OP_WINDOW_DECODE 13
+/* Stage selector for infllmv2_paged_workspace_bytes. */
+#define INFLLMV2_OP_PAGED_ATTN 14
+#define INFLLMV2_OP_PAGED_WEIGHTS 15
+#define INFLLMV2_OP_PAGED_EVICT 16
+
+/* How infllmv2_rope_table stretches positions for contexts longer than the trained ones. */
+#define INFLLMV2_ROPE_NONE 0
+#define INFLLMV2_ROPE_LINEAR 1
+#define INFLLMV2_ROPE_NTK 2
+#define INFLLMV2_ROPE_YARN 3
+#define INFLLMV2_ROPE_FACTORS 4
 
 /* Query layout selector for infllmv2_select_blocks. */
 #define INFLLMV2_MODE_PREFILL 0 /* one query per cached token: query t sits at position t        */
@@ -132,6 +145,40 @@ typedef struct infllmv2_quant_tensor {
     int64_t stride_b, stride_h, stride_t;                   /* of codes  */
     int64_t scale_stride_b, scale_stride_h, scale_stride_t; /* of scales */
 } infllmv2_quant_tensor;
+
+/* A bf16 cache in pages.  A page holds page_size consecutive rows of a sequence for all key-value heads: of `k` and `v` stride_b leads from
+ * page to page, stride_h to the next head, stride_t to the next row of a page.  Row t of sequence b lies in page
+ * table[b * table_stride + t / page_size], row t % page_size.  page_size is a power of two from 16 to 1024; the table has at least
+ * ceil(max_seqlen / page_size) entries per sequence.  A table entry outside 0 .. n_pages - 1 is no page: its rows are seen by no query, and what is
+ * appended to them is dropped.  Sequences may share pages that no call writes. */
+typedef struct infllmv2_pages {
+    infllmv2_tensor k, v;
+    const int32_t *table; /* device */
+    int32_t table_stride;
+    int32_t page_size;
+    int32_t n_pages;
+} infllmv2_pages;
+
+/* What infllmv2_rope_table makes a rotation of. */
+typedef struct infllmv2_rope_config {
+    int32_t rot_dim;            /* channels that rotate, the first of a head: a multiple of 16, 16 to 128     */
+    int32_t scaling;            /* INFLLMV2_ROPE_*                                                           */
+    int32_t original_len;       /* tokens the model was trained on (yarn; factors with amplitude 0)          */
+    double base;                /* angle of pair j from one position to the next: base^(-2 j / rot_dim)      */
+    double factor;              /* by which the context is longer than the trained one, >= 1                 */
+    double beta_fast, beta_slow; /* yarn: turns in original_len above which a pair stays, below which it is stretched */
+    double amplitude;           /* of cosines and sines; 0: 1, yarn 0.1 ln(factor) + 1, factors sqrt(1 + ln(factor) / ln(original_len)) */
+    const double *pair_factors; /* factors: HOST array [rot_dim / 2], pair j turns pair_factors[j] times slower */
+} infllmv2_rope_config;
+
+/* A rotation: pair j of a head's channels is (j, j + rot_dim / 2), or (2 j, 2 j + 1) if interleaved; at position p it turns by p * steps[j] * 2^-64
+ * turns and is multiplied by `amplitude`.  Channels from rot_dim on stay. */
+typedef struct infllmv2_rotation {
+    int32_t rot_dim;
+    int32_t interleaved;
+    float amplitude;
+    const uint64_t *steps; /* device, [rot_dim / 2] */
+} infllmv2_rotation;
 
 /* Human-readable name of a status code (static storage). */
 const char *infllmv2_status_string(int32_t status);
@@ -492,6 +539,82 @@ int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_
                                           const infllmv2_quant_tensor *vq, const int32_t *seqlens, int32_t batch,
                                           int32_t max_seqlen, const infllmv2_tensor *out, float *lse, void *workspace,
                                           size_t workspace_bytes, void *stream);
+
+/*
+ * Rotary positions.  With (a, b) a pair of channels of a row at position p, and theta its angle p * steps * 2^-64 turns,
+ *     a' = amplitude (a cos theta - b sin theta)        b' = amplitude (b cos theta + a sin theta)
+ * in fp32, rounded once to bf16.  The angle is reduced as a whole number, so it is as exact at position 2^31 - 1 as at 1.
+ *
+ * infllmv2_rope_table   HOST function: cfg -> steps[0 .. rot_dim / 2 - 1] (HOST array, to be copied to the device) and the amplitude.  The angles per
+ *                       position: INFLLMV2_ROPE_LINEAR divides them by factor; _NTK takes base * factor^(rot_dim / (rot_dim - 2)) for base (rot_dim 16
+ *                       and more); _YARN keeps those of pairs that make beta_fast turns and more in original_len, divides by factor those of pairs that
+ *                       make beta_slow and fewer, and goes linearly between; _FACTORS divides pair j's by pair_factors[j].
+ * infllmv2_rope         q [batch, max_seqlen, Hq, d] and k [batch, Hkv, >=max_seqlen, d], rows t < seqlens[b], into q_out, k_out (which may be q, k
+ *                       themselves with the same strides).  q and q_out, or k and k_out, may both be NULL.
+ *   positions           in   int32 [batch, max_seqlen], any values; NULL: row t is at position t
+ * infllmv2_rope_bwd     the gradients of its inputs from those of its outputs: the same rows turned by -theta, times the same amplitude.
+ * Of prm the head counts and head_dim count; the rest has to be valid.  rot_dim that is no multiple of 16: INFLLMV2_ERR_UNSUPPORTED.
+ */
+int32_t infllmv2_rope_table(const infllmv2_rope_config *cfg, uint64_t *steps, float *amplitude);
+int32_t infllmv2_rope(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *q, const infllmv2_tensor *k,
+                      const int32_t *positions, const int32_t *seqlens, int32_t batch, int32_t max_seqlen,
+                      const infllmv2_tensor *q_out, const infllmv2_tensor *k_out, void *stream);
+int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *dq_out,
+                          const infllmv2_tensor *dk_out, const int32_t *positions, const int32_t *seqlens, int32_t batch,
+                          int32_t max_seqlen, const infllmv2_tensor *dq, const infllmv2_tensor *dk, void *stream);
+
+/*
+ * A cache in pages (infllmv2_pages).  In all these calls the last n tokens of a sequence are new: n_new[b] of them (DEVICE int32 [batch], clamped
+ * to 0 .. max_new; NULL: max_new of every sequence), seqlens[b] counts them, and new token t is cache row seqlens[b] - n + t.
+ * A sequence with seqlens[b] < n is skipped as a whole.  max_seqlen is at most 2^30, max_new at most 2^24, and max_new times n_q_heads at most 2^30.
+ *
+ * infllmv2_paged_append        k_new, v_new bf16 [batch, Hkv, max_new, d] into the pages; a sequence with seqlens[b] > max_seqlen is skipped too.  With rot
+ *                              (NULL: none) keys are rotated on the way, as by infllmv2_rope.  With q [batch, max_new, Hq, d] the same launch
+ *                              rotates the new queries into q_out (which may be q; both or neither NULL; needs rot).
+ *   positions                  in   int32 [batch, max_new], NULL: of a row its number in the cache (rows move when others are evicted; positions do not)
+ * infllmv2_paged_attn          attention of the new tokens over the cache, causal among themselves:
+ *                              new token t sees rows 0 .. seqlens[b] - n + t.
+ *   q, out                     bf16 [batch, max_new, Hq, d]; rows t >= n ignored / not written
+ *   lse                        out  fp32 [batch, max_new, Hq]
+ *                              bf16 products accumulated in fp32, probabilities rounded to bf16 before the value product, their fp32 sum taken before.
+ *                              A skipped sequence's new tokens, and a query that sees no row (no page) or only scores of -inf, get out 0, lse -inf.  A query that
+ *                              sees a key whose score is NaN or +inf has out and lse NaN.  Values that are not finite reach the queries that see them
+ *                              and no others; values up to the largest keep their mean, those below 2^-90 may lose bits.
+ * infllmv2_paged_attn_weights  what every cached row gets of that attention, added to what it had:
+ *                              weights_out[b, h, t] = (t < seqlens[b] - n ? weights[b, h, t] : 0) + sum over new tokens i that see row t and the query heads
+ *                              g of h of exp(softmax_scale <q_ig, k_t> - lse[b, i, g]),   t < seqlens[b].
+ *   lse                        in   of infllmv2_paged_attn; heads with lse -inf add nothing
+ *   weights                    in   fp32 [batch, Hkv, weights_pitch], weights_pitch >= max_seqlen; NULL: zeros
+ *   weights_out                out  the same layout; may be `weights`.  Entries t >= seqlens[b], and skipped sequences', are not written.  The sums' order is
+ *                              fixed: results repeat bit for bit.
+ * infllmv2_paged_evict         keeps `budget` rows of each sequence and head: the first n_first and the last n_recent, and of the others those with the
+ *                              largest weights, ties to the lower row, a NaN above all numbers.  n_first + n_recent <= budget.  Sequences of up to `budget` rows keep all.
+ *                              Kept rows go, in their order, to rows 0, 1, .. of the sequence in `to`, whose pages have to be others than those that hold a sequence's
+ *                              rows in `from` (the pools may be the same); its table has at least ceil(budget / page_size) entries.
+ *   weights                    in   fp32 [batch, Hkv, weights_pitch], weights_pitch >= max_seqlen
+ *   kept                       out  int32 [batch, Hkv, budget]: the kept rows, ascending, then -1
+ *   weights_out                out  fp32 [batch, Hkv, budget]: their weights, then 0 (may be NULL)
+ *   seqlens_out                out  int32 [batch]: min(seqlens[b], budget)
+ * Workspaces: infllmv2_paged_workspace_bytes(INFLLMV2_OP_PAGED_*, ...) bytes, 256-byte aligned (0: none needed, or the arguments are invalid); enough
+ * for every call with no more sequences, rows and new tokens.  (max_new does not count for INFLLMV2_OP_PAGED_EVICT.)
+ * stride_t of k and v of the pages at most 2^23 elements, of q as well, and group size x its stride_h at most 2^29, else INFLLMV2_ERR_UNSUPPORTED.
+ */
+size_t infllmv2_paged_workspace_bytes(int32_t op, const infllmv2_params *prm, int32_t batch, int32_t max_seqlen, int32_t max_new);
+int32_t infllmv2_paged_append(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *k_new,
+                              const infllmv2_tensor *v_new, const infllmv2_tensor *q, const infllmv2_pages *pages,
+                              const int32_t *positions, const int32_t *n_new, const int32_t *seqlens, int32_t batch,
+                              int32_t max_seqlen, int32_t max_new, const infllmv2_tensor *q_out, void *stream);
+int32_t infllmv2_paged_attn(const infllmv2_params *prm, const infllmv2_tensor *q, const infllmv2_pages *pages, const int32_t *n_new,
+                            const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t max_new, const infllmv2_tensor *out,
+                            float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int32_t infllmv2_paged_attn_weights(const infllmv2_params *prm, const infllmv2_tensor *q, const float *lse,
+                                    const infllmv2_pages *pages, const int32_t *n_new, const int32_t *seqlens, int32_t batch,
+                                    int32_t max_seqlen, int32_t max_new, const float *weights, int32_t weights_pitch,
+                                    float *weights_out, void *workspace, size_t workspace_bytes, void *stream);
+int32_t infllmv2_paged_evict(const infllmv2_params *prm, const float *weights, int32_t weights_pitch, const infllmv2_pages *from,
+                             const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t budget, int32_t n_first,
+                             int32_t n_recent, const infllmv2_pages *to, int32_t *kept, float *weights_out, int32_t *seqlens_out,
+                             void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Query-block-shared selection -- a COMPARISON VARIANT, not the report's method (section 2.1.3 argues

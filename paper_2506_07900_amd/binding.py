@@ -12,6 +12,7 @@ Tensor layouts (bf16, CUDA/HIP device, head_dim contiguous):
   queries, outputs  [B, T, Hq, d]   (decode: T = 1; draft verification: T = n_draft)
   seqlens           int32 [B]
   block_idx         int32 [B, Hkv, Tq, topk]
+  caches in pages   PagedCache: k, v [pages, Hkv, page, d], table int32 [B, pages of the longest sequence]
   caches in 4 bits  QuantCache: codes uint8 [B, Hkv, T, d/2], scales uint8 [B, Hkv, T, d/32]
 """
 import ctypes
@@ -35,6 +36,8 @@ OP_DECODE_STEP = 8
 OP_SELECT_SHARED = 9
 OP_VERIFY_STEP = 10
 OP_WINDOW_PREFILL, OP_WINDOW_BWD, OP_WINDOW_DECODE = 11, 12, 13
+OP_PAGED_ATTN, OP_PAGED_WEIGHTS, OP_PAGED_EVICT = 14, 15, 16
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "factors": 4}
 MODE_PREFILL, MODE_DECODE = 0, 1
 
 EXPORTS = ["infllmv2_status_string", "infllmv2_workspace_bytes", "infllmv2_compress_keys",
@@ -44,7 +47,9 @@ EXPORTS = ["infllmv2_status_string", "infllmv2_workspace_bytes", "infllmv2_compr
            "infllmv2_block_scores",
            "infllmv2_quantize_kv", "infllmv2_dequantize_kv", "infllmv2_append_kv_quant", "infllmv2_sparse_attn_decode_quant",
            "infllmv2_sparse_attn_verify_quant", "infllmv2_window_workspace_bytes", "infllmv2_window_attn_prefill",
-           "infllmv2_window_attn_bwd", "infllmv2_window_attn_decode", "infllmv2_window_attn_decode_quant"]
+           "infllmv2_window_attn_bwd", "infllmv2_window_attn_decode", "infllmv2_window_attn_decode_quant",
+           "infllmv2_rope_table", "infllmv2_rope", "infllmv2_rope_bwd", "infllmv2_paged_workspace_bytes", "infllmv2_paged_append",
+           "infllmv2_paged_attn", "infllmv2_paged_attn_weights", "infllmv2_paged_evict"]
 BENCH_EXPORTS = ["infllmv2_probe_peaks", "infllmv2_probe_detail", "infllmv2_timing_enable", "infllmv2_timing_read"]
 
 
@@ -71,6 +76,37 @@ class QuantCache(NamedTuple):
     """A cache in 4 bits: codes uint8 [B, Hkv, T, d/2], exponent bytes uint8 [B, Hkv, T, d/32] (see infllmv2_quant_tensor)."""
     codes: torch.Tensor
     scales: torch.Tensor
+
+
+class CPages(ctypes.Structure):
+    _fields_ = [("k", CTensor), ("v", CTensor), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32)]
+
+
+class CRopeConfig(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("original_len", ctypes.c_int32)] + [
+        (n, ctypes.c_double) for n in ("base", "factor", "beta_fast", "beta_slow", "amplitude")] + [
+        ("pair_factors", ctypes.POINTER(ctypes.c_double))]
+
+
+class CRotation(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float),
+                ("steps", ctypes.c_void_p)]
+
+
+class Rotation(NamedTuple):
+    """A rotation by positions (see infllmv2_rotation): steps int64 [rot_dim / 2], turns per position times 2^64."""
+    steps: torch.Tensor
+    rot_dim: int
+    interleaved: bool
+    amplitude: float
+
+
+class PagedCache(NamedTuple):
+    """A cache in pages: k, v bf16 [pages, Hkv, page, d], table int32 [B, pages of the longest sequence] (see infllmv2_pages)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
 
 
 @dataclass
@@ -176,6 +212,18 @@ def load_library(path=None):
                        ("window_attn_bwd", [P, i32, i32, T, T, T, T, T, vp, vp, i32, i32, T, T, T, vp, sz, vp]),
                        ("window_attn_decode", [P, i32, i32, T, T, T, vp, i32, i32, T, vp, vp, sz, vp]),
                        ("window_attn_decode_quant", [P, i32, i32, T, Q, Q, vp, i32, i32, T, vp, vp, sz, vp])):
+        fn = getattr(lib, "infllmv2_" + name)
+        fn.restype, fn.argtypes = i32, args
+    R, G = ctypes.POINTER(CRotation), ctypes.POINTER(CPages)
+    lib.infllmv2_paged_workspace_bytes.restype = sz
+    lib.infllmv2_paged_workspace_bytes.argtypes = [i32, P, i32, i32, i32]
+    for name, args in (("rope_table", [ctypes.POINTER(CRopeConfig), ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_float)]),
+                       ("rope", [P, R, T, T, vp, vp, i32, i32, T, T, vp]),
+                       ("rope_bwd", [P, R, T, T, vp, vp, i32, i32, T, T, vp]),
+                       ("paged_append", [P, R, T, T, T, G, vp, vp, vp, i32, i32, i32, T, vp]),
+                       ("paged_attn", [P, T, G, vp, vp, i32, i32, i32, T, vp, vp, sz, vp]),
+                       ("paged_attn_weights", [P, T, vp, G, vp, vp, i32, i32, i32, vp, i32, vp, vp, sz, vp]),
+                       ("paged_evict", [P, vp, i32, G, vp, i32, i32, i32, i32, i32, G, vp, vp, vp, vp, sz, vp])):
         fn = getattr(lib, "infllmv2_" + name)
         fn.restype, fn.argtypes = i32, args
     if hasattr(lib, "infllmv2_timing_enable"):            # the bench build
@@ -470,6 +518,66 @@ def window_attn_decode(prm, n_sink, window, q, k, v, seqlens, max_seqlen, out=No
 def window_attn_decode_quant(prm, n_sink, window, q, kq, vq, seqlens, max_seqlen, out=None, lse=None, workspace=None):
     """The same on a cache in 4 bits."""
     return _native().window_attn_decode_quant(prm.packed(), n_sink, window, q, kq, vq, seqlens, max_seqlen, out, lse, workspace)
+
+
+# ---- rotary positions and a cache in pages ---------------------------------------------------------------
+
+def rope_table(rot_dim, base=10000.0, interleaved=False, scaling="none", factor=1.0, original_len=0, beta_fast=32.0, beta_slow=1.0,
+               pair_factors=None, amplitude=0.0, device=None):
+    """-> Rotation of the first rot_dim channels (a multiple of 16): pairs (j, j + rot_dim / 2), or (2 j, 2 j + 1) if interleaved.  scaling is one of
+    ROPE_SCALINGS; what each takes is in infllmv2_rope_config.  The table goes to `device` (the current one)."""
+    if scaling not in ROPE_SCALINGS:
+        raise InfLLMv2Error("scaling must be one of %s" % ", ".join(ROPE_SCALINGS))
+    half = max(1, rot_dim // 2)
+    if pair_factors is not None and len(pair_factors) != half:
+        raise InfLLMv2Error("pair_factors must have rot_dim / 2 entries")
+    factors = None if pair_factors is None else (ctypes.c_double * half)(*[float(x) for x in pair_factors])
+    cfg = CRopeConfig(rot_dim, ROPE_SCALINGS[scaling], original_len, base, factor, beta_fast, beta_slow, amplitude, factors)
+    steps, amp = (ctypes.c_uint64 * half)(), ctypes.c_float()
+    _check(load_library().infllmv2_rope_table(ctypes.byref(cfg), steps, ctypes.byref(amp)), "infllmv2_rope_table")
+    signed = torch.tensor([x - (1 << 64) if x >> 63 else x for x in steps], dtype=torch.int64)
+    return Rotation(signed.to("cuda" if device is None else device), int(rot_dim), bool(interleaved), amp.value)
+
+
+def rope(prm, rope, q, k, seqlens, max_seqlen, positions=None, q_out=None, k_out=None):
+    """q [B, T, Hq, d], k [B, Hkv, T, d] (either may be None) rotated by their positions (int32 [B, max_seqlen]; None: the row) -> q_out, k_out
+    (allocated if not given; q, k themselves: in place)."""
+    return _native().rope(prm.packed(), rope, q, k, seqlens, max_seqlen, positions, q_out, k_out, 0)
+
+
+def rope_bwd(prm, rope, dq_out, dk_out, seqlens, max_seqlen, positions=None, dq=None, dk=None):
+    """Backward of rope: the gradients of its outputs -> those of its inputs."""
+    return _native().rope(prm.packed(), rope, dq_out, dk_out, seqlens, max_seqlen, positions, dq, dk, 1)
+
+
+def paged_workspace_bytes(op, prm, batch, max_seqlen, max_new):
+    return int(load_library().infllmv2_paged_workspace_bytes(op, ctypes.byref(prm.c()), batch, max_seqlen, max_new))
+
+
+def paged_append(prm, k_new, v_new, cache, seqlens, max_seqlen, n_new=None, rope=None, positions=None, q=None, q_out=None):
+    """The last n_new[b] (None: all n) rows of a sequence from k_new, v_new [B, Hkv, n, d] into the pages of `cache`; with rope the keys, and queries
+    q [B, n, Hq, d] if given, are rotated on the way by positions (int32 [B, n]; None: the row in the cache) -> q_out, or None."""
+    return _native().paged_append(prm.packed(), k_new, v_new, cache, seqlens, max_seqlen, n_new, rope, positions, q, q_out)
+
+
+def paged_attn(prm, q, cache, seqlens, max_seqlen, n_new=None, out=None, lse=None, workspace=None):
+    """The last n_new[b] (None: all n) tokens of a sequence, q [B, n, Hq, d], over its pages, causal among themselves
+    -> out bf16 [B, n, Hq, d], lse fp32 [B, n, Hq]."""
+    return _native().paged_attn(prm.packed(), q, cache, seqlens, max_seqlen, n_new, out, lse, workspace)
+
+
+def paged_attn_weights(prm, q, lse, cache, seqlens, max_seqlen, n_new=None, weights=None, weights_out=None, workspace=None):
+    """What each cached row gets of that attention (lse: paged_attn's), summed over the new tokens and a group's heads and added to `weights` fp32
+    [B, Hkv, >= max_seqlen] (None: 0; new rows start at 0) -> weights_out (may be `weights`)."""
+    return _native().paged_attn_weights(prm.packed(), q, lse, cache, seqlens, max_seqlen, n_new, weights, weights_out, workspace)
+
+
+def paged_evict(prm, weights, cache, seqlens, max_seqlen, budget, n_first, n_recent, to, kept=None, weights_out=None, seqlens_out=None,
+                workspace=None):
+    """The first n_first, the last n_recent and of the others the heaviest rows of `cache`, `budget` in all for each head, in order into the pages of `to`
+    -> kept int32 [B, Hkv, budget] (padded with -1), their weights fp32 [B, Hkv, budget], lengths int32 [B]."""
+    return _native().paged_evict(prm.packed(), weights, cache, seqlens, max_seqlen, budget, n_first, n_recent, to, kept, weights_out, seqlens_out,
+                                 workspace)
 
 
 def select_blocks_shared(prm, q, ck, seqlens, max_seqlen, block_idx=None, workspace=None):

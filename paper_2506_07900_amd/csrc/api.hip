@@ -1,12 +1,21 @@
 // C ABI of the library: argument validation (host only, before any HIP call) and dispatch to
 // the kernel launchers.  See include/infllmv2.h for the contract of every entry point.
+#include <math.h>
+
 #include "common.h"
 #include "internal.h"
+#include "paged.h"
 #include "quant.h"
 
 using namespace infllmv2;
 
 namespace {
+
+#define RETURN_IF_ERR(x)                   \
+    do {                                   \
+        int32_t _s = (x);                  \
+        if (_s != INFLLMV2_OK) return _s;  \
+    } while (0)
 
 constexpr int32_t kMaxDecodeSeqlen = 262144;   // decode selection: at most 256 log-sum-exp partials per head
 constexpr int32_t kMaxDraft = 64;              // one uint64 mask word per drafted token
@@ -135,13 +144,36 @@ int32_t check_workspace(const void *workspace, size_t bytes, size_t need) {
     return need > 0 && (!workspace || bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) ? INFLLMV2_ERR_WORKSPACE : INFLLMV2_OK;
 }
 
-int32_t hip_status(int e) { return e == 0 ? INFLLMV2_OK : INFLLMV2_ERR_HIP; }
+// a cache in pages, with tables of `rows` rows per sequence
+int32_t check_pages(const infllmv2_pages *p, int64_t rows) {
+    if (!p || !p->table || p->n_pages < 0 || p->page_size <= 0 || p->table_stride < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_tensor(&p->k));
+    RETURN_IF_ERR(check_tensor(&p->v));
+    if ((p->page_size & (p->page_size - 1)) != 0 || p->page_size < 16 || p->page_size > 1024) return INFLLMV2_ERR_UNSUPPORTED;
+    if ((int64_t)p->table_stride * p->page_size < rows) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (p->k.stride_t > kMaxTokenStride || p->v.stride_t > kMaxTokenStride) return INFLLMV2_ERR_UNSUPPORTED;
+    return INFLLMV2_OK;
+}
 
-#define RETURN_IF_ERR(x)                   \
-    do {                                   \
-        int32_t _s = (x);                  \
-        if (_s != INFLLMV2_OK) return _s;  \
-    } while (0)
+Pages make_pages(const infllmv2_pages *p) {
+    return Pages{make_tensor(&p->k), make_tensor(&p->v), p->table, p->table_stride, __builtin_ctz((unsigned)p->page_size), p->n_pages};
+}
+
+int32_t check_rotation(const infllmv2_rotation *r) {
+    if (!r || !r->steps || (reinterpret_cast<uintptr_t>(r->steps) & 15u) || r->rot_dim <= 0 || !isfinite(r->amplitude)) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    return r->rot_dim % 16 || r->rot_dim > kHeadDim ? INFLLMV2_ERR_UNSUPPORTED : INFLLMV2_OK;
+}
+
+Rotation make_rotation(const infllmv2_rotation *r, bool back) {
+    return r ? Rotation{r->steps, r->rot_dim, r->interleaved, r->amplitude, back ? -1.f : 1.f} : Rotation{nullptr, 0, 0, 1.f, 1.f};
+}
+
+int32_t check_new(const infllmv2_params *prm, int32_t max_new) {
+    if (max_new < 1) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    return max_new > (1 << 24) || (int64_t)max_new * prm->n_q_heads > (1ll << 30) ? INFLLMV2_ERR_UNSUPPORTED : INFLLMV2_OK;
+}
+
+int32_t hip_status(int e) { return e == 0 ? INFLLMV2_OK : INFLLMV2_ERR_HIP; }
 
 }  // namespace
 
@@ -757,6 +789,177 @@ int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, window_decode_ws_bytes(dm, w)));
     return hip_status(launch_window_decode_quant(dm, w, make_tensor(q), make_quant(kq), make_quant(vq), seqlens, make_tensor(out), lse,
                                                  workspace, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_rope_table(const infllmv2_rope_config *cfg, uint64_t *steps, float *amplitude) {
+    if (!cfg || !steps || !amplitude || cfg->rot_dim <= 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (cfg->rot_dim % 16 || cfg->rot_dim > kHeadDim) return INFLLMV2_ERR_UNSUPPORTED;
+    const int kind = cfg->scaling, half = cfg->rot_dim / 2;
+    if (kind < INFLLMV2_ROPE_NONE || kind > INFLLMV2_ROPE_FACTORS) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (!(cfg->base > 1.0) || !isfinite(cfg->base) || !(cfg->amplitude >= 0.0) || !(cfg->amplitude < 1e30)) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (kind != INFLLMV2_ROPE_NONE && (!(cfg->factor >= 1.0) || !isfinite(cfg->factor))) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const bool trained = kind == INFLLMV2_ROPE_YARN || (kind == INFLLMV2_ROPE_FACTORS && cfg->amplitude == 0.0);
+    if (trained && cfg->original_len < 2) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (kind == INFLLMV2_ROPE_YARN && (!(cfg->beta_fast > cfg->beta_slow) || !(cfg->beta_slow >= 0.0) || !isfinite(cfg->beta_fast)))
+        return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (kind == INFLLMV2_ROPE_FACTORS) {
+        if (!cfg->pair_factors) return INFLLMV2_ERR_INVALID_ARGUMENT;
+        for (int j = 0; j < half; ++j)
+            if (!(cfg->pair_factors[j] >= 1e-3) || !isfinite(cfg->pair_factors[j])) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    }
+    // (in 64-bit mantissas: an angle after 2^31 positions is then exact to 2^-33 turns)
+    const long double factor = cfg->factor, two_pi = 6.283185307179586476925286766559L;
+    long double base = cfg->base;
+    if (kind == INFLLMV2_ROPE_NTK) base *= powl(factor, (long double)cfg->rot_dim / (cfg->rot_dim - 2));
+    for (int j = 0; j < half; ++j) {
+        long double turns = powl(base, -2.0L * j / cfg->rot_dim) / two_pi;                     // per position
+        if (kind == INFLLMV2_ROPE_LINEAR) turns /= factor;
+        if (kind == INFLLMV2_ROPE_YARN) {
+            long double keep = (cfg->original_len * turns - cfg->beta_slow) / ((long double)cfg->beta_fast - cfg->beta_slow);
+            keep = keep < 0.0L ? 0.0L : keep > 1.0L ? 1.0L : keep;
+            turns *= keep + (1.0L - keep) / factor;
+        }
+        if (kind == INFLLMV2_ROPE_FACTORS) turns /= cfg->pair_factors[j];
+        turns -= floorl(turns);                          // (a pair factor below 1 / (2 pi) makes it more than one)
+        const long double scaled = roundl(ldexpl(turns, 64));
+        steps[j] = scaled >= 18446744073709551616.0L ? 0u : (uint64_t)scaled;
+    }
+    double a = cfg->amplitude;
+    if (a == 0.0) {
+        a = 1.0;
+        if (kind == INFLLMV2_ROPE_YARN) a = 0.1 * log(cfg->factor) + 1.0;
+        if (kind == INFLLMV2_ROPE_FACTORS) a = sqrt(1.0 + log(cfg->factor) / log((double)cfg->original_len));
+    }
+    *amplitude = (float)a;
+    return INFLLMV2_OK;
+}
+
+int32_t infllmv2i_rope(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *q, const infllmv2_tensor *k,
+                       const int32_t *positions, const int32_t *seqlens, int32_t batch, int32_t max_seqlen, const infllmv2_tensor *q_out,
+                       const infllmv2_tensor *k_out, void *stream, int32_t back, int32_t fill) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
+    RETURN_IF_ERR(check_rotation(rot));
+    if (!q != !q_out || !k != !k_out || !seqlens) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const infllmv2_tensor *ts[4] = {q, q_out, k, k_out};
+    Tensor made[4];
+    for (int i = 0; i < 4; ++i) {
+        if (!ts[i]) continue;
+        RETURN_IF_ERR(check_tensor(ts[i]));
+        made[i] = make_tensor(ts[i]);
+    }
+    return hip_status(launch_rope(make_dims(prm, batch, max_seqlen, 1, fill), make_rotation(rot, back != 0), q ? &made[0] : nullptr, k ? &made[2] : nullptr,
+                                  positions, seqlens, q ? &made[1] : nullptr, k ? &made[3] : nullptr, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_rope(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *q, const infllmv2_tensor *k,
+                      const int32_t *positions, const int32_t *seqlens, int32_t batch, int32_t max_seqlen, const infllmv2_tensor *q_out,
+                      const infllmv2_tensor *k_out, void *stream) {
+    return infllmv2i_rope(prm, rot, q, k, positions, seqlens, batch, max_seqlen, q_out, k_out, stream, 0, 0);
+}
+
+int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *dq_out, const infllmv2_tensor *dk_out,
+                          const int32_t *positions, const int32_t *seqlens, int32_t batch, int32_t max_seqlen, const infllmv2_tensor *dq,
+                          const infllmv2_tensor *dk, void *stream) {
+    return infllmv2i_rope(prm, rot, dq_out, dk_out, positions, seqlens, batch, max_seqlen, dq, dk, stream, 1, 0);
+}
+
+size_t infllmv2_paged_workspace_bytes(int32_t op, const infllmv2_params *prm, int32_t batch, int32_t max_seqlen, int32_t max_new) {
+    if (check_params(prm) != INFLLMV2_OK || check_sizes(batch, max_seqlen) != INFLLMV2_OK || check_capacity(max_seqlen) != INFLLMV2_OK) return 0;
+    const Dims dm = make_dims(prm, batch, max_seqlen);
+    if (op == INFLLMV2_OP_PAGED_EVICT) return paged_evict_ws_bytes(dm);
+    if (check_new(prm, max_new) != INFLLMV2_OK) return 0;
+    switch (op) {
+        case INFLLMV2_OP_PAGED_ATTN: return paged_attn_ws_bytes(dm, max_new);
+        case INFLLMV2_OP_PAGED_WEIGHTS: return paged_weights_ws_bytes(dm, max_new);
+    }
+    return 0;
+}
+
+int32_t infllmv2_paged_append(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *k_new, const infllmv2_tensor *v_new,
+                              const infllmv2_tensor *q, const infllmv2_pages *pages, const int32_t *positions, const int32_t *n_new,
+                              const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t max_new, const infllmv2_tensor *q_out,
+                              void *stream) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
+    RETURN_IF_ERR(check_new(prm, max_new));
+    if (rot) RETURN_IF_ERR(check_rotation(rot));
+    RETURN_IF_ERR(check_tensor(k_new));
+    RETURN_IF_ERR(check_tensor(v_new));
+    RETURN_IF_ERR(check_pages(pages, max_seqlen));
+    if (!q != !q_out || (q && !rot) || !seqlens) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    Tensor qt, ot;
+    if (q) {
+        RETURN_IF_ERR(check_tensor(q));
+        RETURN_IF_ERR(check_tensor(q_out));
+        qt = make_tensor(q);
+        ot = make_tensor(q_out);
+    }
+    return hip_status(launch_paged_append(make_dims(prm, batch, max_seqlen), make_rotation(rot, false), make_tensor(k_new), make_tensor(v_new),
+                                          q ? &qt : nullptr, make_pages(pages), positions, NewTokens{n_new, max_new}, seqlens, q ? &ot : nullptr,
+                                          reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2i_paged_attn(const infllmv2_params *prm, const infllmv2_tensor *q, const infllmv2_pages *pages, const int32_t *n_new,
+                             const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t max_new, const infllmv2_tensor *out, float *lse,
+                             void *workspace, size_t workspace_bytes, void *stream, int32_t fill) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
+    RETURN_IF_ERR(check_new(prm, max_new));
+    RETURN_IF_ERR(check_tensor(q));
+    RETURN_IF_ERR(check_pages(pages, max_seqlen));
+    RETURN_IF_ERR(check_tensor(out));
+    if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_spans(prm, nullptr, nullptr, q, nullptr));
+    const Dims dm = make_dims(prm, batch, max_seqlen, 1, fill);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, paged_attn_ws_bytes(dm, max_new)));
+    return hip_status(launch_paged_attn(dm, make_tensor(q), make_pages(pages), NewTokens{n_new, max_new}, seqlens, make_tensor(out), lse, workspace,
+                                        reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_paged_attn(const infllmv2_params *prm, const infllmv2_tensor *q, const infllmv2_pages *pages, const int32_t *n_new,
+                            const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t max_new, const infllmv2_tensor *out, float *lse,
+                            void *workspace, size_t workspace_bytes, void *stream) {
+    return infllmv2i_paged_attn(prm, q, pages, n_new, seqlens, batch, max_seqlen, max_new, out, lse, workspace, workspace_bytes, stream, 0);
+}
+
+int32_t infllmv2_paged_attn_weights(const infllmv2_params *prm, const infllmv2_tensor *q, const float *lse, const infllmv2_pages *pages,
+                                    const int32_t *n_new, const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t max_new,
+                                    const float *weights, int32_t weights_pitch, float *weights_out, void *workspace, size_t workspace_bytes,
+                                    void *stream) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
+    RETURN_IF_ERR(check_new(prm, max_new));
+    RETURN_IF_ERR(check_tensor(q));
+    RETURN_IF_ERR(check_pages(pages, max_seqlen));
+    if (!seqlens || !lse || !weights_out || weights_pitch < max_seqlen) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_spans(prm, nullptr, nullptr, q, nullptr));
+    const Dims dm = make_dims(prm, batch, max_seqlen);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, paged_weights_ws_bytes(dm, max_new)));
+    return hip_status(launch_paged_weights(dm, make_tensor(q), lse, make_pages(pages), NewTokens{n_new, max_new}, seqlens, weights, weights_pitch, weights_out,
+                                           workspace, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t infllmv2_paged_evict(const infllmv2_params *prm, const float *weights, int32_t weights_pitch, const infllmv2_pages *from,
+                             const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t budget, int32_t n_first, int32_t n_recent,
+                             const infllmv2_pages *to, int32_t *kept, float *weights_out, int32_t *seqlens_out, void *workspace,
+                             size_t workspace_bytes, void *stream) {
+    RETURN_IF_ERR(check_params(prm));
+    RETURN_IF_ERR(check_sizes(batch, max_seqlen));
+    RETURN_IF_ERR(check_capacity(max_seqlen));
+    if (budget < 1 || n_first < 0 || n_recent < 0 || (int64_t)n_first + n_recent > budget) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    RETURN_IF_ERR(check_capacity(budget));
+    RETURN_IF_ERR(check_pages(from, max_seqlen));
+    RETURN_IF_ERR(check_pages(to, budget));
+    if (!weights || !seqlens || !kept || !seqlens_out || weights_pitch < max_seqlen) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const Dims dm = make_dims(prm, batch, max_seqlen);
+    RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, paged_evict_ws_bytes(dm)));
+    return hip_status(launch_paged_evict(dm, weights, weights_pitch, make_pages(from), seqlens, budget, n_first, n_recent, make_pages(to), kept, weights_out,
+                                         seqlens_out, workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -48,6 +48,15 @@ int32_t infllmv2i_window_attn_bwd(const infllmv2_params *prm, int32_t n_sink, in
                                   const infllmv2_tensor *dv, void *workspace, size_t workspace_bytes, void *stream,
                                   int32_t fill);
 
+/* back != 0: infllmv2_rope_bwd */
+int32_t infllmv2i_rope(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *q, const infllmv2_tensor *k,
+                       const int32_t *positions, const int32_t *seqlens, int32_t batch, int32_t max_seqlen, const infllmv2_tensor *q_out,
+                       const infllmv2_tensor *k_out, void *stream, int32_t back, int32_t fill);
+/* (rows of new tokens behind a sequence's n_new) */
+int32_t infllmv2i_paged_attn(const infllmv2_params *prm, const infllmv2_tensor *q, const infllmv2_pages *pages, const int32_t *n_new,
+                             const int32_t *seqlens, int32_t batch, int32_t max_seqlen, int32_t max_new, const infllmv2_tensor *out, float *lse,
+                             void *workspace, size_t workspace_bytes, void *stream, int32_t fill);
+
 #ifdef __cplusplus
 }
 #endif

@@ -54,6 +54,12 @@ struct Library {
     INFLLMV2_FNI(window_attn_prefill);
     INFLLMV2_FNI(window_attn_bwd);
     INFLLMV2_FNI(window_bwd_scratch_bytes);
+    INFLLMV2_FNI(rope);
+    INFLLMV2_FN(paged_workspace_bytes);
+    INFLLMV2_FN(paged_append);
+    INFLLMV2_FNI(paged_attn);
+    INFLLMV2_FN(paged_attn_weights);
+    INFLLMV2_FN(paged_evict);
 #undef INFLLMV2_FN
 #undef INFLLMV2_FNI
 } lib;
@@ -689,6 +695,208 @@ PyObject *window_decode(Args a) {
 PyObject *window_attn_decode(Args a) { return window_decode<false>(a); }
 PyObject *window_attn_decode_quant(Args a) { return window_decode<true>(a); }
 
+// ---- rotary positions and the cache in pages ----------------------------------------------------------------------------------
+// Rotation(steps int64 [rot_dim / 2], rot_dim, interleaved, amplitude)
+infllmv2_rotation rotation(PyObject *o) {
+    expect(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 4, "rope", " must be a Rotation (of rope_table)");
+    const at::Tensor &steps = tensor(PyTuple_GET_ITEM(o, 0), "rope.steps");
+    here(steps, "rope.steps");
+    infllmv2_rotation r;
+    r.rot_dim = integer(PyTuple_GET_ITEM(o, 1));
+    r.interleaved = integer(PyTuple_GET_ITEM(o, 2));
+    const double amplitude = PyFloat_AsDouble(PyTuple_GET_ITEM(o, 3));
+    if (amplitude == -1.0 && PyErr_Occurred()) throw python_error();
+    r.amplitude = static_cast<float>(amplitude);
+    expect(steps.scalar_type() == at::kLong && steps.is_contiguous() && 2 * steps.numel() == r.rot_dim, "rope.steps", " must be int64 [rot_dim / 2]");
+    r.steps = static_cast<const uint64_t *>(steps.data_ptr());
+    return r;
+}
+const int32_t *words(PyObject *o, const char *name, int64_t n, const char *shape) {           // optional
+    if (o == Py_None) return nullptr;
+    const int32_t *p = i32(o, name);
+    here(THPVariable_Unpack(o), name);
+    expect(THPVariable_Unpack(o).numel() == n, name, shape);
+    return p;
+}
+float *floats(const at::Tensor &t, const char *name, int64_t B, int64_t H, int64_t T) {
+    here(t, name);
+    expect(t.scalar_type() == at::kFloat && t.is_contiguous() && t.dim() == 3 && t.size(0) == B && t.size(1) == H && t.size(2) >= T, name,
+           " must be a contiguous fp32 device tensor [batch, n_kv_heads, rows]");
+    return static_cast<float *>(t.data_ptr());
+}
+// PagedCache(k, v [pages, Hkv, page, d], table int32 [batch, entries])
+infllmv2_pages paged(PyObject *o, const char *name, int64_t B, int64_t T, const infllmv2_params *prm, int64_t *batch = nullptr) {
+    expect(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 3, name, " must be a PagedCache");
+    const at::Tensor &k = kv(PyTuple_GET_ITEM(o, 0), name, -1, 0, prm), &v = kv(PyTuple_GET_ITEM(o, 1), name, -1, 0, prm);
+    expect(k.size(0) == v.size(0) && k.size(2) == v.size(2), name, ": k and v differ in pages or rows of a page");
+    expect(k.size(0) < (1ll << 31) && k.size(2) < (1ll << 31), name, ": too many pages");
+    infllmv2_pages p;
+    p.k = cache(k);
+    p.v = cache(v);
+    p.table = i32(PyTuple_GET_ITEM(o, 2), "table");
+    const at::Tensor &table = THPVariable_Unpack(PyTuple_GET_ITEM(o, 2));
+    here(table, "table");
+    expect(table.dim() == 2 && (B < 0 || table.size(0) == B) && table.size(1) * k.size(2) >= T && table.size(1) < (1ll << 31), "table",
+           " must be [batch, pages of the longest sequence]");
+    if (batch) *batch = table.size(0);
+    p.table_stride = static_cast<int32_t>(table.size(1));
+    p.page_size = static_cast<int32_t>(k.size(2));
+    p.n_pages = static_cast<int32_t>(k.size(0));
+    return p;
+}
+
+// (prm, rope, q | None, k | None, seqlens, max_seqlen, positions | None, q_out | None, k_out | None, back)
+PyObject *rope(Args a) {
+    const infllmv2_params *prm = enter(a[0]);
+    const infllmv2_rotation rot = rotation(a[1]);
+    const int32_t T = capacity(a[5]), back = integer(a[9]);
+    const at::Tensor *q = a[2] == Py_None ? nullptr : &query(a[2], "q", -1, T, prm);
+    const at::Tensor *k = a[3] == Py_None ? nullptr : &kv(a[3], "k", q ? q->size(0) : -1, T, prm);
+    expect(q || k, "q, k", ": at least one must be given");
+    expect((q || a[7] == Py_None) && (k || a[8] == Py_None), "q_out, k_out", ": there is no input for it");
+    const int64_t B = q ? q->size(0) : k->size(0);
+    const int32_t *sl = lengths(a[4], B), *pos = words(a[6], "positions", B * T, " must be [batch, max_seqlen]");
+    Result qo(a[7]), ko(a[8]);
+    const int32_t fill = (!q || (qo.make() && q->size(1) == T)) && (!k || (ko.make() && k->size(2) == T));
+    infllmv2_tensor qd{}, kd{}, qod{}, kod{};
+    if (q) {
+        if (qo.make()) qo.own = fill ? at::empty_like(*q) : at::zeros_like(*q);
+        qd = rows(*q);
+        qod = rows(qo.make() ? qo.own : query(qo.given, "q_out", B, T, prm));
+    }
+    if (k) {
+        if (ko.make()) ko.own = fill ? at::empty_like(*k) : at::zeros_like(*k);
+        kd = cache(*k);
+        kod = cache(ko.make() ? ko.own : kv(ko.given, "k_out", B, T, prm));
+    }
+    run(back ? "infllmv2_rope_bwd" : "infllmv2_rope", [&] {
+        return lib.rope(prm, &rot, q ? &qd : nullptr, k ? &kd : nullptr, pos, sl, static_cast<int32_t>(B), T, q ? &qod : nullptr, k ? &kod : nullptr,
+                        current_stream(), back, fill);
+    });
+    PyObject *r = PyTuple_New(2);
+    PyObject *none[2] = {q ? qo.release() : nullptr, k ? ko.release() : nullptr};
+    for (int i = 0; i < 2; ++i) {
+        if (!none[i]) {
+            Py_INCREF(Py_None);
+            none[i] = Py_None;
+        }
+        PyTuple_SET_ITEM(r, i, none[i]);
+    }
+    return r;
+}
+
+// (prm, k_new, v_new, cache, seqlens, max_seqlen, n_new | None, rope | None, positions | None, q | None, q_out | None)
+PyObject *paged_append(Args a) {
+    const infllmv2_params *prm = enter(a[0]);
+    const int32_t T = capacity(a[5]);
+    const at::Tensor &kn = kv(a[1], "k_new", -1, 1, prm);
+    const int64_t B = kn.size(0), n = kn.size(2);
+    const at::Tensor &vn = kv(a[2], "v_new", B, n, prm);
+    expect(vn.size(2) == n && n < (1ll << 31), "v_new", " must have the rows of k_new");
+    const infllmv2_pages pages = paged(a[3], "cache", B, T, prm);
+    const int32_t *sl = lengths(a[4], B), *counts = words(a[6], "n_new", B, " must be [batch]");
+    infllmv2_rotation rot{};
+    if (a[7] != Py_None) rot = rotation(a[7]);
+    const int32_t *pos = words(a[8], "positions", B * n, " must be [batch, new tokens]");
+    const at::Tensor *q = a[9] == Py_None ? nullptr : &query(a[9], "q", B, n, prm);
+    expect(!q || q->size(1) == n, "q", " must have the rows of k_new");
+    expect(q || a[10] == Py_None, "q_out", ": there is no q for it");
+    Result qo(a[10]);
+    infllmv2_tensor qd{}, qod{};
+    if (q) {
+        if (qo.make()) qo.own = at::zeros_like(*q);       // (rows of skipped sequences and behind n_new are not written)
+        qd = rows(*q);
+        qod = rows(qo.make() ? qo.own : query(qo.given, "q_out", B, n, prm));
+    }
+    const infllmv2_tensor knd = cache(kn), vnd = cache(vn);
+    run("infllmv2_paged_append", [&] {
+        return lib.paged_append(prm, a[7] != Py_None ? &rot : nullptr, &knd, &vnd, q ? &qd : nullptr, &pages, pos, counts, sl, static_cast<int32_t>(B), T,
+                                static_cast<int32_t>(n), q ? &qod : nullptr, current_stream());
+    });
+    if (q) return qo.release();
+    Py_RETURN_NONE;
+}
+
+// (prm, q, cache, seqlens, max_seqlen, n_new | None, out | None, lse | None, workspace | None)
+PyObject *paged_attn(Args a) {
+    const infllmv2_params *prm = enter(a[0]);
+    const int32_t T = capacity(a[4]);
+    const at::Tensor &q = query(a[1], "q", -1, 1, prm);
+    const int64_t B = q.size(0), n = q.size(1);
+    expect(n < (1ll << 31), "q", ": too many rows");
+    const infllmv2_pages pages = paged(a[2], "cache", B, T, prm);
+    const int32_t *sl = lengths(a[3], B), *counts = words(a[5], "n_new", B, " must be [batch]");
+    Attended r(a[6], a[7], q, n, {B, n, prm->n_q_heads}, true, prm);
+    const Workspace ws = scratch(a[8], a[8] == Py_None ? lib.paged_workspace_bytes(INFLLMV2_OP_PAGED_ATTN, prm, static_cast<int32_t>(B), T, static_cast<int32_t>(n)) : 0, q);
+    const infllmv2_tensor qd = rows(q);
+    run("infllmv2_paged_attn", [&] {
+        return lib.paged_attn(prm, &qd, &pages, counts, sl, static_cast<int32_t>(B), T, static_cast<int32_t>(n), &r.od, r.lp, ws.ptr, ws.bytes, current_stream(), r.fill);
+    });
+    return tuple2(r.out, r.lse);
+}
+
+// (prm, q, lse, cache, seqlens, max_seqlen, n_new | None, weights | None, weights_out | None, workspace | None)
+PyObject *paged_attn_weights(Args a) {
+    const infllmv2_params *prm = enter(a[0]);
+    const int32_t T = capacity(a[5]);
+    const at::Tensor &q = query(a[1], "q", -1, 1, prm);
+    const int64_t B = q.size(0), n = q.size(1), H = prm->n_kv_heads;
+    expect(n < (1ll << 31), "q", ": too many rows");
+    const float *lp = lse_of(tensor(a[2], "lse"), B * n * prm->n_q_heads);
+    const infllmv2_pages pages = paged(a[3], "cache", B, T, prm);
+    const int32_t *sl = lengths(a[4], B), *counts = words(a[6], "n_new", B, " must be [batch]");
+    const at::Tensor *had = a[7] == Py_None ? nullptr : &tensor(a[7], "weights");
+    Result wo(a[8]);
+    int64_t pitch = T;
+    if (had) {
+        floats(*had, "weights", B, H, T);
+        pitch = had->size(2);
+    } else if (!wo.make()) {
+        pitch = floats(tensor(wo.given, "weights_out"), "weights_out", B, H, T) ? tensor(wo.given, "weights_out").size(2) : T;
+    }
+    expect(pitch < (1ll << 31), "weights", ": too many rows");
+    if (wo.make()) wo.own = at::zeros({B, H, pitch}, like(q, at::kFloat));   // (entries behind a sequence are not written)
+    const at::Tensor &w = wo.make() ? wo.own : tensor(wo.given, "weights_out");
+    float *wp = floats(w, "weights_out", B, H, T);
+    expect(w.size(2) == pitch, "weights_out", " must have the shape of weights");
+    const Workspace ws = scratch(a[9], a[9] == Py_None ? lib.paged_workspace_bytes(INFLLMV2_OP_PAGED_WEIGHTS, prm, static_cast<int32_t>(B), T, static_cast<int32_t>(n)) : 0, q);
+    const infllmv2_tensor qd = rows(q);
+    run("infllmv2_paged_attn_weights", [&] {
+        return lib.paged_attn_weights(prm, &qd, lp, &pages, counts, sl, static_cast<int32_t>(B), T, static_cast<int32_t>(n),
+                                      had ? static_cast<const float *>(had->data_ptr()) : nullptr, static_cast<int32_t>(pitch), wp, ws.ptr, ws.bytes, current_stream());
+    });
+    return wo.release();
+}
+
+// (prm, weights, cache, seqlens, max_seqlen, budget, n_first, n_recent, to, kept | None, weights_out | None, seqlens_out | None, workspace | None)
+PyObject *paged_evict(Args a) {
+    const infllmv2_params *prm = enter(a[0]);
+    const int32_t T = capacity(a[4]), budget = integer(a[5]), first = integer(a[6]), recent = integer(a[7]);
+    expect(budget >= 1, "budget", " must be positive");
+    const at::Tensor &w = tensor(a[1], "weights");
+    int64_t B;
+    const infllmv2_pages from = paged(a[2], "cache", -1, T, prm, &B), to = paged(a[8], "to", B, budget, prm);
+    const int64_t H = prm->n_kv_heads;
+    const float *wp = floats(w, "weights", B, H, T);
+    expect(w.size(2) < (1ll << 31), "weights", ": too many rows");
+    const int32_t *sl = lengths(a[3], B);
+    Result kept(a[9]), wo(a[10]), so(a[11]);
+    if (kept.make()) kept.own = at::empty({B, H, budget}, like(w, at::kInt));
+    if (wo.make()) wo.own = at::empty({B, H, budget}, like(w, at::kFloat));
+    if (so.make()) so.own = at::empty({B}, like(w, at::kInt));
+    int32_t *kp = kept.make() ? static_cast<int32_t *>(kept.own.data_ptr()) : const_cast<int32_t *>(words(kept.given, "kept", B * H * budget, " must be [batch, n_kv_heads, budget]"));
+    int32_t *sp = so.make() ? static_cast<int32_t *>(so.own.data_ptr()) : const_cast<int32_t *>(words(so.given, "seqlens_out", B, " must be [batch]"));
+    const at::Tensor &wot = wo.make() ? wo.own : tensor(wo.given, "weights_out");
+    float *wop = floats(wot, "weights_out", B, H, budget);
+    expect(wot.size(2) == budget, "weights_out", " must be [batch, n_kv_heads, budget]");
+    const Workspace ws = scratch(a[12], a[12] == Py_None ? lib.paged_workspace_bytes(INFLLMV2_OP_PAGED_EVICT, prm, static_cast<int32_t>(B), T, 1) : 0, w);
+    run("infllmv2_paged_evict", [&] {
+        return lib.paged_evict(prm, wp, static_cast<int32_t>(w.size(2)), &from, sl, static_cast<int32_t>(B), T, budget, first, recent, &to, kp, wop, sp, ws.ptr,
+                               ws.bytes, current_stream());
+    });
+    return tuple3(kept, wo, so);
+}
+
 // (path, error class): the library every later call goes through
 PyObject *bind(Args a) {
     const char *path = PyUnicode_AsUTF8(a[0]);
@@ -723,6 +931,12 @@ PyObject *bind(Args a) {
     symbol(handle, "infllmv2i_window_attn_prefill", l.window_attn_prefill);
     symbol(handle, "infllmv2i_window_attn_bwd", l.window_attn_bwd);
     symbol(handle, "infllmv2i_window_bwd_scratch_bytes", l.window_bwd_scratch_bytes);
+    symbol(handle, "infllmv2i_rope", l.rope);
+    symbol(handle, "infllmv2_paged_workspace_bytes", l.paged_workspace_bytes);
+    symbol(handle, "infllmv2_paged_append", l.paged_append);
+    symbol(handle, "infllmv2i_paged_attn", l.paged_attn);
+    symbol(handle, "infllmv2_paged_attn_weights", l.paged_attn_weights);
+    symbol(handle, "infllmv2_paged_evict", l.paged_evict);
     lib = l;
     Py_RETURN_NONE;
 }
@@ -766,6 +980,11 @@ PyMethodDef methods[] = {
     METHOD(window_attn_bwd, 15),
     METHOD(window_attn_decode, 11),
     METHOD(window_attn_decode_quant, 11),
+    METHOD(rope, 10),
+    METHOD(paged_append, 11),
+    METHOD(paged_attn, 9),
+    METHOD(paged_attn_weights, 10),
+    METHOD(paged_evict, 13),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,500 @@
+// Attention of a sequence's new tokens over its cache in pages, causal among themselves.
+//
+// Query rows are (token, head of the group) with the heads fastest.  Up to 16 of them (single tokens) are the columns of 16x16x32 products, and a
+// workgroup's wavefronts take units of 32 keys in turn; more are taken 128 to a workgroup, 32 to a wavefront, all wavefronts at the same unit.  Keys are split
+// over workgroups where rows are few, and a second kernel joins the parts.
+//
+// Probabilities are 2^(score - m - shift).  m is a whole number near the running maximum, so rescaling by its changes is exact, and it follows only where scores
+// exceed it by more than 2^kSlack.  2^shift exceeds the sum of probabilities that a row can have by then, so values up to the largest of their type do not
+// overflow in the sums, which are divided at the end.
+#include "paged.h"
+
+namespace infllmv2 {
+
+constexpr int kChunkRows = 128;
+constexpr float kSlack = 8.f;
+
+__device__ __forceinline__ int shift_of(int L) { return 32 - __builtin_clz((uint32_t)max(L, 1)) + (int)kSlack; }
+
+// A row's running maximum (a whole number) with a tile's largest score: whether it moves, and by what the sums are multiplied then.
+__device__ __forceinline__ float follow(float &m, float mx) {
+    const float m_new = fmaxf(m, __builtin_ceilf(mx)), alpha = fast_exp2(m - (m_new == -INFINITY ? 0.f : m_new));
+    m = m_new;
+    return alpha;
+}
+
+// The halves of words that are infinities or NaN taken out; -> whether there were any.
+__device__ __forceinline__ bool take_odd_out(bf16x8 &x) {
+    u32x4_t y = __builtin_bit_cast(u32x4_t, x);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool low = (y[i] & 0x7f80u) == 0x7f80u, high = (y[i] & 0x7f800000u) == 0x7f800000u;
+        y[i] = (low ? 0u : y[i] & 0xffffu) | (high ? 0u : y[i] & 0xffff0000u);
+        odd |= low | high;
+    }
+    x = __builtin_bit_cast(bf16x8, y);
+    return odd;
+}
+// What a value that is not finite adds to a row that sees it.
+__device__ __forceinline__ float odd_value(uint2 y, int e, bool sees) {
+    const uint32_t w = e < 2 ? y.x : y.y;
+    const float z = __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    return sees && !(__builtin_fabsf(z) < INFINITY) ? z : 0.f;
+}
+
+// Probabilities rounded to bf16 may add up to 2^-8 more than their sum, and a mean of values near the largest would round to an infinity.
+__device__ __forceinline__ float mean(float x) {
+    constexpr float most = 3.3895313892515355e38f;       // bf16's largest
+    return __builtin_fabsf(x) < INFINITY ? __builtin_amdgcn_fmed3f(x, -most, most) : x;
+}
+
+// ---- 128 rows ------------------------------------------------------------------------------------------------------------
+
+// A wavefront's 32 rows: lane 32 hf + c holds row c.
+struct ChunkRows {
+    float scale, shift;
+    int hf, i, lo, hi;                                   // position of the lane's row; of the wavefront's first and last row
+    TileReader rd;
+    bf16x8 q[8];
+    f32x16 o[4];                                         // channels 32 ct + 8 (e / 4) + 4 hf + e % 4
+    float m, l;                                          // l: of this lane's keys
+    __device__ __forceinline__ explicit ChunkRows(int lane) : hf(lane >> 5), rd(lane), m(-INFINITY), l(0.f) {}
+
+    // keys k0 .. k0 + 31; pages: bit 0 those of the first 16 are there, bit 1 of the others
+    __device__ __forceinline__ void take(const KVHalf &cur, int k0, uint32_t pages) {
+        f32x16 s = zero16();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) s = mfma32(rd.rows(cur.k, ks), q[ks], s);
+        const bool whole = k0 + 31 <= lo && pages == 3u;
+        if (!whole) {
+            int at = i - k0 - 4 * hf;                    // keys up to this one are seen
+            asm volatile("" : "+v"(at));
+            const int at0 = pages & 1u ? at : -1, at1 = pages & 2u ? at : -1;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= (e < 8 ? at0 : at1) ? s[e] : -INFINITY;
+        }
+        float mx = max3(s[0], s[1], s[2]);
+#pragma unroll
+        for (int e = 3; e < 15; e += 2) mx = max3(mx, s[e], s[e + 1]);
+        mx = half_reduce(max3(mx, s[15], s[15]), [](float a, float d) { return fmaxf(a, d); }) * scale;
+        if (__any(mx > m + kSlack)) {
+            const float alpha = follow(m, mx);
+            l *= alpha;
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) o[ct] *= alpha;
+        }
+        const float base = (m == -INFINITY ? 0.f : m) + shift;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = fast_exp2(__builtin_fmaf(s[e], scale, -base));
+            sum[e & 1] += s[e];
+        }
+        l += sum[0] + sum[1];
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8 p = pack8(s, j);            // (bf16: what the matrix cores multiply; the sum is of what they were)
+#pragma unroll
+                for (int ct = 0; ct < 4; ++ct) o[ct] = mfma32(rd.columns(cur.v, j, ct), p, o[ct]);
+            }
+            return;
+        }
+        // A product multiplies a key that a row does not see by 0, and 0 times an infinity or a NaN reaches the row's sum: such values are left out, and added to
+        // the rows that see them.
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const bf16x8 p = pack8(s, j);
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) {
+                bf16x8 x = rd.columns(cur.v, j, ct);
+                odd |= take_odd_out(x);
+                o[ct] = mfma32(x, p, o[ct]);
+            }
+        }
+        if (!__any(odd)) return;
+#pragma unroll 1
+        for (int t = 0; t < 32; ++t) {
+            const bool sees = k0 + t <= i;               // (rows without a page read as zeros)
+            const char *row = cur.v + 64 * t + 8 * hf;
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const uint2 y = *reinterpret_cast<const uint2 *>(row + ct * 2048 + ((e4 ^ ((t >> 2) & 3)) << 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        o[ct][4 * e4 + e] += odd_value(y, e, sees);
+                        __builtin_amdgcn_sched_barrier(0);               // (registers)
+                    }
+                }
+        }
+    }
+};
+
+// Items: (sequence, head), part of the keys, tile of 128 rows, the last fastest.
+__global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_split, int run, Tensor q,
+                                                            const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse,
+                                                            float *__restrict__ o_part, float2 *__restrict__ ml_part) {
+    __shared__ KVHalf slot0, slot1, slot2;
+    const int item = xcd_item(blockIdx.x, run), bs = item / n_tiles, bh = bs / n_split, split = bs - bh * n_split, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    if (b >= dm.batch) return;
+    const int ti = (bs + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Chunk ch(nt, seqlens, b, dm.max_seqlen);
+    const int t0 = ti * (kChunkRows >> lg), t1 = min(ch.n, t0 + (kChunkRows >> lg));
+    ChunkRows r(lane);
+    const int row = 32 * wave + (lane & 31), token = t0 + (row >> lg), hq = h * dm.G + (row & (dm.G - 1));
+    const int end = ch.L > 0 && t0 < ch.n ? ch.before + t1 : 0;          // keys that the workgroup's rows see
+    const int units = (end + 31) >> 5, u0 = (int)((int64_t)units * split / n_split), count = (int)((int64_t)units * (split + 1) / n_split) - u0;
+    if (t0 >= ch.n && (n_split > 1 || !dm.fill)) return;
+    r.scale = dm.scale_log2;
+    r.shift = (float)shift_of(ch.L);
+    r.i = ch.before + token;
+    r.lo = ch.before + t0 + ((32 * wave) >> lg);
+    r.hi = t0 + ((32 * wave) >> lg) < ch.n ? min(ch.before + t0 + ((32 * wave + 31) >> lg), end - 1) : -1;   // (rows behind the last token: nothing)
+    {
+        const __bf16 *qr = q.ptr + b * q.sb + (int64_t)max(0, min(token, ch.n - 1)) * q.st + (int64_t)hq * q.sh + 8 * r.hf;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) r.q[ks] = load8(qr + 16 * ks);
+    }
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) r.o[ct] = zero16();
+    const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh) + 64 * wave, *v_head = reinterpret_cast<const char *>(pg.v.ptr + h * pg.v.sh) + 64 * wave;
+    const uint32_t k_at = (lane >> 2) * (2 * (uint32_t)pg.k.st) + 16 * copy_piece(lane), v_at = (lane >> 2) * (2 * (uint32_t)pg.v.st) + 16 * copy_piece(lane);
+    const int32_t *table = pg.table + (int64_t)b * pg.ld;
+    UnitPages up;
+    // unit x into a slot, four copies of 16 rows each; -> which of its halves have a page.  Those past the last bring zeros.
+    auto stage = [&](KVHalf &dst, int x) __attribute__((always_inline)) -> uint32_t {
+        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + x + lane), x + lane < count ? end : 0);
+        uint32_t there = 0u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int page = __builtin_amdgcn_readlane(j ? up.hi : up.lo, x & 63), first = 32 * (u0 + x) + 16 * j;
+            const bool some = page >= 0, in = some && first + (lane >> 2) < end;
+            there |= some ? 1u << j : 0u;
+            copy_rows(dst.k + wave * 2048 + j * 1024, k_head + page_bytes(pg.k, pg.lg, max(page, 0), first), in ? k_at : kNoRow, 0);
+            copy_rows(dst.v + wave * 2048 + j * 1024, v_head + page_bytes(pg.v, pg.lg, max(page, 0), first), in ? v_at : kNoRow, 0);
+        }
+        return there;
+    };
+    uint32_t p0 = stage(slot0, 0), p1 = stage(slot1, 1), p2 = 0u;
+    auto step = [&](const KVHalf &cur, KVHalf &next, uint32_t pages, uint32_t &pages_next, int x) __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0f74);              // all copies but the next unit's four
+        asm volatile("s_barrier" ::: "memory");          // everyone's, and everyone is past the unit before
+        __builtin_amdgcn_sched_barrier(0);
+        pages_next = stage(next, x + 2);
+        const int k0 = 32 * (u0 + x);
+        if (k0 <= r.hi) r.take(cur, k0, pages);
+    };
+    for (int x = 0; x < count; x += 3) {
+        step(slot0, slot2, p0, p2, x);
+        if (x + 1 < count) step(slot1, slot0, p1, p0, x + 1);
+        if (x + 2 < count) step(slot2, slot1, p2, p1, x + 2);
+    }
+    __builtin_amdgcn_s_waitcnt(0);                       // (the copies past the last unit have landed)
+    __syncthreads();
+    r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
+    const bool live = token < ch.n;
+    if (n_split > 1) {
+        if (!live) return;
+        const int64_t at = (((int64_t)b * nt.most + token) * dm.Hq + hq) * n_split + split;
+        if (r.hf == 0) ml_part[at] = float2{r.m + r.shift, r.l};
+        if (r.l != 0.f) {                                // (a NaN too)
+            float *op = o_part + at * kHeadDim + 4 * r.hf;
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4)
+                    *reinterpret_cast<f32x4 *>(op + 32 * ct + 8 * e4) = f32x4{r.o[ct][4 * e4], r.o[ct][4 * e4 + 1], r.o[ct][4 * e4 + 2], r.o[ct][4 * e4 + 3]};
+        }
+        return;
+    }
+    // rows that see no key, and those behind the last token where they are written: zeros
+    const bool some = live && r.l != 0.f;
+    const float inv = 1.f / r.l;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) r.o[ct][e] = some ? mean(r.o[ct][e] * inv) : 0.f;
+    store_rows((wave < 2 ? slot0.k : slot1.k) + (wave & 1) * kHalfTile, r.o, 1.f, lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
+        const int t = t0 + ((32 * wave + at) >> lg);
+        return t < nt.most && (t < ch.n || dm.fill) ? out.ptr + b * out.sb + (int64_t)t * out.st + (int64_t)(h * dm.G + ((32 * wave + at) & (dm.G - 1))) * out.sh : nullptr;
+    });
+    if (r.hf == 0 && token < nt.most && (live || dm.fill))
+        lse[((int64_t)b * nt.most + token) * dm.Hq + hq] = !live ? 0.f : some ? lse_of(r.m + r.shift, r.l) : -INFINITY;
+}
+
+// ---- up to 16 rows ---------------------------------------------------------------------------------------------------------
+
+// grid (parts of the keys, Hkv, batch).  Column c of the products: head c % G of new token c / G.  A wavefront has its keys in the registers of the first product and its
+// values in LDS, the next unit's under way.
+__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const int32_t *__restrict__ seqlens,
+                                                                Tensor out, float *__restrict__ lse, float *__restrict__ o_part,
+                                                                float2 *__restrict__ ml_part) {
+    __shared__ __align__(16) char V0[4][kHalfTile], V1[4][kHalfTile];
+    __shared__ float2 ml_s[4][16];
+    const int split = blockIdx.x, n_split = gridDim.x, h = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    const Chunk ch(nt, seqlens, b, dm.max_seqlen);
+    const int token = n >> lg, hq = h * dm.G + (n & (dm.G - 1));
+    bf16x8 bq[4];                                        // channels 32 ks + 8 g ..
+    {
+        const __bf16 *qr = q.ptr + b * q.sb + (int64_t)max(0, min(token, ch.n - 1)) * q.st + (int64_t)hq * q.sh + 8 * g;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) bq[ks] = load8(qr + 32 * ks);
+    }
+    const int end = ch.L, units = (end + 31) >> 5, u_end = (int)((int64_t)units * (split + 1) / n_split), u0 = (int)((int64_t)units * split / n_split) + wave;
+    const int count = u0 < u_end ? (u_end - u0 + 3) >> 2 : 0;            // units u0, u0 + 4, ..
+    const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh), *v_head = reinterpret_cast<const char *>(pg.v.ptr + h * pg.v.sh);
+    const uint32_t k_at = n * (2 * (uint32_t)pg.k.st) + 16 * g;
+    const int32_t *table = pg.table + (int64_t)b * pg.ld;
+    struct Unit {
+        bf16x8 k[2][4];
+        uint32_t there;
+        int k0;
+    };
+    UnitPages up;
+    auto fetch = [&](Unit &u, char *vs, int x) __attribute__((always_inline)) {
+        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + 4 * (x + lane)), x + lane < count ? end : 0);
+        u.k0 = 32 * (u0 + 4 * x);
+        u.there = 0u;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int page = __builtin_amdgcn_readlane(t ? up.hi : up.lo, x & 63), first = u.k0 + 16 * t;
+            const bool some = page >= 0;
+            u.there |= some ? 1u << t : 0u;
+            const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(k_head + page_bytes(pg.k, pg.lg, max(page, 0), first)), 0, 0xfffffffeu, 0x00027000);
+            const uint32_t at = some && first + n < end ? k_at : kNoRow;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+                u.k[t][ks] = __builtin_bit_cast(bf16x8, (u32x4_t)__builtin_amdgcn_raw_buffer_load_b128(from, at, 64 * ks, 0));
+            const char *vb = v_head + page_bytes(pg.v, pg.lg, max(page, 0), first);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                // 1 KiB: rows 4 i + lane / 16, whose 16-byte pieces are XORed with what row_swizzle says
+                const int r = 4 * i + g;
+                copy_rows(vs + 4096 * t + 1024 * i, vb, some && first + r < end ? r * (2 * (uint32_t)pg.v.st) + 16 * (n ^ row_swizzle(r)) : kNoRow, 0);
+            }
+        }
+    };
+    f32x4 o[8];                                          // o[c][e]: channel 16 c + 4 g + e of column n
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float shift = (float)shift_of(ch.L);
+    const int last = ch.before + min(token, ch.n - 1);   // the last key that this column sees
+    auto attend = [&](const Unit &u, const char *vs) __attribute__((always_inline)) {
+        f32x4 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) s[t] = mfma16(u.k[t][ks], bq[ks], s[t]);
+        }
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = s[e >> 2][e & 3];             // key 16 (e / 4) + 4 g + e % 4
+        const bool whole = u.k0 + 31 <= ch.before && u.there == 3u;
+        if (!whole) {
+            const int at = last - u.k0 - 4 * g, at0 = u.there & 1u ? at : -1, at1 = u.there & 2u ? at : -1;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = 16 * (e >> 2) + (e & 3) <= (e < 4 ? at0 : at1) ? y[e] : -INFINITY;
+        }
+        const float mx = xgroup_max(max3(max3(max3(y[0], y[1], y[2]), y[3], y[4]), max3(y[5], y[6], y[7]), y[7])) * dm.scale_log2;
+        if (__any(mx > m + kSlack)) {
+            const float alpha = follow(m, mx);
+            l *= alpha;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o[c] *= alpha;
+        }
+        const float base = (m == -INFINITY ? 0.f : m) + shift;
+        float ps = 0.f;
+        bf16x8 p;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float e = fast_exp2(__builtin_fmaf(y[j], dm.scale_log2, -base));
+            ps += e;
+            p[j] = (__bf16)e;
+        }
+        l += ps;                                         // (this lane's keys only: joined over g at the end)
+        const int r = 4 * g + (n >> 2);
+        bool odd = false;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {                    // A: channel 16 c + n, keys 4 g .. and 16 + 4 g ..
+            const char *at = vs + 8 * (n & 1);
+            const int piece = 2 * c + ((n & 3) >> 1);
+            const s16x4 x0 = lds_read_tr16(at + r * 256 + ((piece ^ row_swizzle(r)) << 4));
+            const s16x4 x1 = lds_read_tr16(at + (r + 16) * 256 + ((piece ^ row_swizzle(r)) << 4));
+            bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
+            if (!whole) odd |= take_odd_out(x);
+            o[c] = mfma16(x, p, o[c]);
+        }
+        if (whole || !__any(odd)) return;
+#pragma unroll 1
+        for (int t = 0; t < 32; ++t) {
+            const bool sees = u.k0 + t <= last;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const uint2 w = *reinterpret_cast<const uint2 *>(vs + 256 * t + (((2 * c + (g >> 1)) ^ row_swizzle(t)) << 4) + 8 * (g & 1));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[c][e] += odd_value(w, e, sees);
+            }
+        }
+    };
+    {
+        Unit a, c;
+        char *v0 = V0[wave], *v1 = V1[wave];
+        auto step = [&](Unit &cur, Unit &next, char *vc, char *vn, int x) __attribute__((always_inline)) {
+            reads_done();
+            if (x + 1 < count) fetch(next, vn, x + 1);
+            copies_landed(x + 1 < count);
+            attend(cur, vc);
+        };
+        if (count > 0) fetch(a, v0, 0);
+        for (int x = 0; x < count; x += 2) {
+            step(a, c, v0, v1, x);
+            if (x + 1 < count) step(c, a, v1, v0, x + 1);
+        }
+    }
+    reads_done();
+    l = xgroup_sum(l);
+    // ---- the wavefronts' states into one -----------------------------------------------------------------------------------
+    if (g == 0) ml_s[wave][n] = float2{m, l};
+    __syncthreads();
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) M = fmaxf(M, ml_s[i][n].x);
+    const float w = fast_exp2(m - (M == -INFINITY ? 0.f : M));
+    float *mine = reinterpret_cast<float *>(V0[wave]);   // [column][channel]
+#pragma unroll
+    for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (c ^ (n & 7)) + 4 * g) = o[c] * w;
+    __syncthreads();
+    const int col = tid >> 4, c8 = 8 * (tid & 15), ct = col >> lg;       // a thread joins eight channels of a column
+    if (ct >= nt.most || (ct >= ch.n && (n_split > 1 || !dm.fill))) return;
+    float den = 0.f, Mc = -INFINITY, y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
+    const float bc = Mc == -INFINITY ? 0.f : Mc;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        den += ml_s[i][col].y * fast_exp2(ml_s[i][col].x - bc);
+        const float *from = reinterpret_cast<const float *>(V0[i]) + col * kHeadDim + 16 * ((c8 >> 4) ^ (col & 7)) + (c8 & 15);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] += from[e];
+    }
+    const int hc = h * dm.G + (col & (dm.G - 1));
+    const int64_t row = ((int64_t)b * nt.most + ct) * dm.Hq + hc;
+    if (n_split == 1) {
+        const bool some = ct < ch.n && den != 0.f;
+        bf16x8 z;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = (__bf16)(some ? mean(y[e] / den) : 0.f);
+        *reinterpret_cast<uint4 *>(out.ptr + b * out.sb + (int64_t)ct * out.st + (int64_t)hc * out.sh + c8) = __builtin_bit_cast(uint4, z);
+        if (c8 == 0) lse[row] = ct >= ch.n ? 0.f : some ? lse_of(bc + shift, den) : -INFINITY;
+    } else {
+        const int64_t at = row * n_split + split;
+        if (den != 0.f) {
+            float4 *op = reinterpret_cast<float4 *>(o_part + at * kHeadDim + c8);
+            op[0] = float4{y[0], y[1], y[2], y[3]};
+            op[1] = float4{y[4], y[5], y[6], y[7]};
+        }
+        if (c8 == 0) ml_part[at] = float2{bc + shift, den};
+    }
+}
+
+// ---- joining the parts --------------------------------------------------------------------------------------------------------
+
+// 32 lanes to a row, four channels each.  A part whose sum is 0 has no channels.
+__global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, int64_t rows, const float *__restrict__ o_part,
+                                                          const float2 *__restrict__ ml_part, const int32_t *__restrict__ seqlens, Tensor out,
+                                                          float *__restrict__ lse) {
+    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const int c4 = 4 * (threadIdx.x & 31);
+    const int64_t bt = row / dm.Hq;
+    const int hq = (int)(row - bt * dm.Hq), b = (int)(bt / nt.most), t = (int)(bt - (int64_t)b * nt.most);
+    const int n = nt.counts ? clamp_len(nt.counts[b], nt.most) : nt.most;
+    if (t >= n && !dm.fill) return;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    float M = -INFINITY, den = 0.f;
+    const bool live = t < n && clamp_len(seqlens[b], dm.max_seqlen) >= n;
+    if (live) {
+        const float2 *ml = ml_part + row * n_split;
+        for (int s = 0; s < n_split; ++s) M = ml[s].y != 0.f ? fmaxf(M, ml[s].x) : M;
+        const float *o = o_part + row * n_split * kHeadDim + c4;
+        for (int s = 0; s < n_split; ++s) {
+            if (ml[s].y == 0.f) continue;
+            const float w = fast_exp2(ml[s].x - M);
+            den += ml[s].y * w;
+            y += *reinterpret_cast<const f32x4 *>(o + (int64_t)s * kHeadDim) * w;
+        }
+    }
+    const bool some = den != 0.f;
+    bf16x4 z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = (__bf16)(some ? mean(y[e] / den) : 0.f);
+    *reinterpret_cast<uint2 *>(out.ptr + b * out.sb + (int64_t)t * out.st + (int64_t)hq * out.sh + c4) = __builtin_bit_cast(uint2, z);
+    if (c4 == 0) lse[row] = t >= n ? 0.f : some ? lse_of(M, den) : -INFINITY;
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------------
+static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+constexpr int kMaxParts = 64;
+struct PagedPlan {
+    bool few;
+    int64_t items;                                       // of one part
+    int tiles, parts;
+};
+static int64_t most_parts(const Dims &dm) { return min((int64_t)kMaxParts, ((int64_t)dm.max_seqlen + 255) / 256); }   // 256 keys and more to a part
+static PagedPlan paged_plan(const Dims &dm, int max_new) {
+    PagedPlan p;
+    p.few = (int64_t)max_new * dm.G <= 16;
+    p.tiles = p.few ? 1 : (int)(((int64_t)max_new * dm.G + kChunkRows - 1) / kChunkRows);
+    p.items = (int64_t)dm.batch * dm.Hkv * p.tiles;
+    const int64_t chip = p.few ? 512 : 768;              // workgroups that run at a time
+    p.parts = p.items >= 512 ? 1 : (int)max((int64_t)1, min(most_parts(dm), (chip + p.items - 1) / max((int64_t)1, p.items)));
+    return p;
+}
+// (a bound that grows with each size: parts of a tile's 128 rows, no more than all tiles of the few-item calls can have)
+size_t paged_attn_ws_bytes(const Dims &dm, int max_new) {
+    if (dm.batch <= 0 || max_new <= 0) return 0;
+    const int64_t per = (int64_t)max_new * dm.G <= 16 ? 16 : kChunkRows;
+    const int64_t items = (int64_t)dm.batch * dm.Hkv * (((int64_t)max_new * dm.G + per - 1) / per), most = most_parts(dm);
+    if (most <= 1) return 0;
+    const size_t rows = (size_t)(min(min(items, (int64_t)512) * most, min(items, (int64_t)512) + 768) * per);
+    return align256(rows * kHeadDim * sizeof(float)) + align256(rows * sizeof(float2));
+}
+
+int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, const int32_t *seqlens, Tensor out, float *lse, void *ws, hipStream_t stream) {
+    if (dm.batch <= 0 || nt.most <= 0) return 0;
+    const int lg = __builtin_ctz(dm.G);
+    const PagedPlan p = paged_plan(dm, nt.most);
+    const int64_t rows = (int64_t)dm.batch * nt.most * dm.Hq;
+    float *o_part = reinterpret_cast<float *>(ws);
+    float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) + align256((size_t)rows * p.parts * kHeadDim * sizeof(float)));
+    if (p.few) {
+        timing_begin("paged_attn_few_kernel", stream);
+        hipLaunchKernelGGL(paged_attn_few_kernel, dim3(p.parts, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part);
+    } else {
+        const int64_t items = p.items * p.parts;
+        const int run = xcd_run_length(items);
+        timing_begin("paged_attn_kernel", stream);
+        hipLaunchKernelGGL(paged_attn_kernel, dim3(xcd_grid(items, run)), dim3(256), 0, stream, dm, pg, nt, lg, p.tiles, p.parts, run, q, seqlens, out, lse,
+                           o_part, ml_part);
+    }
+    timing_end(stream);
+    if (p.parts > 1) {
+        timing_begin("paged_merge_kernel", stream);
+        hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, seqlens, out, lse);
+        timing_end(stream);
+    }
+    return (int)hipGetLastError();
+}
+
+}  // namespace infllmv2

@@ -1,0 +1,154 @@
+// Eviction by weight: which rows of a sequence and head stay, and these rows, in order, into other pages.
+#include "paged.h"
+
+namespace infllmv2 {
+
+constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
+
+// Numbers in the order of the floats they are made of: -0 as 0, a NaN above all.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (x != x) return 0xffffffffu;
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// A workgroup to a sequence and head: the c-th largest weight of the rows that may go, by their eight highest bits, the next eight, ..; then the rows above it and the first
+// of those equal to it, in order.
+__global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const float *__restrict__ weights, int pitch, const int32_t *__restrict__ seqlens,
+                                                                  int budget, int first, int recent, int32_t *__restrict__ kept) {
+    __shared__ uint32_t hist[256];
+    __shared__ uint32_t found[2];                        // the digit, and how many are above it
+    __shared__ int2 counts[kPickWaves];
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
+    const int64_t bh = (int64_t)b * dm.Hkv + h;
+    int32_t *out = kept + bh * budget;
+    if (L <= budget) {
+        for (int j = tid; j < budget; j += kPickThreads) out[j] = j < L ? j : -1;
+        return;
+    }
+    for (int j = tid; j < first; j += kPickThreads) out[j] = j;
+    for (int j = tid; j < recent; j += kPickThreads) out[budget - recent + j] = L - recent + j;
+    const int lo = first, hi = L - recent, want = budget - first - recent;                     // want < hi - lo
+    if (want == 0) return;
+    const float *w = weights + bh * pitch;
+    uint32_t prefix = 0u, mask = 0u;
+    int left = want;                                     // how many of those with this prefix
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) hist[tid] = 0u;
+        __syncthreads();
+        for (int j = lo + tid; j < hi; j += kPickThreads) {
+            const uint32_t x = order_of(w[j]);
+            if ((x & mask) == prefix) atomicAdd(&hist[(x >> shift) & 255u], 1u);
+        }
+        __syncthreads();
+        if (wave == 0) {                                 // lane l: digits 255 - 4 l .., the highest first
+            uint32_t c[4], all = 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) all += c[i] = hist[255 - 4 * lane - i];
+            uint32_t upto = all;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t o = __shfl_up(upto, d);
+                upto += lane >= d ? o : 0u;
+            }
+            uint32_t above = upto - all;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (above < (uint32_t)left && (uint32_t)left <= above + c[i]) {
+                    found[0] = 255 - 4 * lane - i;
+                    found[1] = above;
+                }
+                above += c[i];
+            }
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        mask |= 255u << shift;
+        left -= (int)found[1];
+        __syncthreads();
+    }
+    // rows above `prefix`, and the first `left` of those equal to it; a wavefront takes a run of rows
+    const int each = ((hi - lo + kPickWaves - 1) / kPickWaves + 63) / 64 * 64, from = min(hi, lo + wave * each), to = min(hi, from + each);
+    int above = 0, equal = 0;
+    for (int j = from; j < to; j += 64) {
+        const uint32_t x = j + lane < to ? order_of(w[j + lane]) : 0u;
+        above += __popcll(__ballot(x > prefix));
+        equal += __popcll(__ballot(j + lane < to && x == prefix));
+    }
+    if (lane == 0) counts[wave] = int2{above, equal};
+    __syncthreads();
+    int at = first, ties = 0;                            // rows kept, and equal ones, before this run
+    for (int i = 0; i < wave; ++i) {
+        at += counts[i].x + min(counts[i].y, max(0, left - ties));
+        ties += counts[i].y;
+    }
+    for (int j = from; j < to; j += 64) {
+        const uint32_t x = j + lane < to ? order_of(w[j + lane]) : 0u;
+        const uint64_t below = (1ull << lane) - 1ull, eq = __ballot(j + lane < to && x == prefix);
+        const bool keep = j + lane < to && (x > prefix || (x == prefix && ties + __popcll(eq & below) < left));
+        const uint64_t who = __ballot(keep);
+        if (keep) out[at + __popcll(who & below)] = j + lane;
+        at += __popcll(who);
+        ties += __popcll(eq);
+    }
+}
+
+// 16 lanes to a row, 64 rows to a workgroup; grid (rows / 64, Hkv, batch).  Bound by traffic.
+__global__ __launch_bounds__(256) void evict_move_kernel(Dims dm, const float *__restrict__ weights, int pitch, Pages from, const int32_t *__restrict__ seqlens,
+                                                         int budget, Pages to, const int32_t *__restrict__ kept, float *__restrict__ weights_out,
+                                                         int32_t *__restrict__ seqlens_out) {
+    const int h = blockIdx.y, b = blockIdx.z, piece = threadIdx.x & 15;
+    const int64_t bh = (int64_t)b * dm.Hkv + h;
+    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) seqlens_out[b] = min(clamp_len(seqlens[b], dm.max_seqlen), budget);
+    const char *kf = reinterpret_cast<const char *>(from.k.ptr + h * from.k.sh) + 16 * piece, *vf = reinterpret_cast<const char *>(from.v.ptr + h * from.v.sh) + 16 * piece;
+    char *kt = reinterpret_cast<char *>(to.k.ptr + h * to.k.sh) + 16 * piece, *vt = reinterpret_cast<char *>(to.v.ptr + h * to.v.sh) + 16 * piece;
+    u32x4_t x[4], y[4];
+    int row[4], src[4], dst[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = 64 * blockIdx.x + 16 * i + (threadIdx.x >> 4);
+        row[i] = j < budget ? kept[bh * budget + j] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = 64 * blockIdx.x + 16 * i + (threadIdx.x >> 4);
+        src[i] = row[i] >= 0 ? from.table[(int64_t)b * from.ld + (row[i] >> from.lg)] : -1;
+        dst[i] = to.table[(int64_t)b * to.ld + (min(j, budget - 1) >> to.lg)];
+        if (weights_out && piece == 0 && j < budget) weights_out[bh * budget + j] = row[i] >= 0 ? weights[bh * pitch + row[i]] : 0.f;
+    }
+    bool moves[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        moves[i] = (uint32_t)src[i] < (uint32_t)from.count && (uint32_t)dst[i] < (uint32_t)to.count;
+        x[i] = y[i] = u32x4_t{0u, 0u, 0u, 0u};
+        if (moves[i]) {
+            x[i] = *reinterpret_cast<const u32x4_t *>(kf + page_bytes(from.k, from.lg, src[i], row[i]));
+            y[i] = *reinterpret_cast<const u32x4_t *>(vf + page_bytes(from.v, from.lg, src[i], row[i]));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = 64 * blockIdx.x + 16 * i + (threadIdx.x >> 4);
+        if (!moves[i]) continue;
+        *reinterpret_cast<u32x4_t *>(kt + page_bytes(to.k, to.lg, dst[i], j)) = x[i];
+        *reinterpret_cast<u32x4_t *>(vt + page_bytes(to.v, to.lg, dst[i], j)) = y[i];
+    }
+}
+
+size_t paged_evict_ws_bytes(const Dims &) { return 0; }
+
+int launch_paged_evict(const Dims &dm, const float *weights, int pitch, const Pages &from, const int32_t *seqlens, int budget, int first, int recent,
+                       const Pages &to, int32_t *kept, float *weights_out, int32_t *seqlens_out, void *, hipStream_t stream) {
+    if (dm.batch <= 0) return 0;
+    timing_begin("evict_pick_kernel", stream);
+    hipLaunchKernelGGL(evict_pick_kernel, dim3(dm.Hkv, dm.batch), dim3(kPickThreads), 0, stream, dm, weights, pitch, seqlens, budget, first, recent, kept);
+    timing_end(stream);
+    timing_begin("evict_move_kernel", stream);
+    hipLaunchKernelGGL(evict_move_kernel, dim3((budget + 63) / 64, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, weights, pitch, from, seqlens, budget, to, kept,
+                       weights_out, seqlens_out);
+    timing_end(stream);
+    return (int)hipGetLastError();
+}
+
+}  // namespace infllmv2
