@@ -11,6 +11,8 @@
 
 namespace infllmv2 {
 
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
 constexpr int kChunkRows = 128;
 constexpr float kSlack = 8.f;
 
@@ -54,26 +56,15 @@ __device__ __forceinline__ float mean(float x) {
 // A wavefront's 32 rows: lane 32 hf + c holds row c.
 struct ChunkRows {
     float scale, shift;
-    int hf, i, lo, hi;                                   // position of the lane's row; of the wavefront's first and last row
+    int hf, i;                                           // position of the lane's row
     TileReader rd;
     bf16x8 q[8];
     f32x16 o[4];                                         // channels 32 ct + 8 (e / 4) + 4 hf + e % 4
     float m, l;                                          // l: of this lane's keys
     __device__ __forceinline__ explicit ChunkRows(int lane) : hf(lane >> 5), rd(lane), m(-INFINITY), l(0.f) {}
 
-    // keys k0 .. k0 + 31; pages: bit 0 those of the first 16 are there, bit 1 of the others
-    __device__ __forceinline__ void take(const KVHalf &cur, int k0, uint32_t pages) {
-        f32x16 s = zero16();
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) s = mfma32(rd.rows(cur.k, ks), q[ks], s);
-        const bool whole = k0 + 31 <= lo && pages == 3u;
-        if (!whole) {
-            int at = i - k0 - 4 * hf;                    // keys up to this one are seen
-            asm volatile("" : "+v"(at));
-            const int at0 = pages & 1u ? at : -1, at1 = pages & 2u ? at : -1;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= (e < 8 ? at0 : at1) ? s[e] : -INFINITY;
-        }
+    // A unit's scores to probabilities, in place; rows' sums and, where maxima move, all that was added up follow.
+    __device__ __forceinline__ void probabilities(f32x16 &s) {
         float mx = max3(s[0], s[1], s[2]);
 #pragma unroll
         for (int e = 3; e < 15; e += 2) mx = max3(mx, s[e], s[e + 1]);
@@ -92,17 +83,32 @@ struct ChunkRows {
             sum[e & 1] += s[e];
         }
         l += sum[0] + sum[1];
-        if (whole) {
+    }
+    __device__ __forceinline__ f32x16 scores(const char *k) const {
+        f32x16 s = zero16();
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bf16x8 p = pack8(s, j);            // (bf16: what the matrix cores multiply; the sum is of what they were)
+        for (int ks = 0; ks < 8; ++ks) s = mfma32(rd.rows(k, ks), q[ks], s);
+        return s;
+    }
+    // 32 keys that all of the workgroup's rows see
+    __device__ __forceinline__ void take(const KVHalf &cur) {
+        f32x16 s = scores(cur.k);
+        probabilities(s);
 #pragma unroll
-                for (int ct = 0; ct < 4; ++ct) o[ct] = mfma32(rd.columns(cur.v, j, ct), p, o[ct]);
-            }
-            return;
+        for (int j = 0; j < 2; ++j) {
+            const bf16x8 p = pack8(s, j);                // (bf16: what the matrix cores multiply; the sum is of what they were)
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) o[ct] = mfma32(rd.columns(cur.v, j, ct), p, o[ct]);
         }
-        // A product multiplies a key that a row does not see by 0, and 0 times an infinity or a NaN reaches the row's sum: such values are left out, and added to
-        // the rows that see them.
+    }
+    // Keys k0 .. k0 + 31 that not all rows see; pages: bit 0 those of the first 16 have one, bit 1 of the others.  A product multiplies a key that a row does not see by 0, and 0 times an infinity or a NaN reaches the row's sum: such values
+    // are left out, and added to the rows that see them.
+    __device__ __forceinline__ void take_edge(const KVHalf &cur, int k0, uint32_t pages) {
+        f32x16 s = scores(cur.k);
+        const int at = i - k0 - 4 * hf, at0 = pages & 1u ? at : -1, at1 = pages & 2u ? at : -1;      // keys up to this one are seen
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= (e < 8 ? at0 : at1) ? s[e] : -INFINITY;
+        probabilities(s);
         bool odd = false;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -112,6 +118,7 @@ struct ChunkRows {
                 bf16x8 x = rd.columns(cur.v, j, ct);
                 odd |= take_odd_out(x);
                 o[ct] = mfma32(x, p, o[ct]);
+                __builtin_amdgcn_sched_barrier(0);       // (registers)
             }
         }
         if (!__any(odd)) return;
@@ -127,7 +134,7 @@ struct ChunkRows {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         o[ct][4 * e4 + e] += odd_value(y, e, sees);
-                        __builtin_amdgcn_sched_barrier(0);               // (registers)
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 }
         }
@@ -153,8 +160,6 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
     r.scale = dm.scale_log2;
     r.shift = (float)shift_of(ch.L);
     r.i = ch.before + token;
-    r.lo = ch.before + t0 + ((32 * wave) >> lg);
-    r.hi = t0 + ((32 * wave) >> lg) < ch.n ? min(ch.before + t0 + ((32 * wave + 31) >> lg), end - 1) : -1;   // (rows behind the last token: nothing)
     {
         const __bf16 *qr = q.ptr + b * q.sb + (int64_t)max(0, min(token, ch.n - 1)) * q.st + (int64_t)hq * q.sh + 8 * r.hf;
 #pragma unroll
@@ -166,9 +171,11 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
     const uint32_t k_at = (lane >> 2) * (2 * (uint32_t)pg.k.st) + 16 * copy_piece(lane), v_at = (lane >> 2) * (2 * (uint32_t)pg.v.st) + 16 * copy_piece(lane);
     const int32_t *table = pg.table + (int64_t)b * pg.ld;
     UnitPages up;
+    auto look_up = [&](int x) __attribute__((always_inline)) {           // (before the wait for copies: behind it the compiler would wait for all of them)
+        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + x + lane), x + lane < count ? end : 0);
+    };
     // unit x into a slot, four copies of 16 rows each; -> which of its halves have a page.  Those past the last bring zeros.
     auto stage = [&](KVHalf &dst, int x) __attribute__((always_inline)) -> uint32_t {
-        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + x + lane), x + lane < count ? end : 0);
         uint32_t there = 0u;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -180,20 +187,42 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
         }
         return there;
     };
-    uint32_t p0 = stage(slot0, 0), p1 = stage(slot1, 1), p2 = 0u;
-    auto step = [&](const KVHalf &cur, KVHalf &next, uint32_t pages, uint32_t &pages_next, int x) __attribute__((always_inline)) {
+    // Unit x lies in slot x % 3.  The first `whole` are seen by all rows; from the first of them that has no page on, all are taken as the others are.
+    look_up(0);
+    uint32_t p0 = stage(slot0, 0), p1 = stage(slot1, 1), p2 = 3u;
+    int whole = max(0, min(count, ((ch.before + t0 + 1) >> 5) - u0));
+    if (p1 != 3u) whole = min(whole, 1);
+    if (p0 != 3u) whole = 0;
+    const bool alive = t0 + ((32 * wave) >> lg) < ch.n;  // (of no token: these rows only help to fetch)
+    auto arrived = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0f74);              // all copies but the next unit's four
         asm volatile("s_barrier" ::: "memory");          // everyone's, and everyone is past the unit before
         __builtin_amdgcn_sched_barrier(0);
-        pages_next = stage(next, x + 2);
-        const int k0 = 32 * (u0 + x);
-        if (k0 <= r.hi) r.take(cur, k0, pages);
     };
-    for (int x = 0; x < count; x += 3) {
-        step(slot0, slot2, p0, p2, x);
-        if (x + 1 < count) step(slot1, slot0, p1, p0, x + 1);
-        if (x + 2 < count) step(slot2, slot1, p2, p1, x + 2);
+    auto step = [&](const KVHalf &cur, KVHalf &next, uint32_t &pages_next, int x) __attribute__((always_inline)) {
+        look_up(x + 2);
+        arrived();
+        pages_next = stage(next, x + 2);
+        whole = pages_next != 3u ? min(whole, x + 2) : whole;
+        if (alive) r.take(cur);
+    };
+    for (int x = 0; x < whole; x += 3) {
+        step(slot0, slot2, p2, x);
+        if (x + 1 < whole) step(slot1, slot0, p0, x + 1);
+        if (x + 2 < whole) step(slot2, slot1, p1, x + 2);
+    }
+#pragma unroll 1
+    for (int x = whole; x < count; ++x) {
+        const int at = x % 3;
+        KVHalf *const cur = at == 0 ? &slot0 : at == 1 ? &slot1 : &slot2, *const next = at == 0 ? &slot2 : at == 1 ? &slot0 : &slot1;
+        look_up(x + 2);
+        arrived();
+        const uint32_t there = at == 0 ? p0 : at == 1 ? p1 : p2, then = stage(*next, x + 2);
+        p0 = at == 1 ? then : p0;
+        p1 = at == 2 ? then : p1;
+        p2 = at == 0 ? then : p2;
+        if (alive) r.take_edge(*cur, 32 * (u0 + x), there);
     }
     __builtin_amdgcn_s_waitcnt(0);                       // (the copies past the last unit have landed)
     __syncthreads();
@@ -293,6 +322,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(Dims dm, Pages p
             s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) s[t] = mfma16(u.k[t][ks], bq[ks], s[t]);
+            settle(s[t]);
         }
         float y[8];
 #pragma unroll
@@ -409,37 +439,61 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(Dims dm, Pages p
 
 // ---- joining the parts --------------------------------------------------------------------------------------------------------
 
-// 32 lanes to a row, four channels each.  A part whose sum is 0 has no channels.
+// kWaves wavefronts to a row, two channels to a lane, parts wave, wave + kWaves, ..: all of its parts' channels are asked for before any is used, so a row costs two round trips.
+// A part whose sum is 0 has no channels; one that has stands in for it.
+template <int kWaves>
 __global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, int64_t rows, const float *__restrict__ o_part,
                                                           const float2 *__restrict__ ml_part, const int32_t *__restrict__ seqlens, Tensor out,
                                                           float *__restrict__ lse) {
-    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row >= rows) return;
-    const int c4 = 4 * (threadIdx.x & 31);
+    __shared__ f32x2_t joined[4][64];
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % kWaves;
+    const int64_t row = (int64_t)blockIdx.x * (4 / kWaves) + id / kWaves;
+    if (row >= rows) return;                             // (kWaves = 1 where a workgroup has more than one row: no barrier follows)
     const int64_t bt = row / dm.Hq;
     const int hq = (int)(row - bt * dm.Hq), b = (int)(bt / nt.most), t = (int)(bt - (int64_t)b * nt.most);
-    const int n = nt.counts ? clamp_len(nt.counts[b], nt.most) : nt.most;
+    const int n = nt.counts ? clamp_len(uniform_load(nt.counts + b), nt.most) : nt.most;
     if (t >= n && !dm.fill) return;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    float M = -INFINITY, den = 0.f;
-    const bool live = t < n && clamp_len(seqlens[b], dm.max_seqlen) >= n;
-    if (live) {
-        const float2 *ml = ml_part + row * n_split;
-        for (int s = 0; s < n_split; ++s) M = ml[s].y != 0.f ? fmaxf(M, ml[s].x) : M;
-        const float *o = o_part + row * n_split * kHeadDim + c4;
-        for (int s = 0; s < n_split; ++s) {
-            if (ml[s].y == 0.f) continue;
-            const float w = fast_exp2(ml[s].x - M);
-            den += ml[s].y * w;
-            y += *reinterpret_cast<const f32x4 *>(o + (int64_t)s * kHeadDim) * w;
+    const bool live = t < n && clamp_len(uniform_load(seqlens + b), dm.max_seqlen) >= n;
+    const float2 ml = live && lane < n_split ? ml_part[row * n_split + lane] : float2{-INFINITY, 0.f};
+    const uint64_t have = __ballot(ml.y != 0.f);         // (a NaN too)
+    float M = ml.y != 0.f ? ml.x : -INFINITY, den = 0.f;
+    f32x2_t y = {0.f, 0.f};
+    if (have) {
+        M = row_reduce(M, [](float a, float d) { return fmaxf(a, d); });
+        M = xgroup_max(M);
+        const float w = ml.y != 0.f ? fast_exp2(ml.x - M) : 0.f;
+        den = row_reduce(ml.y != 0.f ? ml.y * w : 0.f, [](float a, float d) { return a + d; });
+        den = xgroup_sum(den);
+        const int first = __builtin_ctzll(have);
+        const float *o = o_part + row * n_split * kHeadDim + 2 * lane;
+        constexpr int kStep = 16;
+        for (int s0 = wave; s0 < n_split; s0 += kStep * kWaves) {
+            f32x2_t x[kStep];
+#pragma unroll
+            for (int i = 0; i < kStep; ++i) {
+                const int s = s0 + kWaves * i, at = s < n_split && (have >> (s & 63)) & 1ull ? s : first;
+                x[i] = *reinterpret_cast<const f32x2_t *>(o + (int64_t)at * kHeadDim);
+            }
+#pragma unroll
+            for (int i = 0; i < kStep; ++i) {
+                const int s = s0 + kWaves * i;
+                if (s < n_split && (have >> (s & 63)) & 1ull) y += x[i] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+            }
         }
     }
-    const bool some = den != 0.f;
-    bf16x4 z;
+    if constexpr (kWaves > 1) {
+        joined[id][lane] = y;
+        __syncthreads();
+        if (wave > 0) return;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = (__bf16)(some ? mean(y[e] / den) : 0.f);
-    *reinterpret_cast<uint2 *>(out.ptr + b * out.sb + (int64_t)t * out.st + (int64_t)hq * out.sh + c4) = __builtin_bit_cast(uint2, z);
-    if (c4 == 0) lse[row] = t >= n ? 0.f : some ? lse_of(M, den) : -INFINITY;
+        for (int i = 1; i < kWaves; ++i) y += joined[i][lane];
+    }
+    const bool some = den != 0.f;
+    bf16x2_t z;
+    z[0] = (__bf16)(some ? mean(y[0] / den) : 0.f);
+    z[1] = (__bf16)(some ? mean(y[1] / den) : 0.f);
+    *reinterpret_cast<uint32_t *>(out.ptr + b * out.sb + (int64_t)t * out.st + (int64_t)hq * out.sh + 2 * lane) = __builtin_bit_cast(uint32_t, z);
+    if (lane == 0) lse[row] = t >= n ? 0.f : some ? lse_of(M, den) : -INFINITY;
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
@@ -491,7 +545,8 @@ int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, c
     timing_end(stream);
     if (p.parts > 1) {
         timing_begin("paged_merge_kernel", stream);
-        hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, seqlens, out, lse);
+        const bool many = p.parts > 16;
+        hipLaunchKernelGGL((many ? paged_merge_kernel<4> : paged_merge_kernel<1>), dim3((unsigned)(many ? rows : (rows + 3) / 4)), dim3(256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, seqlens, out, lse);
         timing_end(stream);
     }
     return (int)hipGetLastError();

@@ -12,11 +12,15 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A workgroup to a sequence and head: the c-th largest weight of the rows that may go, by their eight highest bits, the next eight, ..; then the rows above it and the first
-// of those equal to it, in order.
+// A workgroup to a sequence and head: the smallest weight that stays, by digits of 11, 11 and 10 bits from the highest on (11: exponents and two bits of mantissa spread a
+// wavefront's counts over many words; all lanes' in one word cost an addition); then the rows above it and the first of those equal to it, in order.  A wavefront holds a run of
+// rows, of up to 64 kPer in registers, of more it reads them again for each digit.
+constexpr int kDigits = 2048;
+template <int kPer>
 __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const float *__restrict__ weights, int pitch, const int32_t *__restrict__ seqlens,
                                                                   int budget, int first, int recent, int32_t *__restrict__ kept) {
-    __shared__ uint32_t hist[256];
+    __shared__ uint32_t hist[kDigits];
+    __shared__ uint32_t wave_sums[kPickWaves];
     __shared__ uint32_t found[2];                        // the digit, and how many are above it
     __shared__ int2 counts[kPickWaves];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -32,50 +36,75 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
     const int lo = first, hi = L - recent, want = budget - first - recent;                     // want < hi - lo
     if (want == 0) return;
     const float *w = weights + bh * pitch;
+    const int each = ((hi - lo + kPickWaves - 1) / kPickWaves + 63) / 64, from = min(hi, lo + wave * 64 * each), to = min(hi, from + 64 * each);
+    const bool held = each <= kPer;
+    uint32_t x[kPer];                                    // row from + 64 i + lane
+    auto load = [&](int base) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int j = base + 64 * i + lane;
+            x[i] = j < to ? __float_as_uint(w[j]) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] = base + 64 * i + lane < to ? order_of(__uint_as_float(x[i])) : 0u;    // (0: of no number)
+    };
+    // f(i, base) over a run's rows, kPer steps at a time
+    auto rows = [&](auto f) __attribute__((always_inline)) {
+        for (int base = from; base < to; base += 64 * kPer) {
+            if (!held) load(base);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (base + 64 * i < to) f(x[i], base + 64 * i);
+        }
+    };
+    if (held) load(from);
     uint32_t prefix = 0u, mask = 0u;
     int left = want;                                     // how many of those with this prefix
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0u;
+#pragma unroll 1
+    for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
+        hist[tid] = hist[tid + kPickThreads] = 0u;
         __syncthreads();
-        for (int j = lo + tid; j < hi; j += kPickThreads) {
-            const uint32_t x = order_of(w[j]);
-            if ((x & mask) == prefix) atomicAdd(&hist[(x >> shift) & 255u], 1u);
+        rows([&](uint32_t y, int) __attribute__((always_inline)) {
+            const uint32_t digit = (y >> shift) & (kDigits - 1u) & (shift == 0 ? 1023u : ~0u);
+            const bool counts_ = y != 0u && (y & mask) == prefix;
+            const uint64_t who = __ballot(counts_);
+            if (!who) return;
+            const uint32_t some = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(who));
+            if (__ballot(counts_ && digit != some) == 0ull) {
+                if (lane == 0) atomicAdd(&hist[some], (uint32_t)__popcll(who));
+            } else if (counts_) {
+                atomicAdd(&hist[digit], 1u);
+            }
+        });
+        __syncthreads();
+        // thread i: digits 2047 - 2 i and the one below, so that sums run from the highest on
+        const uint32_t c0 = hist[kDigits - 1 - 2 * tid], c1 = hist[kDigits - 2 - 2 * tid];
+        uint32_t upto = c0 + c1;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(upto, d);
+            upto += lane >= d ? o : 0u;
         }
+        if (lane == 63) wave_sums[wave] = upto;
         __syncthreads();
-        if (wave == 0) {                                 // lane l: digits 255 - 4 l .., the highest first
-            uint32_t c[4], all = 0u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) all += c[i] = hist[255 - 4 * lane - i];
-            uint32_t upto = all;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t o = __shfl_up(upto, d);
-                upto += lane >= d ? o : 0u;
-            }
-            uint32_t above = upto - all;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (above < (uint32_t)left && (uint32_t)left <= above + c[i]) {
-                    found[0] = 255 - 4 * lane - i;
-                    found[1] = above;
-                }
-                above += c[i];
-            }
+        uint32_t above = upto - c0 - c1;
+        for (int i = 0; i < wave; ++i) above += wave_sums[i];
+        if (above < (uint32_t)left && (uint32_t)left <= above + c0 + c1) {
+            const bool second = (uint32_t)left > above + c0;
+            found[0] = kDigits - 1 - 2 * tid - (second ? 1 : 0);
+            found[1] = above + (second ? c0 : 0u);
         }
         __syncthreads();
         prefix |= found[0] << shift;
-        mask |= 255u << shift;
+        mask |= (shift == 0 ? 1023u : kDigits - 1u) << shift;
         left -= (int)found[1];
-        __syncthreads();
     }
-    // rows above `prefix`, and the first `left` of those equal to it; a wavefront takes a run of rows
-    const int each = ((hi - lo + kPickWaves - 1) / kPickWaves + 63) / 64 * 64, from = min(hi, lo + wave * each), to = min(hi, from + each);
+    // rows above `prefix`, and the first `left` of those equal to it
     int above = 0, equal = 0;
-    for (int j = from; j < to; j += 64) {
-        const uint32_t x = j + lane < to ? order_of(w[j + lane]) : 0u;
-        above += __popcll(__ballot(x > prefix));
-        equal += __popcll(__ballot(j + lane < to && x == prefix));
-    }
+    rows([&](uint32_t y, int) __attribute__((always_inline)) {
+        above += __popcll(__ballot(y > prefix));
+        equal += __popcll(__ballot(y == prefix));
+    });
     if (lane == 0) counts[wave] = int2{above, equal};
     __syncthreads();
     int at = first, ties = 0;                            // rows kept, and equal ones, before this run
@@ -83,15 +112,15 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
         at += counts[i].x + min(counts[i].y, max(0, left - ties));
         ties += counts[i].y;
     }
-    for (int j = from; j < to; j += 64) {
-        const uint32_t x = j + lane < to ? order_of(w[j + lane]) : 0u;
-        const uint64_t below = (1ull << lane) - 1ull, eq = __ballot(j + lane < to && x == prefix);
-        const bool keep = j + lane < to && (x > prefix || (x == prefix && ties + __popcll(eq & below) < left));
+    const uint64_t below = (1ull << lane) - 1ull;
+    rows([&](uint32_t y, int base) __attribute__((always_inline)) {
+        const uint64_t eq = __ballot(y == prefix);
+        const bool keep = y > prefix || (y == prefix && ties + __popcll(eq & below) < left);
         const uint64_t who = __ballot(keep);
-        if (keep) out[at + __popcll(who & below)] = j + lane;
+        if (keep) out[at + __popcll(who & below)] = base + lane;
         at += __popcll(who);
         ties += __popcll(eq);
-    }
+    });
 }
 
 // 16 lanes to a row, 64 rows to a workgroup; grid (rows / 64, Hkv, batch).  Bound by traffic.
@@ -142,7 +171,8 @@ int launch_paged_evict(const Dims &dm, const float *weights, int pitch, const Pa
                        const Pages &to, int32_t *kept, float *weights_out, int32_t *seqlens_out, void *, hipStream_t stream) {
     if (dm.batch <= 0) return 0;
     timing_begin("evict_pick_kernel", stream);
-    hipLaunchKernelGGL(evict_pick_kernel, dim3(dm.Hkv, dm.batch), dim3(kPickThreads), 0, stream, dm, weights, pitch, seqlens, budget, first, recent, kept);
+    const int64_t rows = (dm.max_seqlen + kPickThreads - 1) / kPickThreads;
+    hipLaunchKernelGGL((rows <= 8 ? evict_pick_kernel<8> : evict_pick_kernel<32>), dim3(dm.Hkv, dm.batch), dim3(kPickThreads), 0, stream, dm, weights, pitch, seqlens, budget, first, recent, kept);
     timing_end(stream);
     timing_begin("evict_move_kernel", stream);
     hipLaunchKernelGGL(evict_move_kernel, dim3((budget + 63) / 64, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, weights, pitch, from, seqlens, budget, to, kept,

@@ -151,6 +151,7 @@ __global__ __launch_bounds__(256, 4) void paged_weights_kernel(Dims dm, Pages pg
         f32x16 s = zero16();
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) s = mfma32(k[ks], rd.rows(cur, ks), s);
+        settle(s);
         if (k0 + 31 > t) {
             const int at = t + (c >> lg) - k0 - 4 * hf;  // keys up to this one are seen
 #pragma unroll
