@@ -189,6 +189,7 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
     };
     // Unit x lies in slot x % 3.  The first `whole` are seen by all rows; from the first of them that has no page on, all are taken as the others are.
     look_up(0);
+    __builtin_amdgcn_sched_barrier(0);                   // (queries are asked for before the copies: else each step waits for a unit more)
     uint32_t p0 = stage(slot0, 0), p1 = stage(slot1, 1), p2 = 3u;
     int whole = max(0, min(count, ((ch.before + t0 + 1) >> 5) - u0));
     if (p1 != 3u) whole = min(whole, 1);
@@ -209,8 +210,10 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
     };
     for (int x = 0; x < whole; x += 3) {
         step(slot0, slot2, p2, x);
-        if (x + 1 < whole) step(slot1, slot0, p0, x + 1);
-        if (x + 2 < whole) step(slot2, slot1, p1, x + 2);
+        if (x + 1 >= whole) break;
+        step(slot1, slot0, p0, x + 1);
+        if (x + 2 >= whole) break;
+        step(slot2, slot1, p1, x + 2);
     }
 #pragma unroll 1
     for (int x = whole; x < count; ++x) {
@@ -261,11 +264,12 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
 
 // grid (parts of the keys, Hkv, batch).  Column c of the products: head c % G of new token c / G.  A wavefront has its keys in the registers of the first product and its
 // values in LDS, the next unit's under way.
-__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const int32_t *__restrict__ seqlens,
+template <int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const int32_t *__restrict__ seqlens,
                                                                 Tensor out, float *__restrict__ lse, float *__restrict__ o_part,
                                                                 float2 *__restrict__ ml_part) {
-    __shared__ __align__(16) char V0[4][kHalfTile], V1[4][kHalfTile];
-    __shared__ float2 ml_s[4][16];
+    __shared__ __align__(16) char V0[kWaves][kHalfTile], V1[kWaves][kHalfTile];
+    __shared__ float2 ml_s[kWaves][16];
     const int split = blockIdx.x, n_split = gridDim.x, h = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const Chunk ch(nt, seqlens, b, dm.max_seqlen);
@@ -277,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(Dims dm, Pages p
         for (int ks = 0; ks < 4; ++ks) bq[ks] = load8(qr + 32 * ks);
     }
     const int end = ch.L, units = (end + 31) >> 5, u_end = (int)((int64_t)units * (split + 1) / n_split), u0 = (int)((int64_t)units * split / n_split) + wave;
-    const int count = u0 < u_end ? (u_end - u0 + 3) >> 2 : 0;            // units u0, u0 + 4, ..
+    const int count = u0 < u_end ? (u_end - u0 + kWaves - 1) / kWaves : 0;   // units u0, u0 + kWaves, ..
     const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh), *v_head = reinterpret_cast<const char *>(pg.v.ptr + h * pg.v.sh);
     const uint32_t k_at = n * (2 * (uint32_t)pg.k.st) + 16 * g;
     const int32_t *table = pg.table + (int64_t)b * pg.ld;
@@ -288,8 +292,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(Dims dm, Pages p
     };
     UnitPages up;
     auto fetch = [&](Unit &u, char *vs, int x) __attribute__((always_inline)) {
-        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + 4 * (x + lane)), x + lane < count ? end : 0);
-        u.k0 = 32 * (u0 + 4 * x);
+        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + kWaves * (x + lane)), x + lane < count ? end : 0);
+        u.k0 = 32 * (u0 + kWaves * x);
         u.there = 0u;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -396,22 +400,22 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(Dims dm, Pages p
     __syncthreads();
     float M = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) M = fmaxf(M, ml_s[i][n].x);
+    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
     const float w = fast_exp2(m - (M == -INFINITY ? 0.f : M));
     float *mine = reinterpret_cast<float *>(V0[wave]);   // [column][channel]
 #pragma unroll
     for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (c ^ (n & 7)) + 4 * g) = o[c] * w;
     __syncthreads();
     const int col = tid >> 4, c8 = 8 * (tid & 15), ct = col >> lg;       // a thread joins eight channels of a column
-    if (ct >= nt.most || (ct >= ch.n && (n_split > 1 || !dm.fill))) return;
+    if (col >= 16 || ct >= nt.most || (ct >= ch.n && (n_split > 1 || !dm.fill))) return;
     float den = 0.f, Mc = -INFINITY, y[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
+    for (int i = 0; i < kWaves; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
     const float bc = Mc == -INFINITY ? 0.f : Mc;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kWaves; ++i) {
         den += ml_s[i][col].y * fast_exp2(ml_s[i][col].x - bc);
         const float *from = reinterpret_cast<const float *>(V0[i]) + col * kHeadDim + 16 * ((c8 >> 4) ^ (col & 7)) + (c8 & 15);
 #pragma unroll
@@ -501,7 +505,7 @@ static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int kMaxParts = 64;
 struct PagedPlan {
-    bool few;
+    bool few, wide;                                      // wide: eight wavefronts
     int64_t items;                                       // of one part
     int tiles, parts;
 };
@@ -512,6 +516,7 @@ static PagedPlan paged_plan(const Dims &dm, int max_new) {
     p.tiles = p.few ? 1 : (int)(((int64_t)max_new * dm.G + kChunkRows - 1) / kChunkRows);
     p.items = (int64_t)dm.batch * dm.Hkv * p.tiles;
     const int64_t chip = p.few ? 512 : 768;              // workgroups that run at a time
+    p.wide = p.few && p.items * kMaxParts <= 256;
     p.parts = p.items >= 512 ? 1 : (int)max((int64_t)1, min(most_parts(dm), (chip + p.items - 1) / max((int64_t)1, p.items)));
     return p;
 }
@@ -534,7 +539,7 @@ int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, c
     float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) + align256((size_t)rows * p.parts * kHeadDim * sizeof(float)));
     if (p.few) {
         timing_begin("paged_attn_few_kernel", stream);
-        hipLaunchKernelGGL(paged_attn_few_kernel, dim3(p.parts, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part);
+        hipLaunchKernelGGL((p.wide ? paged_attn_few_kernel<8> : paged_attn_few_kernel<4>), dim3(p.parts, dm.Hkv, dm.batch), dim3(p.wide ? 512 : 256), 0, stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part);
     } else {
         const int64_t items = p.items * p.parts;
         const int run = xcd_run_length(items);

@@ -12,6 +12,17 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// The sum of lanes 0 .. lane: within rows of sixteen by shifts, then the rows' sums.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
+    int y = (int)x;
+    y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, true);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, true);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, true);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, true);
+    const int r0 = __builtin_amdgcn_readlane(y, 15), r1 = r0 + __builtin_amdgcn_readlane(y, 31), r2 = r1 + __builtin_amdgcn_readlane(y, 47);
+    return (uint32_t)(y + (lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2));
+}
+
 // A workgroup to a sequence and head: the smallest weight that stays, by digits of 11, 11 and 10 bits from the highest on (11: exponents and two bits of mantissa spread a
 // wavefront's counts over many words; all lanes' in one word cost an addition); then the rows above it and the first of those equal to it, in order.  A wavefront holds a run of
 // rows, of up to 64 kPer in registers, of more it reads them again for each digit.
@@ -62,33 +73,28 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
     int left = want;                                     // how many of those with this prefix
 #pragma unroll 1
     for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
+        const uint32_t digits = shift == 0 ? 1023u : kDigits - 1u;
         hist[tid] = hist[tid + kPickThreads] = 0u;
         __syncthreads();
         rows([&](uint32_t y, int) __attribute__((always_inline)) {
-            const uint32_t digit = (y >> shift) & (kDigits - 1u) & (shift == 0 ? 1023u : ~0u);
-            const bool counts_ = y != 0u && (y & mask) == prefix;
-            const uint64_t who = __ballot(counts_);
+            const uint64_t who = __ballot((y & mask) == prefix);             // (numbers that are none count as the lowest, which are never reached)
             if (!who) return;
-            const uint32_t some = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(who));
-            if (__ballot(counts_ && digit != some) == 0ull) {
+            const uint32_t digit = (y >> shift) & digits, some = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(who));
+            const uint64_t same = __ballot(digit == some);
+            if ((who & ~same) == 0ull) {
                 if (lane == 0) atomicAdd(&hist[some], (uint32_t)__popcll(who));
-            } else if (counts_) {
+            } else if ((who >> lane) & 1ull) {
                 atomicAdd(&hist[digit], 1u);
             }
         });
         __syncthreads();
         // thread i: digits 2047 - 2 i and the one below, so that sums run from the highest on
         const uint32_t c0 = hist[kDigits - 1 - 2 * tid], c1 = hist[kDigits - 2 - 2 * tid];
-        uint32_t upto = c0 + c1;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(upto, d);
-            upto += lane >= d ? o : 0u;
-        }
+        const uint32_t upto = wave_scan(c0 + c1, lane);
         if (lane == 63) wave_sums[wave] = upto;
         __syncthreads();
-        uint32_t above = upto - c0 - c1;
-        for (int i = 0; i < wave; ++i) above += wave_sums[i];
+        const uint32_t before = wave_scan(lane < kPickWaves ? wave_sums[lane] : 0u, lane);
+        const uint32_t above = upto - c0 - c1 + (wave ? (uint32_t)__builtin_amdgcn_readlane((int)before, wave - 1) : 0u);
         if (above < (uint32_t)left && (uint32_t)left <= above + c0 + c1) {
             const bool second = (uint32_t)left > above + c0;
             found[0] = kDigits - 1 - 2 * tid - (second ? 1 : 0);
@@ -96,7 +102,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
         }
         __syncthreads();
         prefix |= found[0] << shift;
-        mask |= (shift == 0 ? 1023u : kDigits - 1u) << shift;
+        mask |= digits << shift;
         left -= (int)found[1];
     }
     // rows above `prefix`, and the first `left` of those equal to it
@@ -107,11 +113,10 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
     });
     if (lane == 0) counts[wave] = int2{above, equal};
     __syncthreads();
-    int at = first, ties = 0;                            // rows kept, and equal ones, before this run
-    for (int i = 0; i < wave; ++i) {
-        at += counts[i].x + min(counts[i].y, max(0, left - ties));
-        ties += counts[i].y;
-    }
+    const int2 mine = lane < wave ? counts[lane] : int2{0, 0};
+    int at = (int)wave_scan((uint32_t)mine.x, lane), ties = (int)wave_scan((uint32_t)mine.y, lane);
+    ties = __builtin_amdgcn_readlane(ties, 63);          // rows kept, and equal ones, before this run
+    at = first + __builtin_amdgcn_readlane(at, 63) + min(ties, left);
     const uint64_t below = (1ull << lane) - 1ull;
     rows([&](uint32_t y, int base) __attribute__((always_inline)) {
         const uint64_t eq = __ballot(y == prefix);

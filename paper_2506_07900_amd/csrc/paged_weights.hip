@@ -90,10 +90,12 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(Dims dm, Pages p
 
 // More rows: a workgroup takes 128 keys, 32 to a wavefront, which hold them in registers, and walks over the rows that see any of them, 32 at a time through LDS.
 // What a lane adds up is one column's share of each of its keys.  Bound by the exponentials and the products, which are half of the attention's.
-__global__ __launch_bounds__(256, 4) void paged_weights_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int run, Tensor q, const float *__restrict__ lse,
-                                                               const int32_t *__restrict__ seqlens, const float *weights, int pitch, float *weights_out) {
+// Where tiles of keys are fewer than the workgroups that run at a time, a tile's rows are cut into parts, and a second kernel adds these up.
+__global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_part, int run, Tensor q, const float *__restrict__ lse,
+                                                               const int32_t *__restrict__ seqlens, const float *weights, int pitch, float *weights_out,
+                                                               float *__restrict__ partial) {
     __shared__ __align__(16) char slot0[kHalfTile], slot1[kHalfTile], slot2[kHalfTile];
-    const int item = xcd_item(blockIdx.x, run), bh = item / n_tiles, ti = item - bh * n_tiles, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int item = xcd_item(blockIdx.x, run), bp = item / n_tiles, ti = item - bp * n_tiles, bh = bp / n_part, part = bp - bh * n_part, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     if (b >= dm.batch) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, hf = lane >> 5;
     const Chunk ch(nt, seqlens, b, dm.max_seqlen);
@@ -113,7 +115,8 @@ __global__ __launch_bounds__(256, 4) void paged_weights_kernel(Dims dm, Pages pg
         there = (lanes & 1u) | ((lanes >> 16) & 1u) << 1;
     }
     // ---- the rows: (token, head of the group), heads fastest, 32 to a unit -------------------------------------------------
-    const int per = 32 >> lg, u0 = max(0, first - ch.before) / per, count = (ch.n + per - 1) / per - u0;
+    const int per = 32 >> lg, seen_from = max(0, first - ch.before) / per, all = (ch.n + per - 1) / per - seen_from;
+    const int u0 = seen_from + (int)((int64_t)all * part / n_part), count = seen_from + (int)((int64_t)all * (part + 1) / n_part) - u0;
     const char *q_head = reinterpret_cast<const char *>(q.ptr + b * q.sb + (int64_t)h * dm.G * q.sh) + 64 * wave;
     uint32_t q_at[2];
 #pragma unroll
@@ -122,49 +125,77 @@ __global__ __launch_bounds__(256, 4) void paged_weights_kernel(Dims dm, Pages pg
         q_at[j] = 2 * ((row >> lg) * (uint32_t)q.st + (row & (dm.G - 1)) * (uint32_t)q.sh) + 16 * copy_piece(lane);
     }
     auto stage = [&](char *dst, int x) __attribute__((always_inline)) {                        // two copies for every unit; rows behind the last are zeros
-        const int t = per * (u0 + max(0, min(x, count - 1))), rows = x < count ? (ch.n - t) << lg : 0;
+        const int t = per * (u0 + max(0, min(x, count - 1))), rows = x < count ? min(ch.n - t, per) << lg : 0;
         const char *from = q_head + 2 * (int64_t)t * q.st;
 #pragma unroll
         for (int j = 0; j < 2; ++j) copy_rows(dst + wave * 2048 + j * 1024, from, 16 * j + (lane >> 2) < rows ? q_at[j] : kNoRow, 0);
     };
-    const float *lse_at = lse + ((int64_t)b * nt.most + (c >> lg)) * dm.Hq + h * dm.G + (c & (dm.G - 1));
+    const float *lse_at = lse + ((int64_t)b * nt.most + min(c >> lg, nt.most - 1)) * dm.Hq + h * dm.G + (c & (dm.G - 1));
     auto row_lse = [&](int x) __attribute__((always_inline)) {
-        const int t = per * (u0 + x);
-        return x < count && t + (c >> lg) < ch.n ? lse_log2(lse_at[(int64_t)t * dm.Hq]) : INFINITY;
+        return lse_at[(int64_t)min(per * (u0 + x), max(0, ch.n - 1 - (c >> lg))) * dm.Hq];     // (of a row behind the last token: anything)
+    };
+    auto row_z = [&](float z, int x) __attribute__((always_inline)) {    // (made of it where it is used: it is two steps on its way)
+        return x < count && per * (u0 + x) + (c >> lg) < ch.n ? lse_log2(z) : INFINITY;
     };
     const TileReader rd(lane);
     float sum[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) sum[e] = 0.f;
-    float z0 = row_lse(0), z1 = row_lse(1), z2 = INFINITY;
+    // Unit x lies in slot x % 3.  A step takes the exponentials of unit x and the products of unit x + 1, an instruction of one between those of the other: four wavefronts to a SIMD
+    // that do one after the other overlap little (matrix cores 38 %, vector unit 60 % of the time, together all of it).
+    auto arrived = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0f72);              // all copies but the newest unit's two
+        asm volatile("s_barrier" ::: "memory");          // everyone's, and everyone has read the unit before
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    float z0 = row_lse(0), z1 = row_lse(1), z2 = row_lse(2);
     stage(slot0, 0);
     stage(slot1, 1);
-    auto step = [&](const char *cur, char *next, float z, float &z_next, int x) __attribute__((always_inline)) {
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0f72);              // all copies but the next unit's two
-        asm volatile("s_barrier" ::: "memory");          // everyone's, and everyone is past the unit before
-        __builtin_amdgcn_sched_barrier(0);
-        z_next = row_lse(x + 2);
-        stage(next, x + 2);
-        const int t = ch.before + per * (u0 + x);        // position of the unit's first token
-        if (k0 > t + per - 1) return;
-        f32x16 s = zero16();
+    arrived();
+    f32x16 s = zero16();
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) s = mfma32(k[ks], rd.rows(cur, ks), s);
-        settle(s);
+    for (int ks = 0; ks < 8; ++ks) s = mfma32(k[ks], rd.rows(slot0, ks), s);
+    stage(slot2, 2);
+    settle(s);
+    auto step = [&](const char *next, char *after, float &z, int x) __attribute__((always_inline)) {
+        arrived();
+        const float zx = row_z(z, x);
+        z = row_lse(x + 3);
+        stage(after, x + 3);
+        bf16x8 qx[8];
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) qx[ks] = rd.rows(next, ks);
+        f32x16 s_next = zero16();
+        const int t = ch.before + per * (u0 + x);        // position of the unit's first token
         if (k0 + 31 > t) {
             const int at = t + (c >> lg) - k0 - 4 * hf;  // keys up to this one are seen
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum[e] += 8 * (e >> 2) + (e & 3) <= at ? fast_exp2(__builtin_fmaf(s[e], dm.scale_log2, -z)) : 0.f;
+            for (int e = 0; e < 16; ++e) sum[e] += 8 * (e >> 2) + (e & 3) <= at ? fast_exp2(__builtin_fmaf(s[e], dm.scale_log2, -zx)) : 0.f;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) s_next = mfma32(k[ks], qx[ks], s_next);
         } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum[e] += fast_exp2(__builtin_fmaf(s[e], dm.scale_log2, -z));
+            for (int ks = 0; ks < 8; ++ks) s_next = mfma32(k[ks], qx[ks], s_next);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[e] += fast_exp2(__builtin_fmaf(s[e], dm.scale_log2, -zx));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // a product
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);       // two to be scaled
+                __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);       // their exponentials
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);       // added up
+            }
         }
+        settle(s_next);
+        s = s_next;
     };
     for (int x = 0; x < count; x += 3) {
-        step(slot0, slot2, z0, z2, x);
-        if (x + 1 < count) step(slot1, slot0, z1, z0, x + 1);
-        if (x + 2 < count) step(slot2, slot1, z2, z1, x + 2);
+        step(slot1, slot0, z0, x);
+        if (x + 1 >= count) break;
+        step(slot2, slot1, z1, x + 1);
+        if (x + 2 >= count) break;
+        step(slot0, slot2, z2, x + 2);
     }
     __builtin_amdgcn_s_waitcnt(0);                       // (the copies past the last unit have landed)
     // ---- over the columns -------------------------------------------------------------------------------------------------
@@ -178,15 +209,38 @@ __global__ __launch_bounds__(256, 4) void paged_weights_kernel(Dims dm, Pages pg
     }
     const int key = k0 + 8 * (c >> 2) + 4 * hf + (c & 3);
     if (c >= 16 || key >= ch.L) return;
-    const int64_t at = ((int64_t)b * dm.Hkv + h) * pitch + key;
+    const int64_t at = (int64_t)bh * pitch + key;
     const bool seen = (there >> (c >> 3)) & 1u;          // (a row without a page gets nothing)
-    weights_out[at] = (weights && key < ch.before ? weights[at] : 0.f) + (seen ? mine : 0.f);
+    if (n_part > 1) partial[(((int64_t)bh * n_tiles + ti) * n_part + part) * 128 + (key - first)] = seen ? mine : 0.f;
+    else weights_out[at] = (weights && key < ch.before ? weights[at] : 0.f) + (seen ? mine : 0.f);
 }
 
-size_t paged_weights_ws_bytes(const Dims &, int) { return 0; }
+// grid (tiles, Hkv, batch), a thread to a key.
+__global__ __launch_bounds__(128) void paged_weights_join_kernel(Dims dm, NewTokens nt, int n_part, const int32_t *__restrict__ seqlens,
+                                                                 const float *__restrict__ partial, const float *weights, int pitch, float *weights_out) {
+    const int h = blockIdx.y, b = blockIdx.z, key = 128 * blockIdx.x + threadIdx.x;
+    const Chunk ch(nt, seqlens, b, dm.max_seqlen);
+    if (key >= ch.L) return;
+    const int64_t bh = (int64_t)b * dm.Hkv + h, at = bh * pitch + key;
+    const float *from = partial + (bh * gridDim.x + blockIdx.x) * n_part * 128 + threadIdx.x;
+    float sum = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < n_part; ++i) sum += from[128 * i];
+    weights_out[at] = (weights && key < ch.before ? weights[at] : 0.f) + sum;
+}
+
+constexpr int kWeightItems = 3072;                       // workgroups that run at a time
+static int64_t weight_items(const Dims &dm) { return ((int64_t)dm.max_seqlen + 127) / 128 * dm.Hkv * dm.batch; }
+static int64_t most_weight_parts(const Dims &dm, int max_new) { return max((int64_t)1, (int64_t)max_new * dm.G / 128); }    // four units of rows and more to a part
+// (a bound that grows with each size)
+size_t paged_weights_ws_bytes(const Dims &dm, int max_new) {
+    const int64_t items = min(weight_items(dm), (int64_t)kWeightItems - 1), most = most_weight_parts(dm, max_new);
+    if ((int64_t)max_new * dm.G <= 16 || most <= 1) return 0;
+    return (size_t)min(items * most, items + kWeightItems) * 128 * sizeof(float);
+}
 
 int launch_paged_weights(const Dims &dm, Tensor q, const float *lse, const Pages &pg, NewTokens nt, const int32_t *seqlens, const float *weights, int pitch,
-                         float *weights_out, void *, hipStream_t stream) {
+                         float *weights_out, void *ws, hipStream_t stream) {
     if (dm.batch <= 0 || nt.most <= 0 || dm.max_seqlen <= 0) return 0;
     const int lg = __builtin_ctz(dm.G);
     if ((int64_t)nt.most * dm.G <= 16) {
@@ -195,15 +249,24 @@ int launch_paged_weights(const Dims &dm, Tensor q, const float *lse, const Pages
         timing_begin("paged_weights_few_kernel", stream);
         hipLaunchKernelGGL(paged_weights_few_kernel, dim3(parts, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, pg, nt, lg, q, lse, seqlens, weights, pitch,
                            weights_out);
-    } else {
-        const int tiles = (int)(((int64_t)dm.max_seqlen + 127) / 128);
-        const int64_t items = (int64_t)tiles * dm.Hkv * dm.batch;
-        const int run = xcd_run_length(items);
-        timing_begin("paged_weights_kernel", stream);
-        hipLaunchKernelGGL(paged_weights_kernel, dim3(xcd_grid(items, run)), dim3(256), 0, stream, dm, pg, nt, lg, tiles, run, q, lse, seqlens, weights, pitch,
-                           weights_out);
+        timing_end(stream);
+        return (int)hipGetLastError();
     }
+    const int tiles = (int)(((int64_t)dm.max_seqlen + 127) / 128);
+    const int64_t items = weight_items(dm);
+    const int parts = items >= kWeightItems ? 1 : (int)min(most_weight_parts(dm, nt.most), (kWeightItems + items - 1) / items);
+    const int run = xcd_run_length(items * parts);
+    float *partial = reinterpret_cast<float *>(ws);
+    timing_begin("paged_weights_kernel", stream);
+    hipLaunchKernelGGL(paged_weights_kernel, dim3(xcd_grid(items * parts, run)), dim3(256), 0, stream, dm, pg, nt, lg, tiles, parts, run, q, lse, seqlens,
+                       weights, pitch, weights_out, partial);
     timing_end(stream);
+    if (parts > 1) {
+        timing_begin("paged_weights_join_kernel", stream);
+        hipLaunchKernelGGL(paged_weights_join_kernel, dim3(tiles, dm.Hkv, dm.batch), dim3(128), 0, stream, dm, nt, parts, seqlens, partial, weights, pitch,
+                           weights_out);
+        timing_end(stream);
+    }
     return (int)hipGetLastError();
 }
 
