@@ -142,20 +142,26 @@ struct ChunkRows {
 };
 
 // Items: (sequence, head), part of the keys, tile of 128 rows, the last fastest.
-__global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_split, int run, Tensor q,
+// kGroups groups of four wavefronts take every kGroups-th unit and are joined in LDS at the end.  Three fill a compute unit as three workgroups of one do, with a third of the parts.
+template <int kGroups>
+__global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_split, int run, Tensor q,
                                                             const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse,
                                                             float *__restrict__ o_part, float2 *__restrict__ ml_part) {
-    __shared__ KVHalf slot0, slot1, slot2;
+    __shared__ KVHalf slots0[kGroups], slots1[kGroups], slots2[kGroups];
+    __shared__ float2 ml_s[kGroups][4][64];
     const int item = xcd_item(blockIdx.x, run), bs = item / n_tiles, bh = bs / n_split, split = bs - bh * n_split, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     if (b >= dm.batch) return;
     const int ti = (bs + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id & 3, group = id >> 2;
+    KVHalf &slot0 = slots0[group], &slot1 = slots1[group], &slot2 = slots2[group];
     const Chunk ch(nt, seqlens, b, dm.max_seqlen);
     const int t0 = ti * (kChunkRows >> lg), t1 = min(ch.n, t0 + (kChunkRows >> lg));
     ChunkRows r(lane);
     const int row = 32 * wave + (lane & 31), token = t0 + (row >> lg), hq = h * dm.G + (row & (dm.G - 1));
     const int end = ch.L > 0 && t0 < ch.n ? ch.before + t1 : 0;          // keys that the workgroup's rows see
-    const int units = (end + 31) >> 5, u0 = (int)((int64_t)units * split / n_split), count = (int)((int64_t)units * (split + 1) / n_split) - u0;
+    const int units = (end + 31) >> 5, from = (int)((int64_t)units * split / n_split), all = (int)((int64_t)units * (split + 1) / n_split) - from;
+    const int count = (all - group + kGroups - 1) / kGroups;              // this group's units
+    auto unit = [&](int x) __attribute__((always_inline)) { return from + group + kGroups * x; };
     if (t0 >= ch.n && (n_split > 1 || !dm.fill)) return;
     r.scale = dm.scale_log2;
     r.shift = (float)shift_of(ch.L);
@@ -172,14 +178,14 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
     const int32_t *table = pg.table + (int64_t)b * pg.ld;
     UnitPages up;
     auto look_up = [&](int x) __attribute__((always_inline)) {           // (before the wait for copies: behind it the compiler would wait for all of them)
-        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + x + lane), x + lane < count ? end : 0);
+        if ((x & 63) == 0) up.load(pg, table, 32 * unit(x + lane), x + lane < count ? end : 0);
     };
     // unit x into a slot, four copies of 16 rows each; -> which of its halves have a page.  Those past the last bring zeros.
     auto stage = [&](KVHalf &dst, int x) __attribute__((always_inline)) -> uint32_t {
         uint32_t there = 0u;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int page = __builtin_amdgcn_readlane(j ? up.hi : up.lo, x & 63), first = 32 * (u0 + x) + 16 * j;
+            const int page = __builtin_amdgcn_readlane(j ? up.hi : up.lo, x & 63), first = 32 * unit(x) + 16 * j;
             const bool some = page >= 0, in = some && first + (lane >> 2) < end;
             there |= some ? 1u << j : 0u;
             copy_rows(dst.k + wave * 2048 + j * 1024, k_head + page_bytes(pg.k, pg.lg, max(page, 0), first), in ? k_at : kNoRow, 0);
@@ -191,7 +197,7 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
     look_up(0);
     __builtin_amdgcn_sched_barrier(0);                   // (queries are asked for before the copies: else each step waits for a unit more)
     uint32_t p0 = stage(slot0, 0), p1 = stage(slot1, 1), p2 = 3u;
-    int whole = max(0, min(count, ((ch.before + t0 + 1) >> 5) - u0));
+    int whole = max(0, min(count, (((ch.before + t0 + 1) >> 5) - from - group + kGroups - 1) / kGroups));
     if (p1 != 3u) whole = min(whole, 1);
     if (p0 != 3u) whole = 0;
     const bool alive = t0 + ((32 * wave) >> lg) < ch.n;  // (of no token: these rows only help to fetch)
@@ -225,10 +231,55 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
         p0 = at == 1 ? then : p0;
         p1 = at == 2 ? then : p1;
         p2 = at == 0 ? then : p2;
-        if (alive) r.take_edge(*cur, 32 * (u0 + x), there);
+        if (alive) r.take_edge(*cur, 32 * unit(x), there);
     }
+    if (kGroups > 1 && count < (all + kGroups - 1) / kGroups) asm volatile("s_barrier" ::: "memory");   // (the first groups have one unit more)
     __builtin_amdgcn_s_waitcnt(0);                       // (the copies past the last unit have landed)
     __syncthreads();
+    char *mine = (wave < 2 ? slots0[0].k : slots1[0].k) + (wave & 1) * kHalfTile;              // 8 KiB of this wavefront's own
+    if constexpr (kGroups > 1) {                         // a row's state is in the same lanes of all groups: the others hand theirs to the first
+        static_assert(kGroups == 3, "nine slots hold the states of two groups");
+        auto block = [&](int g) __attribute__((always_inline)) {
+            const int i = 4 * (g - 1) + wave;
+            return reinterpret_cast<char *>(i < 3 ? &slots0[i] : i < 6 ? &slots1[i - 3] : &slots2[i - 6]) + 16 * lane;
+        };
+        if (group > 0) {
+            ml_s[group][wave][lane] = float2{r.m, r.l};
+            char *at = block(group);
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4)
+                    *reinterpret_cast<f32x4 *>(at + 1024 * (4 * ct + e4)) = f32x4{r.o[ct][4 * e4], r.o[ct][4 * e4 + 1], r.o[ct][4 * e4 + 2], r.o[ct][4 * e4 + 3]};
+        }
+        __syncthreads();
+        if (group > 0) return;
+        float M = r.m;
+#pragma unroll
+        for (int g = 1; g < kGroups; ++g) M = fmaxf(M, ml_s[g][wave][lane].x);
+        const float base = M == -INFINITY ? 0.f : M, own = fast_exp2(r.m - base);
+        r.m = M;
+        r.l *= own;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) r.o[ct] *= own;
+#pragma unroll
+        for (int g = 1; g < kGroups; ++g) {
+            const float2 other = ml_s[g][wave][lane];
+            const float theirs = fast_exp2(other.x - base);
+            r.l += other.y * theirs;
+            const char *at = block(g);
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(at + 1024 * (4 * ct + e4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) r.o[ct][4 * e4 + e] += x[e] * theirs;
+                }
+        }
+        mine = block(1) - 16 * lane;                     // (read by this wavefront alone)
+        reads_done();
+    }
     r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
     const bool live = token < ch.n;
     if (n_split > 1) {
@@ -252,7 +303,7 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
         for (int e = 0; e < 16; ++e) r.o[ct][e] = some ? mean(r.o[ct][e] * inv) : 0.f;
-    store_rows((wave < 2 ? slot0.k : slot1.k) + (wave & 1) * kHalfTile, r.o, 1.f, lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
+    store_rows(mine, r.o, 1.f, lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
         const int t = t0 + ((32 * wave + at) >> lg);
         return t < nt.most && (t < ch.n || dm.fill) ? out.ptr + b * out.sb + (int64_t)t * out.st + (int64_t)(h * dm.G + ((32 * wave + at) & (dm.G - 1))) * out.sh : nullptr;
     });
@@ -264,12 +315,12 @@ __global__ __launch_bounds__(256, 3) void paged_attn_kernel(Dims dm, Pages pg, N
 
 // grid (parts of the keys, Hkv, batch).  Column c of the products: head c % G of new token c / G.  A wavefront has its keys in the registers of the first product and its
 // values in LDS, the next unit's under way.
-template <int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const int32_t *__restrict__ seqlens,
+constexpr int kFewWaves = 4;
+__global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const int32_t *__restrict__ seqlens,
                                                                 Tensor out, float *__restrict__ lse, float *__restrict__ o_part,
                                                                 float2 *__restrict__ ml_part) {
-    __shared__ __align__(16) char V0[kWaves][kHalfTile], V1[kWaves][kHalfTile];
-    __shared__ float2 ml_s[kWaves][16];
+    __shared__ __align__(16) char V0[kFewWaves][kHalfTile], V1[kFewWaves][kHalfTile];
+    __shared__ float2 ml_s[kFewWaves][16];
     const int split = blockIdx.x, n_split = gridDim.x, h = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const Chunk ch(nt, seqlens, b, dm.max_seqlen);
@@ -281,7 +332,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_few_kernel(Dims dm,
         for (int ks = 0; ks < 4; ++ks) bq[ks] = load8(qr + 32 * ks);
     }
     const int end = ch.L, units = (end + 31) >> 5, u_end = (int)((int64_t)units * (split + 1) / n_split), u0 = (int)((int64_t)units * split / n_split) + wave;
-    const int count = u0 < u_end ? (u_end - u0 + kWaves - 1) / kWaves : 0;   // units u0, u0 + kWaves, ..
+    const int count = u0 < u_end ? (u_end - u0 + kFewWaves - 1) / kFewWaves : 0;   // units u0, u0 + kFewWaves, ..
     const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh), *v_head = reinterpret_cast<const char *>(pg.v.ptr + h * pg.v.sh);
     const uint32_t k_at = n * (2 * (uint32_t)pg.k.st) + 16 * g;
     const int32_t *table = pg.table + (int64_t)b * pg.ld;
@@ -292,8 +343,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_few_kernel(Dims dm,
     };
     UnitPages up;
     auto fetch = [&](Unit &u, char *vs, int x) __attribute__((always_inline)) {
-        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + kWaves * (x + lane)), x + lane < count ? end : 0);
-        u.k0 = 32 * (u0 + kWaves * x);
+        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + kFewWaves * (x + lane)), x + lane < count ? end : 0);
+        u.k0 = 32 * (u0 + kFewWaves * x);
         u.there = 0u;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -400,22 +451,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_few_kernel(Dims dm,
     __syncthreads();
     float M = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
+    for (int i = 0; i < kFewWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
     const float w = fast_exp2(m - (M == -INFINITY ? 0.f : M));
     float *mine = reinterpret_cast<float *>(V0[wave]);   // [column][channel]
 #pragma unroll
     for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (c ^ (n & 7)) + 4 * g) = o[c] * w;
     __syncthreads();
     const int col = tid >> 4, c8 = 8 * (tid & 15), ct = col >> lg;       // a thread joins eight channels of a column
-    if (col >= 16 || ct >= nt.most || (ct >= ch.n && (n_split > 1 || !dm.fill))) return;
+    if (ct >= nt.most || (ct >= ch.n && (n_split > 1 || !dm.fill))) return;
     float den = 0.f, Mc = -INFINITY, y[8];
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
+    for (int i = 0; i < kFewWaves; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
     const float bc = Mc == -INFINITY ? 0.f : Mc;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
+    for (int i = 0; i < kFewWaves; ++i) {
         den += ml_s[i][col].y * fast_exp2(ml_s[i][col].x - bc);
         const float *from = reinterpret_cast<const float *>(V0[i]) + col * kHeadDim + 16 * ((c8 >> 4) ^ (col & 7)) + (c8 & 15);
 #pragma unroll
@@ -443,12 +494,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_few_kernel(Dims dm,
 
 // ---- joining the parts --------------------------------------------------------------------------------------------------------
 
-// kWaves wavefronts to a row, two channels to a lane, parts wave, wave + kWaves, ..: all of its parts' channels are asked for before any is used, so a row costs two round trips.
-// A part whose sum is 0 has no channels; one that has stands in for it.
+// kWaves wavefronts to a row, two channels to a lane, parts wave, wave + kWaves, ..: sums and channels are asked for together, before it is known which parts have any (one whose sum is
+// 0 has not, and what lies in its place is not looked at), so a row of up to 16 kWaves parts costs one round trip.
 template <int kWaves>
 __global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, int64_t rows, const float *__restrict__ o_part,
-                                                          const float2 *__restrict__ ml_part, const int32_t *__restrict__ seqlens, Tensor out,
-                                                          float *__restrict__ lse) {
+                                                          const float2 *__restrict__ ml_part, Tensor out, float *__restrict__ lse) {
     __shared__ f32x2_t joined[4][64];
     const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % kWaves;
     const int64_t row = (int64_t)blockIdx.x * (4 / kWaves) + id / kWaves;
@@ -457,27 +507,27 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt,
     const int hq = (int)(row - bt * dm.Hq), b = (int)(bt / nt.most), t = (int)(bt - (int64_t)b * nt.most);
     const int n = nt.counts ? clamp_len(uniform_load(nt.counts + b), nt.most) : nt.most;
     if (t >= n && !dm.fill) return;
-    const bool live = t < n && clamp_len(uniform_load(seqlens + b), dm.max_seqlen) >= n;
-    const float2 ml = live && lane < n_split ? ml_part[row * n_split + lane] : float2{-INFINITY, 0.f};
-    const uint64_t have = __ballot(ml.y != 0.f);         // (a NaN too)
-    float M = ml.y != 0.f ? ml.x : -INFINITY, den = 0.f;
     f32x2_t y = {0.f, 0.f};
-    if (have) {
+    float M = -INFINITY, den = 0.f;
+    if (t < n) {                                         // (a skipped sequence's parts have no sums)
+        const float2 ml = lane < n_split ? ml_part[row * n_split + lane] : float2{-INFINITY, 0.f};
+        const float *o = o_part + row * n_split * kHeadDim + 2 * lane;
+        constexpr int kStep = 16;
+        f32x2_t x[kStep];
+        auto ask = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kStep; ++i) x[i] = *reinterpret_cast<const f32x2_t *>(o + (int64_t)min(s0 + kWaves * i, n_split - 1) * kHeadDim);
+        };
+        ask(wave);
+        const uint64_t have = __ballot(ml.y != 0.f);     // (a NaN too)
+        M = ml.y != 0.f ? ml.x : -INFINITY;
         M = row_reduce(M, [](float a, float d) { return fmaxf(a, d); });
         M = xgroup_max(M);
         const float w = ml.y != 0.f ? fast_exp2(ml.x - M) : 0.f;
         den = row_reduce(ml.y != 0.f ? ml.y * w : 0.f, [](float a, float d) { return a + d; });
         den = xgroup_sum(den);
-        const int first = __builtin_ctzll(have);
-        const float *o = o_part + row * n_split * kHeadDim + 2 * lane;
-        constexpr int kStep = 16;
         for (int s0 = wave; s0 < n_split; s0 += kStep * kWaves) {
-            f32x2_t x[kStep];
-#pragma unroll
-            for (int i = 0; i < kStep; ++i) {
-                const int s = s0 + kWaves * i, at = s < n_split && (have >> (s & 63)) & 1ull ? s : first;
-                x[i] = *reinterpret_cast<const f32x2_t *>(o + (int64_t)at * kHeadDim);
-            }
+            if (s0 > wave) ask(s0);
 #pragma unroll
             for (int i = 0; i < kStep; ++i) {
                 const int s = s0 + kWaves * i;
@@ -503,30 +553,38 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt,
 // ---- host side -------------------------------------------------------------------------------------------------------------
 static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 64;                            // what a wavefront of paged_merge_kernel holds the sums of
+// Up to 16 rows: two workgroups to a compute unit run at a time, and the keys are cut into as many parts.  More rows: with 768 tiles and more three workgroups of one group to a compute
+// unit; with fewer, workgroups of three groups, one to a compute unit, and parts where even they are fewer than the compute units.
 struct PagedPlan {
-    bool few, wide;                                      // wide: eight wavefronts
-    int64_t items;                                       // of one part
+    bool few, groups;
     int tiles, parts;
+    int64_t items;                                       // of one part
 };
-static int64_t most_parts(const Dims &dm) { return min((int64_t)kMaxParts, ((int64_t)dm.max_seqlen + 255) / 256); }   // 256 keys and more to a part
+static int64_t paged_tiles(const Dims &dm, int64_t max_new) {
+    const int64_t rows = max_new * dm.G;
+    return rows <= 16 ? 1 : (rows + kChunkRows - 1) / kChunkRows;
+}
+static int64_t most_parts(const Dims &dm, bool few) {    // 256 keys and more to a part, a group's eight units
+    return max((int64_t)1, min((int64_t)kMaxParts, few ? ((int64_t)dm.max_seqlen + 255) / 256 : (int64_t)dm.max_seqlen / 768));
+}
 static PagedPlan paged_plan(const Dims &dm, int max_new) {
     PagedPlan p;
     p.few = (int64_t)max_new * dm.G <= 16;
-    p.tiles = p.few ? 1 : (int)(((int64_t)max_new * dm.G + kChunkRows - 1) / kChunkRows);
+    p.tiles = (int)paged_tiles(dm, max_new);
     p.items = (int64_t)dm.batch * dm.Hkv * p.tiles;
-    const int64_t chip = p.few ? 512 : 768;              // workgroups that run at a time
-    p.wide = p.few && p.items * kMaxParts <= 256;
-    p.parts = p.items >= 512 ? 1 : (int)max((int64_t)1, min(most_parts(dm), (chip + p.items - 1) / max((int64_t)1, p.items)));
+    p.groups = p.items < 768;
+    const int64_t chip = p.few ? 512 : 256;
+    p.parts = (int)max((int64_t)1, min(most_parts(dm, p.few), chip / p.items));
     return p;
 }
-// (a bound that grows with each size: parts of a tile's 128 rows, no more than all tiles of the few-item calls can have)
+// (a bound that grows with each size: of the parts of few tiles)
 size_t paged_attn_ws_bytes(const Dims &dm, int max_new) {
     if (dm.batch <= 0 || max_new <= 0) return 0;
-    const int64_t per = (int64_t)max_new * dm.G <= 16 ? 16 : kChunkRows;
-    const int64_t items = (int64_t)dm.batch * dm.Hkv * (((int64_t)max_new * dm.G + per - 1) / per), most = most_parts(dm);
+    const bool few = (int64_t)max_new * dm.G <= 16;
+    const int64_t items = min((int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new), (int64_t)512), most = most_parts(dm, true);
     if (most <= 1) return 0;
-    const size_t rows = (size_t)(min(min(items, (int64_t)512) * most, min(items, (int64_t)512) + 768) * per);
+    const size_t rows = (size_t)(min(items * most, items + 512) * (few ? 16 : kChunkRows));
     return align256(rows * kHeadDim * sizeof(float)) + align256(rows * sizeof(float2));
 }
 
@@ -539,19 +597,19 @@ int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, c
     float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) + align256((size_t)rows * p.parts * kHeadDim * sizeof(float)));
     if (p.few) {
         timing_begin("paged_attn_few_kernel", stream);
-        hipLaunchKernelGGL((p.wide ? paged_attn_few_kernel<8> : paged_attn_few_kernel<4>), dim3(p.parts, dm.Hkv, dm.batch), dim3(p.wide ? 512 : 256), 0, stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part);
+        hipLaunchKernelGGL(paged_attn_few_kernel, dim3(p.parts, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part);
     } else {
         const int64_t items = p.items * p.parts;
         const int run = xcd_run_length(items);
         timing_begin("paged_attn_kernel", stream);
-        hipLaunchKernelGGL(paged_attn_kernel, dim3(xcd_grid(items, run)), dim3(256), 0, stream, dm, pg, nt, lg, p.tiles, p.parts, run, q, seqlens, out, lse,
+        hipLaunchKernelGGL((p.groups ? paged_attn_kernel<3> : paged_attn_kernel<1>), dim3(xcd_grid(items, run)), dim3(p.groups ? 768 : 256), 0, stream, dm, pg, nt, lg, p.tiles, p.parts, run, q, seqlens, out, lse,
                            o_part, ml_part);
     }
     timing_end(stream);
     if (p.parts > 1) {
         timing_begin("paged_merge_kernel", stream);
         const bool many = p.parts > 16;
-        hipLaunchKernelGGL((many ? paged_merge_kernel<4> : paged_merge_kernel<1>), dim3((unsigned)(many ? rows : (rows + 3) / 4)), dim3(256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, seqlens, out, lse);
+        hipLaunchKernelGGL((many ? paged_merge_kernel<4> : paged_merge_kernel<1>), dim3((unsigned)(many ? rows : (rows + 3) / 4)), dim3(256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, out, lse);
         timing_end(stream);
     }
     return (int)hipGetLastError();
