@@ -298,12 +298,20 @@ __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, P
     }
     // rows that see no key, and those behind the last token where they are written: zeros
     const bool some = live && r.l != 0.f;
-    const float inv = 1.f / r.l;
+    const float inv = some ? 1.f / r.l : 0.f;
+    float most = 0.f;
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
+    for (int ct = 0; ct < 4; ++ct) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) r.o[ct][e] = some ? mean(r.o[ct][e] * inv) : 0.f;
-    store_rows(mine, r.o, 1.f, lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
+        for (int e = 0; e < 16; e += 2) most = __builtin_elementwise_maximum(most, __builtin_elementwise_maximum(__builtin_fabsf(r.o[ct][e]), __builtin_fabsf(r.o[ct][e + 1])));
+    }
+    if (__builtin_expect(__any(!(most * inv < 3.3e38f)), 0)) {           // (near the largest, or no number)
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r.o[ct][e] = some ? mean(r.o[ct][e] * inv) * r.l : 0.f;
+    }
+    store_rows(mine, r.o, inv, lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
         const int t = t0 + ((32 * wave + at) >> lg);
         return t < nt.most && (t < ch.n || dm.fill) ? out.ptr + b * out.sb + (int64_t)t * out.st + (int64_t)(h * dm.G + ((32 * wave + at) & (dm.G - 1))) * out.sh : nullptr;
     });
@@ -565,9 +573,7 @@ static int64_t paged_tiles(const Dims &dm, int64_t max_new) {
     const int64_t rows = max_new * dm.G;
     return rows <= 16 ? 1 : (rows + kChunkRows - 1) / kChunkRows;
 }
-static int64_t most_parts(const Dims &dm, bool few) {    // 256 keys and more to a part, a group's eight units
-    return max((int64_t)1, min((int64_t)kMaxParts, few ? ((int64_t)dm.max_seqlen + 255) / 256 : (int64_t)dm.max_seqlen / 768));
-}
+static int64_t most_parts(const Dims &dm) { return max((int64_t)1, min((int64_t)kMaxParts, ((int64_t)dm.max_seqlen + 255) / 256)); }   // 256 keys and more to a part
 static PagedPlan paged_plan(const Dims &dm, int max_new) {
     PagedPlan p;
     p.few = (int64_t)max_new * dm.G <= 16;
@@ -575,14 +581,14 @@ static PagedPlan paged_plan(const Dims &dm, int max_new) {
     p.items = (int64_t)dm.batch * dm.Hkv * p.tiles;
     p.groups = p.items < 768;
     const int64_t chip = p.few ? 512 : 256;
-    p.parts = (int)max((int64_t)1, min(most_parts(dm, p.few), chip / p.items));
+    p.parts = (int)max((int64_t)1, min(most_parts(dm), chip / p.items));
     return p;
 }
 // (a bound that grows with each size: of the parts of few tiles)
 size_t paged_attn_ws_bytes(const Dims &dm, int max_new) {
     if (dm.batch <= 0 || max_new <= 0) return 0;
     const bool few = (int64_t)max_new * dm.G <= 16;
-    const int64_t items = min((int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new), (int64_t)512), most = most_parts(dm, true);
+    const int64_t items = min((int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new), (int64_t)512), most = most_parts(dm);
     if (most <= 1) return 0;
     const size_t rows = (size_t)(min(items * most, items + 512) * (few ? 16 : kChunkRows));
     return align256(rows * kHeadDim * sizeof(float)) + align256(rows * sizeof(float2));

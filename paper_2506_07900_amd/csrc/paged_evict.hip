@@ -26,7 +26,7 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
 // A workgroup to a sequence and head: the smallest weight that stays, by digits of 11, 11 and 10 bits from the highest on (11: exponents and two bits of mantissa spread a
 // wavefront's counts over many words; all lanes' in one word cost an addition); then the rows above it and the first of those equal to it, in order.  A wavefront holds a run of
 // rows, of up to 64 kPer in registers, of more it reads them again for each digit.
-constexpr int kDigits = 2048;
+constexpr int kDigits = 2048, kListed = 512;
 template <int kPer>
 __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const float *__restrict__ weights, int pitch, const int32_t *__restrict__ seqlens,
                                                                   int budget, int first, int recent, int32_t *__restrict__ kept) {
@@ -34,6 +34,8 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
     __shared__ uint32_t wave_sums[kPickWaves];
     __shared__ uint32_t found[2];                        // the digit, and how many are above it
     __shared__ int2 counts[kPickWaves];
+    __shared__ uint32_t list[kPickWaves][kListed];
+    __shared__ int over;
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int L = clamp_len(uniform_load(seqlens + b), dm.max_seqlen);
     const int64_t bh = (int64_t)b * dm.Hkv + h;
@@ -70,23 +72,37 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
     };
     if (held) load(from);
     uint32_t prefix = 0u, mask = 0u;
-    int left = want;                                     // how many of those with this prefix
+    int left = want, above = 0, equal = 0;               // how many of those with this prefix; this run's rows above the last one that stays, and equal to it
+    int listed = 0;                                      // this run's numbers with the first digit, in LDS unless some run has more than fit
+    bool fits = false;
+    auto count = [&](uint32_t y, uint32_t digits, int shift) __attribute__((always_inline)) {
+        const uint64_t who = __ballot((y & mask) == prefix);             // (numbers that are none count as the lowest, which are never reached)
+        if (!who) return;
+        const uint32_t digit = (y >> shift) & digits, some = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(who));
+        const uint64_t same = __ballot(digit == some);
+        if ((who & ~same) == 0ull) {
+            if (lane == 0) atomicAdd(&hist[some], (uint32_t)__popcll(who));
+        } else if ((who >> lane) & 1ull) {
+            atomicAdd(&hist[digit], 1u);
+        }
+    };
 #pragma unroll 1
     for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
         const uint32_t digits = shift == 0 ? 1023u : kDigits - 1u;
         hist[tid] = hist[tid + kPickThreads] = 0u;
+        if (tid == 0) over = 0;
         __syncthreads();
-        rows([&](uint32_t y, int) __attribute__((always_inline)) {
-            const uint64_t who = __ballot((y & mask) == prefix);             // (numbers that are none count as the lowest, which are never reached)
-            if (!who) return;
-            const uint32_t digit = (y >> shift) & digits, some = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(who));
-            const uint64_t same = __ballot(digit == some);
-            if ((who & ~same) == 0ull) {
-                if (lane == 0) atomicAdd(&hist[some], (uint32_t)__popcll(who));
-            } else if ((who >> lane) & 1ull) {
-                atomicAdd(&hist[digit], 1u);
-            }
-        });
+        if (shift == 21) {
+            rows([&](uint32_t y, int) __attribute__((always_inline)) {
+                const uint32_t digit = y >> 21, some = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+                if (__ballot(digit != some) != 0ull) atomicAdd(&hist[digit], 1u);
+                else if (lane == 0) atomicAdd(&hist[digit], 64u);
+            });
+        } else if (fits) {
+            for (int j = lane; j - lane < listed; j += 64) count(j < listed ? list[wave][j] : 0u, digits, shift);
+        } else {
+            rows([&](uint32_t y, int) __attribute__((always_inline)) { count(y, digits, shift); });
+        }
         __syncthreads();
         // thread i: digits 2047 - 2 i and the one below, so that sums run from the highest on
         const uint32_t c0 = hist[kDigits - 1 - 2 * tid], c1 = hist[kDigits - 2 - 2 * tid];
@@ -94,29 +110,58 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
         if (lane == 63) wave_sums[wave] = upto;
         __syncthreads();
         const uint32_t before = wave_scan(lane < kPickWaves ? wave_sums[lane] : 0u, lane);
-        const uint32_t above = upto - c0 - c1 + (wave ? (uint32_t)__builtin_amdgcn_readlane((int)before, wave - 1) : 0u);
-        if (above < (uint32_t)left && (uint32_t)left <= above + c0 + c1) {
-            const bool second = (uint32_t)left > above + c0;
+        const uint32_t more = upto - c0 - c1 + (wave ? (uint32_t)__builtin_amdgcn_readlane((int)before, wave - 1) : 0u);
+        if (more < (uint32_t)left && (uint32_t)left <= more + c0 + c1) {
+            const bool second = (uint32_t)left > more + c0;
             found[0] = kDigits - 1 - 2 * tid - (second ? 1 : 0);
-            found[1] = above + (second ? c0 : 0u);
+            found[1] = more + (second ? c0 : 0u);
         }
         __syncthreads();
-        prefix |= found[0] << shift;
+        const uint32_t digit = found[0];
+        prefix |= digit << shift;
         mask |= digits << shift;
         left -= (int)found[1];
+        if (shift < 21) continue;
+        rows([&](uint32_t y, int) __attribute__((always_inline)) {       // (the other digits are looked for among few)
+            above += __popcll(__ballot((y >> 21) > digit));
+            const uint64_t who = __ballot((y >> 21) == digit);
+            if (!who) return;
+            const int at = listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+            if (((who >> lane) & 1ull) && at < kListed) list[wave][at] = y;
+            listed += __popcll(who);
+        });
+        if (listed > kListed) over = 1;
+        __syncthreads();
+        fits = over == 0;
     }
     // rows above `prefix`, and the first `left` of those equal to it
-    int above = 0, equal = 0;
-    rows([&](uint32_t y, int) __attribute__((always_inline)) {
-        above += __popcll(__ballot(y > prefix));
-        equal += __popcll(__ballot(y == prefix));
-    });
+    if (fits) {
+        for (int j = lane; j - lane < listed; j += 64) {
+            const uint32_t y = j < listed ? list[wave][j] : 0u;
+            above += __popcll(__ballot(y > prefix));
+            equal += __popcll(__ballot(y == prefix));
+        }
+    } else {
+        above = 0;
+        rows([&](uint32_t y, int) __attribute__((always_inline)) {
+            above += __popcll(__ballot(y > prefix));
+            equal += __popcll(__ballot(y == prefix));
+        });
+    }
     if (lane == 0) counts[wave] = int2{above, equal};
     __syncthreads();
-    const int2 mine = lane < wave ? counts[lane] : int2{0, 0};
-    int at = (int)wave_scan((uint32_t)mine.x, lane), ties = (int)wave_scan((uint32_t)mine.y, lane);
-    ties = __builtin_amdgcn_readlane(ties, 63);          // rows kept, and equal ones, before this run
-    at = first + __builtin_amdgcn_readlane(at, 63) + min(ties, left);
+    const int2 mine = lane < kPickWaves ? counts[lane] : int2{0, 0};
+    const int above_upto = (int)wave_scan((uint32_t)mine.x, lane), equal_upto = (int)wave_scan((uint32_t)mine.y, lane);
+    int ties = wave ? __builtin_amdgcn_readlane(equal_upto, wave - 1) : 0;                     // equal rows before this run, and rows kept
+    int at = first + (wave ? __builtin_amdgcn_readlane(above_upto, wave - 1) : 0) + min(ties, left);
+    if (__builtin_amdgcn_readlane(equal_upto, 63) == left) {             // all that are equal stay
+        rows([&](uint32_t y, int base) __attribute__((always_inline)) {
+            const uint64_t who = __ballot(y >= prefix);
+            if (y >= prefix) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u))] = base + lane;
+            at += __popcll(who);
+        });
+        return;
+    }
     const uint64_t below = (1ull << lane) - 1ull;
     rows([&](uint32_t y, int base) __attribute__((always_inline)) {
         const uint64_t eq = __ballot(y == prefix);
