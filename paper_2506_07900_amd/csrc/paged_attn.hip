@@ -503,14 +503,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
 // ---- joining the parts --------------------------------------------------------------------------------------------------------
 
 // kWaves wavefronts to a row, two channels to a lane, parts wave, wave + kWaves, ..: sums and channels are asked for together, before it is known which parts have any (one whose sum is
-// 0 has not, and what lies in its place is not looked at), so a row of up to 16 kWaves parts costs one round trip.
+// 0 has not, and what lies in its place is not looked at): a row costs one round trip.
 template <int kWaves>
-__global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, int64_t rows, const float *__restrict__ o_part,
+__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, int64_t rows, const float *__restrict__ o_part,
                                                           const float2 *__restrict__ ml_part, Tensor out, float *__restrict__ lse) {
-    __shared__ f32x2_t joined[4][64];
-    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % kWaves;
-    const int64_t row = (int64_t)blockIdx.x * (4 / kWaves) + id / kWaves;
-    if (row >= rows) return;                             // (kWaves = 1 where a workgroup has more than one row: no barrier follows)
+    __shared__ f32x2_t joined[kWaves][64];
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = kWaves == 1 ? 0 : id;
+    const int64_t row = kWaves == 1 ? (int64_t)blockIdx.x * 4 + id : blockIdx.x;
+    if (row >= rows) return;                             // (more than one row to a workgroup: no barrier follows)
     const int64_t bt = row / dm.Hq;
     const int hq = (int)(row - bt * dm.Hq), b = (int)(bt / nt.most), t = (int)(bt - (int64_t)b * nt.most);
     const int n = nt.counts ? clamp_len(uniform_load(nt.counts + b), nt.most) : nt.most;
@@ -519,28 +519,25 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt,
     float M = -INFINITY, den = 0.f;
     if (t < n) {                                         // (a skipped sequence's parts have no sums)
         const float2 ml = lane < n_split ? ml_part[row * n_split + lane] : float2{-INFINITY, 0.f};
+        const float2 ml2 = kWaves == 8 && 64 + lane < n_split ? ml_part[row * n_split + 64 + lane] : float2{-INFINITY, 0.f};
         const float *o = o_part + row * n_split * kHeadDim + 2 * lane;
-        constexpr int kStep = 16;
+        constexpr int kStep = 16;                        // (of kWaves = 1: all parts, of 4 up to 64, of 8 up to 128)
         f32x2_t x[kStep];
-        auto ask = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < kStep; ++i) x[i] = *reinterpret_cast<const f32x2_t *>(o + (int64_t)min(s0 + kWaves * i, n_split - 1) * kHeadDim);
-        };
-        ask(wave);
-        const uint64_t have = __ballot(ml.y != 0.f);     // (a NaN too)
-        M = ml.y != 0.f ? ml.x : -INFINITY;
+        for (int i = 0; i < kStep; ++i) x[i] = *reinterpret_cast<const f32x2_t *>(o + (int64_t)min(wave + kWaves * i, n_split - 1) * kHeadDim);
+        const uint64_t have = __ballot(ml.y != 0.f), have2 = kWaves == 8 ? __ballot(ml2.y != 0.f) : 0ull;    // (a NaN too)
+        M = fmaxf(ml.y != 0.f ? ml.x : -INFINITY, ml2.y != 0.f ? ml2.x : -INFINITY);
         M = row_reduce(M, [](float a, float d) { return fmaxf(a, d); });
         M = xgroup_max(M);
-        const float w = ml.y != 0.f ? fast_exp2(ml.x - M) : 0.f;
-        den = row_reduce(ml.y != 0.f ? ml.y * w : 0.f, [](float a, float d) { return a + d; });
+        const float w = ml.y != 0.f ? fast_exp2(ml.x - M) : 0.f, w2 = ml2.y != 0.f ? fast_exp2(ml2.x - M) : 0.f;
+        den = (ml.y != 0.f ? ml.y * w : 0.f) + (ml2.y != 0.f ? ml2.y * w2 : 0.f);
+        den = row_reduce(den, [](float a, float d) { return a + d; });
         den = xgroup_sum(den);
-        for (int s0 = wave; s0 < n_split; s0 += kStep * kWaves) {
-            if (s0 > wave) ask(s0);
 #pragma unroll
-            for (int i = 0; i < kStep; ++i) {
-                const int s = s0 + kWaves * i;
-                if (s < n_split && (have >> (s & 63)) & 1ull) y += x[i] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
-            }
+        for (int i = 0; i < kStep; ++i) {
+            const int s = wave + kWaves * i;
+            const bool high = kWaves == 8 && i >= 8;     // (a constant: s >= 64)
+            if (((high ? have2 : have) >> (s & 63)) & 1ull) y += x[i] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(high ? w2 : w), s & 63));
         }
     }
     if constexpr (kWaves > 1) {
@@ -561,7 +558,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(Dims dm, NewTokens nt,
 // ---- host side -------------------------------------------------------------------------------------------------------------
 static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-constexpr int kMaxParts = 64;                            // what a wavefront of paged_merge_kernel holds the sums of
+constexpr int kMaxParts = 128, kMaxChunkParts = 64;      // what paged_merge_kernel joins; of tiles of 128 rows
 // Up to 16 rows: two workgroups to a compute unit run at a time, and the keys are cut into as many parts.  More rows: with 768 tiles and more three workgroups of one group to a compute
 // unit; with fewer, workgroups of three groups, one to a compute unit, and parts where even they are fewer than the compute units.
 struct PagedPlan {
@@ -573,7 +570,9 @@ static int64_t paged_tiles(const Dims &dm, int64_t max_new) {
     const int64_t rows = max_new * dm.G;
     return rows <= 16 ? 1 : (rows + kChunkRows - 1) / kChunkRows;
 }
-static int64_t most_parts(const Dims &dm) { return max((int64_t)1, min((int64_t)kMaxParts, ((int64_t)dm.max_seqlen + 255) / 256)); }   // 256 keys and more to a part
+static int64_t most_parts(const Dims &dm, bool few) {    // 128 keys and more to a part of few rows, a unit to a wavefront, or 256
+    return max((int64_t)1, few ? min((int64_t)kMaxParts, ((int64_t)dm.max_seqlen + 127) / 128) : min((int64_t)kMaxChunkParts, ((int64_t)dm.max_seqlen + 255) / 256));
+}
 static PagedPlan paged_plan(const Dims &dm, int max_new) {
     PagedPlan p;
     p.few = (int64_t)max_new * dm.G <= 16;
@@ -581,14 +580,16 @@ static PagedPlan paged_plan(const Dims &dm, int max_new) {
     p.items = (int64_t)dm.batch * dm.Hkv * p.tiles;
     p.groups = p.items < 768;
     const int64_t chip = p.few ? 512 : 256;
-    p.parts = (int)max((int64_t)1, min(most_parts(dm), chip / p.items));
+    // (of few rows and short caches one launch: 300 tokens 8.6 / 9.2 us, 500 10.3 / 9.3; 64 sequences of 1000 17.2 / 19.4, 32 of 768 12.9 / 12.1)
+    const bool alone = p.few && (dm.max_seqlen <= 320 || (dm.max_seqlen <= 1024 && p.items >= 128));
+    p.parts = alone ? 1 : (int)max((int64_t)1, min(most_parts(dm, p.few), chip / p.items));
     return p;
 }
 // (a bound that grows with each size: of the parts of few tiles)
 size_t paged_attn_ws_bytes(const Dims &dm, int max_new) {
     if (dm.batch <= 0 || max_new <= 0) return 0;
     const bool few = (int64_t)max_new * dm.G <= 16;
-    const int64_t items = min((int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new), (int64_t)512), most = most_parts(dm);
+    const int64_t items = min((int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new), (int64_t)512), most = most_parts(dm, true);
     if (most <= 1) return 0;
     const size_t rows = (size_t)(min(items * most, items + 512) * (few ? 16 : kChunkRows));
     return align256(rows * kHeadDim * sizeof(float)) + align256(rows * sizeof(float2));
@@ -614,8 +615,9 @@ int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, c
     timing_end(stream);
     if (p.parts > 1) {
         timing_begin("paged_merge_kernel", stream);
-        const bool many = p.parts > 16;
-        hipLaunchKernelGGL((many ? paged_merge_kernel<4> : paged_merge_kernel<1>), dim3((unsigned)(many ? rows : (rows + 3) / 4)), dim3(256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, out, lse);
+        const int waves = p.parts > 64 ? 8 : p.parts > 16 ? 4 : 1;
+        hipLaunchKernelGGL((waves == 8 ? paged_merge_kernel<8> : waves == 4 ? paged_merge_kernel<4> : paged_merge_kernel<1>),
+                           dim3((unsigned)(waves > 1 ? rows : (rows + 3) / 4)), dim3(waves == 8 ? 512 : 256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, out, lse);
         timing_end(stream);
     }
     return (int)hipGetLastError();
