@@ -299,6 +299,7 @@ __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, P
     // rows that see no key, and those behind the last token where they are written: zeros
     const bool some = live && r.l != 0.f;
     const float inv = some ? 1.f / r.l : 0.f;
+    float factor = inv;
     float most = 0.f;
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) {
@@ -309,9 +310,10 @@ __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, P
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) r.o[ct][e] = some ? mean(r.o[ct][e] * inv) * r.l : 0.f;
+            for (int e = 0; e < 16; ++e) r.o[ct][e] = some ? mean(r.o[ct][e] * inv) : 0.f;
+        factor = 1.f;                                    // (the same products: other rows of the wavefront come out the same)
     }
-    store_rows(mine, r.o, inv, lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
+    store_rows(mine, r.o, factor, lane, [&](int at) __attribute__((always_inline)) -> __bf16 * {
         const int t = t0 + ((32 * wave + at) >> lg);
         return t < nt.most && (t < ch.n || dm.fill) ? out.ptr + b * out.sb + (int64_t)t * out.st + (int64_t)(h * dm.G + ((32 * wave + at) & (dm.G - 1))) * out.sh : nullptr;
     });

@@ -329,6 +329,12 @@ ATTENTION = [
     (8, 2, 128, [5000], None, 129, False),
     (32, 2, 16, [2100], None, 333, False),
     (16, 16, 32, [150], None, 100, False),
+    # as many tiles as fill the chip with workgroups of one group; keys in parts by eight, four, one wavefront each
+    (16, 16, 64, [801, 800, 513, 799, 800, 700, 801, 650], [700, 700, 513, 1, 0, 700, 699, 650], 700, True),
+    (4, 1, 1024, [20000], None, 1, True),
+    (16, 1, 16, [9000, 20], None, 1, False),
+    (8, 1, 64, [1200, 321], None, 2, False),
+    (32, 2, 32, [6000, 300], [40, 17], 40, True),
 ]
 
 
@@ -440,6 +446,39 @@ def test_attention_of_equal_and_extreme_scores():
         big = (q.float() * 3000).bfloat16()                       # scores of tens of thousands: one key takes all
         out, lse = binding.paged_attn(prm, big, cache, i32([length]), length)
         check_attention(prm, cache, big, [length], [n], out, lse)
+
+
+@pytest.mark.parametrize("hq,hkv,n,length,batch", [(32, 2, 1, 3000, 8), (4, 1, 4, 300, 2), (8, 2, 60, 2500, 1), (16, 16, 600, 700, 10), (32, 2, 500, 4000, 1)])
+def test_attention_of_large_scores(hq, hkv, n, length, batch):
+    """scores of thousands: a maximum that lacked some of a product would leave exponentials that overflow"""
+    prm, gen = binding.Params(hq, hkv), gen_of(n)
+    cache = filled(gen, [length] * batch, hkv, 64)
+    for size in (300, 3000):
+        q = (normal(gen, batch, n, hq, D).float() * size).bfloat16()
+        out, lse = binding.paged_attn(prm, q, cache, i32([length] * batch), length)
+        assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+        check_attention(prm, cache, q[:1], [length], [n], out[:1], lse[:1])
+
+
+def test_attention_of_many_tiles_with_odd_values_and_pages():
+    """the form for many tiles: what a hidden infinity, a missing page and a row without any leave alone"""
+    gen = gen_of(55)
+    hq, hkv, n, b = 16, 16, 640, 10
+    prm, lengths = binding.Params(hq, hkv), [700 - 3 * i for i in range(b)]
+    cache = filled(gen, lengths, hkv, 16)
+    q = normal(gen, b, n, hq, D)
+    cache.table[3, 7], cache.table[4, 0], cache.table[5, :] = -1, 2 ** 30, -7
+    out, lse = binding.paged_attn(prm, q, cache, i32(lengths), 700)
+    check_attention(prm, cache, q, lengths, [n] * b, out, lse)
+    v = cache.v.clone()
+    t = lengths[0] - 100
+    v[int(cache.table[0, t // 16]), :, t % 16, 9] = NAN
+    again, _ = binding.paged_attn(prm, q, cache._replace(v=v), i32(lengths), 700)
+    first = t - (lengths[0] - n)                                  # the first query that sees it
+    assert torch.equal(again[1:], out[1:]) and torch.equal(again[0, :first], out[0, :first])
+    assert bool(torch.isnan(again[0, first:, :, 9]).all())
+    keep = torch.arange(D, device="cuda") != 9
+    assert torch.equal(again[0, :, :, keep], out[0, :, :, keep])
 
 
 # ---- weights -------------------------------------------------------------------------------------------------------------
@@ -659,6 +698,45 @@ def test_serving_run():
             want, tol = weights64(qr[j], lse[j], rows_of(to, to.k, j, now[j]), now[j] - 1, seen_rows(to, j, now[j]))
             assert bool(((total[j, :, :now[j]].double() - before[j, :, :now[j]].double() - want).abs() <= tol + 2.0 ** -22 * total[j, :, :now[j]]).all())
         positions += 1
+
+
+def test_graphs_that_share_a_workspace_and_calls_side_by_side():
+    """two captured graphs of different calls over one workspace, replayed in turn; and two streams with a workspace each"""
+    gen = gen_of(12)
+    prm = binding.Params(16, 2)
+    cases = [(5000, 1), (3000, 40), (900, 300)]
+    caches = [filled(gen, [length], 2, 32) for length, _ in cases]
+    qs = [normal(gen, 1, n, 16, D) for _, n in cases]
+    sls = [i32([length]) for length, _ in cases]
+    need = max(max(binding.paged_workspace_bytes(op, prm, 1, length, n) for length, n in cases) for op in (binding.OP_PAGED_ATTN, binding.OP_PAGED_WEIGHTS))
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+
+    def call(i, work):
+        out, lse = binding.paged_attn(prm, qs[i], caches[i], sls[i], cases[i][0], workspace=work)
+        return out, lse, binding.paged_attn_weights(prm, qs[i], lse, caches[i], sls[i], cases[i][0], workspace=work)
+
+    want = [[x.clone() for x in call(i, ws)] for i in range(3)]
+    graphs, got = [], []
+    for i in range(3):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(call(i, ws))
+        graphs.append(g)
+    for turn in range(4):
+        for i in (0, 1, 2, 1, 0):
+            for x in got[i]:
+                x.zero_()
+            ws.fill_(255)                                         # (what it holds before does not matter)
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(got[i], want[i]))
+    streams, works, side = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(ws) for _ in range(2)], [None, None]
+    for turn in range(5):
+        for j, i in ((0, 1), (1, 2)):
+            with torch.cuda.stream(streams[j]):
+                side[j] = call(i, works[j])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for j, i in ((0, 1), (1, 2)) for x, y in zip(side[j], want[i]))
 
 
 def test_another_stream_and_order():
