@@ -50,6 +50,14 @@ struct UnitPages {
         hi = page_of(pg, table, row + 16, end);
     }
 };
+// A store of 16 bytes.  kStream: past the caches.  A call that writes more than all L2s hold leaves its first results nowhere near their reader anyway, and its stores then run
+// beside the loads at 6 TB/s instead of 4.7 to 5.7 (8000 new tokens, 36 heads: 29.6 -> 23.2 us; 32768 tokens, 34 heads: 99.6 -> 94.9; 144000 evicted rows 80.8 -> 76.2).
+constexpr int64_t kAllL2 = 32ll << 20;
+template <bool kStream>
+__device__ __forceinline__ void store16(char *p, u32x4_t x) {
+    if constexpr (kStream) __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(p));
+    else *reinterpret_cast<u32x4_t *>(p) = x;
+}
 // Byte offset of row `row` of a page from the pool's start.
 __device__ __forceinline__ int64_t page_bytes(const Tensor &t, int lg, int page, int row) {
     return 2 * ((int64_t)page * t.sb + (int64_t)(row & ((1 << lg) - 1)) * t.st);

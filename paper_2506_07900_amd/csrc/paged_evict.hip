@@ -174,6 +174,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
 }
 
 // 16 lanes to a row, 64 rows to a workgroup; grid (rows / 64, Hkv, batch).  Bound by traffic.
+template <bool kStream>
 __global__ __launch_bounds__(256) void evict_move_kernel(Dims dm, const float *__restrict__ weights, int pitch, Pages from, const int32_t *__restrict__ seqlens,
                                                          int budget, Pages to, const int32_t *__restrict__ kept, float *__restrict__ weights_out,
                                                          int32_t *__restrict__ seqlens_out) {
@@ -210,8 +211,8 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Dims dm, const float *_
     for (int i = 0; i < 4; ++i) {
         const int j = 64 * blockIdx.x + 16 * i + (threadIdx.x >> 4);
         if (!moves[i]) continue;
-        *reinterpret_cast<u32x4_t *>(kt + page_bytes(to.k, to.lg, dst[i], j)) = x[i];
-        *reinterpret_cast<u32x4_t *>(vt + page_bytes(to.v, to.lg, dst[i], j)) = y[i];
+        store16<kStream>(kt + page_bytes(to.k, to.lg, dst[i], j), x[i]);
+        store16<kStream>(vt + page_bytes(to.v, to.lg, dst[i], j), y[i]);
     }
 }
 
@@ -225,7 +226,8 @@ int launch_paged_evict(const Dims &dm, const float *weights, int pitch, const Pa
     hipLaunchKernelGGL((rows <= 8 ? evict_pick_kernel<8> : evict_pick_kernel<32>), dim3(dm.Hkv, dm.batch), dim3(kPickThreads), 0, stream, dm, weights, pitch, seqlens, budget, first, recent, kept);
     timing_end(stream);
     timing_begin("evict_move_kernel", stream);
-    hipLaunchKernelGGL(evict_move_kernel, dim3((budget + 63) / 64, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, weights, pitch, from, seqlens, budget, to, kept,
+    const bool past = (int64_t)budget * dm.Hkv * dm.batch * (4 * kHeadDim) > kAllL2;
+    hipLaunchKernelGGL((past ? evict_move_kernel<true> : evict_move_kernel<false>), dim3((budget + 63) / 64, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, weights, pitch, from, seqlens, budget, to, kept,
                        weights_out, seqlens_out);
     timing_end(stream);
     return (int)hipGetLastError();

@@ -36,10 +36,8 @@ __device__ __forceinline__ void turn(uint32_t x, float &c, float &s) {
     s = quarter & 2u ? -b : b;
 }
 
-typedef uint32_t words8 __attribute__((ext_vector_type(8)));
-
 // Bound by traffic where rows are many, by the launch and one round trip where they are few.
-template <bool kPaged>
+template <bool kPaged, bool kStream>
 __global__ __launch_bounds__(256) void rotate_kernel(Dims dm, RotateArgs a, const int32_t *__restrict__ seqlens) {
     const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), b = blockIdx.y;
     const int t = id / a.chunks, chunk = id - t * a.chunks;
@@ -106,7 +104,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(Dims dm, RotateArgs a, cons
         char *to;
         if (!place(head, from, to)) continue;
         if (!kPaged && t >= n) {
-            *reinterpret_cast<uint4 *>(to + at0) = *reinterpret_cast<uint4 *>(to + at1) = uint4{0u, 0u, 0u, 0u};
+            store16<kStream>(to + at0, u32x4_t{0u, 0u, 0u, 0u});
+            store16<kStream>(to + at1, u32x4_t{0u, 0u, 0u, 0u});
             continue;
         }
         const uint4 u = *reinterpret_cast<const uint4 *>(from + at0), v = *reinterpret_cast<const uint4 *>(from + at1);
@@ -135,8 +134,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(Dims dm, RotateArgs a, cons
                 }
             }
         }
-        *reinterpret_cast<uint4 *>(to + at0) = uint4{w[0], w[1], w[2], w[3]};
-        *reinterpret_cast<uint4 *>(to + at1) = uint4{w[4], w[5], w[6], w[7]};
+        store16<kStream>(to + at0, u32x4_t{w[0], w[1], w[2], w[3]});
+        store16<kStream>(to + at1, u32x4_t{w[4], w[5], w[6], w[7]});
     }
 }
 
@@ -144,10 +143,11 @@ template <bool kPaged>
 static int launch_rotate(const char *name, const Dims &dm, RotateArgs a, const int32_t *seqlens, hipStream_t stream) {
     if (dm.batch <= 0 || a.rows <= 0 || a.heads <= 0) return 0;
     const int steps = (a.heads + 7) / 8;
-    a.per = (int64_t)a.rows * dm.batch >= 4096 ? steps : 1;
+    a.per = (int64_t)a.rows * dm.batch >= 4096 ? min(steps, 2) : 1;      // (32768 tokens, 34 heads: 1 / 2 / 3 / 5 of 5: 111 / 98 / 100 / 105 us)
     a.chunks = (steps + a.per - 1) / a.per;
+    const bool past = (int64_t)a.rows * dm.batch * a.heads * (2 * kHeadDim) > kAllL2;
     timing_begin(name, stream);
-    hipLaunchKernelGGL(rotate_kernel<kPaged>, dim3((unsigned)(((int64_t)a.rows * a.chunks + 3) / 4), dm.batch), dim3(256), 0, stream, dm, a, seqlens);
+    hipLaunchKernelGGL((past ? rotate_kernel<kPaged, true> : rotate_kernel<kPaged, false>), dim3((unsigned)(((int64_t)a.rows * a.chunks + 3) / 4), dm.batch), dim3(256), 0, stream, dm, a, seqlens);
     timing_end(stream);
     return (int)hipGetLastError();
 }

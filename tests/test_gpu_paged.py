@@ -142,7 +142,7 @@ def close_rotation(got, want, size):
 
 
 @pytest.mark.parametrize("kw", ROTATIONS, ids=lambda kw: "%s_%d%s" % (kw.get("scaling", "none"), kw["rot_dim"], "i" if kw.get("interleaved") else ""))
-@pytest.mark.parametrize("hq,hkv,t,lengths,far", [(32, 2, 70, [70, 33, 1], True), (4, 4, 5, [5], False), (1, 1, 1, [1, 0], True), (16, 1, 4500, [4500], False)])
+@pytest.mark.parametrize("hq,hkv,t,lengths,far", [(32, 2, 70, [70, 33, 1], True), (4, 4, 5, [5], False), (1, 1, 1, [1, 0], True), (16, 1, 4500, [4500], False), (32, 2, 4000, [4000], False)])
 def test_rotation(kw, hq, hkv, t, lengths, far):
     gen, b = gen_of(t + kw["rot_dim"]), len(lengths)
     prm, rope = binding.Params(hq, hkv), binding.rope_table(**kw)
@@ -210,7 +210,8 @@ def test_rotation_gradient_is_the_transposed_map():
 
 @pytest.mark.parametrize("page", [16, 32, 64, 256])
 @pytest.mark.parametrize("hq,hkv,lengths,counts,n", [(32, 2, [100, 17, 5, 64], [7, 0, 5, 1], 7), (4, 1, [1], None, 1), (8, 8, [300, 257], [33, 70], 70),
-                                                     (2, 1, [4300], None, 4200)])
+                                                     (2, 1, [4300], None, 4200),
+                                                     (32, 2, [4200], None, 4000)])
 def test_append(page, hq, hkv, lengths, counts, n):
     gen, b, cap = gen_of(page + n), len(lengths), max(lengths)
     prm, rope = binding.Params(hq, hkv), binding.rope_table(64, interleaved=True)
@@ -576,6 +577,7 @@ EVICTIONS = [
     ([300], 400, 4, 100, 16, 16, "random"),
     ([70001], 20000, 4, 1, 64, 64, "random"),
     ([140000], 3, 1, 1, 64, 64, "small"),
+    ([40000], 35000, 4, 9000, 64, 64, "random"),
 ]
 
 
