@@ -50,6 +50,69 @@ struct UnitPages {
         hi = page_of(pg, table, row + 16, end);
     }
 };
+// The sum of lanes 0 .. lane: within rows of sixteen by shifts, then the rows' sums.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
+    int y = (int)x;
+    y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, true);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, true);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, true);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, true);
+    const int r0 = __builtin_amdgcn_readlane(y, 15), r1 = r0 + __builtin_amdgcn_readlane(y, 31), r2 = r1 + __builtin_amdgcn_readlane(y, 47);
+    return (uint32_t)(y + (lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2));
+}
+
+// The units of 32 keys of a batch's sequences, end to end, dealt to workgroups in runs of `per`: workgroup x takes units x per ..; what it has of sequence b is part x + b of
+// all, so a sequence's parts lie side by side.  `aim` workgroups, and fewer where a sequence would come to more than `most` parts.  All lanes of a wavefront.
+// (Each sequence cut into as many, 64 of 1501 to 32749 rows wait for the longest's parts: 226 us instead of 205.)  Sequences of about one length are cut into as many all the same, so that no
+// workgroup has of two: `per` units to a part, `parts` to a sequence, workgroup x part x % parts of sequence x / parts (64 of 5000 rows 64.7 us without).
+struct BatchUnits {
+    const int32_t *seqlens;
+    NewTokens nt;
+    int batch, cap, each, per, parts, total, before, mine;      // before, mine: units before this lane's `each` sequences, and of them
+    __device__ __forceinline__ int of(int b) const {     // b uniform
+        if (each == 1) return __builtin_amdgcn_readlane(mine, b);        // (up to 64 sequences: no further load)
+        const int L = clamp_len(uniform_load(seqlens + b), cap), n = nt.counts ? clamp_len(uniform_load(nt.counts + b), nt.most) : nt.most;
+        return L < n ? 0 : (L + 31) >> 5;
+    }
+    __device__ __forceinline__ int of_lane(int b) const {
+        if (b >= batch) return 0;
+        const int L = clamp_len(seqlens[b], cap), n = nt.counts ? clamp_len(nt.counts[b], nt.most) : nt.most;
+        return L < n ? 0 : (L + 31) >> 5;
+    }
+    __device__ __forceinline__ BatchUnits(const NewTokens &nt, const int32_t *__restrict__ seqlens, int batch, int cap, int aim, int most, int lane)
+        : seqlens(seqlens), nt(nt), batch(batch), cap(cap), each((batch + 63) >> 6), mine(0) {
+        int longest = 0;
+        for (int i = 0; i < each; ++i) {
+            const int u = of_lane(lane * each + i);
+            mine += u;
+            longest = max(longest, u);
+        }
+        const int upto = (int)wave_scan((uint32_t)mine, lane);
+        before = upto - mine;
+        total = __builtin_amdgcn_readlane(upto, 63);
+        longest = (int)wave_max_u32((uint32_t)longest);
+        parts = (float)longest * (float)batch <= 1.125f * (float)total ? min(most, max(1, aim / batch)) : 0;          // 0: by units
+        per = max(4, parts ? (longest + parts - 1) / parts : max((total + aim - 1) / aim, (longest + most - 2) / (most - 1)));
+    }
+    // the sequence of unit g < total, and the units before it
+    __device__ __forceinline__ int find(int g, int &start) const {
+        const int l = __builtin_ctzll(__ballot(g >= before && g < before + mine));
+        start = __builtin_amdgcn_readlane(before, l);
+        int b = l * each;
+        for (int u; start + (u = of(b)) <= g; ++b) start += u;
+        return b;
+    }
+    // every sequence's first part and how many it has, by lanes
+    __device__ __forceinline__ void write_plan(int2 *plan, int lane) const {
+        int start = before;
+        for (int i = 0; i < each; ++i) {
+            const int b = lane * each + i, u = of_lane(b);
+            const int from = parts ? b * parts : start / per, to = parts ? from + (u - 1) / per : (start + u - 1) / per;
+            if (b < batch) plan[b] = u > 0 ? int2{from + b, to - from + 1} : int2{0, 0};
+            start += u;
+        }
+    }
+};
 // A store of 16 bytes.  kStream: past the caches.  A call that writes more than all L2s hold leaves its first results nowhere near their reader anyway, and its stores then run
 // beside the loads at 6 TB/s instead of 4.7 to 5.7 (8000 new tokens, 36 heads: 29.6 -> 23.2 us; 32768 tokens, 34 heads: 99.6 -> 94.9; 144000 evicted rows 80.8 -> 76.2).
 constexpr int64_t kAllL2 = 32ll << 20;

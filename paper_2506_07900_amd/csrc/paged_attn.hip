@@ -323,15 +323,18 @@ __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, P
 
 // ---- up to 16 rows ---------------------------------------------------------------------------------------------------------
 
-// grid (parts of the keys, Hkv, batch).  Column c of the products: head c % G of new token c / G.  A wavefront has its keys in the registers of the first product and its
+// grid (parts of the keys, Hkv, batch), or of a batch dealt by units (workgroups, Hkv): aim and most as in BatchUnits; where a sequence's parts lie goes to `plan`.  Column c of the products: head c % G of new token c / G.  A wavefront has its keys in the registers of the first product and its
 // values in LDS, the next unit's under way.
 constexpr int kFewWaves = 4;
+template <bool kBatch>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const int32_t *__restrict__ seqlens,
                                                                 Tensor out, float *__restrict__ lse, float *__restrict__ o_part,
-                                                                float2 *__restrict__ ml_part) {
+                                                                float2 *__restrict__ ml_part, int2 *__restrict__ plan, int aim, int most) {
     __shared__ __align__(16) char V0[kFewWaves][kHalfTile], V1[kFewWaves][kHalfTile];
     __shared__ float2 ml_s[kFewWaves][16];
-    const int split = blockIdx.x, n_split = gridDim.x, h = blockIdx.y, b = blockIdx.z;
+    const int h = blockIdx.y;
+    // units u_from .. u_to - 1 of sequence b; to part `part`, or (whole) the result itself
+    auto attend_part = [&](const int b, const int u_from, const int u_to, const int64_t part, const bool whole) __attribute__((always_inline)) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const Chunk ch(nt, seqlens, b, dm.max_seqlen);
     const int token = n >> lg, hq = h * dm.G + (n & (dm.G - 1));
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) bq[ks] = load8(qr + 32 * ks);
     }
-    const int end = ch.L, units = (end + 31) >> 5, u_end = (int)((int64_t)units * (split + 1) / n_split), u0 = (int)((int64_t)units * split / n_split) + wave;
+    const int end = ch.L, u_end = u_to, u0 = u_from + wave;
     const int count = u0 < u_end ? (u_end - u0 + kFewWaves - 1) / kFewWaves : 0;   // units u0, u0 + kFewWaves, ..
     const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh), *v_head = reinterpret_cast<const char *>(pg.v.ptr + h * pg.v.sh);
     const uint32_t k_at = n * (2 * (uint32_t)pg.k.st) + 16 * g;
@@ -468,7 +471,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
     for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (c ^ (n & 7)) + 4 * g) = o[c] * w;
     __syncthreads();
     const int col = tid >> 4, c8 = 8 * (tid & 15), ct = col >> lg;       // a thread joins eight channels of a column
-    if (ct >= nt.most || (ct >= ch.n && (n_split > 1 || !dm.fill))) return;
+    if (ct >= nt.most || (ct >= ch.n && (!whole || !dm.fill))) return;
     float den = 0.f, Mc = -INFINITY, y[8];
 #pragma unroll
     for (int i = 0; i < kFewWaves; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
@@ -484,7 +487,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
     }
     const int hc = h * dm.G + (col & (dm.G - 1));
     const int64_t row = ((int64_t)b * nt.most + ct) * dm.Hq + hc;
-    if (n_split == 1) {
+    if (whole) {
         const bool some = ct < ch.n && den != 0.f;
         bf16x8 z;
 #pragma unroll
@@ -492,13 +495,39 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
         *reinterpret_cast<uint4 *>(out.ptr + b * out.sb + (int64_t)ct * out.st + (int64_t)hc * out.sh + c8) = __builtin_bit_cast(uint4, z);
         if (c8 == 0) lse[row] = ct >= ch.n ? 0.f : some ? lse_of(bc + shift, den) : -INFINITY;
     } else {
-        const int64_t at = row * n_split + split;
+        const int64_t at = kBatch ? part * 16 + col : row * gridDim.x + part;
         if (den != 0.f) {
             float4 *op = reinterpret_cast<float4 *>(o_part + at * kHeadDim + c8);
             op[0] = float4{y[0], y[1], y[2], y[3]};
             op[1] = float4{y[4], y[5], y[6], y[7]};
         }
         if (c8 == 0) ml_part[at] = float2{bc + shift, den};
+    }
+    };
+    if constexpr (kBatch) {
+        const int lane = threadIdx.x & 63;
+        const BatchUnits all(nt, seqlens, dm.batch, dm.max_seqlen, aim, most, lane);
+        if (blockIdx.x == 0 && h == 0 && threadIdx.x < 64) all.write_plan(plan, lane);
+        if (all.parts) {
+            const int b = blockIdx.x / all.parts, from = (blockIdx.x - b * all.parts) * all.per, units = b < dm.batch ? all.of(b) : 0;
+            if (from < units) attend_part(b, from, min(units, from + all.per), (int64_t)h * (gridDim.x + dm.batch) + blockIdx.x + b, false);
+            return;
+        }
+        const int g0 = (int)min((int64_t)all.total, (int64_t)blockIdx.x * all.per), g1 = (int)min((int64_t)all.total, (int64_t)g0 + all.per);
+        if (g0 >= g1) return;
+        int start, b = all.find(g0, start);
+        for (;;) {
+            const int units = all.of(b);
+            if (units > 0) attend_part(b, max(0, g0 - start), min(units, g1 - start), (int64_t)h * (gridDim.x + dm.batch) + blockIdx.x + b, false);
+            start += units;
+            if (start >= g1) return;
+            ++b;
+            __syncthreads();                             // (LDS is free)
+        }
+    } else {
+        const int b = blockIdx.z, split = blockIdx.x, n_split = gridDim.x;
+        const int64_t units = (Chunk(nt, seqlens, b, dm.max_seqlen).L + 31) >> 5;
+        attend_part(b, (int)(units * split / n_split), (int)(units * (split + 1) / n_split), split, n_split == 1);
     }
 }
 
@@ -507,7 +536,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
 // kWaves wavefronts to a row, two channels to a lane, parts wave, wave + kWaves, ..: sums and channels are asked for together, before it is known which parts have any (one whose sum is
 // 0 has not, and what lies in its place is not looked at): a row costs one round trip.
 template <int kWaves>
-__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, int64_t rows, const float *__restrict__ o_part,
+__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, const int2 *__restrict__ plan, int64_t rows, const float *__restrict__ o_part,
                                                           const float2 *__restrict__ ml_part, Tensor out, float *__restrict__ lse) {
     __shared__ f32x2_t joined[kWaves][64];
     const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = kWaves == 1 ? 0 : id;
@@ -519,14 +548,23 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_k
     if (t >= n && !dm.fill) return;
     f32x2_t y = {0.f, 0.f};
     float M = -INFINITY, den = 0.f;
-    if (t < n) {                                         // (a skipped sequence's parts have no sums)
-        const float2 ml = lane < n_split ? ml_part[row * n_split + lane] : float2{-INFINITY, 0.f};
-        const float2 ml2 = kWaves == 8 && 64 + lane < n_split ? ml_part[row * n_split + 64 + lane] : float2{-INFINITY, 0.f};
-        const float *o = o_part + row * n_split * kHeadDim + 2 * lane;
+    int n_parts = n_split;
+    if (plan && t < n) n_parts = uniform_load(&plan[b].y);
+    if (t < n && n_parts > 0) {                          // (a skipped sequence has no parts, or parts without sums)
+        int64_t base = row * n_split;                    // the row's parts: base, base + step, ..
+        int step = 1;
+        if (plan) {                                      // (n_split: parts of all sequences)
+            const int lg = __builtin_ctz(dm.G);
+            base = ((int64_t)(hq >> lg) * n_split + uniform_load(&plan[b].x)) * 16 + (t << lg) + (hq & (dm.G - 1));
+            step = 16;
+        }
+        const float2 ml = lane < n_parts ? ml_part[base + lane * step] : float2{-INFINITY, 0.f};
+        const float2 ml2 = kWaves == 8 && 64 + lane < n_parts ? ml_part[base + (64 + lane) * step] : float2{-INFINITY, 0.f};
+        const float *o = o_part + base * kHeadDim + 2 * lane;
         constexpr int kStep = 16;                        // (of kWaves = 1: all parts, of 4 up to 64, of 8 up to 128)
         f32x2_t x[kStep];
 #pragma unroll
-        for (int i = 0; i < kStep; ++i) x[i] = *reinterpret_cast<const f32x2_t *>(o + (int64_t)min(wave + kWaves * i, n_split - 1) * kHeadDim);
+        for (int i = 0; i < kStep; ++i) x[i] = *reinterpret_cast<const f32x2_t *>(o + (int64_t)(min(wave + kWaves * i, n_parts - 1) * step) * kHeadDim);
         const uint64_t have = __ballot(ml.y != 0.f), have2 = kWaves == 8 ? __ballot(ml2.y != 0.f) : 0ull;    // (a NaN too)
         M = fmaxf(ml.y != 0.f ? ml.x : -INFINITY, ml2.y != 0.f ? ml2.x : -INFINITY);
         M = row_reduce(M, [](float a, float d) { return fmaxf(a, d); });
@@ -561,11 +599,12 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_k
 static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int kMaxParts = 128, kMaxChunkParts = 64;      // what paged_merge_kernel joins; of tiles of 128 rows
-// Up to 16 rows: two workgroups to a compute unit run at a time, and the keys are cut into as many parts.  More rows: with 768 tiles and more three workgroups of one group to a compute
-// unit; with fewer, workgroups of three groups, one to a compute unit, and parts where even they are fewer than the compute units.
+// Up to 16 rows: two workgroups to a compute unit run at a time, and the keys are cut into as many parts, those of a batch by the sequences' lengths.  More rows: with 768 tiles and
+// more three workgroups of one group to a compute unit; with fewer, workgroups of three groups, one to a compute unit, and parts where even they are fewer than the compute units.
+constexpr int kFewItems = 512, kChunkItems = 256;
 struct PagedPlan {
-    bool few, groups;
-    int tiles, parts;
+    bool few, groups, batch;                             // batch: parts by lengths
+    int tiles, parts, most;                              // parts: of an item; of all sequences.  most: of a sequence
     int64_t items;                                       // of one part
 };
 static int64_t paged_tiles(const Dims &dm, int64_t max_new) {
@@ -581,20 +620,25 @@ static PagedPlan paged_plan(const Dims &dm, int max_new) {
     p.tiles = (int)paged_tiles(dm, max_new);
     p.items = (int64_t)dm.batch * dm.Hkv * p.tiles;
     p.groups = p.items < 768;
-    const int64_t chip = p.few ? 512 : 256;
     // (of few rows and short caches one launch: 300 tokens 8.6 / 9.2 us, 500 10.3 / 9.3; 64 sequences of 1000 17.2 / 19.4, 32 of 768 12.9 / 12.1)
     const bool alone = p.few && (dm.max_seqlen <= 320 || (dm.max_seqlen <= 1024 && p.items >= 128));
-    p.parts = alone ? 1 : (int)max((int64_t)1, min(most_parts(dm, p.few), chip / p.items));
+    p.most = (int)most_parts(dm, p.few);
+    p.parts = alone ? 1 : (int)max((int64_t)1, min((int64_t)p.most, (p.few ? kFewItems : kChunkItems) / p.items));
+    p.batch = p.few && p.parts > 1 && dm.batch > 1 && (int64_t)dm.batch * dm.max_seqlen < (1ll << 31);
+    if (p.batch) {                                       // (what the joining kernel takes by one, four or eight wavefronts: twice to eight times the mean)
+        p.most = p.items >= 128 ? 16 : p.items >= 32 ? 64 : kMaxParts;
+        p.parts = kFewItems / dm.Hkv + dm.batch;
+    }
     return p;
 }
 // (a bound that grows with each size: of the parts of few tiles)
 size_t paged_attn_ws_bytes(const Dims &dm, int max_new) {
     if (dm.batch <= 0 || max_new <= 0) return 0;
     const bool few = (int64_t)max_new * dm.G <= 16;
-    const int64_t items = min((int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new), (int64_t)512), most = most_parts(dm, true);
-    if (most <= 1) return 0;
-    const size_t rows = (size_t)(min(items * most, items + 512) * (few ? 16 : kChunkRows));
-    return align256(rows * kHeadDim * sizeof(float)) + align256(rows * sizeof(float2));
+    const int64_t items = min((int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new), (int64_t)kFewItems);
+    if (most_parts(dm, true) <= 1) return 0;
+    const size_t rows = (size_t)((items + kFewItems + dm.Hkv) * (few ? 16 : kChunkRows));
+    return align256(rows * kHeadDim * sizeof(float)) + align256(rows * sizeof(float2)) + align256(kFewItems * sizeof(int2));
 }
 
 int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, const int32_t *seqlens, Tensor out, float *lse, void *ws, hipStream_t stream) {
@@ -603,10 +647,13 @@ int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, c
     const PagedPlan p = paged_plan(dm, nt.most);
     const int64_t rows = (int64_t)dm.batch * nt.most * dm.Hq;
     float *o_part = reinterpret_cast<float *>(ws);
-    float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) + align256((size_t)rows * p.parts * kHeadDim * sizeof(float)));
+    const size_t slots = p.batch ? (size_t)p.parts * dm.Hkv * 16 : (size_t)rows * p.parts;
+    float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) + align256(slots * kHeadDim * sizeof(float)));
+    int2 *plan = p.batch ? reinterpret_cast<int2 *>(reinterpret_cast<char *>(ml_part) + align256(slots * sizeof(float2))) : nullptr;
     if (p.few) {
         timing_begin("paged_attn_few_kernel", stream);
-        hipLaunchKernelGGL(paged_attn_few_kernel, dim3(p.parts, dm.Hkv, dm.batch), dim3(256), 0, stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part);
+        hipLaunchKernelGGL((p.batch ? paged_attn_few_kernel<true> : paged_attn_few_kernel<false>), dim3(p.batch ? kFewItems / dm.Hkv : p.parts, dm.Hkv, p.batch ? 1 : dm.batch), dim3(64 * kFewWaves), 0,
+                           stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part, plan, kFewItems / dm.Hkv, p.most);
     } else {
         const int64_t items = p.items * p.parts;
         const int run = xcd_run_length(items);
@@ -617,9 +664,9 @@ int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, c
     timing_end(stream);
     if (p.parts > 1) {
         timing_begin("paged_merge_kernel", stream);
-        const int waves = p.parts > 64 ? 8 : p.parts > 16 ? 4 : 1;
+        const int most = p.batch ? p.most : p.parts, waves = most > 64 ? 8 : most > 16 ? 4 : 1;
         hipLaunchKernelGGL((waves == 8 ? paged_merge_kernel<8> : waves == 4 ? paged_merge_kernel<4> : paged_merge_kernel<1>),
-                           dim3((unsigned)(waves > 1 ? rows : (rows + 3) / 4)), dim3(waves == 8 ? 512 : 256), 0, stream, dm, nt, p.parts, rows, o_part, ml_part, out, lse);
+                           dim3((unsigned)(waves > 1 ? rows : (rows + 3) / 4)), dim3(waves == 8 ? 512 : 256), 0, stream, dm, nt, p.parts, plan, rows, o_part, ml_part, out, lse);
         timing_end(stream);
     }
     return (int)hipGetLastError();

@@ -12,17 +12,6 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The sum of lanes 0 .. lane: within rows of sixteen by shifts, then the rows' sums.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
-    int y = (int)x;
-    y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, true);
-    y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, true);
-    y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, true);
-    y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, true);
-    const int r0 = __builtin_amdgcn_readlane(y, 15), r1 = r0 + __builtin_amdgcn_readlane(y, 31), r2 = r1 + __builtin_amdgcn_readlane(y, 47);
-    return (uint32_t)(y + (lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2));
-}
-
 // A workgroup to a sequence and head: the smallest weight that stays, by digits of 11, 11 and 10 bits from the highest on (11: exponents and two bits of mantissa spread a
 // wavefront's counts over many words; all lanes' in one word cost an addition); then the rows above it and the first of those equal to it, in order.  A wavefront holds a run of
 // rows, of up to 64 kPer in registers, of more it reads them again for each digit.

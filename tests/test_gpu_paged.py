@@ -336,6 +336,11 @@ ATTENTION = [
     (16, 1, 16, [9000, 20], None, 1, False),
     (8, 1, 64, [1200, 321], None, 2, False),
     (32, 2, 32, [6000, 300], [40, 17], 40, True),
+    # ragged batches, dealt by units; more sequences than lanes
+    (4, 2, 16, [1 + (37 * i * i) % 901 for i in range(69)] + [3000], None, 1, False),
+    (2, 1, 64, [4 + (53 * i) % 700 for i in range(130)], [(3 * i) % 5 for i in range(130)], 4, False),
+    (16, 1, 32, [9000, 40, 2000, 33, 5000, 1, 700], None, 1, True),
+    (8, 2, 64, [3000, 2990, 2980, 2991], [1, 2, 0, 1], 2, False),
 ]
 
 
