@@ -228,6 +228,8 @@ def _prepare_own(s):
     if "frequencies" in s:
         s["rope"] = binding.rope_table(c["rot"], base=BASE, interleaved=c["interleaved"], scaling=c["scaling"], factor=c["factor"],
                                        original_len=c["original"], pair_factors=_pair_factors(c) if c["scaling"] == "factors" else None)
+    if s["positions"] is not None:                               # (the call takes one for each row of each sequence)
+        s["positions"] = s["positions"].expand(b, -1).contiguous()
     if "k_pages" in s:
         s["cache"] = binding.PagedCache(s["k_pages"], s["v_pages"], s["table"])
     if c["kind"] == "append":
