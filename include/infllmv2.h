@@ -590,7 +590,8 @@ int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *r
  * infllmv2_paged_evict         keeps `budget` rows of each sequence and head: the first n_first and the last n_recent, and of the others those with the
  *                              largest weights, ties to the lower row, a NaN above all numbers.  n_first + n_recent <= budget.  Sequences of up to `budget` rows keep all.
  *                              Kept rows go, in their order, to rows 0, 1, .. of the sequence in `to`, whose pages have to be others than those that hold a sequence's
- *                              rows in `from` (the pools may be the same); its table has at least ceil(budget / page_size) entries.
+ *                              rows in `from` (the pools may be the same); its table has at least
+ *                              ceil(min(budget, max_seqlen) / page_size) entries.
  *   weights                    in   fp32 [batch, Hkv, weights_pitch], weights_pitch >= max_seqlen
  *   kept                       out  int32 [batch, Hkv, budget]: the kept rows, ascending, then -1
  *   weights_out                out  fp32 [batch, Hkv, budget]: their weights, then 0 (may be NULL)

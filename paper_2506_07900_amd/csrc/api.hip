@@ -954,7 +954,7 @@ int32_t infllmv2_paged_evict(const infllmv2_params *prm, const float *weights, i
     if (budget < 1 || n_first < 0 || n_recent < 0 || (int64_t)n_first + n_recent > budget) return INFLLMV2_ERR_INVALID_ARGUMENT;
     RETURN_IF_ERR(check_capacity(budget));
     RETURN_IF_ERR(check_pages(from, max_seqlen));
-    RETURN_IF_ERR(check_pages(to, budget));
+    RETURN_IF_ERR(check_pages(to, budget < max_seqlen ? budget : max_seqlen));
     if (!weights || !seqlens || !kept || !seqlens_out || weights_pitch < max_seqlen) return INFLLMV2_ERR_INVALID_ARGUMENT;
     const Dims dm = make_dims(prm, batch, max_seqlen);
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, paged_evict_ws_bytes(dm)));

@@ -875,7 +875,7 @@ PyObject *paged_evict(Args a) {
     expect(budget >= 1, "budget", " must be positive");
     const at::Tensor &w = tensor(a[1], "weights");
     int64_t B;
-    const infllmv2_pages from = paged(a[2], "cache", -1, T, prm, &B), to = paged(a[8], "to", B, budget, prm);
+    const infllmv2_pages from = paged(a[2], "cache", -1, T, prm, &B), to = paged(a[8], "to", B, std::min(budget, T), prm);
     const int64_t H = prm->n_kv_heads;
     const float *wp = floats(w, "weights", B, H, T);
     expect(w.size(2) < (1ll << 31), "weights", ": too many rows");

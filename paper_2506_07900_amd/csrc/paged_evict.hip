@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Dims dm, const float *_
     for (int i = 0; i < 4; ++i) {
         const int j = 64 * blockIdx.x + 16 * i + (threadIdx.x >> 4);
         src[i] = row[i] >= 0 ? from.table[(int64_t)b * from.ld + (row[i] >> from.lg)] : -1;
-        dst[i] = to.table[(int64_t)b * to.ld + (min(j, budget - 1) >> to.lg)];
+        dst[i] = row[i] >= 0 ? to.table[(int64_t)b * to.ld + (j >> to.lg)] : -1;               // (its table may end with the rows that there can be)
         if (weights_out && piece == 0 && j < budget) weights_out[bh * budget + j] = row[i] >= 0 ? weights[bh * pitch + row[i]] : 0.f;
     }
     bool moves[4];

@@ -591,7 +591,7 @@ def test_eviction(lengths, budget, first, recent, page, to_page, kind):
     gen, hkv = gen_of(budget), 2
     prm, b, cap = binding.Params(8, hkv), len(lengths), max(lengths)
     cache = filled(gen, [max(1, x) for x in lengths], hkv, page)
-    to = make_pages(gen, [budget] * b, hkv, to_page, fill=7.0)
+    to = make_pages(gen, [min(budget, cap)] * b, hkv, to_page, fill=7.0)
     w = torch.rand((b, hkv, cap + 3), generator=gen, device="cuda")
     if kind == "ties":
         w = (w * 4).floor()

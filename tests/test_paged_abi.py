@@ -99,8 +99,11 @@ def test_more_refusals(lib):
     assert call(lib, "paged_attn_weights", _10=4095) == INVALID
     assert call(lib, "paged_evict", _2=4095) == INVALID
     for budget, first, recent, want in ((0, 0, 0, INVALID), (10, 6, 5, INVALID), (10, -1, 5, INVALID), (10, 5, -1, INVALID), (10, 5, 5, 0),
-                                        (2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, INVALID), (4097, 0, 0, INVALID), (4096, 0, 0, 0)):
+                                        (2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, INVALID), (5000, 0, 0, 0), (4096, 0, 0, 0)):
         assert call(lib, "paged_evict", _7=budget, _8=first, _9=recent) == want
+    # the kept rows' table: for the budget, or for all rows there can be
+    for budget, stride, want in ((1000, 16, 0), (1000, 15, INVALID), (1 << 20, 64, 0), (1 << 20, 63, INVALID)):
+        assert call(lib, "paged_evict", _7=budget, _10=pages(stride=stride)) == want
     # a workspace that is missing, small or crooked, where one is needed
     need = lib.infllmv2_paged_workspace_bytes(binding.OP_PAGED_ATTN, ctypes.byref(params()), 1, 4096, 4)
     assert need > 0
