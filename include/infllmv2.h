@@ -579,7 +579,7 @@ int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *r
  *                              bf16 products accumulated in fp32, probabilities rounded to bf16 before the value product, their fp32 sum taken before.
  *                              A skipped sequence's new tokens, and a query that sees no row (no page) or only scores of -inf, get out 0, lse -inf.  A query that
  *                              sees a key whose score is NaN or +inf has out and lse NaN.  Values that are not finite reach the queries that see them
- *                              and no others; values up to the largest keep their mean, those below 2^-90 may lose bits.
+ *                              and no others; values up to the largest keep their mean, those below 2^-85 may lose bits.
  * infllmv2_paged_attn_weights  what every cached row gets of that attention, added to what it had:
  *                              weights_out[b, h, t] = (t < seqlens[b] - n ? weights[b, h, t] : 0) + sum over new tokens i that see row t and the query heads
  *                              g of h of exp(softmax_scale <q_ig, k_t> - lse[b, i, g]),   t < seqlens[b].

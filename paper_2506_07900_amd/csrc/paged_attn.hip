@@ -142,7 +142,9 @@ struct ChunkRows {
 };
 
 // Items: (sequence, head), part of the keys, tile of 128 rows, the last fastest.
-// kGroups groups of four wavefronts take every kGroups-th unit and are joined in LDS at the end.  Three fill a compute unit as three workgroups of one do, with a third of the parts.
+// kGroups groups of four wavefronts take every kGroups-th unit and are joined in LDS at the end.  Three fill a compute unit as three workgroups of one do, with a third of the parts
+// (1000 new tokens of 65000, 16 : 2 heads: 615 -> 527 us; 2 x 2048 of 4096, 8 : 8: 99.9 -> 74.2).  8192 of 65536, 32 : 2: 7.6 to 7.7 ms, 1.07 to 1.08 PFLOP/s: matrix cores and vector unit busy
+// 57 and 59 % at 1.85 GHz.  A unit's scores ahead, between the exponentials of the one before, takes registers for two wavefronts to a SIMD only: 8.6 ms against 8.2 in turn.
 template <int kGroups>
 __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_split, int run, Tensor q,
                                                             const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse,
@@ -323,8 +325,10 @@ __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, P
 
 // ---- up to 16 rows ---------------------------------------------------------------------------------------------------------
 
-// grid (parts of the keys, Hkv, batch), or of a batch dealt by units (workgroups, Hkv): aim and most as in BatchUnits; where a sequence's parts lie goes to `plan`.  Column c of the products: head c % G of new token c / G.  A wavefront has its keys in the registers of the first product and its
-// values in LDS, the next unit's under way.
+// grid (parts of the keys, Hkv, batch), or of a batch dealt by units (workgroups, Hkv): aim and most as in BatchUnits; where a sequence's parts lie goes to `plan`.
+// Column c of the products: head c % G of new token c / G.  A wavefront has its keys in the registers of the first product and its values in LDS, the next unit's under way: 32 KiB
+// a wavefront, two workgroups to a compute unit.  Bound by traffic where rows are many (64 sequences of 1501 to 32749 rows: 201 us, 5.6 TB/s), by a chain of round trips
+// (length, table, keys) where they are few (one of 20011: 7.6 us, and 4.3 to join).
 constexpr int kFewWaves = 4;
 template <bool kBatch>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const int32_t *__restrict__ seqlens,
@@ -335,174 +339,174 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
     const int h = blockIdx.y;
     // units u_from .. u_to - 1 of sequence b; to part `part`, or (whole) the result itself
     auto attend_part = [&](const int b, const int u_from, const int u_to, const int64_t part, const bool whole) __attribute__((always_inline)) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const Chunk ch(nt, seqlens, b, dm.max_seqlen);
-    const int token = n >> lg, hq = h * dm.G + (n & (dm.G - 1));
-    bf16x8 bq[4];                                        // channels 32 ks + 8 g ..
-    {
-        const __bf16 *qr = q.ptr + b * q.sb + (int64_t)max(0, min(token, ch.n - 1)) * q.st + (int64_t)hq * q.sh + 8 * g;
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+        const Chunk ch(nt, seqlens, b, dm.max_seqlen);
+        const int token = n >> lg, hq = h * dm.G + (n & (dm.G - 1));
+        bf16x8 bq[4];                                        // channels 32 ks + 8 g ..
+        {
+            const __bf16 *qr = q.ptr + b * q.sb + (int64_t)max(0, min(token, ch.n - 1)) * q.st + (int64_t)hq * q.sh + 8 * g;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) bq[ks] = load8(qr + 32 * ks);
-    }
-    const int end = ch.L, u_end = u_to, u0 = u_from + wave;
-    const int count = u0 < u_end ? (u_end - u0 + kFewWaves - 1) / kFewWaves : 0;   // units u0, u0 + kFewWaves, ..
-    const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh), *v_head = reinterpret_cast<const char *>(pg.v.ptr + h * pg.v.sh);
-    const uint32_t k_at = n * (2 * (uint32_t)pg.k.st) + 16 * g;
-    const int32_t *table = pg.table + (int64_t)b * pg.ld;
-    struct Unit {
-        bf16x8 k[2][4];
-        uint32_t there;
-        int k0;
-    };
-    UnitPages up;
-    auto fetch = [&](Unit &u, char *vs, int x) __attribute__((always_inline)) {
-        if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + kFewWaves * (x + lane)), x + lane < count ? end : 0);
-        u.k0 = 32 * (u0 + kFewWaves * x);
-        u.there = 0u;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int page = __builtin_amdgcn_readlane(t ? up.hi : up.lo, x & 63), first = u.k0 + 16 * t;
-            const bool some = page >= 0;
-            u.there |= some ? 1u << t : 0u;
-            const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(k_head + page_bytes(pg.k, pg.lg, max(page, 0), first)), 0, 0xfffffffeu, 0x00027000);
-            const uint32_t at = some && first + n < end ? k_at : kNoRow;
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-                u.k[t][ks] = __builtin_bit_cast(bf16x8, (u32x4_t)__builtin_amdgcn_raw_buffer_load_b128(from, at, 64 * ks, 0));
-            const char *vb = v_head + page_bytes(pg.v, pg.lg, max(page, 0), first);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {                // 1 KiB: rows 4 i + lane / 16, whose 16-byte pieces are XORed with what row_swizzle says
-                const int r = 4 * i + g;
-                copy_rows(vs + 4096 * t + 1024 * i, vb, some && first + r < end ? r * (2 * (uint32_t)pg.v.st) + 16 * (n ^ row_swizzle(r)) : kNoRow, 0);
-            }
+            for (int ks = 0; ks < 4; ++ks) bq[ks] = load8(qr + 32 * ks);
         }
-    };
-    f32x4 o[8];                                          // o[c][e]: channel 16 c + 4 g + e of column n
-    float m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float shift = (float)shift_of(ch.L);
-    const int last = ch.before + min(token, ch.n - 1);   // the last key that this column sees
-    auto attend = [&](const Unit &u, const char *vs) __attribute__((always_inline)) {
-        f32x4 s[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) s[t] = mfma16(u.k[t][ks], bq[ks], s[t]);
-            settle(s[t]);
-        }
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = s[e >> 2][e & 3];             // key 16 (e / 4) + 4 g + e % 4
-        const bool whole = u.k0 + 31 <= ch.before && u.there == 3u;
-        if (!whole) {
-            const int at = last - u.k0 - 4 * g, at0 = u.there & 1u ? at : -1, at1 = u.there & 2u ? at : -1;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = 16 * (e >> 2) + (e & 3) <= (e < 4 ? at0 : at1) ? y[e] : -INFINITY;
-        }
-        const float mx = xgroup_max(max3(max3(max3(y[0], y[1], y[2]), y[3], y[4]), max3(y[5], y[6], y[7]), y[7])) * dm.scale_log2;
-        if (__any(mx > m + kSlack)) {
-            const float alpha = follow(m, mx);
-            l *= alpha;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) o[c] *= alpha;
-        }
-        const float base = (m == -INFINITY ? 0.f : m) + shift;
-        float ps = 0.f;
-        bf16x8 p;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float e = fast_exp2(__builtin_fmaf(y[j], dm.scale_log2, -base));
-            ps += e;
-            p[j] = (__bf16)e;
-        }
-        l += ps;                                         // (this lane's keys only: joined over g at the end)
-        const int r = 4 * g + (n >> 2);
-        bool odd = false;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {                    // A: channel 16 c + n, keys 4 g .. and 16 + 4 g ..
-            const char *at = vs + 8 * (n & 1);
-            const int piece = 2 * c + ((n & 3) >> 1);
-            const s16x4 x0 = lds_read_tr16(at + r * 256 + ((piece ^ row_swizzle(r)) << 4));
-            const s16x4 x1 = lds_read_tr16(at + (r + 16) * 256 + ((piece ^ row_swizzle(r)) << 4));
-            bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
-            if (!whole) odd |= take_odd_out(x);
-            o[c] = mfma16(x, p, o[c]);
-        }
-        if (whole || !__any(odd)) return;
-#pragma unroll 1
-        for (int t = 0; t < 32; ++t) {
-            const bool sees = u.k0 + t <= last;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const uint2 w = *reinterpret_cast<const uint2 *>(vs + 256 * t + (((2 * c + (g >> 1)) ^ row_swizzle(t)) << 4) + 8 * (g & 1));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[c][e] += odd_value(w, e, sees);
-            }
-        }
-    };
-    {
-        Unit a, c;
-        char *v0 = V0[wave], *v1 = V1[wave];
-        auto step = [&](Unit &cur, Unit &next, char *vc, char *vn, int x) __attribute__((always_inline)) {
-            reads_done();
-            if (x + 1 < count) fetch(next, vn, x + 1);
-            copies_landed(x + 1 < count);
-            attend(cur, vc);
+        const int end = ch.L, u_end = u_to, u0 = u_from + wave;
+        const int count = u0 < u_end ? (u_end - u0 + kFewWaves - 1) / kFewWaves : 0;   // units u0, u0 + kFewWaves, ..
+        const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh), *v_head = reinterpret_cast<const char *>(pg.v.ptr + h * pg.v.sh);
+        const uint32_t k_at = n * (2 * (uint32_t)pg.k.st) + 16 * g;
+        const int32_t *table = pg.table + (int64_t)b * pg.ld;
+        struct Unit {
+            bf16x8 k[2][4];
+            uint32_t there;
+            int k0;
         };
-        if (count > 0) fetch(a, v0, 0);
-        for (int x = 0; x < count; x += 2) {
-            step(a, c, v0, v1, x);
-            if (x + 1 < count) step(c, a, v1, v0, x + 1);
+        UnitPages up;
+        auto fetch = [&](Unit &u, char *vs, int x) __attribute__((always_inline)) {
+            if ((x & 63) == 0) up.load(pg, table, 32 * (u0 + kFewWaves * (x + lane)), x + lane < count ? end : 0);
+            u.k0 = 32 * (u0 + kFewWaves * x);
+            u.there = 0u;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int page = __builtin_amdgcn_readlane(t ? up.hi : up.lo, x & 63), first = u.k0 + 16 * t;
+                const bool some = page >= 0;
+                u.there |= some ? 1u << t : 0u;
+                const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(k_head + page_bytes(pg.k, pg.lg, max(page, 0), first)), 0, 0xfffffffeu, 0x00027000);
+                const uint32_t at = some && first + n < end ? k_at : kNoRow;
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                    u.k[t][ks] = __builtin_bit_cast(bf16x8, (u32x4_t)__builtin_amdgcn_raw_buffer_load_b128(from, at, 64 * ks, 0));
+                const char *vb = v_head + page_bytes(pg.v, pg.lg, max(page, 0), first);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                // 1 KiB: rows 4 i + lane / 16, whose 16-byte pieces are XORed with what row_swizzle says
+                    const int r = 4 * i + g;
+                    copy_rows(vs + 4096 * t + 1024 * i, vb, some && first + r < end ? r * (2 * (uint32_t)pg.v.st) + 16 * (n ^ row_swizzle(r)) : kNoRow, 0);
+                }
+            }
+        };
+        f32x4 o[8];                                          // o[c][e]: channel 16 c + 4 g + e of column n
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float shift = (float)shift_of(ch.L);
+        const int last = ch.before + min(token, ch.n - 1);   // the last key that this column sees
+        auto attend = [&](const Unit &u, const char *vs) __attribute__((always_inline)) {
+            f32x4 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) s[t] = mfma16(u.k[t][ks], bq[ks], s[t]);
+                settle(s[t]);
+            }
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = s[e >> 2][e & 3];             // key 16 (e / 4) + 4 g + e % 4
+            const bool whole = u.k0 + 31 <= ch.before && u.there == 3u;
+            if (!whole) {
+                const int at = last - u.k0 - 4 * g, at0 = u.there & 1u ? at : -1, at1 = u.there & 2u ? at : -1;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = 16 * (e >> 2) + (e & 3) <= (e < 4 ? at0 : at1) ? y[e] : -INFINITY;
+            }
+            const float mx = xgroup_max(max3(max3(max3(y[0], y[1], y[2]), y[3], y[4]), max3(y[5], y[6], y[7]), y[7])) * dm.scale_log2;
+            if (__any(mx > m + kSlack)) {
+                const float alpha = follow(m, mx);
+                l *= alpha;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) o[c] *= alpha;
+            }
+            const float base = (m == -INFINITY ? 0.f : m) + shift;
+            float ps = 0.f;
+            bf16x8 p;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float e = fast_exp2(__builtin_fmaf(y[j], dm.scale_log2, -base));
+                ps += e;
+                p[j] = (__bf16)e;
+            }
+            l += ps;                                         // (this lane's keys only: joined over g at the end)
+            const int r = 4 * g + (n >> 2);
+            bool odd = false;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {                    // A: channel 16 c + n, keys 4 g .. and 16 + 4 g ..
+                const char *at = vs + 8 * (n & 1);
+                const int piece = 2 * c + ((n & 3) >> 1);
+                const s16x4 x0 = lds_read_tr16(at + r * 256 + ((piece ^ row_swizzle(r)) << 4));
+                const s16x4 x1 = lds_read_tr16(at + (r + 16) * 256 + ((piece ^ row_swizzle(r)) << 4));
+                bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
+                if (!whole) odd |= take_odd_out(x);
+                o[c] = mfma16(x, p, o[c]);
+            }
+            if (whole || !__any(odd)) return;
+#pragma unroll 1
+            for (int t = 0; t < 32; ++t) {
+                const bool sees = u.k0 + t <= last;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(vs + 256 * t + (((2 * c + (g >> 1)) ^ row_swizzle(t)) << 4) + 8 * (g & 1));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[c][e] += odd_value(w, e, sees);
+                }
+            }
+        };
+        {
+            Unit a, c;
+            char *v0 = V0[wave], *v1 = V1[wave];
+            auto step = [&](Unit &cur, Unit &next, char *vc, char *vn, int x) __attribute__((always_inline)) {
+                reads_done();
+                if (x + 1 < count) fetch(next, vn, x + 1);
+                copies_landed(x + 1 < count);
+                attend(cur, vc);
+            };
+            if (count > 0) fetch(a, v0, 0);
+            for (int x = 0; x < count; x += 2) {
+                step(a, c, v0, v1, x);
+                if (x + 1 < count) step(c, a, v1, v0, x + 1);
+            }
         }
-    }
-    reads_done();
-    l = xgroup_sum(l);
-    // ---- the wavefronts' states into one -----------------------------------------------------------------------------------
-    if (g == 0) ml_s[wave][n] = float2{m, l};
-    __syncthreads();
-    float M = -INFINITY;
+        reads_done();
+        l = xgroup_sum(l);
+        // ---- the wavefronts' states into one -----------------------------------------------------------------------------------
+        if (g == 0) ml_s[wave][n] = float2{m, l};
+        __syncthreads();
+        float M = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kFewWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
-    const float w = fast_exp2(m - (M == -INFINITY ? 0.f : M));
-    float *mine = reinterpret_cast<float *>(V0[wave]);   // [column][channel]
+        for (int i = 0; i < kFewWaves; ++i) M = fmaxf(M, ml_s[i][n].x);
+        const float w = fast_exp2(m - (M == -INFINITY ? 0.f : M));
+        float *mine = reinterpret_cast<float *>(V0[wave]);   // [column][channel]
 #pragma unroll
-    for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (c ^ (n & 7)) + 4 * g) = o[c] * w;
-    __syncthreads();
-    const int col = tid >> 4, c8 = 8 * (tid & 15), ct = col >> lg;       // a thread joins eight channels of a column
-    if (ct >= nt.most || (ct >= ch.n && (!whole || !dm.fill))) return;
-    float den = 0.f, Mc = -INFINITY, y[8];
+        for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4 *>(mine + n * kHeadDim + 16 * (c ^ (n & 7)) + 4 * g) = o[c] * w;
+        __syncthreads();
+        const int col = tid >> 4, c8 = 8 * (tid & 15), ct = col >> lg;       // a thread joins eight channels of a column
+        if (ct >= nt.most || (ct >= ch.n && (!whole || !dm.fill))) return;
+        float den = 0.f, Mc = -INFINITY, y[8];
 #pragma unroll
-    for (int i = 0; i < kFewWaves; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
-    const float bc = Mc == -INFINITY ? 0.f : Mc;
+        for (int i = 0; i < kFewWaves; ++i) Mc = fmaxf(Mc, ml_s[i][col].x);
+        const float bc = Mc == -INFINITY ? 0.f : Mc;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = 0.f;
+        for (int e = 0; e < 8; ++e) y[e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < kFewWaves; ++i) {
-        den += ml_s[i][col].y * fast_exp2(ml_s[i][col].x - bc);
-        const float *from = reinterpret_cast<const float *>(V0[i]) + col * kHeadDim + 16 * ((c8 >> 4) ^ (col & 7)) + (c8 & 15);
+        for (int i = 0; i < kFewWaves; ++i) {
+            den += ml_s[i][col].y * fast_exp2(ml_s[i][col].x - bc);
+            const float *from = reinterpret_cast<const float *>(V0[i]) + col * kHeadDim + 16 * ((c8 >> 4) ^ (col & 7)) + (c8 & 15);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] += from[e];
-    }
-    const int hc = h * dm.G + (col & (dm.G - 1));
-    const int64_t row = ((int64_t)b * nt.most + ct) * dm.Hq + hc;
-    if (whole) {
-        const bool some = ct < ch.n && den != 0.f;
-        bf16x8 z;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = (__bf16)(some ? mean(y[e] / den) : 0.f);
-        *reinterpret_cast<uint4 *>(out.ptr + b * out.sb + (int64_t)ct * out.st + (int64_t)hc * out.sh + c8) = __builtin_bit_cast(uint4, z);
-        if (c8 == 0) lse[row] = ct >= ch.n ? 0.f : some ? lse_of(bc + shift, den) : -INFINITY;
-    } else {
-        const int64_t at = kBatch ? part * 16 + col : row * gridDim.x + part;
-        if (den != 0.f) {
-            float4 *op = reinterpret_cast<float4 *>(o_part + at * kHeadDim + c8);
-            op[0] = float4{y[0], y[1], y[2], y[3]};
-            op[1] = float4{y[4], y[5], y[6], y[7]};
+            for (int e = 0; e < 8; ++e) y[e] += from[e];
         }
-        if (c8 == 0) ml_part[at] = float2{bc + shift, den};
-    }
+        const int hc = h * dm.G + (col & (dm.G - 1));
+        const int64_t row = ((int64_t)b * nt.most + ct) * dm.Hq + hc;
+        if (whole) {
+            const bool some = ct < ch.n && den != 0.f;
+            bf16x8 z;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = (__bf16)(some ? mean(y[e] / den) : 0.f);
+            *reinterpret_cast<uint4 *>(out.ptr + b * out.sb + (int64_t)ct * out.st + (int64_t)hc * out.sh + c8) = __builtin_bit_cast(uint4, z);
+            if (c8 == 0) lse[row] = ct >= ch.n ? 0.f : some ? lse_of(bc + shift, den) : -INFINITY;
+        } else {
+            const int64_t at = kBatch ? part * 16 + col : row * gridDim.x + part;
+            if (den != 0.f) {
+                float4 *op = reinterpret_cast<float4 *>(o_part + at * kHeadDim + c8);
+                op[0] = float4{y[0], y[1], y[2], y[3]};
+                op[1] = float4{y[4], y[5], y[6], y[7]};
+            }
+            if (c8 == 0) ml_part[at] = float2{bc + shift, den};
+        }
     };
     if constexpr (kBatch) {
         const int lane = threadIdx.x & 63;

@@ -8,7 +8,8 @@ namespace infllmv2 {
 // exp(score - lse) as a power of two: nothing for a head whose lse is -inf
 __device__ __forceinline__ float lse_log2(float x) { return x == -INFINITY ? INFINITY : x * kLog2e; }
 
-// Up to 16 query rows, all columns of one product; a wavefront takes units of 32 keys in turn.  grid (parts, Hkv, batch).  Bound by the keys' traffic.
+// Up to 16 query rows, all columns of one product; a wavefront takes units of 32 keys in turn.  grid (parts, Hkv, batch).  Bound by the keys' traffic
+// (64 sequences of 4001 to 8191 rows: 43.7 us, 4.7 TB/s; one of 20000: 5.5, a chain of round trips).
 __global__ __launch_bounds__(256) void paged_weights_few_kernel(Dims dm, Pages pg, NewTokens nt, int lg, Tensor q, const float *__restrict__ lse,
                                                                 const int32_t *__restrict__ seqlens, const float *weights, int pitch, float *weights_out) {
     const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -90,7 +91,8 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(Dims dm, Pages p
 
 // More rows: a workgroup takes 128 keys, 32 to a wavefront, which hold them in registers, and walks over the rows that see any of them, 32 at a time through LDS.
 // What a lane adds up is one column's share of each of its keys.  Bound by the exponentials and the products, which are half of the attention's.
-// Where tiles of keys are fewer than the workgroups that run at a time, a tile's rows are cut into parts, and a second kernel adds these up.
+// 4096 new tokens over 32749 rows, 32 : 2 heads: 1.07 ms, 0.96 PFLOP/s, vector unit busy 72 %, matrix cores 54 %, at 1.9 GHz.
+// Where tiles of keys are fewer than keep the chip evenly busy, a tile's rows are cut into parts, and a second kernel adds these up.
 __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_part, int run, Tensor q, const float *__restrict__ lse,
                                                                const int32_t *__restrict__ seqlens, const float *weights, int pitch, float *weights_out,
                                                                float *__restrict__ partial) {
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(128) void paged_weights_join_kernel(Dims dm, NewTok
     weights_out[at] = (weights && key < ch.before ? weights[at] : 0.f) + sum;
 }
 
-constexpr int kWeightItems = 3072;                       // workgroups that run at a time
+constexpr int kWeightItems = 3072;                       // four rounds of workgroups (1024 / 3072: 1230 / 1072 us)
 static int64_t weight_items(const Dims &dm) { return ((int64_t)dm.max_seqlen + 127) / 128 * dm.Hkv * dm.batch; }
 static int64_t most_weight_parts(const Dims &dm, int max_new) { return max((int64_t)1, (int64_t)max_new * dm.G / 128); }    // four units of rows and more to a part
 // (a bound that grows with each size)

@@ -244,6 +244,53 @@ def test_append(page, hq, hkv, lengths, counts, n):
             assert torch.equal(x.view(torch.int16), y.view(torch.int16))
 
 
+def test_counts_of_new_tokens_outside_their_range():
+    """more than there are rows for: all of them; less than none: none"""
+    gen = gen_of(31)
+    prm, lengths = binding.Params(4, 2), [300, 200, 100]
+    for n in (2, 6, 40):
+        cache = filled(gen, lengths, 2, 16)
+        q, k = normal(gen, 3, n, 4, D), normal(gen, 3, 2, n, D)
+        got, want = [], []
+        for counts, results in (([1000, -7, -2 ** 31], got), ([n, 0, 0], want)):
+            c = cache._replace(k=cache.k.clone(), v=cache.v.clone())
+            binding.paged_append(prm, k, k, c, i32(lengths), 300, n_new=i32(counts))
+            out, lse = binding.paged_attn(prm, q, c, i32(lengths), 300, n_new=i32(counts))
+            results += [c.k.view(torch.int16), c.v.view(torch.int16), out, lse,
+                        binding.paged_attn_weights(prm, q, lse, c, i32(lengths), 300, n_new=i32(counts))]
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_c_calls_without_what_is_optional():
+    """the C entry points with null pointers for what they may do without"""
+    import ctypes
+    from paper_2506_07900_amd.binding import CPages, CTensor
+    gen, lib = gen_of(32), binding.load_library()
+    prm, length, budget = binding.Params(4, 2), 500, 100
+    cache, to = filled(gen, [length], 2, 16), make_pages(gen, [budget], 2, 16, fill=0.0)
+    w, sl = torch.rand((1, 2, length), generator=gen, device="cuda"), i32([length])
+    kept, lengths = torch.zeros((1, 2, budget), dtype=torch.int32, device="cuda"), i32([0])
+
+    def pages(c):
+        d = [CTensor(x.data_ptr(), x.stride(0), x.stride(1), x.stride(2)) for x in c[:2]]
+        return CPages(d[0], d[1], c.table.data_ptr(), c.table.shape[1], c.k.shape[2], c.k.shape[0])
+
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    p, f, t = prm.c(), pages(cache), pages(to)
+    assert lib.infllmv2_paged_evict(ctypes.byref(p), w.data_ptr(), length, ctypes.byref(f), sl.data_ptr(), 1, length, budget, 4, 10, ctypes.byref(t), kept.data_ptr(),
+                                    None, lengths.data_ptr(), None, 0, stream) == 0
+    first = to.k.clone()
+    ref = binding.paged_evict(prm, w, cache, sl, length, budget, 4, 10, to)
+    assert torch.equal(kept, ref[0]) and torch.equal(lengths, ref[2]) and torch.equal(first, to.k)
+    q = normal(gen, 1, 1, 4, D)
+    _, lse = binding.paged_attn(prm, q, cache, sl, length)
+    out = torch.zeros((1, 2, length), device="cuda")
+    qd = CTensor(q.data_ptr(), q.stride(0), q.stride(2), q.stride(1))
+    assert lib.infllmv2_paged_attn_weights(ctypes.byref(p), ctypes.byref(qd), lse.data_ptr(), ctypes.byref(f), None, sl.data_ptr(), 1, length, 1, None, length, out.data_ptr(),
+                                           None, 0, stream) == 0
+    assert torch.equal(out, binding.paged_attn_weights(prm, q, lse, cache, sl, length))
+
+
 def test_append_skips():
     """sequences shorter than what is new, longer than the bound, rows without a page"""
     gen = gen_of(9)
