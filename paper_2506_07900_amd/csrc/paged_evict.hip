@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
     for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
         const uint32_t digits = shift == 0 ? 1023u : kDigits - 1u;
         hist[tid] = hist[tid + kPickThreads] = 0u;
-        if (tid == 0) over = 0;
+        if (shift == 21 && tid == 0) over = 0;           // (once: a later pass would clear it before all have read it)
         __syncthreads();
         if (shift == 21) {
             rows([&](uint32_t y, int) __attribute__((always_inline)) {

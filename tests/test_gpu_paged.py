@@ -671,6 +671,21 @@ def test_eviction(lengths, budget, first, recent, page, to_page, kind):
         assert torch.equal(got.view(torch.int16), want.view(torch.int16))
 
 
+def test_eviction_of_ties_in_many_workgroups():
+    """more numbers with the first digit than a run's list takes: all wavefronts have to go on alike, in every workgroup"""
+    gen, hkv, b, cap, budget = gen_of(9), 4, 128, 20000, 3001
+    prm = binding.Params(4, hkv)
+    lengths = [cap - 37 * i for i in range(b)]
+    cache = make_pages(gen, [16] * b, hkv, 16)
+    cache = binding.PagedCache(cache.k, cache.v, torch.full((b, cap // 16), -1, dtype=torch.int32, device="cuda"))
+    to = binding.PagedCache(cache.k, cache.v, torch.full((b, budget // 16 + 1), -1, dtype=torch.int32, device="cuda"))
+    w = 1.0 + torch.randint(0, 3, (b, hkv, cap), generator=gen, device="cuda").float() * 2.0 ** -23      # (equal but for their last bits)
+    hidden = torch.arange(cap, device="cuda") >= torch.tensor(lengths, device="cuda")[:, None, None]
+    want = torch.where(hidden, -1.0, w).sort(dim=-1, descending=True, stable=True).indices[:, :, :budget].sort(dim=-1).values.int()
+    for _ in range(20):
+        assert torch.equal(binding.paged_evict(prm, w, cache, i32(lengths), cap, budget, 0, 0, to)[0], want)
+
+
 def test_eviction_with_rows_without_pages():
     gen = gen_of(1)
     prm = binding.Params(2, 1)
