@@ -231,7 +231,7 @@ __global__ __launch_bounds__(128) void paged_weights_join_kernel(Dims dm, NewTok
     weights_out[at] = (weights && key < ch.before ? weights[at] : 0.f) + sum;
 }
 
-constexpr int kWeightItems = 3072;                       // four rounds of workgroups (1024 / 3072: 1230 / 1072 us)
+constexpr int kWeightItems = 12 * 256;                   // four rounds of three workgroups to a compute unit (without parts / with: 1230 / 1072 us)
 static int64_t weight_items(const Dims &dm) { return ((int64_t)dm.max_seqlen + 127) / 128 * dm.Hkv * dm.batch; }
 static int64_t most_weight_parts(const Dims &dm, int max_new) { return max((int64_t)1, (int64_t)max_new * dm.G / 128); }    // four units of rows and more to a part
 // (a bound that grows with each size)
