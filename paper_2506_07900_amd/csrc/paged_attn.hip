@@ -141,20 +141,80 @@ struct ChunkRows {
     }
 };
 
-// Items: (sequence, head), part of the keys, tile of 128 rows, the last fastest.
+// Where tiles are few: those that hold new tokens, of all sequences, each with its keys cut into as many parts as there are workgroups for.  Items are numbered by sequence, head, part and
+// tile, the last fastest; item x has the 128 partial rows 128 x ..  All lanes of a wavefront.  (As many parts as for `most` tokens of each, 37 and 21 new tokens of 32749 rows, 16 : 2 heads,
+// leave 42 of 252 workgroups without work: 40.0 us instead of 36.2.  Where all have as many it costs up to 0.8 us: 8 of 64 tokens, 34.4 / 35.2.)
+constexpr int kChunkItems = 256;
+struct ChunkTiles {
+    const int32_t *seqlens;
+    NewTokens nt;
+    int batch, cap, lg, each, before, mine, total, parts;       // before, mine: tiles before this lane's `each` sequences, and of them
+    __device__ __forceinline__ int of(int b) const {
+        if (b >= batch) return 0;
+        const int L = clamp_len(seqlens[b], cap), n = nt.counts ? clamp_len(nt.counts[b], nt.most) : nt.most;
+        return L < n ? 0 : (int)((((int64_t)n << lg) + kChunkRows - 1) / kChunkRows);
+    }
+    __device__ __forceinline__ ChunkTiles(const NewTokens &nt, const int32_t *__restrict__ seqlens, int batch, int cap, int lg, int heads, int most, int lane)
+        : seqlens(seqlens), nt(nt), batch(batch), cap(cap), lg(lg), each((batch + 63) >> 6), mine(0) {
+        for (int i = 0; i < each; ++i) mine += of(lane * each + i);
+        const int upto = (int)wave_scan((uint32_t)mine, lane);
+        before = upto - mine;
+        total = __builtin_amdgcn_readlane(upto, 63);
+        parts = max(1, min(most, kChunkItems / max(1, total * heads)));
+    }
+    // the sequence of tile g < total, the tiles before it and its own
+    __device__ __forceinline__ int find(int g, int &start, int &tiles) const {
+        const int l = __builtin_ctzll(__ballot(g >= before && g < before + mine));
+        start = __builtin_amdgcn_readlane(before, l);
+        tiles = __builtin_amdgcn_readlane(mine, l);
+        int b = l * each;
+        if (each > 1)
+            for (; start + (tiles = __builtin_amdgcn_readfirstlane(of(b))) <= g; ++b) start += tiles;
+        return b;
+    }
+    // every sequence's first item, and its tiles (0: of none) and parts, by lanes
+    __device__ __forceinline__ void write_plan(int2 *plan, int heads, int lane) const {
+        int start = before;
+        for (int i = 0; i < each; ++i) {
+            const int b = lane * each + i, n = of(b);
+            if (b < batch) plan[b] = int2{start * heads * parts, n | parts << 16};
+            start += n;
+        }
+    }
+};
+
+// Items: (sequence, head), tile of 128 rows, the last fastest, or (kParts) as ChunkTiles numbers them, n_tiles: most parts.
 // kGroups groups of four wavefronts take every kGroups-th unit and are joined in LDS at the end.  Three fill a compute unit as three workgroups of one do, with a third of the parts
 // (1000 new tokens of 65000, 16 : 2 heads: 615 -> 527 us; 2 x 2048 of 4096, 8 : 8: 99.9 -> 74.2).  8192 of 65536, 32 : 2: 7.6 to 7.7 ms, 1.07 to 1.08 PFLOP/s: matrix cores and vector unit busy
 // 57 and 59 % at 1.85 GHz.  A unit's scores ahead, between the exponentials of the one before, takes registers for two wavefronts to a SIMD only: 8.6 ms against 8.2 in turn.
-template <int kGroups>
-__global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_split, int run, Tensor q,
+template <int kGroups, bool kParts>
+__global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int run, Tensor q,
                                                             const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse,
-                                                            float *__restrict__ o_part, float2 *__restrict__ ml_part) {
+                                                            float *__restrict__ o_part, float2 *__restrict__ ml_part, int2 *__restrict__ plan) {
     __shared__ KVHalf slots0[kGroups], slots1[kGroups], slots2[kGroups];
     __shared__ float2 ml_s[kGroups][4][64];
-    const int item = xcd_item(blockIdx.x, run), bs = item / n_tiles, bh = bs / n_split, split = bs - bh * n_split, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
-    if (b >= dm.batch) return;
-    const int ti = (bs + 1) * n_tiles - 1 - item;        // the last rows, which see most keys, first
-    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id & 3, group = id >> 2;
+    const int item = xcd_item(blockIdx.x, run), lane = threadIdx.x & 63;
+    int b, h, ti, split = 0, n_split = 1, slot = 0;      // ti: the last rows, which see most keys, first
+    if constexpr (kParts) {
+        const ChunkTiles all(nt, seqlens, dm.batch, dm.max_seqlen, lg, dm.Hkv, n_tiles, lane);
+        if (blockIdx.x == 0 && threadIdx.x < 64) all.write_plan(plan, dm.Hkv, lane);
+        n_split = all.parts;
+        if (item >= all.total * dm.Hkv * n_split) return;
+        int start, tiles;
+        b = all.find(item / (dm.Hkv * n_split), start, tiles);
+        const int x = item - start * (dm.Hkv * n_split), hs = x / tiles;
+        h = hs / n_split;
+        split = hs - h * n_split;
+        ti = (hs + 1) * tiles - 1 - x;
+        slot = start * (dm.Hkv * n_split) + hs * tiles + ti;
+    } else {
+        const int bh = item / n_tiles;
+        b = bh / dm.Hkv;
+        h = bh - b * dm.Hkv;
+        ti = (bh + 1) * n_tiles - 1 - item;
+        if (b >= dm.batch) return;
+    }
+    const int id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id & 3, group = id >> 2;
     KVHalf &slot0 = slots0[group], &slot1 = slots1[group], &slot2 = slots2[group];
     const Chunk ch(nt, seqlens, b, dm.max_seqlen);
     const int t0 = ti * (kChunkRows >> lg), t1 = min(ch.n, t0 + (kChunkRows >> lg));
@@ -164,7 +224,7 @@ __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, P
     const int units = (end + 31) >> 5, from = (int)((int64_t)units * split / n_split), all = (int)((int64_t)units * (split + 1) / n_split) - from;
     const int count = (all - group + kGroups - 1) / kGroups;              // this group's units
     auto unit = [&](int x) __attribute__((always_inline)) { return from + group + kGroups * x; };
-    if (t0 >= ch.n && (n_split > 1 || !dm.fill)) return;
+    if (!kParts && t0 >= ch.n && !dm.fill) return;
     r.scale = dm.scale_log2;
     r.shift = (float)shift_of(ch.L);
     r.i = ch.before + token;
@@ -271,22 +331,24 @@ __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, P
             r.l += other.y * theirs;
             const char *at = block(g);
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct)
+            for (int ct = 0; ct < 4; ++ct) {
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
                     const f32x4 x = *reinterpret_cast<const f32x4 *>(at + 1024 * (4 * ct + e4));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) r.o[ct][4 * e4 + e] += x[e] * theirs;
                 }
+                asm volatile("" : "+v"(r.o[ct]));        // (here: else the additions move behind the branch below, and all of x is kept for them)
+            }
         }
         mine = block(1) - 16 * lane;                     // (read by this wavefront alone)
         reads_done();
     }
     r.l = half_reduce(r.l, [](float a, float d) { return a + d; });
     const bool live = token < ch.n;
-    if (n_split > 1) {
+    if constexpr (kParts) {
         if (!live) return;
-        const int64_t at = (((int64_t)b * nt.most + token) * dm.Hq + hq) * n_split + split;
+        const int64_t at = (int64_t)slot * kChunkRows + row;
         if (r.hf == 0) ml_part[at] = float2{r.m + r.shift, r.l};
         if (r.l != 0.f) {                                // (a NaN too)
             float *op = o_part + at * kHeadDim + 4 * r.hf;
@@ -539,7 +601,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
 
 // kWaves wavefronts to a row, two channels to a lane, parts wave, wave + kWaves, ..: sums and channels are asked for together, before it is known which parts have any (one whose sum is
 // 0 has not, and what lies in its place is not looked at): a row costs one round trip.
-template <int kWaves>
+template <int kWaves, bool kTiles>
 __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_kernel(Dims dm, NewTokens nt, int n_split, const int2 *__restrict__ plan, int64_t rows, const float *__restrict__ o_part,
                                                           const float2 *__restrict__ ml_part, Tensor out, float *__restrict__ lse) {
     __shared__ f32x2_t joined[kWaves][64];
@@ -554,11 +616,17 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_k
     float M = -INFINITY, den = 0.f;
     int n_parts = n_split;
     if (plan && t < n) n_parts = uniform_load(&plan[b].y);
+    const int tiles = n_parts & 0xffff;                  // (kTiles)
+    if constexpr (kTiles) n_parts = tiles ? n_parts >> 16 : 0;
     if (t < n && n_parts > 0) {                          // (a skipped sequence has no parts, or parts without sums)
         int64_t base = row * n_split;                    // the row's parts: base, base + step, ..
         int step = 1;
-        if (plan) {                                      // (n_split: parts of all sequences)
-            const int lg = __builtin_ctz(dm.G);
+        const int lg = __builtin_ctz(dm.G);
+        if constexpr (kTiles) {
+            const int at = (t << lg) + (hq & (dm.G - 1));
+            base = (int64_t)(uniform_load(&plan[b].x) + (hq >> lg) * n_parts * tiles + at / kChunkRows) * kChunkRows + at % kChunkRows;
+            step = tiles * kChunkRows;
+        } else if (plan) {                               // (n_split: parts of all sequences)
             base = ((int64_t)(hq >> lg) * n_split + uniform_load(&plan[b].x)) * 16 + (t << lg) + (hq & (dm.G - 1));
             step = 16;
         }
@@ -605,7 +673,7 @@ static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kMaxParts = 128, kMaxChunkParts = 64;      // what paged_merge_kernel joins; of tiles of 128 rows
 // Up to 16 rows: two workgroups to a compute unit run at a time, and the keys are cut into as many parts, those of a batch by the sequences' lengths.  More rows: with 768 tiles and
 // more three workgroups of one group to a compute unit; with fewer, workgroups of three groups, one to a compute unit, and parts where even they are fewer than the compute units.
-constexpr int kFewItems = 512, kChunkItems = 256;
+constexpr int kFewItems = 512;
 struct PagedPlan {
     bool few, groups, batch;                             // batch: parts by lengths
     int tiles, parts, most;                              // parts: of an item; of all sequences.  most: of a sequence
@@ -633,6 +701,7 @@ static PagedPlan paged_plan(const Dims &dm, int max_new) {
         p.most = p.items >= 128 ? 16 : p.items >= 32 ? 64 : kMaxParts;
         p.parts = kFewItems / dm.Hkv + dm.batch;
     }
+    if (!p.few && p.parts <= 16) p.most = min(p.most, 16);              // (of tiles with new tokens only: a wavefront joins up to 16)
     return p;
 }
 // (a bound that grows with each size: of the parts of few tiles)
@@ -651,26 +720,28 @@ int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, c
     const PagedPlan p = paged_plan(dm, nt.most);
     const int64_t rows = (int64_t)dm.batch * nt.most * dm.Hq;
     float *o_part = reinterpret_cast<float *>(ws);
-    const size_t slots = p.batch ? (size_t)p.parts * dm.Hkv * 16 : (size_t)rows * p.parts;
+    const size_t slots = !p.few ? (size_t)kChunkItems * kChunkRows : p.batch ? (size_t)p.parts * dm.Hkv * 16 : (size_t)rows * p.parts;
     float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) + align256(slots * kHeadDim * sizeof(float)));
-    int2 *plan = p.batch ? reinterpret_cast<int2 *>(reinterpret_cast<char *>(ml_part) + align256(slots * sizeof(float2))) : nullptr;
+    int2 *plan = p.batch || (!p.few && p.parts > 1) ? reinterpret_cast<int2 *>(reinterpret_cast<char *>(ml_part) + align256(slots * sizeof(float2))) : nullptr;
     if (p.few) {
         timing_begin("paged_attn_few_kernel", stream);
         hipLaunchKernelGGL((p.batch ? paged_attn_few_kernel<true> : paged_attn_few_kernel<false>), dim3(p.batch ? kFewItems / dm.Hkv : p.parts, dm.Hkv, p.batch ? 1 : dm.batch), dim3(64 * kFewWaves), 0,
                            stream, dm, pg, nt, lg, q, seqlens, out, lse, o_part, ml_part, plan, kFewItems / dm.Hkv, p.most);
     } else {
-        const int64_t items = p.items * p.parts;
+        const int64_t items = p.parts > 1 ? kChunkItems : p.items;
         const int run = xcd_run_length(items);
         timing_begin("paged_attn_kernel", stream);
-        hipLaunchKernelGGL((p.groups ? paged_attn_kernel<3> : paged_attn_kernel<1>), dim3(xcd_grid(items, run)), dim3(p.groups ? 768 : 256), 0, stream, dm, pg, nt, lg, p.tiles, p.parts, run, q, seqlens, out, lse,
-                           o_part, ml_part);
+        hipLaunchKernelGGL((p.parts > 1 ? paged_attn_kernel<3, true> : p.groups ? paged_attn_kernel<3, false> : paged_attn_kernel<1, false>), dim3(xcd_grid(items, run)), dim3(p.groups ? 768 : 256), 0,
+                           stream, dm, pg, nt, lg, p.parts > 1 ? p.most : p.tiles, run, q, seqlens, out, lse, o_part, ml_part, plan);
     }
     timing_end(stream);
     if (p.parts > 1) {
         timing_begin("paged_merge_kernel", stream);
-        const int most = p.batch ? p.most : p.parts, waves = most > 64 ? 8 : most > 16 ? 4 : 1;
-        hipLaunchKernelGGL((waves == 8 ? paged_merge_kernel<8> : waves == 4 ? paged_merge_kernel<4> : paged_merge_kernel<1>),
-                           dim3((unsigned)(waves > 1 ? rows : (rows + 3) / 4)), dim3(waves == 8 ? 512 : 256), 0, stream, dm, nt, p.parts, plan, rows, o_part, ml_part, out, lse);
+        const int most = p.batch || !p.few ? p.most : p.parts, waves = most > 64 ? 8 : most > 16 ? 4 : 1;
+        const auto join = !p.few ? (waves == 4 ? paged_merge_kernel<4, true> : paged_merge_kernel<1, true>)
+                                 : waves == 8 ? paged_merge_kernel<8, false> : waves == 4 ? paged_merge_kernel<4, false> : paged_merge_kernel<1, false>;
+        hipLaunchKernelGGL(join, dim3((unsigned)(waves > 1 ? rows : (rows + 3) / 4)), dim3(waves == 8 ? 512 : 256), 0, stream, dm, nt, p.parts, plan, rows, o_part,
+                           ml_part, out, lse);
         timing_end(stream);
     }
     return (int)hipGetLastError();

@@ -534,6 +534,36 @@ def test_attention_of_many_tiles_with_odd_values_and_pages():
     assert torch.equal(again[0, :, :, keep], out[0, :, :, keep])
 
 
+CHUNKS = [
+    # hq, hkv, page, lengths, counts, n: parts by what is there
+    (16, 1, 32, [8 + (97 * i) % 900 for i in range(100)], [(5 * i) % 9 for i in range(100)], 8),
+    (16, 1, 16, [4 + (53 * i) % 1200 for i in range(128)], [8 if i % 37 == 3 else 0 for i in range(128)], 8),
+    (8, 2, 64, [9000, 50, 40, 3000, 257], [60, 50, 41, 0, 1], 60),
+    (4, 1, 16, [5000, 3000], [1, 500], 500),
+    (4, 2, 64, [700, 600], [0, 0], 100),
+    (4, 2, 64, [90, 600, 3], [100, 0, 4], 100),
+    (32, 2, 128, [4000], [9], 700),
+    (16, 1, 64, [64 + 31 * i for i in range(65)], [8] * 65, 8),
+]
+
+
+@pytest.mark.parametrize("hq,hkv,page,lengths,counts,n", CHUNKS)
+def test_attention_of_few_tiles(hq, hkv, page, lengths, counts, n):
+    gen, b, cap = gen_of(len(lengths) + n), len(lengths), max(lengths)
+    prm = binding.Params(hq, hkv)
+    cache = filled(gen, lengths, hkv, page)
+    q = normal(gen, b, n, hq, D)
+    out, lse = binding.paged_attn(prm, q, cache, i32(lengths), cap, n_new=i32(counts))
+    check_attention(prm, cache, q, lengths, counts, out, lse)
+    for i, m in enumerate(counts):
+        assert not bool(out[i, m:].any()) and not bool(lse[i, m:].any())
+    given, given_lse = torch.full_like(q, 7.0), torch.full((b, n, hq), 7.0, device="cuda")
+    binding.paged_attn(prm, q, cache, i32(lengths), cap, n_new=i32(counts), out=given, lse=given_lse)
+    for i, m in enumerate(counts):
+        assert torch.equal(given[i, :m], out[i, :m]) and torch.equal(given_lse[i, :m], lse[i, :m])
+        assert bool((given[i, m:] == 7).all()) and bool((given_lse[i, m:] == 7).all())
+
+
 # ---- weights -------------------------------------------------------------------------------------------------------------
 
 def weights64(q, lse, k, first, there):
