@@ -701,9 +701,10 @@ def test_eviction(lengths, budget, first, recent, page, to_page, kind):
         assert torch.equal(got.view(torch.int16), want.view(torch.int16))
 
 
-def test_eviction_of_ties_in_many_workgroups():
+@pytest.mark.parametrize("cap", [12000, 20000])
+def test_eviction_of_ties_in_many_workgroups(cap):
     """more numbers with the first digit than a run's list takes: all wavefronts have to go on alike, in every workgroup"""
-    gen, hkv, b, cap, budget = gen_of(9), 4, 128, 20000, 3001
+    gen, hkv, b, budget = gen_of(9), 4, 128, 3001
     prm = binding.Params(4, hkv)
     lengths = [cap - 37 * i for i in range(b)]
     cache = make_pages(gen, [16] * b, hkv, 16)
@@ -714,6 +715,39 @@ def test_eviction_of_ties_in_many_workgroups():
     want = torch.where(hidden, -1.0, w).sort(dim=-1, descending=True, stable=True).indices[:, :, :budget].sort(dim=-1).values.int()
     for _ in range(20):
         assert torch.equal(binding.paged_evict(prm, w, cache, i32(lengths), cap, budget, 0, 0, to)[0], want)
+
+
+@pytest.mark.parametrize("kind", ["equal", "ties", "odd", "random"])
+@pytest.mark.parametrize("lengths,cap,budget,first,recent", [([20000, 900, 0, 4097], 20000, 1000, 4, 30), ([40001, 16384], 40001, 12000, 0, 0), ([90000], 90000, 89999, 64, 0),
+                                                             ([300001, 262145, 5], 300001, 1, 0, 0), ([270000], 400000, 100000, 10, 60000), ([600000], 600000, 600000 - 4096, 0, 0),
+                                                             ([16385, 3], 16385, 16384, 8000, 8383)])
+def test_eviction_in_parts(lengths, cap, budget, first, recent, kind):
+    gen, hkv, b, page = gen_of(cap + budget), 2, len(lengths), 64
+    prm = binding.Params(2, hkv)
+    pools = [torch.zeros((4, hkv, page, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    cache, to = (binding.PagedCache(*pools, torch.full((b, (n + page - 1) // page), -1, dtype=torch.int32, device="cuda")) for n in (cap, budget))
+    w = torch.rand((b, hkv, cap + 5), generator=gen, device="cuda")
+    if kind == "equal":
+        w = torch.full_like(w, 0.25)
+    elif kind == "ties":
+        w = (w * 5).floor() - 2.0
+    elif kind == "odd":
+        w = torch.where(w < 0.2, -math.inf, torch.where(w < 0.3, math.inf, torch.where(w < 0.4, NAN, (w - 0.7) * 1e-39)))
+    kept, wo, so = binding.paged_evict(prm, w, cache, i32(lengths), cap, budget, first, recent, to)
+    for i, length in enumerate(lengths):
+        m = min(length, budget)
+        assert int(so[i]) == m
+        key = w[i, :, :length].nan_to_num(nan=math.inf, posinf=3e38, neginf=-3e38)      # (a NaN above infinity; no number here is near them)
+        if length > budget:
+            fixed = torch.zeros_like(key)
+            fixed[:, :first], fixed[:, length - recent:] = 1.0, 1.0
+            order = key.sort(dim=-1, descending=True, stable=True).indices
+            order = order.gather(1, fixed.gather(1, order).sort(dim=-1, descending=True, stable=True).indices)       # those that stay in any case before all others
+            want = order[:, :budget].sort(dim=-1).values.int()
+        else:
+            want = torch.cat((torch.arange(m, device="cuda"), torch.full((budget - m,), -1, device="cuda"))).int().expand(hkv, budget)
+        assert torch.equal(kept[i], want)
+        assert torch.equal(wo[i, :, :m].view(torch.int32), w[i].gather(1, want[:, :m].long()).view(torch.int32)) and not bool(wo[i, :, m:].any())
 
 
 def test_eviction_with_rows_without_pages():

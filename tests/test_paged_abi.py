@@ -111,6 +111,14 @@ def test_more_refusals(lib):
         assert call(lib, "paged_attn", _5=1, _10=ws, _11=size) == WORKSPACE
 
 
+def test_eviction_of_long_sequences_needs_a_workspace(lib):
+    one = lambda b, t: lib.infllmv2_paged_workspace_bytes(binding.OP_PAGED_EVICT, ctypes.byref(params()), b, t, 1)   # noqa: E731
+    assert one(1, 16384) == 0 and one(1, 16385) > 0 and one(0, 100000) == 0
+    got = [one(2, t) for t in (1, 16385, 20480, 20481, 262143, 262144, 262145, 524288, 524289, 1 << 20, (1 << 20) + 1, 1 << 30)]
+    assert got == sorted(got)
+    assert one(1, (1 << 30) + 1) == 0
+
+
 @pytest.mark.parametrize("op", [binding.OP_PAGED_ATTN, binding.OP_PAGED_WEIGHTS, binding.OP_PAGED_EVICT])
 def test_workspaces_grow_with_every_size(lib, op):
     sizes = [1, 2, 3, 7, 16, 17, 64, 255, 256, 257, 511, 512, 513, 600, 1024, 5000, 65535]
