@@ -15,7 +15,7 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 // A workgroup to a sequence and head: the smallest weight that stays, by digits of 11, 11 and 10 bits from the highest on (11: exponents and two bits of mantissa spread a
 // wavefront's counts over many words; all lanes' in one word cost an addition); then the rows above it and the first of those equal to it, in order.  A wavefront holds a run of
 // up to 64 kPer rows in registers.
-// 64 of 5001 to 9001 rows at a time: 13 us, of which the weights' way 2.5, counts, sums and three barriers for each digit, and the list of those that have the first.
+// 64 of 5001 to 9001 rows at a time: 9.6 us, of which the weights' way 2.5; counts, sums and three barriers for each digit, and the list of those that have the first.
 constexpr int kDigits = 2048, kListed = 512, kMostPer = 16;
 template <int kPer>
 __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const float *__restrict__ weights, int pitch, const int32_t *__restrict__ seqlens,
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(Dims dm, const
 
 // Parts of `rows` rows, a workgroup to a part, three launches: the first digits' counts of each part; from all parts' the first digit, and each part's numbers that have it into a list;
 // from all lists the other digits, and each part's rows that stay.  Every workgroup of a sequence and head works the digits out for itself.  Bound by launches and, in each, round trips:
-// 32749 rows of two heads 16 us (a workgroup to a head, its rows in registers: 18.5), 131072 25 (73).
+// 32749 rows of two heads 3.6 + 5.6 + 7.2 us (a workgroup to a head, its rows in registers: 18.2), 131072 25 (73).
 constexpr int kPartRows = 4096, kMostParts = 64, kGathered = 16384;
 struct EvictParts {
     int rows, most;                                      // parts that there can be
