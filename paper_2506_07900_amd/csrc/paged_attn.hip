@@ -671,8 +671,8 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void paged_merge_k
 static inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int kMaxParts = 128, kMaxChunkParts = 64;      // what paged_merge_kernel joins; of tiles of 128 rows
-// Up to 16 rows: two workgroups to a compute unit run at a time, and the keys are cut into as many parts, those of a batch by the sequences' lengths.  More rows: with 768 tiles and
-// more three workgroups of one group to a compute unit; with fewer, workgroups of three groups, one to a compute unit, and parts where even they are fewer than the compute units.
+// Up to 16 rows: two workgroups to a compute unit run at a time, and the keys are cut into as many parts, those of a batch by the sequences' lengths.  More rows: with more tiles than
+// compute units up to three workgroups of one group to each; with fewer, unless the keys are few, workgroups of three groups, and parts of the keys where they are fewer than half.
 constexpr int kFewItems = 512;
 struct PagedPlan {
     bool few, groups, batch;                             // batch: parts by lengths
@@ -691,9 +691,12 @@ static PagedPlan paged_plan(const Dims &dm, int max_new) {
     p.few = (int64_t)max_new * dm.G <= 16;
     p.tiles = (int)paged_tiles(dm, max_new);
     p.items = (int64_t)dm.batch * dm.Hkv * p.tiles;
-    p.groups = p.items < 768;
+    // (three groups / one: 250 tiles of 2000 rows 37 / 52 us, 304 of 800 40 / 33, of 6000 186 / 185, 504 of 3000 109 / 107, of 6000 202 / 207; 20 new tokens of 100 / 300 / 500 rows
+    // 12.8 / 9.5, 15.3 / 14.1, 17.8 / 18.3)
+    p.groups = p.items <= kChunkItems && dm.max_seqlen > 448;
     // (of few rows and short caches one launch: 300 tokens 8.6 / 9.2 us, 500 10.3 / 9.3; 64 sequences of 1000 17.2 / 19.4, 32 of 768 12.9 / 12.1)
-    const bool alone = p.few && (dm.max_seqlen <= 320 || (dm.max_seqlen <= 1024 && p.items >= 128));
+    // (of tiles: 20 new tokens of 300 / 500 / 700 / 1000 rows, 32 : 2 heads: 15.3 / 17.7 / 20.2 / 24.3 in one launch, 17.2 / 18.4 / 18.7 / 18.8 in parts)
+    const bool alone = p.few ? dm.max_seqlen <= 320 || (dm.max_seqlen <= 1024 && p.items >= 128) : dm.max_seqlen <= 512;
     p.most = (int)most_parts(dm, p.few);
     p.parts = alone ? 1 : (int)max((int64_t)1, min((int64_t)p.most, (p.few ? kFewItems : kChunkItems) / p.items));
     p.batch = p.few && p.parts > 1 && dm.batch > 1 && (int64_t)dm.batch * dm.max_seqlen < (1ll << 31);

@@ -544,6 +544,11 @@ CHUNKS = [
     (4, 2, 64, [90, 600, 3], [100, 0, 4], 100),
     (32, 2, 128, [4000], [9], 700),
     (16, 1, 64, [64 + 31 * i for i in range(65)], [8] * 65, 8),
+    # no more tiles than compute units, without parts: three groups, and with fewer keys one
+    (16, 16, 64, [801, 640, 500, 30], [300, 256, 1, 30], 300),
+    (16, 16, 32, [440, 300, 299, 30], [300, 256, 300, 30], 300),
+    (8, 2, 16, [512, 449, 448], [60, 60, 0], 60),
+    (8, 2, 16, [513, 449, 448], [60, 60, 0], 60),
 ]
 
 
@@ -562,6 +567,27 @@ def test_attention_of_few_tiles(hq, hkv, page, lengths, counts, n):
     for i, m in enumerate(counts):
         assert torch.equal(given[i, :m], out[i, :m]) and torch.equal(given_lse[i, :m], lse[i, :m])
         assert bool((given[i, m:] == 7).all()) and bool((given_lse[i, m:] == 7).all())
+
+
+@pytest.mark.parametrize("cap", [700, 440])
+def test_attention_of_as_many_tiles_as_compute_units_with_odd_values_and_pages(cap):
+    gen = gen_of(cap)
+    hq, hkv, n, b = 16, 16, 300, 4
+    prm, lengths = binding.Params(hq, hkv), [cap - 3 * i for i in range(b)]
+    cache = filled(gen, lengths, hkv, 16)
+    q = normal(gen, b, n, hq, D)
+    cache.table[2, 7], cache.table[3, :] = -1, -7
+    out, lse = binding.paged_attn(prm, q, cache, i32(lengths), cap)
+    check_attention(prm, cache, q, lengths, [n] * b, out, lse)
+    v = cache.v.clone()
+    t = cap - 100
+    v[int(cache.table[0, t // 16]), :, t % 16, 9] = -math.inf
+    again, _ = binding.paged_attn(prm, q, cache._replace(v=v), i32(lengths), cap)
+    first = t - (cap - n)                                         # the first query that sees it
+    assert torch.equal(again[1:], out[1:]) and torch.equal(again[0, :first], out[0, :first])
+    assert bool((again[0, first:, :, 9] == -math.inf).all())
+    keep = torch.arange(D, device="cuda") != 9
+    assert torch.equal(again[0, :, :, keep], out[0, :, :, keep])
 
 
 # ---- weights -------------------------------------------------------------------------------------------------------------
