@@ -231,9 +231,15 @@ __global__ __launch_bounds__(128) void paged_weights_join_kernel(Dims dm, NewTok
     weights_out[at] = (weights && key < ch.before ? weights[at] : 0.f) + sum;
 }
 
-constexpr int kWeightItems = 12 * 256;                   // four rounds of three workgroups to a compute unit (without parts / with: 1230 / 1072 us)
+// Workgroups run three to a compute unit.  Parts fill one such round, of at least four units of rows; four rounds, whose last is seldom empty for long, of at least 64 units
+// (all of a tile / one round / four: 4096 tokens of 32749 rows, 32 : 2 heads, 1115 / 1114 / 1056 us; 1000 of 1000 201 / 18.7 / 27.9; 8 x 64 of 8192, 8 : 2, 19.5 / 18.6 / 27.6).
+constexpr int kWeightRound = 3 * 256, kWeightItems = 4 * kWeightRound;
 static int64_t weight_items(const Dims &dm) { return ((int64_t)dm.max_seqlen + 127) / 128 * dm.Hkv * dm.batch; }
-static int64_t most_weight_parts(const Dims &dm, int max_new) { return max((int64_t)1, (int64_t)max_new * dm.G / 128); }    // four units of rows and more to a part
+static int64_t most_weight_parts(const Dims &dm, int max_new) { return max((int64_t)1, (int64_t)max_new * dm.G / 128); }
+static int weight_parts(const Dims &dm, int max_new) {
+    const int64_t items = weight_items(dm), most = most_weight_parts(dm, max_new);
+    return (int)max((int64_t)1, max(min(most, kWeightRound / items), min(most / 16, (kWeightItems + items - 1) / items)));
+}
 // (a bound that grows with each size)
 size_t paged_weights_ws_bytes(const Dims &dm, int max_new) {
     const int64_t items = min(weight_items(dm), (int64_t)kWeightItems - 1), most = most_weight_parts(dm, max_new);
@@ -256,7 +262,7 @@ int launch_paged_weights(const Dims &dm, Tensor q, const float *lse, const Pages
     }
     const int tiles = (int)(((int64_t)dm.max_seqlen + 127) / 128);
     const int64_t items = weight_items(dm);
-    const int parts = items >= kWeightItems ? 1 : (int)min(most_weight_parts(dm, nt.most), (kWeightItems + items - 1) / items);
+    const int parts = weight_parts(dm, nt.most);
     const int run = xcd_run_length(items * parts);
     float *partial = reinterpret_cast<float *>(ws);
     timing_begin("paged_weights_kernel", stream);
