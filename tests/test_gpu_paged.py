@@ -898,6 +898,50 @@ def test_graphs_that_share_a_workspace_and_calls_side_by_side():
         assert all(torch.equal(x, y) for j, i in ((0, 1), (1, 2)) for x, y in zip(side[j], want[i]))
 
 
+def test_eviction_and_attention_in_a_graph_whose_lengths_change():
+    """captured once for the longest; what is replayed reads the lengths, counts and weights of its time, and nothing that an earlier replay left in the workspace"""
+    gen = gen_of(77)
+    hq, hkv, b, cap, n, budget, page = 16, 2, 3, 20000, 24, 700, 64
+    prm = binding.Params(hq, hkv)
+    cache = filled(gen, [cap] * b, hkv, page)
+    to = make_pages(gen, [budget] * b, hkv, page, fill=0.0)
+    q, w = normal(gen, b, n, hq, D), torch.rand((b, hkv, cap), generator=gen, device="cuda")
+    sl, counts = i32([cap] * b), i32([n] * b)
+    ws = [torch.empty(max(256, binding.paged_workspace_bytes(op, prm, b, cap, n)), dtype=torch.uint8, device="cuda") for op in (binding.OP_PAGED_ATTN, binding.OP_PAGED_WEIGHTS, binding.OP_PAGED_EVICT)]
+
+    def run():
+        out, lse = binding.paged_attn(prm, q, cache, sl, cap, n_new=counts, workspace=ws[0])
+        weights = binding.paged_attn_weights(prm, q, lse, cache, sl, cap, n_new=counts, weights=w, workspace=ws[1])
+        return (out, lse, weights) + tuple(binding.paged_evict(prm, weights, cache, sl, cap, budget, 4, 64, to, workspace=ws[2])) + (to.k, to.v)
+
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for lengths, new in (([cap, cap, cap], [n, n, n]), ([5, 16385, 900], [5, 0, 1]), ([0, 0, 3], [0, 1, 4]), ([19999, 700, 701], [1, 24, 24]), ([cap, 4100, 12], [n, 7, 12])):
+        sl.copy_(i32(lengths))
+        counts.copy_(i32(new))
+        w.copy_(torch.rand(w.shape, generator=gen, device="cuda") * 4)
+        for x in ws:
+            x.fill_(255)
+        to.k.zero_(), to.v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [x.clone() for x in got]
+        for x in ws:
+            x.fill_(0)
+        to.k.zero_(), to.v.zero_()
+        eager = run()
+        for i, (x, y) in enumerate(zip(replayed, eager)):
+            assert torch.equal(x, y), i
+        kept, so = replayed[3], replayed[5]
+        for i, length in enumerate(lengths):
+            assert int(so[i]) == min(length, budget)
+            for h in range(hkv):
+                rows = choice(replayed[2][i, h].tolist(), length, budget, 4, 64)
+                assert kept[i, h].tolist() == rows + [-1] * (budget - len(rows))
+
+
 def test_another_stream_and_order():
     """calls go to the current stream"""
     gen = gen_of(4)
