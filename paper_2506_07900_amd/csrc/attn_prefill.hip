@@ -445,6 +445,7 @@ __global__ __launch_bounds__(256, (AttnCfg<kG, kTiles, kSplit>::kWavesPerSimd)) 
                     for (int ks = 0; ks < 4; ++ks) qu[ks] = ql[(u * 4 + ks) * 64];
 #pragma unroll
                     for (int r = 0; r < 2; ++r) s[u][r] = scores(r, qu);
+                    settle<1>(s[u][0], s[u][1]);
                 }
                 if (edge) {
                     const int tok = t0 + u * kTPT + tn;

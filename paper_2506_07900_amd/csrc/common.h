@@ -133,6 +133,14 @@ __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// Wait states behind a product whose result is first read where two paths meet.  The hardware does not wait there by itself: a 16x16x32 product's result takes 8 states, a 32x32x16 one's 12.
+// The compiler counts them along one path only, and behind a branch that skips a few instructions the other had a single state (then a maximum read sums without the last product's part),
+// or 5 to 10.  Where that happens these stand on both paths; tests/test_wait_states.py searches every kernel for its shortest path.
+template <int kStates, typename T>
+__device__ __forceinline__ void settle(T &x) { asm volatile("s_nop %1" : "+v"(x) : "n"(kStates - 1)); }
+template <int kStates, typename T>
+__device__ __forceinline__ void settle(T &x, T &y) { asm volatile("s_nop %2" : "+v"(x), "+v"(y) : "n"(kStates - 1)); }
+
 __device__ inline bf16x8 load8(const __bf16 *p) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(p));
 }

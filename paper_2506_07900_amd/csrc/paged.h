@@ -31,11 +31,6 @@ struct Chunk {
     }
 };
 
-// Behind a product whose result is first read beyond a branch.  The wait states that the compiler counts there (the branch and an s_nop, 12 in all for a 32x32x16 product)
-// let a maximum read sums without the last product's part; 16 did not in 20 x 32 x 4 calls of 8 units, these are 20.  In one piece of straight code its 12 are enough.
-template <typename T>
-__device__ __forceinline__ void settle(T &x) { asm volatile("s_nop 7" : "+v"(x)); }
-
 // The page of 16 rows from `row` on (page sizes are multiples of 16), -1: none, and none behind `end`.
 __device__ __forceinline__ int page_of(const Pages &pg, const int32_t *__restrict__ table, int row, int end) {
     if (row >= end) return -1;

@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_attn_few_kernel(Dims 
                 s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks) s[t] = mfma16(u.k[t][ks], bq[ks], s[t]);
-                settle(s[t]);
+                settle<8>(s[t]);
             }
             float y[8];
 #pragma unroll

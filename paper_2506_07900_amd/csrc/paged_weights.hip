@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) s = mfma32(k[ks], rd.rows(slot0, ks), s);
     stage(slot2, 2);
-    settle(s);
+    settle<8>(s);
     auto step = [&](const char *next, char *after, float &z, int x) __attribute__((always_inline)) {
         arrived();
         const float zx = row_z(z, x);
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
                 __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);       // added up
             }
         }
-        settle(s_next);
+        settle<8>(s_next);
         s = s_next;
     };
     for (int x = 0; x < count; x += 3) {

@@ -242,6 +242,7 @@ __global__ __launch_bounds__(256, 1) void window_dq_few_kernel(Dims dm, WindowAr
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = rd.columns(cur.k, j >> 2, j & 3);
         __builtin_amdgcn_sched_barrier(0);
+        settle<8>(s, dp);
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = fast_exp2(__builtin_fmaf(s[e], c, -ref)) * dp[e];
         if (!(k0 + 31 <= t0 && (k0 + 32 <= win.n_sink || hi - k0 < win.window))) {

@@ -120,6 +120,7 @@ __device__ __forceinline__ void take_half(QueryRows &r, const KVHalf &cur, int k
         for (int i = 0; i < 8; ++i) x[i] = r.rd.columns(cur.v, i >> 2, i & 3);
         __builtin_amdgcn_sched_barrier(0);
     }
+    settle<8>(s);
     if (!(k0 + 31 <= r.lo && (k0 + 32 <= r.win.n_sink || r.hi - k0 < r.win.window))) {
         int at = k0 + 4 * r.hf;
         asm volatile("" : "+v"(at));
