@@ -583,7 +583,7 @@ int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *r
  * infllmv2_paged_attn_weights  what every cached row gets of that attention, added to what it had:
  *                              weights_out[b, h, t] = (t < seqlens[b] - n ? weights[b, h, t] : 0) + sum over new tokens i that see row t and the query heads
  *                              g of h of exp(softmax_scale <q_ig, k_t> - lse[b, i, g]),   t < seqlens[b].
- *   lse                        in   of infllmv2_paged_attn; heads with lse -inf add nothing
+ *   lse                        in   of infllmv2_paged_attn; heads with lse -inf add nothing, whatever their scores are
  *   weights                    in   fp32 [batch, Hkv, weights_pitch], weights_pitch >= max_seqlen; NULL: zeros
  *   weights_out                out  the same layout; may be `weights`.  Entries t >= seqlens[b], and skipped sequences', are not written.  The sums' order is
  *                              fixed: results repeat bit for bit.

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(Dims dm, Pages p
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) bq[ks] = zero8();
     }
-    const int last = live ? ch.before + token : -1;      // the last key that this column sees
+    const int last = live && z < INFINITY ? ch.before + token : -1;      // the last key that this column sees; a head without a sum adds nothing, whatever its scores are
     const char *k_head = reinterpret_cast<const char *>(pg.k.ptr + h * pg.k.sh);
     const uint32_t k_at = n * (2 * (uint32_t)pg.k.st) + 16 * g;
     const int32_t *table = pg.table + (int64_t)b * pg.ld;
@@ -97,6 +97,7 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
                                                                const int32_t *__restrict__ seqlens, const float *weights, int pitch, float *weights_out,
                                                                float *__restrict__ partial) {
     __shared__ __align__(16) char slot0[kHalfTile], slot1[kHalfTile], slot2[kHalfTile];
+    __shared__ int odd_s[4];
     const int item = xcd_item(blockIdx.x, run), bp = item / n_tiles, ti = item - bp * n_tiles, bh = bp / n_part, part = bp - bh * n_part, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     if (b >= dm.batch) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, hf = lane >> 5;
@@ -141,8 +142,9 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
     };
     const TileReader rd(lane);
     float sum[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+    // 2^(score - inf) is 0 for a row behind the last token or without a sum, unless its score is NaN or infinite.  If a sum is no number, the walk is taken again with such rows left out by
+    // comparison (in every unit at once, by a test of the row's z: 1071 -> 1112 us).
+    bool careful = false;
     // Unit x lies in slot x % 3.  A step takes the exponentials of unit x and the products of unit x + 1, an instruction of one between those of the other: four wavefronts to a SIMD
     // that do one after the other overlap little (matrix cores 38 %, vector unit 60 % of the time, together all of it).
     auto arrived = [&]() __attribute__((always_inline)) {
@@ -151,15 +153,8 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
         asm volatile("s_barrier" ::: "memory");          // everyone's, and everyone has read the unit before
         __builtin_amdgcn_sched_barrier(0);
     };
-    float z0 = row_lse(0), z1 = row_lse(1), z2 = row_lse(2);
-    stage(slot0, 0);
-    stage(slot1, 1);
-    arrived();
-    f32x16 s = zero16();
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) s = mfma32(k[ks], rd.rows(slot0, ks), s);
-    stage(slot2, 2);
-    settle<8>(s);
+    float z0, z1, z2;
+    f32x16 s;
     auto step = [&](const char *next, char *after, float &z, int x) __attribute__((always_inline)) {
         arrived();
         const float zx = row_z(z, x);
@@ -170,8 +165,8 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
         for (int ks = 0; ks < 8; ++ks) qx[ks] = rd.rows(next, ks);
         f32x16 s_next = zero16();
         const int t = ch.before + per * (u0 + x);        // position of the unit's first token
-        if (k0 + 31 > t) {
-            const int at = t + (c >> lg) - k0 - 4 * hf;  // keys up to this one are seen
+        if (k0 + 31 > t || careful) {
+            const int at = zx < INFINITY ? t + (c >> lg) - k0 - 4 * hf : -1;          // keys up to this one are seen
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum[e] += 8 * (e >> 2) + (e & 3) <= at ? fast_exp2(__builtin_fmaf(s[e], dm.scale_log2, -zx)) : 0.f;
 #pragma unroll
@@ -192,14 +187,37 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
         settle<8>(s_next);
         s = s_next;
     };
-    for (int x = 0; x < count; x += 3) {
-        step(slot1, slot0, z0, x);
-        if (x + 1 >= count) break;
-        step(slot2, slot1, z1, x + 1);
-        if (x + 2 >= count) break;
-        step(slot0, slot2, z2, x + 2);
+#pragma unroll 1
+    for (;;) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+        z0 = row_lse(0), z1 = row_lse(1), z2 = row_lse(2);
+        stage(slot0, 0);
+        stage(slot1, 1);
+        arrived();
+        s = zero16();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) s = mfma32(k[ks], rd.rows(slot0, ks), s);
+        stage(slot2, 2);
+        settle<8>(s);
+        for (int x = 0; x < count; x += 3) {
+            step(slot1, slot0, z0, x);
+            if (x + 1 >= count) break;
+            step(slot2, slot1, z1, x + 1);
+            if (x + 2 >= count) break;
+            step(slot0, slot2, z2, x + 2);
+        }
+        __builtin_amdgcn_s_waitcnt(0);                   // (the copies past the last unit have landed)
+        if (careful) break;
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) odd |= sum[e] != sum[e];
+        if (lane == 0) odd_s[wave] = 0;
+        if (odd) odd_s[wave] = 1;                        // (same wavefront: LDS keeps the order)
+        __syncthreads();                                 // (the slots are free, too)
+        if ((odd_s[0] | odd_s[1] | odd_s[2] | odd_s[3]) == 0) break;
+        careful = true;
     }
-    __builtin_amdgcn_s_waitcnt(0);                       // (the copies past the last unit have landed)
     // ---- over the columns -------------------------------------------------------------------------------------------------
     float mine = 0.f;                                    // of key 8 (c / 4) + 4 hf + c % 4 in lanes c < 16
 #pragma unroll

@@ -1,0 +1,58 @@
+"""The paged cache's calls on values that are not finite, where their answer is a number all the same."""
+import math
+
+import pytest
+import torch
+
+from paper_2506_07900_amd import binding
+from test_gpu_paged import D, NAN, filled, gen_of, i32, normal, rows_of, seen_rows, weights64
+
+pytestmark = pytest.mark.gpu
+
+
+# single tokens and chunks whose last 32 rows of (token, head) are filled and are not; several parts of a tile's rows
+SHAPES = [(16, 1, 1, 300), (4, 1, 3, 90), (16, 1, 3, 200), (16, 1, 4, 200), (8, 2, 37, 300), (2, 1, 33, 129), (1, 1, 100, 100), (16, 1, 700, 900)]
+
+
+@pytest.mark.parametrize("hq,hkv,n,length", SHAPES)
+def test_weights_of_keys_whose_scores_are_minus_infinity(hq, hkv, n, length):
+    """such a key gets nothing, wherever it lies: seen by all new tokens, or one of them itself"""
+    prm, gen = binding.Params(hq, hkv), gen_of(n)
+    cache = filled(gen, [length], hkv, 16)
+    q = normal(gen, 1, n, hq, D)
+    q[..., 3] = 1.0                                               # all queries go against the infinity
+    at = sorted({0, length - 1, length // 2, max(0, length - n), max(0, length - n - 1)})
+    for t in at:
+        cache.k[int(cache.table[0, t // 16]), :, t % 16, 3] = -math.inf
+    _, lse = binding.paged_attn(prm, q, cache, i32([length]), length)
+    got = binding.paged_attn_weights(prm, q, lse, cache, i32([length]), length)
+    had = torch.rand((1, hkv, length), generator=gen, device="cuda")
+    more = binding.paged_attn_weights(prm, q, lse, cache, i32([length]), length, weights=had)
+    k = rows_of(cache, cache.k, 0, length)
+    k[:, at] = 0.0
+    there = seen_rows(cache, 0, length)
+    there[at] = False
+    want, tol = weights64(q[0], lse[0], k, length - n, there)
+    assert bool(torch.isfinite(got).all()) and not bool(got[0, :, at].any())
+    assert bool(((got[0].double() - want).abs() <= tol).all())
+    had[:, :, length - n:] = 0
+    assert torch.equal(more, had + got)
+
+
+@pytest.mark.parametrize("hq,hkv,n,length", SHAPES)
+def test_weights_of_heads_without_a_sum(hq, hkv, n, length):
+    """heads whose lse is -inf add nothing, whatever their queries are"""
+    prm, gen = binding.Params(hq, hkv), gen_of(n + 1)
+    cache = filled(gen, [length], hkv, 16)
+    q = normal(gen, 1, n, hq, D)
+    _, lse = binding.paged_attn(prm, q, cache, i32([length]), length)
+    none = torch.rand((n, hq), generator=gen, device="cuda") < 0.3
+    none[0, 0] = True
+    lse[0][none] = -math.inf
+    clean = torch.where(none[None, :, :, None], 0, q)
+    want, tol = weights64(clean[0], lse[0], rows_of(cache, cache.k, 0, length), length - n, seen_rows(cache, 0, length))
+    kinds = torch.randint(0, 3, (n, hq), generator=gen, device="cuda")
+    for i, x in enumerate((NAN, math.inf, 3e38)):
+        q[0][none & (kinds == i)] = x
+    got = binding.paged_attn_weights(prm, q, lse, cache, i32([length]), length)
+    assert bool(((got[0].double() - want).abs() <= tol).all())
