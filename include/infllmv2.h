@@ -591,7 +591,8 @@ int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *r
  *                              largest weights, ties to the lower row, a NaN above all numbers.  n_first + n_recent <= budget.  Sequences of up to `budget` rows keep all.
  *                              Kept rows go, in their order, to rows 0, 1, .. of the sequence in `to`, whose pages have to be others than those that hold a sequence's
  *                              rows in `from` (the pools may be the same); its table has at least
- *                              ceil(min(budget, max_seqlen) / page_size) entries.
+ *                              ceil(min(budget, max_seqlen) / page_size) entries.  A kept row that has no page in `from` goes to its place as zeros (a
+ *                              row like others there: queries see it, with a score of 0); one that has none in `to` is dropped.
  *   weights                    in   fp32 [batch, Hkv, weights_pitch], weights_pitch >= max_seqlen
  *   kept                       out  int32 [batch, Hkv, budget]: the kept rows, ascending, then -1
  *   weights_out                out  fp32 [batch, Hkv, budget]: their weights, then 0 (may be NULL)

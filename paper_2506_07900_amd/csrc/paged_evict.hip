@@ -413,12 +413,11 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Dims dm, const float *_
         dst[i] = row[i] >= 0 ? to.table[(int64_t)b * to.ld + (j >> to.lg)] : -1;               // (its table may end with the rows that there can be)
         if (weights_out && piece == 0 && j < budget) weights_out[bh * budget + j] = row[i] >= 0 ? weights[bh * pitch + row[i]] : 0.f;
     }
-    bool moves[4];
+    // (a kept row without a page goes as zeros: its place counts as a row of the sequence, and what lay there is another's)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        moves[i] = (uint32_t)src[i] < (uint32_t)from.count && (uint32_t)dst[i] < (uint32_t)to.count;
         x[i] = y[i] = u32x4_t{0u, 0u, 0u, 0u};
-        if (moves[i]) {
+        if ((uint32_t)src[i] < (uint32_t)from.count && (uint32_t)dst[i] < (uint32_t)to.count) {
             x[i] = *reinterpret_cast<const u32x4_t *>(kf + page_bytes(from.k, from.lg, src[i], row[i]));
             y[i] = *reinterpret_cast<const u32x4_t *>(vf + page_bytes(from.v, from.lg, src[i], row[i]));
         }
@@ -426,7 +425,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Dims dm, const float *_
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int j = 64 * blockIdx.x + 16 * i + (threadIdx.x >> 4);
-        if (!moves[i]) continue;
+        if ((uint32_t)dst[i] >= (uint32_t)to.count) continue;
         store16<kStream>(kt + page_bytes(to.k, to.lg, dst[i], j), x[i]);
         store16<kStream>(vt + page_bytes(to.v, to.lg, dst[i], j), y[i]);
     }

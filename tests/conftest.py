@@ -17,7 +17,19 @@ def pytest_configure(config):
         warnings.warn("pytest-timeout is not installed: the time limits of the GPU tests are not enforced")
 
 
+# Tests that expect a wrong value.  They run, and have to fail at just that.
+WRONG_VALUES = {
+    "test_gpu_paged.py::test_eviction_with_rows_without_pages":
+        "expects a kept row without a page to leave in its place what lay there before, which queries then see as the sequence's; it goes there as zeros "
+        "(test_gpu_paged_values.py::test_eviction_of_rows_without_pages)",
+}
+
+
 def pytest_collection_modifyitems(config, items):
+    for item in items:
+        reason = WRONG_VALUES.get(item.nodeid.split("/")[-1])
+        if reason:
+            item.add_marker(pytest.mark.xfail(reason=reason, raises=AssertionError, strict=True))
     try:
         import torch
         has_gpu = torch.cuda.is_available()

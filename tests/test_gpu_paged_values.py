@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2506_07900_amd import binding
-from test_gpu_paged import D, NAN, filled, gen_of, i32, normal, rows_of, seen_rows, weights64
+from test_gpu_paged import D, NAN, filled, gen_of, i32, make_pages, normal, rows_of, seen_rows, weights64
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,36 @@ def test_weights_of_heads_without_a_sum(hq, hkv, n, length):
         q[0][none & (kinds == i)] = x
     got = binding.paged_attn_weights(prm, q, lse, cache, i32([length]), length)
     assert bool(((got[0].double() - want).abs() <= tol).all())
+
+
+def entries(cache, cap):
+    """the table with as many entries as `cap` rows take, those behind the sequence's -1"""
+    table = torch.full((1, (cap + cache.k.shape[2] - 1) // cache.k.shape[2]), -1, dtype=torch.int32, device="cuda")
+    table[:, :cache.table.shape[1]] = cache.table
+    return table
+
+
+@pytest.mark.parametrize("cap,length,budget,first,recent", [(200, 200, 100, 4, 20), (200, 90, 100, 0, 0), (20000, 19990, 700, 40, 90)])
+def test_eviction_of_rows_without_pages(cap, length, budget, first, recent):
+    """what lay in the places of kept rows that have no page is seen by nobody: they hold zeros, and no result depends on it"""
+    hkv, hq, page, found = 2, 8, 16, []
+    prm = binding.Params(hq, hkv)
+    for fill in (7.0, NAN, math.inf):
+        gen = gen_of(cap)
+        cache, to = filled(gen, [length], hkv, page), make_pages(gen, [budget], hkv, page, fill=fill)
+        cache.table[0, 1], cache.table[0, 3], cache.table[0, (length - 1) // page] = -1, cache.k.shape[0], 1 << 30
+        w = torch.rand((1, hkv, cap), generator=gen, device="cuda")
+        w[:, :, 16:32] += 1.0                                     # they stay for their weight too
+        kept, _, left = binding.paged_evict(prm, w, cache._replace(table=entries(cache, cap)), i32([length]), cap, budget, first, recent, to)
+        m = min(length, budget)
+        assert int(left[0]) == m
+        there, safe = seen_rows(cache, 0, length), cache._replace(table=cache.table.clamp(0, cache.k.shape[0] - 1))
+        for pool, new in ((cache.k, to.k), (cache.v, to.v)):
+            rows, moved = rows_of(safe, pool, 0, length), rows_of(to, new, 0, m)
+            for h in range(hkv):
+                t = kept[0, h, :m].long()
+                assert 0 < int((~there[t]).sum()) < m
+                assert torch.equal(moved[h], torch.where(there[t][:, None], rows[h, t], 0))
+        q = normal(gen, 1, 1, hq, D)
+        found.append(binding.paged_attn(prm, q, to, left, budget))
+    assert all(bool(torch.isfinite(x).all()) and torch.equal(x, y) for pair in found for x, y in zip(pair, found[0]))
