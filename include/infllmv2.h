@@ -553,7 +553,8 @@ int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_
  *                       themselves with the same strides).  q and q_out, or k and k_out, may both be NULL.
  *   positions           in   int32 [batch, max_seqlen], any values; NULL: row t is at position t
  * infllmv2_rope_bwd     the gradients of its inputs from those of its outputs: the same rows turned by -theta, times the same amplitude.
- * Of prm the head counts and head_dim count; the rest has to be valid.  rot_dim that is no multiple of 16: INFLLMV2_ERR_UNSUPPORTED.
+ * Of prm the head counts and head_dim count; the rest has to be valid.  rot_dim that is no multiple of 16: INFLLMV2_ERR_UNSUPPORTED, and so are
+ * max_seqlen above 2^30 and max_seqlen * ceil((n_q_heads + n_kv_heads) / 8) above 2^30.
  */
 int32_t infllmv2_rope_table(const infllmv2_rope_config *cfg, uint64_t *steps, float *amplitude);
 int32_t infllmv2_rope(const infllmv2_params *prm, const infllmv2_rotation *rot, const infllmv2_tensor *q, const infllmv2_tensor *k,
@@ -566,7 +567,9 @@ int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *r
 /*
  * A cache in pages (infllmv2_pages).  In all these calls the last n tokens of a sequence are new: n_new[b] of them (DEVICE int32 [batch], clamped
  * to 0 .. max_new; NULL: max_new of every sequence), seqlens[b] counts them, and new token t is cache row seqlens[b] - n + t.
- * A sequence with seqlens[b] < n is skipped as a whole.  max_seqlen is at most 2^30, max_new at most 2^24, and max_new times n_q_heads at most 2^30.
+ * A sequence with seqlens[b] < n is skipped as a whole.  max_seqlen is at most 2^30, max_new at most 2^24, max_new times n_q_heads at most 2^30,
+ * batch * n_kv_heads * ceil(max_new * group size / 128) at most 2^23 (attention), batch * n_kv_heads * ceil(max_seqlen / 128) at most 2^30 (weights), and budget at most 2^30 - 64;
+ * INFLLMV2_ERR_UNSUPPORTED beyond.
  *
  * infllmv2_paged_append        k_new, v_new bf16 [batch, Hkv, max_new, d] into the pages; a sequence with seqlens[b] > max_seqlen is skipped too.  With rot
  *                              (NULL: none) keys are rotated on the way, as by infllmv2_rope.  With q [batch, max_new, Hq, d] the same launch

@@ -842,6 +842,7 @@ int32_t infllmv2i_rope(const infllmv2_params *prm, const infllmv2_rotation *rot,
     RETURN_IF_ERR(check_capacity(max_seqlen));
     RETURN_IF_ERR(check_rotation(rot));
     if (!q != !q_out || !k != !k_out || !seqlens) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (rotate_wavefronts(max_seqlen, (int64_t)prm->n_q_heads + prm->n_kv_heads) > (1ll << 30)) return INFLLMV2_ERR_UNSUPPORTED;
     const infllmv2_tensor *ts[4] = {q, q_out, k, k_out};
     Tensor made[4];
     for (int i = 0; i < 4; ++i) {
@@ -915,6 +916,7 @@ int32_t infllmv2i_paged_attn(const infllmv2_params *prm, const infllmv2_tensor *
     if (!seqlens || !lse) return INFLLMV2_ERR_INVALID_ARGUMENT;
     RETURN_IF_ERR(check_spans(prm, nullptr, nullptr, q, nullptr));
     const Dims dm = make_dims(prm, batch, max_seqlen, 1, fill);
+    if (paged_attn_groups(dm, max_new) > (1ll << kLgGroups)) return INFLLMV2_ERR_UNSUPPORTED;
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, paged_attn_ws_bytes(dm, max_new)));
     return hip_status(launch_paged_attn(dm, make_tensor(q), make_pages(pages), NewTokens{n_new, max_new}, seqlens, make_tensor(out), lse, workspace,
                                         reinterpret_cast<hipStream_t>(stream)));
@@ -939,6 +941,7 @@ int32_t infllmv2_paged_attn_weights(const infllmv2_params *prm, const infllmv2_t
     if (!seqlens || !lse || !weights_out || weights_pitch < max_seqlen) return INFLLMV2_ERR_INVALID_ARGUMENT;
     RETURN_IF_ERR(check_spans(prm, nullptr, nullptr, q, nullptr));
     const Dims dm = make_dims(prm, batch, max_seqlen);
+    if (paged_weights_groups(dm) > (1ll << 30)) return INFLLMV2_ERR_UNSUPPORTED;
     RETURN_IF_ERR(check_workspace(workspace, workspace_bytes, paged_weights_ws_bytes(dm, max_new)));
     return hip_status(launch_paged_weights(dm, make_tensor(q), lse, make_pages(pages), NewTokens{n_new, max_new}, seqlens, weights, weights_pitch, weights_out,
                                            workspace, reinterpret_cast<hipStream_t>(stream)));
@@ -952,7 +955,7 @@ int32_t infllmv2_paged_evict(const infllmv2_params *prm, const float *weights, i
     RETURN_IF_ERR(check_sizes(batch, max_seqlen));
     RETURN_IF_ERR(check_capacity(max_seqlen));
     if (budget < 1 || n_first < 0 || n_recent < 0 || (int64_t)n_first + n_recent > budget) return INFLLMV2_ERR_INVALID_ARGUMENT;
-    RETURN_IF_ERR(check_capacity(budget));
+    if (budget > (1 << 30) - 64) return INFLLMV2_ERR_UNSUPPORTED;          // (64 of them to a workgroup of 256 threads: the last are kept below 2^32)
     RETURN_IF_ERR(check_pages(from, max_seqlen));
     RETURN_IF_ERR(check_pages(to, budget < max_seqlen ? budget : max_seqlen));
     if (!weights || !seqlens || !kept || !seqlens_out || weights_pitch < max_seqlen) return INFLLMV2_ERR_INVALID_ARGUMENT;

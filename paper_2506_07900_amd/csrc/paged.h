@@ -121,6 +121,14 @@ __device__ __forceinline__ int64_t page_bytes(const Tensor &t, int lg, int page,
     return 2 * ((int64_t)page * t.sb + (int64_t)(row & ((1 << lg) - 1)) * t.st);
 }
 
+// A launch has fewer than 2^32 threads along a dimension: of more the runtime starts what is left modulo 2^32, without an error.  Workgroups of 256 beyond 2^23 go along another one.
+constexpr int kLgGroups = 23;
+inline unsigned groups_x(int64_t groups) { return (unsigned)min(groups, (int64_t)1 << kLgGroups); }
+inline unsigned groups_beyond(int64_t groups) { return (unsigned)((groups + (1 << kLgGroups) - 1) >> kLgGroups); }
+
+int64_t paged_attn_groups(const Dims &dm, int max_new);
+int64_t paged_weights_groups(const Dims &dm);            // at least, of chunks
+int64_t rotate_wavefronts(int64_t rows, int64_t heads);  // of a sequence, at most
 size_t paged_attn_ws_bytes(const Dims &dm, int max_new);
 int launch_paged_attn(const Dims &dm, Tensor q, const Pages &pg, NewTokens nt, const int32_t *seqlens, Tensor out, float *lse, void *ws, hipStream_t stream);
 size_t paged_weights_ws_bytes(const Dims &dm, int max_new);

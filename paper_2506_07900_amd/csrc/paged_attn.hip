@@ -683,6 +683,7 @@ static int64_t paged_tiles(const Dims &dm, int64_t max_new) {
     const int64_t rows = max_new * dm.G;
     return rows <= 16 ? 1 : (rows + kChunkRows - 1) / kChunkRows;
 }
+int64_t paged_attn_groups(const Dims &dm, int max_new) { return (int64_t)max_new * dm.G <= 16 ? 0 : (int64_t)dm.batch * dm.Hkv * paged_tiles(dm, max_new); }
 static int64_t most_parts(const Dims &dm, bool few) {    // 128 keys and more to a part of few rows, a unit to a wavefront, or 256
     return max((int64_t)1, few ? min((int64_t)kMaxParts, ((int64_t)dm.max_seqlen + 127) / 128) : min((int64_t)kMaxChunkParts, ((int64_t)dm.max_seqlen + 255) / 256));
 }

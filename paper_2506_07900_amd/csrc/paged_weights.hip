@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg
                                                                float *__restrict__ partial) {
     __shared__ __align__(16) char slot0[kHalfTile], slot1[kHalfTile], slot2[kHalfTile];
     __shared__ int odd_s[4];
-    const int item = xcd_item(blockIdx.x, run), bp = item / n_tiles, ti = item - bp * n_tiles, bh = bp / n_part, part = bp - bh * n_part, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
+    const int item = xcd_item((blockIdx.y << kLgGroups) + blockIdx.x, run), bp = item / n_tiles, ti = item - bp * n_tiles, bh = bp / n_part, part = bp - bh * n_part, b = bh / dm.Hkv, h = bh - b * dm.Hkv;
     if (b >= dm.batch) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, hf = lane >> 5;
     const Chunk ch(nt, seqlens, b, dm.max_seqlen);
@@ -253,6 +253,7 @@ __global__ __launch_bounds__(128) void paged_weights_join_kernel(Dims dm, NewTok
 // (all of a tile / one round / four: 4096 tokens of 32749 rows, 32 : 2 heads, 1115 / 1114 / 1056 us; 1000 of 1000 201 / 18.7 / 27.9; 8 x 64 of 8192, 8 : 2, 19.5 / 18.6 / 27.6).
 constexpr int kWeightRound = 3 * 256, kWeightItems = 4 * kWeightRound;
 static int64_t weight_items(const Dims &dm) { return ((int64_t)dm.max_seqlen + 127) / 128 * dm.Hkv * dm.batch; }
+int64_t paged_weights_groups(const Dims &dm) { return weight_items(dm); }
 static int64_t most_weight_parts(const Dims &dm, int max_new) { return max((int64_t)1, (int64_t)max_new * dm.G / 128); }
 static int weight_parts(const Dims &dm, int max_new) {
     const int64_t items = weight_items(dm), most = most_weight_parts(dm, max_new);
@@ -284,7 +285,8 @@ int launch_paged_weights(const Dims &dm, Tensor q, const float *lse, const Pages
     const int run = xcd_run_length(items * parts);
     float *partial = reinterpret_cast<float *>(ws);
     timing_begin("paged_weights_kernel", stream);
-    hipLaunchKernelGGL(paged_weights_kernel, dim3(xcd_grid(items * parts, run)), dim3(256), 0, stream, dm, pg, nt, lg, tiles, parts, run, q, lse, seqlens,
+    const int64_t groups = xcd_grid(items * parts, run);
+    hipLaunchKernelGGL(paged_weights_kernel, dim3(groups_x(groups), groups_beyond(groups)), dim3(256), 0, stream, dm, pg, nt, lg, tiles, parts, run, q, lse, seqlens,
                        weights, pitch, weights_out, partial);
     timing_end(stream);
     if (parts > 1) {

@@ -39,7 +39,7 @@ __device__ __forceinline__ void turn(uint32_t x, float &c, float &s) {
 // Bound by traffic where rows are many (32768 tokens of 34 heads: 95 us, 6.0 TB/s), by the launch and round trips where they are few (777 tokens of 5: 4.1 us).
 template <bool kPaged, bool kStream>
 __global__ __launch_bounds__(256) void rotate_kernel(Dims dm, RotateArgs a, const int32_t *__restrict__ seqlens) {
-    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), b = blockIdx.y;
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(((blockIdx.z << kLgGroups) + blockIdx.x) * 4 + (threadIdx.x >> 6)), b = blockIdx.y;
     const int t = id / a.chunks, chunk = id - t * a.chunks;
     if (t >= a.rows) return;
     int n, before = 0;
@@ -148,6 +148,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(Dims dm, RotateArgs a, cons
     }
 }
 
+int64_t rotate_wavefronts(int64_t rows, int64_t heads) { return rows * ((heads + 7) / 8); }
+
 template <bool kPaged>
 static int launch_rotate(const char *name, const Dims &dm, RotateArgs a, const int32_t *seqlens, hipStream_t stream) {
     if (dm.batch <= 0 || a.rows <= 0 || a.heads <= 0) return 0;
@@ -155,8 +157,9 @@ static int launch_rotate(const char *name, const Dims &dm, RotateArgs a, const i
     a.per = (int64_t)a.rows * dm.batch >= 4096 ? min(steps, 2) : 1;      // (32768 tokens, 34 heads: 1 / 2 / 3 / 5 of 5: 111 / 98 / 100 / 105 us)
     a.chunks = (steps + a.per - 1) / a.per;
     const bool past = (int64_t)a.rows * dm.batch * a.heads * (2 * kHeadDim) > kAllL2;
+    const int64_t groups = ((int64_t)a.rows * a.chunks + 3) / 4;
     timing_begin(name, stream);
-    hipLaunchKernelGGL((past ? rotate_kernel<kPaged, true> : rotate_kernel<kPaged, false>), dim3((unsigned)(((int64_t)a.rows * a.chunks + 3) / 4), dm.batch), dim3(256), 0, stream, dm, a, seqlens);
+    hipLaunchKernelGGL((past ? rotate_kernel<kPaged, true> : rotate_kernel<kPaged, false>), dim3(groups_x(groups), dm.batch, groups_beyond(groups)), dim3(256), 0, stream, dm, a, seqlens);
     timing_end(stream);
     return (int)hipGetLastError();
 }
