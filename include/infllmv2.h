@@ -548,7 +548,8 @@ int32_t infllmv2_window_attn_decode_quant(const infllmv2_params *prm, int32_t n_
  * infllmv2_rope_table   HOST function: cfg -> steps[0 .. rot_dim / 2 - 1] (HOST array, to be copied to the device) and the amplitude.  The angles per
  *                       position: INFLLMV2_ROPE_LINEAR divides them by factor; _NTK takes base * factor^(rot_dim / (rot_dim - 2)) for base (rot_dim 16
  *                       and more); _YARN keeps those of pairs that make beta_fast turns and more in original_len, divides by factor those of pairs that
- *                       make beta_slow and fewer, and goes linearly between; _FACTORS divides pair j's by pair_factors[j].
+ *                       make beta_slow and fewer, and between them goes linearly in the turns (not in the pair's number j, as some implementations do:
+ *                       for those take _FACTORS); _FACTORS divides pair j's by pair_factors[j].
  * infllmv2_rope         q [batch, max_seqlen, Hq, d] and k [batch, Hkv, >=max_seqlen, d], rows t < seqlens[b], into q_out, k_out (which may be q, k
  *                       themselves with the same strides).  q and q_out, or k and k_out, may both be NULL.
  *   positions           in   int32 [batch, max_seqlen], any values; NULL: row t is at position t
@@ -565,7 +566,7 @@ int32_t infllmv2_rope_bwd(const infllmv2_params *prm, const infllmv2_rotation *r
                           int32_t max_seqlen, const infllmv2_tensor *dq, const infllmv2_tensor *dk, void *stream);
 
 /*
- * A cache in pages (infllmv2_pages).  In all these calls the last n tokens of a sequence are new: n_new[b] of them (DEVICE int32 [batch], clamped
+ * A cache in pages (infllmv2_pages), for attention over all its rows: the sparse calls above read contiguous caches only.  In all these calls the last n tokens of a sequence are new: n_new[b] of them (DEVICE int32 [batch], clamped
  * to 0 .. max_new; NULL: max_new of every sequence), seqlens[b] counts them, and new token t is cache row seqlens[b] - n + t.
  * A sequence with seqlens[b] < n is skipped as a whole.  max_seqlen is at most 2^30, max_new at most 2^24, max_new times n_q_heads at most 2^30,
  * batch * n_kv_heads * ceil(max_new * group size / 128) at most 2^23 (attention), batch * n_kv_heads * ceil(max_seqlen / 128) at most 2^30 (weights), and budget at most 2^30 - 64;

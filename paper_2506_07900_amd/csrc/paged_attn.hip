@@ -185,8 +185,8 @@ struct ChunkTiles {
 
 // Items: (sequence, head), tile of 128 rows, the last fastest, or (kParts) as ChunkTiles numbers them, n_tiles: most parts.
 // kGroups groups of four wavefronts take every kGroups-th unit and are joined in LDS at the end.  Three fill a compute unit as three workgroups of one do, with a third of the parts
-// (1000 new tokens of 65000, 16 : 2 heads: 615 -> 527 us; 2 x 2048 of 4096, 8 : 8: 99.9 -> 74.2).  8192 of 65536, 32 : 2: 7.6 to 7.7 ms, 1.07 to 1.08 PFLOP/s: matrix cores and vector unit busy
-// 57 and 59 % at 1.85 GHz.  A unit's scores ahead, between the exponentials of the one before, takes registers for two wavefronts to a SIMD only: 8.6 ms against 8.2 in turn.
+// (1000 new tokens of 65000, 16 : 2 heads: 615 -> 527 us; 2 x 2048 of 4096, 8 : 8: 99.9 -> 74.2).  8192 of 65536, 32 : 2: 7.4 to 7.9 ms by card, 1.04 to 1.11 PFLOP/s: matrix cores and vector unit busy
+// 57 and 59 % at 1.9 to 1.8 GHz.  A unit's scores ahead, between the exponentials of the one before, takes registers for two wavefronts to a SIMD only: 8.6 ms against 8.2 in turn.
 template <int kGroups, bool kParts>
 __global__ __launch_bounds__(256 * kGroups, 3) void paged_attn_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int run, Tensor q,
                                                             const int32_t *__restrict__ seqlens, Tensor out, float *__restrict__ lse,

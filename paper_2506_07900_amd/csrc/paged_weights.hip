@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(Dims dm, Pages p
 
 // More rows: a workgroup takes 128 keys, 32 to a wavefront, which hold them in registers, and walks over the rows that see any of them, 32 at a time through LDS.
 // What a lane adds up is one column's share of each of its keys.  Bound by the exponentials and the products, which are half of the attention's.
-// 4096 new tokens over 32749 rows, 32 : 2 heads: 1.07 ms, 0.96 PFLOP/s, vector unit busy 72 %, matrix cores 54 %, at 1.9 GHz.
+// 4096 new tokens over 32749 rows, 32 : 2 heads: 1.09 to 1.12 ms by card, 0.92 to 0.95 PFLOP/s, vector unit busy 71 %, matrix cores 53 %, at 1.84 GHz.
 // Where tiles of keys are fewer than keep the chip evenly busy, a tile's rows are cut into parts, and a second kernel adds these up.
 __global__ __launch_bounds__(256, 3) void paged_weights_kernel(Dims dm, Pages pg, NewTokens nt, int lg, int n_tiles, int n_part, int run, Tensor q, const float *__restrict__ lse,
                                                                const int32_t *__restrict__ seqlens, const float *weights, int pitch, float *weights_out,
