@@ -30,8 +30,8 @@ def test_weights_of_many_rows(cap):
     prm, gen = binding.Params(hkv * group, hkv), gen_of(7)
     cache = filled(gen, lengths, hkv, 1024)
     q = normal(gen, 1, n, hkv * group, D)
-    _, lse = binding.paged_attn(prm, q, cache, i32(lengths), 3072)
-    want = binding.paged_attn_weights(prm, q, lse, cache, i32(lengths), 3072)
+    _, lse = binding.paged_attn(prm, q, cache, i32(lengths), 3000)
+    want = binding.paged_attn_weights(prm, q, lse, cache, i32(lengths), 3000)
     table = torch.zeros((1, cap // 1024 + 1), dtype=torch.int32, device="cuda")
     table[:, :3] = cache.table
     got = binding.paged_attn_weights(prm, q, lse, cache._replace(table=table), i32(lengths), cap)
